@@ -20,7 +20,9 @@
  * entropy bracket from greedy at delta and 2 delta (lam_removal_ceiling), the
  * rank-invariance certificate (lam_score_topk_certified) and a per-block
  * fixed-length codec of the store's codes (lam_store_block_*,
- * lam_score_topk_blocks).
+ * lam_score_topk_blocks).  Beside them stands the memory of the model that
+ * reads the retrieved records: a paged key/value cache held in 4 bits, attention
+ * over it, and eviction by accumulated attention weight (lam_kv_*).
  *
  * Conventions for every call:
  *   - Pointers named *_dev are device pointers on the context's device; the
@@ -397,6 +399,115 @@ typedef struct lam_ceiling_stats {
  * (as lam_dedup_ingest); ENOMEM if the two stores do not fit. */
 lam_status lam_removal_ceiling(lam_ctx* ctx, const float* x_dev, int64_t n, int32_t dim, double tau,
                                int64_t batch, lam_ceiling_stats* out);
+
+/* ------------------------------------------------------------------ 4-bit key/value cache */
+
+/* The context that retrieved records enter is held by the model as keys and
+ * values; these calls keep that cache in 4 bits, attend over it and bound its
+ * length.  A cached token's key (and value) of one head is cut into blocks of 32
+ * consecutive channels; a block holds 4-bit codes (a sign and one of the
+ * magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6) and one byte e + 127, and stands for
+ * code * 2^e.  e is the smallest integer with 6 * 2^e >= max |x| of the block,
+ * held to [-23, 13], so every value is exact in float16 and bfloat16; a code is
+ * the nearest to x / 2^e, halfway cases to the even-numbered magnitude.  For
+ * max |x| <= 49152, |x - x_hat| <= 2^e, and <= max |x| / 3 unless e = -23.
+ *
+ * Memory is pages of page_size tokens (a power of two, 32 to 1024) in a pool
+ * [n_pages][kv_heads][lam_kv_page_bytes] of the caller's, 16-byte aligned.  One
+ * head's part of a page of T tokens and D channels: key codes [T][D/2] (channel
+ * 2i in the low half of byte i), value codes [T/4][16][4][D/32] (16 runs of D/16
+ * channels, four tokens' runs together), key scales [T][D/32], value scales
+ * [T/4][D/32][4].  head_dim is 64, 128 or 256 (a smaller head is padded with
+ * zero channels). */
+enum { LAM_F16 = 0, LAM_BF16 = 1 };
+
+/* D * T * 17 / 16: bytes of one head's part of a page; -1 for sizes outside the above. */
+int64_t lam_kv_page_bytes(int32_t head_dim, int32_t page_size);
+
+/* The sequences of one call.  Token t of sequence s lies in page
+ * table[s * table_stride + t / page_size].  lengths[s] counts the sequence's
+ * cached tokens, the ones of this call (append: those it writes) included: the
+ * call's rows of sequence s are its last n_s tokens.  Rows of all sequences
+ * follow each other: those of s are starts[s] to starts[s + 1] - 1, or, where
+ * starts is NULL, rows / n_seqs each.  table, lengths and starts are read on the
+ * device: pages outside the pool, tokens past the table's columns and rows
+ * outside [0, rows) are not touched (append: counted; attend and evict: as if
+ * masked, left in place). */
+typedef struct lam_kv_view {
+  uint8_t* pages_dev;
+  int64_t n_pages;
+  const int32_t* table_dev;      /* [n_seqs][table_cols], rows table_stride apart */
+  int64_t table_stride;
+  const int32_t* lengths_dev;    /* [n_seqs] */
+  const int32_t* starts_dev;     /* [n_seqs + 1], or NULL */
+  int64_t rows;                  /* rows of this call over all sequences */
+  int32_t n_seqs, table_cols, kv_heads, head_dim, page_size, dtype;
+} lam_kv_view;
+
+/* A value per cached token: element (s, h, t) at p[s * seq_stride + h * head_stride + t], t < cols. */
+typedef struct lam_kv_slots {
+  void* p_dev;                   /* NULL: none */
+  int64_t seq_stride, head_stride;
+  int32_t cols;
+} lam_kv_slots;
+
+/* Quantizes rows of keys and values ([rows][kv_heads][head_dim] of view->dtype,
+ * row and head strides in elements, channels contiguous) into the cache.
+ * weights (float32) and positions (int32), where given, get 0 and first[s] + i
+ * for row i of sequence s (first_dev: int32[n_seqs], required with positions).
+ * status_dev (three uint32 of the caller's, or NULL) is added to: [0] when
+ * elements are NaN or Inf (stored as 0), [1] when a block's max |x| is over 49152
+ * (stored as 49152), [2] when a token has no place (not stored); the counts are
+ * of the device threads that met them.  Asynchronous. */
+lam_status lam_kv_append(lam_ctx* ctx, const lam_kv_view* view, const void* k_dev, int64_t k_row_stride,
+                         int64_t k_head_stride, const void* v_dev, int64_t v_row_stride, int64_t v_head_stride,
+                         const lam_kv_slots* weights, const lam_kv_slots* positions, const int32_t* first_dev,
+                         uint32_t* status_dev);
+
+/* The values the cache holds for the call's rows, [rows][kv_heads][head_dim] of
+ * view->dtype, contiguous (exact in both types).  Tokens without a place read
+ * as 0.  Asynchronous. */
+lam_status lam_kv_read(lam_ctx* ctx, const lam_kv_view* view, void* k_dev, void* v_dev);
+
+/* Attention of the call's rows over the cache: for query head j of key/value
+ * head h = j / (q_heads / kv_heads), row i of sequence s,
+ *   out = sum_t p_t v_hat_t,  p = softmax_t(scale * q . k_hat_t)
+ * over the tokens t < lengths[s], with causal != 0 only t <= lengths[s] - n_s + i,
+ * with a mask only those with mask(s, h, t) != 0 (uint8; tokens past its columns
+ * are masked; head_stride 0 for one mask of all heads).  A row with no token left
+ * gets 0 (lse -inf).  Scores, maxima and sums are float32; p enters the product
+ * with the values as float16 relative to the row's maximum so far.  A query with
+ * NaN or Inf spoils its own row only.  q [rows][q_heads][head_dim] of
+ * view->dtype, out likewise and contiguous; lse_dev (float32[rows][q_heads], or
+ * NULL): log sum_t exp(scale * q . k_hat_t).
+ * weights (float32, or NULL): the sum of p over the call's rows of s and the
+ * query heads of h is added to element (s, h, t); tokens past its columns are
+ * left out.  max_length: an upper bound of lengths that the launch is sized by
+ * (longer sequences are cut to it); <= 0 for the table's.  Context scratch: per
+ * query row and part of the length 4 (head_dim + 2) bytes, where the length is
+ * split.  Asynchronous. */
+lam_status lam_kv_attend(lam_ctx* ctx, const lam_kv_view* view, const void* q_dev, int64_t q_row_stride,
+                         int64_t q_head_stride, int32_t q_heads, double scale, int causal, int64_t max_length,
+                         const lam_kv_slots* mask, const lam_kv_slots* weights, void* out_dev, float* lse_dev);
+
+/* Brings every sequence of more than `budget` tokens back to budget tokens, each
+ * head by itself: the tokens that stay are those protected, then those of the
+ * largest score, equal ones in the order of their slots.  With position(s, h, t)
+ * (int32, or NULL: t), protected are positions below `sinks` and the `recent`
+ * positions up to that of the last slot; sinks + recent <= budget.  A NaN score
+ * is below every other.  Kept slots below budget stay where they are; the i-th slot
+ * given up below budget takes the i-th one kept beyond it, so keys, values,
+ * scores and positions of as few tokens as possible move.  Outputs: kept_dev
+ * (int32 [n_seqs][kv_heads][budget], the old slot of each new one, -1 past the
+ * length), scores_out and positions_out (at least budget columns, which may be
+ * scores and positions themselves; 0 and -1 past the length; positions_out may
+ * be NULL), lengths_out_dev (int32 [n_seqs]: min(length, budget); may be the
+ * view's).  Lengths are cut to the columns of scores and positions.  view->rows,
+ * starts and dtype are not used.  Sequences must not share pages.  Asynchronous. */
+lam_status lam_kv_evict(lam_ctx* ctx, const lam_kv_view* view, const lam_kv_slots* scores,
+                        const lam_kv_slots* positions, int32_t budget, int32_t recent, int32_t sinks,
+                        int32_t* kept_dev, const lam_kv_slots* scores_out, const lam_kv_slots* positions_out,
+                        int32_t* lengths_out_dev);
 
 /* ------------------------------------------------------------------ bandwidth anchor */
 

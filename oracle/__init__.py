@@ -15,7 +15,9 @@ Retrieval-Score Error Bound):
   * ``oracle.score`` -- retrieval scores against the dequantized store, top-k,
     and the Hoelder bound eps*||q||_1 (Appendix "Rank invariance, in full");
   * ``oracle.invariants`` -- checkers for the paper's theorems (Theorem "Score
-    deficit", Proposition "greedy is simultaneously a cover and a packing").
+    deficit", Proposition "greedy is simultaneously a cover and a packing");
+  * ``oracle.kv`` -- the model's key/value cache in 4 bits: its block format and
+    page layout, attention over it and eviction by accumulated weight.
 
 Floating point is binary64; every decision that floating point could get wrong
 near a tie is re-taken in exact rational (or exact integer) arithmetic.
@@ -24,4 +26,4 @@ Only ``tests/``, ``__graft_entry__.smoke()`` and the ``cpu_baseline`` leg of
 ``bench.py`` may import this package.  It shares no code with the GPU library
 and imports nothing from it.
 """
-from . import qeps, dedup, score, invariants  # noqa: F401
+from . import qeps, dedup, score, invariants, kv  # noqa: F401

@@ -18,6 +18,10 @@ built (``python paper_2609_32256_amd/build.py``) importing this module fails.
     lam.removal_ceiling(x, tau=0.95)               # greedy at delta and at 2 delta
     b = lam.Store(768, 0.95, 1 << 20, eps_band=0.2 / 768 ** 0.5, band_width=4)
                                                    # banded candidates over Q_eps codes
+    pages = lam.kv_pages(4096, kv_heads=8, head_dim=128)   # the model's key/value cache, in 4 bits
+    lam.kv_append(k, v, pages, table, lengths)     # rows quantized into it
+    o = lam.kv_attend(q, pages, table, lengths, weights=w)  # attention; what each token received
+    lam.kv_evict(pages, table, lengths, w, budget, 128)     # back to the budget
 """
 from __future__ import annotations
 
@@ -82,6 +86,17 @@ class BlockStats(ctypes.Structure):
         return {f: getattr(self, f) for f, _ in self._fields_ if f != "pad"}
 
 
+class KvView(ctypes.Structure):
+    _fields_ = [("pages", _P), ("n_pages", _I64), ("table", _P), ("table_stride", _I64), ("lengths", _P),
+                ("starts", _P), ("rows", _I64), ("n_seqs", ctypes.c_int32), ("table_cols", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("dtype", ctypes.c_int32)]
+
+
+class KvSlots(ctypes.Structure):
+    _fields_ = [("p", _P), ("seq_stride", _I64), ("head_stride", _I64), ("cols", ctypes.c_int32)]
+
+
 class CeilingStats(ctypes.Structure):
     _fields_ = [("n", _I64), ("kept", _I64), ("kept_2delta", _I64), ("tau", ctypes.c_double),
                 ("tau_2delta", ctypes.c_double), ("removal", ctypes.c_double), ("ceiling", ctypes.c_double),
@@ -131,6 +146,15 @@ _SIGS = {
                             ctypes.c_int),
     "lam_score_topk": ([_P, _P, _P, _I64, ctypes.c_int32, _P, _P, _P], ctypes.c_int),
     "lam_score_topk_noalloc": ([_P, _P, _P, _I64, ctypes.c_int32, _P, _P, _P], ctypes.c_int),
+    "lam_kv_page_bytes": ([ctypes.c_int32, ctypes.c_int32], _I64),
+    "lam_kv_append": ([_P, ctypes.POINTER(KvView), _P, _I64, _I64, _P, _I64, _I64, ctypes.POINTER(KvSlots),
+                       ctypes.POINTER(KvSlots), _P, _P], ctypes.c_int),
+    "lam_kv_read": ([_P, ctypes.POINTER(KvView), _P, _P], ctypes.c_int),
+    "lam_kv_attend": ([_P, ctypes.POINTER(KvView), _P, _I64, _I64, ctypes.c_int32, ctypes.c_double, ctypes.c_int, _I64,
+                       ctypes.POINTER(KvSlots), ctypes.POINTER(KvSlots), _P, _P], ctypes.c_int),
+    "lam_kv_evict": ([_P, ctypes.POINTER(KvView), ctypes.POINTER(KvSlots), ctypes.POINTER(KvSlots), ctypes.c_int32,
+                      ctypes.c_int32, ctypes.c_int32, _P, ctypes.POINTER(KvSlots), ctypes.POINTER(KvSlots), _P],
+                     ctypes.c_int),
     "lam_triad": ([_P, _P, _P, _P, _I64, ctypes.c_float], ctypes.c_int),
 }
 for _name, (_args, _res) in _SIGS.items():
@@ -317,6 +341,202 @@ def triad(a: torch.Tensor, b: torch.Tensor, c: torch.Tensor, s: float = 3.0, ctx
     return c
 
 
+# ---------------------------------------------------------------- 4-bit key/value cache
+_KV_DTYPES = {torch.float16: 0, torch.bfloat16: 1}
+
+
+def kv_pages(n_pages: int, kv_heads: int, head_dim: int, page_size: int = 64, device=None) -> torch.Tensor:
+    """An empty pool of cache pages: uint8 (n_pages, kv_heads, bytes of a head's
+    page).  head_dim 64, 128 or 256; page_size a power of two, 32 to 1024."""
+    size = _lib.lam_kv_page_bytes(int(head_dim), int(page_size))
+    if size < 0:
+        raise ValueError("head_dim must be 64, 128 or 256 and page_size a power of two from 32 to 1024")
+    return torch.zeros((int(n_pages), int(kv_heads), size), dtype=torch.uint8, device=device or "cuda")
+
+
+def _kv_tensor(t, dtype, dims, name, device):
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the cache on {device}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
+    if t.dim() != dims:
+        raise ValueError(f"{name} must have {dims} dimensions")
+    return t
+
+
+def _kv_view(ctx, pages, table, lengths, starts, rows, head_dim, dtype):
+    """The C view of a call.  Tensors whose last axis is not contiguous are
+    copied where the library only reads them, refused where it writes."""
+    if not isinstance(pages, torch.Tensor) or not pages.is_cuda:
+        raise TypeError("pages must be a CUDA (HIP) tensor")
+    dev = pages.device
+    if dev.index != ctx.device:
+        raise ValueError(f"pages are on {dev}, the context on cuda:{ctx.device}")
+    _kv_tensor(pages, torch.uint8, 3, "pages", dev)
+    if not pages.is_contiguous():
+        raise ValueError("pages must be contiguous")
+    size, per = pages.shape[2], head_dim + head_dim // 16
+    if per <= 0 or size % per or _lib.lam_kv_page_bytes(head_dim, size // per) != size:
+        raise ValueError(f"pages of {size} bytes a head do not hold heads of {head_dim} channels")
+    _kv_tensor(table, torch.int32, 2, "table", dev)
+    _kv_tensor(lengths, torch.int32, 1, "lengths", dev)
+    if table.stride(1) != 1 and table.shape[1] > 1 or table.stride(0) < table.shape[1]:
+        table = table.contiguous()
+    lengths = lengths.contiguous()
+    n = lengths.shape[0]
+    if table.shape[0] != n:
+        raise ValueError("table and lengths must have a row for each sequence")
+    if starts is not None:
+        starts = _kv_tensor(starts, torch.int32, 1, "starts", dev).contiguous()
+        if starts.shape[0] != n + 1:
+            raise ValueError("starts must have an entry for each sequence and one more")
+    elif rows and (n == 0 or rows % n):
+        raise ValueError("without starts every sequence has the same number of rows")
+    v = KvView(pages.data_ptr(), pages.shape[0], table.data_ptr(), table.stride(0), lengths.data_ptr(),
+               None if starts is None else starts.data_ptr(), rows, n, table.shape[1], pages.shape[1], head_dim,
+               size // per, _KV_DTYPES[dtype])
+    return v, (table, lengths, starts)   # kept until the launch is queued
+
+
+def _kv_rows(t, heads, name, device):
+    """(rows, heads, head_dim) in float16 or bfloat16, channels contiguous."""
+    if not isinstance(t, torch.Tensor) or t.dtype not in _KV_DTYPES:
+        raise TypeError(f"{name} must be a float16 or bfloat16 tensor")
+    _kv_tensor(t, t.dtype, 3, name, device)
+    if heads is not None and t.shape[1] != heads:
+        raise ValueError(f"{name} must have {heads} heads")
+    return t if t.stride(2) == 1 and min(t.stride()) > 0 else t.contiguous()
+
+
+def _kv_slots(t, dtype, view, name, device, shared=False, copy=False):
+    """A value per cached token: (sequences, heads or 1 where shared, slots)."""
+    if t is None:
+        return None, None
+    _kv_tensor(t, dtype, 3, name, device)
+    if t.shape[0] != view.n_seqs or not (t.shape[1] == view.kv_heads or (shared and t.shape[1] == 1)):
+        raise ValueError(f"{name} must be (sequences, heads, slots)")
+    if t.stride(2) != 1 and t.shape[2] > 1:
+        if not copy:
+            raise ValueError(f"the slots of {name} must be contiguous")
+        t = t.contiguous()
+    head = 0 if t.shape[1] == 1 else t.stride(1)
+    return KvSlots(t.data_ptr(), t.stride(0), head, t.shape[2]), t
+
+
+def _ref(s):
+    return ctypes.byref(s) if s is not None else None
+
+
+def kv_append(k: torch.Tensor, v: torch.Tensor, pages: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor,
+              starts: torch.Tensor | None = None, weights: torch.Tensor | None = None,
+              positions: torch.Tensor | None = None, first: torch.Tensor | None = None,
+              status: torch.Tensor | None = None, ctx: Context | None = None) -> None:
+    """Quantize rows of keys and values (rows, kv_heads, head_dim) into the last
+    tokens of their sequences (lam_kv_append).  lengths counts the new tokens in;
+    starts gives each sequence's rows, None: equally many each.  weights of the
+    new tokens become 0, positions first[s], first[s] + 1, ...; status: int32
+    tensor of 3, counts of non-finite, out-of-range and misplaced input."""
+    ctx = ctx or default_context()
+    dev = pages.device if isinstance(pages, torch.Tensor) else None
+    k = _kv_rows(k, None, "k", dev)
+    v = _kv_rows(v, k.shape[1], "v", dev)
+    if v.shape != k.shape or v.dtype != k.dtype:
+        raise ValueError("k and v must have the same shape and dtype")
+    view, hold = _kv_view(ctx, pages, table, lengths, starts, k.shape[0], k.shape[2], k.dtype)
+    if k.shape[1] != view.kv_heads:
+        raise ValueError(f"k must have {view.kv_heads} heads")
+    w, _ = _kv_slots(weights, torch.float32, view, "weights", dev)
+    p, _ = _kv_slots(positions, torch.int32, view, "positions", dev)
+    if first is not None:
+        first = _kv_tensor(first, torch.int32, 1, "first", dev).contiguous()
+        if first.shape[0] != view.n_seqs:
+            raise ValueError("first must have an entry for each sequence")
+    if status is not None:
+        _kv_tensor(status, torch.int32, 1, "status", dev)
+        if not status.is_contiguous() or status.numel() < 3:
+            raise ValueError("status must be a contiguous int32 tensor of at least 3 entries")
+    _check(_lib.lam_kv_append(ctx.handle, ctypes.byref(view), k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(),
+                              v.stride(0), v.stride(1), _ref(w), _ref(p), _ptr(first), _ptr(status)))
+
+
+def kv_read(pages: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, rows: int, head_dim: int,
+            dtype: torch.dtype = torch.bfloat16, starts: torch.Tensor | None = None, ctx: Context | None = None):
+    """The values the cache holds for the last tokens of the sequences, addressed
+    as by kv_append: (k, v), each (rows, kv_heads, head_dim) (lam_kv_read)."""
+    ctx = ctx or default_context()
+    if dtype not in _KV_DTYPES:
+        raise TypeError("dtype must be float16 or bfloat16")
+    view, hold = _kv_view(ctx, pages, table, lengths, starts, int(rows), int(head_dim), dtype)
+    k, v = (torch.empty((int(rows), view.kv_heads, int(head_dim)), dtype=dtype, device=pages.device) for _ in range(2))
+    _check(_lib.lam_kv_read(ctx.handle, ctypes.byref(view), k.data_ptr(), v.data_ptr()))
+    return k, v
+
+
+def kv_attend(q: torch.Tensor, pages: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor,
+              starts: torch.Tensor | None = None, causal: bool = True, scale: float | None = None,
+              mask: torch.Tensor | None = None, weights: torch.Tensor | None = None, max_length: int | None = None,
+              out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
+              ctx: Context | None = None) -> torch.Tensor:
+    """Attention of the sequences' last tokens over the cache (lam_kv_attend): q
+    and the result (rows, q_heads, head_dim).  scale: 1 / sqrt(head_dim) by
+    default.  mask (bool or uint8: sequences, kv_heads or 1, slots) leaves cached
+    tokens out; weights (float32: sequences, kv_heads, slots) is added to what
+    each token received; lse (float32: rows, q_heads) receives the scores' log
+    sums.  max_length, where the caller knows a bound of lengths, sizes the launch."""
+    ctx = ctx or default_context()
+    dev = pages.device if isinstance(pages, torch.Tensor) else None
+    q = _kv_rows(q, None, "q", dev)
+    view, hold = _kv_view(ctx, pages, table, lengths, starts, q.shape[0], q.shape[2], q.dtype)
+    if mask is not None and mask.dtype == torch.bool:
+        mask = mask.view(torch.uint8)
+    m, hold_mask = _kv_slots(mask, torch.uint8, view, "mask", dev, shared=True, copy=True)
+    w, _ = _kv_slots(weights, torch.float32, view, "weights", dev)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+    elif _kv_tensor(out, q.dtype, 3, "out", dev).shape != q.shape or not out.is_contiguous():
+        raise ValueError("out must be contiguous and of q's shape")
+    if lse is not None and (_kv_tensor(lse, torch.float32, 2, "lse", dev).shape != q.shape[:2] or not lse.is_contiguous()):
+        raise ValueError("lse must be contiguous and (rows, q_heads)")
+    _check(_lib.lam_kv_attend(ctx.handle, ctypes.byref(view), q.data_ptr(), q.stride(0), q.stride(1), q.shape[1],
+                              q.shape[2] ** -0.5 if scale is None else float(scale), int(bool(causal)),
+                              0 if max_length is None else max(1, int(max_length)), _ref(m), _ref(w), out.data_ptr(),
+                              _ptr(lse)))
+    return out
+
+
+def kv_evict(pages: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, scores: torch.Tensor, budget: int,
+             head_dim: int, recent: int = 0, sinks: int = 0, positions: torch.Tensor | None = None, out=None,
+             ctx: Context | None = None):
+    """Bring sequences of more than `budget` tokens back to budget tokens
+    (lam_kv_evict): those of the largest scores stay, the `recent` newest and the
+    `sinks` first positions whatever their scores.  Returns (kept, scores,
+    positions, lengths): the old slot of each new one (sequences, kv_heads,
+    budget), the new slots' scores and positions, and the new lengths.  out:
+    (scores, positions or None, lengths) to write to, which may be the inputs
+    (only their first budget slots are written)."""
+    ctx = ctx or default_context()
+    dev = pages.device if isinstance(pages, torch.Tensor) else None
+    view, hold = _kv_view(ctx, pages, table, lengths, None, 0, int(head_dim), torch.float16)
+    s, hold_s = _kv_slots(scores, torch.float32, view, "scores", dev, copy=True)
+    p, hold_p = _kv_slots(positions, torch.int32, view, "positions", dev, copy=True)
+    if s is None:
+        raise TypeError("scores must be a CUDA (HIP) tensor")
+    shape = (view.n_seqs, view.kv_heads, int(budget))
+    if out is None:
+        out = (torch.empty(shape, dtype=torch.float32, device=dev), torch.empty(shape, dtype=torch.int32, device=dev),
+               torch.empty(view.n_seqs, dtype=torch.int32, device=dev))
+    so, _ = _kv_slots(out[0], torch.float32, view, "out scores", dev)
+    po, _ = _kv_slots(out[1], torch.int32, view, "out positions", dev)
+    if _kv_tensor(out[2], torch.int32, 1, "out lengths", dev).shape[0] != view.n_seqs or not out[2].is_contiguous():
+        raise ValueError("out lengths must be contiguous, an entry for each sequence")
+    kept = torch.empty(shape, dtype=torch.int32, device=dev)
+    _check(_lib.lam_kv_evict(ctx.handle, ctypes.byref(view), _ref(s), _ref(p), int(budget), int(recent), int(sinks),
+                             kept.data_ptr(), _ref(so), _ref(po), out[2].data_ptr()))
+    return kept, out[0], out[1], out[2]
+
+
 # ---------------------------------------------------------------- store
 class Store:
     """The retained set of the greedy near-duplicate test, on one device."""
@@ -491,4 +711,5 @@ class Store:
 
 
 __all__ = ["LamError", "QParams", "IngestStats", "StoreInfo", "Context", "default_context", "quantize",
-           "dequantize", "triad", "Store", "qeps_plan", "removal_ceiling", "CeilingStats", "abi_version", "EXPORTED", "LIB_PATH"]
+           "dequantize", "triad", "Store", "qeps_plan", "removal_ceiling", "CeilingStats", "kv_pages", "kv_append", "kv_read", "kv_attend",
+           "kv_evict", "abi_version", "EXPORTED", "LIB_PATH"]

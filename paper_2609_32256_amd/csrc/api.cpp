@@ -44,20 +44,6 @@ void DevBuf::release() {
   bytes = 0;
 }
 
-// Makes the context's device current for the scope of one API call.
-struct DeviceGuard {
-  int prev = -1;
-  bool ok = true;
-  explicit DeviceGuard(int dev) {
-    if (hipGetDevice(&prev) != hipSuccess) prev = -1;
-    if (prev != dev) ok = hipSetDevice(dev) == hipSuccess;
-  }
-  ~DeviceGuard() {
-    int cur = -1;
-    if (prev >= 0 && hipGetDevice(&cur) == hipSuccess && cur != prev) (void)hipSetDevice(prev);
-  }
-};
-
 // Whether launches of kernel `name` are timed: every kernel, or those named in
 // the comma-separated list of lam_ctx_profile_only.
 static bool prof_selected(const lam_ctx* ctx, const char* name) {

@@ -44,6 +44,20 @@ struct Status {
     if (s_ != LAM_OK) return s_;                                                 \
   } while (0)
 
+// Makes the context's device current for the scope of one API call.
+struct DeviceGuard {
+  int prev = -1;
+  bool ok = true;
+  explicit DeviceGuard(int dev) {
+    if (hipGetDevice(&prev) != hipSuccess) prev = -1;
+    if (prev != dev) ok = hipSetDevice(dev) == hipSuccess;
+  }
+  ~DeviceGuard() {
+    int cur = -1;
+    if (prev >= 0 && hipGetDevice(&cur) == hipSuccess && cur != prev) (void)hipSetDevice(prev);
+  }
+};
+
 // ------------------------------------------------------------------ device buffer
 // Context scratch slots: 0-6 ingest (dedup.hip), 7-11 scoring (score.hip),
 // then the ones below.
@@ -52,7 +66,8 @@ constexpr int kScratchCertify = 13;      // top-(k+1) lists of the certified sco
 constexpr int kScratchBlocks = 14;       // block codec: row word counts and scan sums
 constexpr int kScratchExpand = 15;       // block codec: codes expanded back to the b-bit stream for scoring
 constexpr int kScratchLsh = 16;          // banded candidates: chunk keys and the chunk's own index
-constexpr int kScratchSlots = 17;
+constexpr int kScratchKv = 17;           // 4-bit cache: partial results of split attention; eviction's lists
+constexpr int kScratchSlots = 18;
 
 struct DevBuf {
   void* p = nullptr;
@@ -214,6 +229,19 @@ lam_status score_certify(lam_ctx* ctx, const lam_store* st, const float* q, int6
 lam_status block_encode(lam_ctx* ctx, lam_store* st, lam_block_stats* out);
 // decode the blocks to float32 (xhat) or back to the b-bit code stream (codes_out)
 lam_status block_decode(lam_ctx* ctx, const lam_store* st, float* xhat, uint32_t* codes_out);
+
+// ------------------------------------------------------------------ 4-bit cache (kv_cache.hip, kv_attend.hip)
+lam_status launch_kv_append(lam_ctx* ctx, const lam_kv_view& v, const void* k, int64_t k_row, int64_t k_head,
+                            const void* val, int64_t v_row, int64_t v_head, const lam_kv_slots& weights,
+                            const lam_kv_slots& positions, const int32_t* first, uint32_t* status);
+lam_status launch_kv_read(lam_ctx* ctx, const lam_kv_view& v, void* k, void* val);
+lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, int64_t q_row, int64_t q_head,
+                            int32_t q_heads, float scale, bool causal, int64_t max_length, const lam_kv_slots& mask,
+                            const lam_kv_slots& weights, void* out, float* lse);
+lam_status launch_kv_evict(lam_ctx* ctx, const lam_kv_view& v, const lam_kv_slots& scores,
+                           const lam_kv_slots& positions, int32_t budget, int32_t recent, int32_t sinks,
+                           int32_t* kept, const lam_kv_slots& scores_out, const lam_kv_slots& positions_out,
+                           int32_t* lengths_out);
 
 // Empties the band index of a store and puts back the entries of its first
 // keep_rows rows (no-op for a store without a band index).

@@ -56,6 +56,12 @@ __device__ __forceinline__ double wave_sum_f64(double v) {
   return __longlong_as_double((long long)(((unsigned long long)rhi << 32) | rlo));
 }
 
+// The largest of each quad's four values, in all four lanes (which must be active together).
+__device__ __forceinline__ float quad_max_f32(float v) {
+  v = fmaxf(v, __int_as_float(LAM_DPP_MOVE(__float_as_int(v), __float_as_int(v), 0xb1, 0xf)));
+  return fmaxf(v, __int_as_float(LAM_DPP_MOVE(__float_as_int(v), __float_as_int(v), 0x4e, 0xf)));
+}
+
 #undef LAM_DPP_MOVE
 #undef LAM_WAVE_DPP_STEPS
 
