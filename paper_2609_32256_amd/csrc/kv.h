@@ -35,6 +35,11 @@ struct KvLayout {
   }
 };
 
+// The caller's index arrays do not change while a kernel reads them: through the
+// constant address space, entries that a whole wave shares are scalar loads.
+typedef const int32_t __attribute__((address_space(4)))* kv_const_i32;
+__device__ __forceinline__ kv_const_i32 kv_const(const int32_t* p) { return (kv_const_i32)(uintptr_t)p; }
+
 struct KvArgs {
   uint8_t* pages;
   int64_t n_pages;
@@ -72,7 +77,7 @@ struct KvArgs {
   // cached tokens of sequence s that the table has columns for
   __device__ int length(int s) const {
     const int64_t cap = (int64_t)table_cols << page_shift;
-    const int l = lengths[s];
+    const int l = kv_const(lengths)[s];
     return l < 0 ? 0 : (l > cap ? (int)cap : l);
   }
   // page of column c of sequence s, or -1

@@ -38,6 +38,7 @@ constexpr int kAttRows = 16;
 // within float16, and those 2^-21 below the maximum are still normal numbers.
 constexpr float kLift = 7.0f, kSpan = 15.0f;
 constexpr float kNoMax = -3.0e38f;   // no token seen yet
+constexpr int64_t kKeptBytes = 1LL << 30;   // most scratch for kept scores
 
 struct AttendArgs {
   KvArgs c;
@@ -54,6 +55,8 @@ struct AttendArgs {
   uint16_t* out;
   float* lse;             // natural logarithm, the caller's
   float* lse2;            // base 2, for the weights
+  float* kept;            // scores of every row's tokens, base 2: [row * q_heads + head][kept_cols], or null
+  int64_t kept_cols;
   float* part_m;          // [row * q_heads + head][splits]
   float* part_l;
   float* part_o;          // [row * q_heads + head][splits][D]
@@ -69,27 +72,48 @@ struct TileRows {
   int len, end_full; // cached tokens, cut and not
 };
 
-__device__ __forceinline__ TileRows tile_rows(const AttendArgs& a, int64_t t) {
+__device__ __forceinline__ TileRows tile_rows(const AttendArgs& a, uint32_t t) {
   TileRows w;
+  int64_t next;
+  int length;
   if (!a.c.starts) {
-    w.s = (int)(t / a.tiles_per_seq);
-    w.r0 = (int)(t % a.tiles_per_seq) * kAttRows;
+    const uint32_t per = (uint32_t)a.tiles_per_seq;
+    w.s = (int)(t / per);
+    w.r0 = (int)(t % per) * kAttRows;
+    w.first = (int64_t)w.s * a.c.per_seq;
+    next = w.first + a.c.per_seq;
+    length = a.c.length(w.s);
   } else {
-    // sequence s has its tiles from floor(start(s) * group / 16) + s on, a bound
-    // that leaves room for every partial tile and that a search can use
-    int lo = 0, hi = a.c.n_seqs;
-    while (hi - lo > 1) {
-      const int m = (lo + hi) >> 1;
-      if (a.c.start(m) * a.group / kAttRows + m <= t) lo = m; else hi = m;
+    // Sequence s has its tiles from floor(start(s) * group / 16) + s on, a bound that
+    // leaves room for every partial tile and rises with s: the last s whose bound
+    // is at most t is found by all lanes at once, 64 sequences a step, each lane
+    // with its sequence's rows and length in hand (a search by halves had cost a
+    // round trip to memory for each step).
+    const int lane = threadIdx.x & 63;
+    w.s = 0;
+    w.r0 = -1;
+    w.first = next = 0;
+    length = 0;
+    for (int b = 0; b < a.c.n_seqs; b += 64) {
+      const int s = min(b + lane, a.c.n_seqs - 1);
+      const int64_t s0 = a.c.start(s), s1 = a.c.start(s + 1);
+      const int l = a.c.length(s);
+      const uint32_t at = (uint32_t)(s0 * a.group / kAttRows) + (uint32_t)s;
+      const unsigned long long in = __ballot(b + lane < a.c.n_seqs && at <= t);
+      if (in == 0) break;
+      const int last = (int)__popcll(in) - 1;
+      w.s = b + last;
+      w.first = (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)s0, last);
+      next = (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)s1, last);
+      length = __builtin_amdgcn_readlane(l, last);
+      w.r0 = (int)min((t - (uint32_t)__builtin_amdgcn_readlane((int)at, last)) * (uint32_t)kAttRows, 0x7fffff00u);
+      if (last < 63) break;
     }
-    w.s = lo;
-    w.r0 = (int)min((t - (a.c.start(lo) * a.group / kAttRows + lo)) * kAttRows, (int64_t)0x7fffff00);
   }
-  w.first = a.c.start(w.s);
-  w.n = (int)max((int64_t)0, a.c.start(w.s + 1) - w.first);
+  w.n = (int)max((int64_t)0, next - w.first);
   w.pairs = w.n * a.group;
-  w.end_full = a.c.length(w.s);
-  w.len = (int)min((int64_t)w.end_full, a.cut);
+  w.end_full = length;
+  w.len = (int)min((int64_t)length, a.cut);
   if (w.r0 < 0 || w.r0 >= w.pairs) w.s = -1;
   return w;
 }
@@ -101,7 +125,8 @@ __device__ __forceinline__ int pair_end(const AttendArgs& a, const TileRows& w, 
 }
 
 // B operands of the 16 query rows: lane (c, g) holds channels g D/4 + 8 j + 0..7
-// of pair r0 + c as step j.
+// of pair r0 + c as step j.  Columns past the last pair repeat it; nothing of
+// theirs is written.
 template <int D>
 __device__ __forceinline__ void load_q(const AttendArgs& a, const TileRows& w, int h, int r0, uint4 q[D / 32]) {
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
@@ -109,18 +134,17 @@ __device__ __forceinline__ void load_q(const AttendArgs& a, const TileRows& w, i
   const int rr = min(r, w.pairs - 1);
   const uint16_t* p =
       a.q + (w.first + rr / a.group) * a.q_row + (int64_t)(h * a.group + rr % a.group) * a.q_head + g * (D / 4);
+  if (a.q_wide) {
 #pragma unroll
-  for (int j = 0; j < D / 32; ++j) {
-    uint4 u;
-    if (a.q_wide) {
-      u = *reinterpret_cast<const uint4*>(p + 8 * j);
-    } else {
+    for (int j = 0; j < D / 32; ++j) q[j] = *reinterpret_cast<const uint4*>(p + 8 * j);
+  } else {
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j) {
       uint32_t x[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) x[i] = (uint32_t)p[8 * j + 2 * i] | ((uint32_t)p[8 * j + 2 * i + 1] << 16);
-      u = uint4{x[0], x[1], x[2], x[3]};
+      q[j] = uint4{x[0], x[1], x[2], x[3]};
     }
-    q[j] = r < w.pairs ? u : uint4{0, 0, 0, 0};
   }
 }
 
@@ -139,57 +163,83 @@ struct Codes {
   uint32_t s[2];
 };
 
+// Loads of a strip go through a buffer resource over its head's part of the page:
+// one of no bytes stands for a strip past the end or a page outside the pool and
+// reads as zeros without touching memory, so no load hangs on a branch and the
+// compiler can count those in flight.  Codes are read once and marked so
+// (non-temporal: 199 -> 173 us for eight sequences of 131,072 tokens, 6.6 TB/s).
+constexpr int kNonTemporal = 2;
+
+// The codes and the scales of a strip at token t of a page: resources whose base
+// is the strip's, so that what a lane adds is constant.
+struct StripRsrc {
+  __amdgpu_buffer_rsrc_t codes, scales;
+};
+
 template <int D>
-__device__ __forceinline__ void load_words(const uint8_t* p, uint32_t w[D / 32]) {
+__device__ __forceinline__ StripRsrc strip_rsrc(uint8_t* head, int T, int t, bool ok) {
+  const int bytes = ok ? (int)KvLayout<D>::head_bytes(T) : 0;
+  return StripRsrc{__builtin_amdgcn_make_buffer_rsrc(head + t * (D / 2), (short)0, bytes, 0x00020000),
+                   __builtin_amdgcn_make_buffer_rsrc(head + T * D + t * (D / 32), (short)0, bytes, 0x00020000)};
+}
+
+template <int D>
+__device__ __forceinline__ void load_words(__amdgpu_buffer_rsrc_t rs, uint32_t at, uint32_t w[D / 32]) {
   if constexpr (D == 64) {
-    const uint2 u = *reinterpret_cast<const uint2*>(p);
+    const uint2 u = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(rs, at, 0, kNonTemporal));
     w[0] = u.x, w[1] = u.y;
   } else {
 #pragma unroll
     for (int j = 0; j < D / 128; ++j) {
-      const uint4 u = *reinterpret_cast<const uint4*>(p + 16 * j);
+      const uint4 u = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rs, at + 16 * j, 0, kNonTemporal));
       w[4 * j] = u.x, w[4 * j + 1] = u.y, w[4 * j + 2] = u.z, w[4 * j + 3] = u.w;
     }
   }
 }
 
-// Keys: tile kt of a strip, token t + 16 kt + c, the lane's quarter of the channels.
+// Where a lane's codes and scales lie from a strip's bases on.
 template <int D>
-__device__ __forceinline__ void load_keys(const uint8_t* page, int T, int t, Codes<D>& k) {
-  using L = KvLayout<D>;
-  const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+struct LaneAt {
+  uint32_t k, ks, shift, v, vs;
+  __device__ __forceinline__ explicit LaneAt(int T) {
+    const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+    k = c * (D / 2) + g * (D / 8);
+    // the word that holds the lane's scale bytes, and their place in it
+    const int b = c * (D / 32) + (D == 64 ? g >> 1 : D == 128 ? g : 2 * g);
+    ks = b & ~3;
+    shift = (b & 3) * 8;
+    v = T * (D / 2) + (g * 16 + c) * (D / 8);
+    vs = T * (D / 32) + (g * (D / 32) + c * (D / 16) / kKvBlock) * 4;
+  }
+};
+
+// Keys: tile kt of a strip, token 16 kt + c, the lane's quarter of the channels.
+template <int D>
+__device__ __forceinline__ void load_keys(const StripRsrc& rs, const LaneAt<D>& at, Codes<D>& k) {
 #pragma unroll
   for (int kt = 0; kt < 2; ++kt) {
-    const int tt = t + 16 * kt + c;
-    load_words<D>(page + L::k_codes(tt) + g * (D / 8), k.w[kt]);
-    const uint8_t* s = page + L::k_scales(T, tt);
-    if constexpr (D == 64) k.s[kt] = s[g >> 1];
-    else if constexpr (D == 128) k.s[kt] = s[g];
-    else k.s[kt] = *reinterpret_cast<const uint16_t*>(s + 2 * g);
+    load_words<D>(rs.codes, at.k + 16 * kt * (D / 2), k.w[kt]);
+    k.s[kt] = __builtin_amdgcn_raw_buffer_load_b32(rs.scales, at.ks + 16 * kt * (D / 32), 0, 0);
   }
 }
 
-// Values: half `half` of a strip, tokens t + 16 half + 4 g + 0..3, run c of the channels.
+// Values: half `half` of a strip, tokens 16 half + 4 g + 0..3, run c of the channels.
 template <int D>
-__device__ __forceinline__ void load_vals(const uint8_t* page, int T, int t, Codes<D>& v) {
-  using L = KvLayout<D>;
-  const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+__device__ __forceinline__ void load_vals(const StripRsrc& rs, const LaneAt<D>& at, Codes<D>& v) {
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
-    const int tt = t + 16 * half + 4 * g;
-    load_words<D>(page + L::v_codes(T, tt, c), v.w[half]);
-    v.s[half] = *reinterpret_cast<const uint32_t*>(page + L::v_scales(T, tt, c * (D / 16) / kKvBlock));
+    load_words<D>(rs.codes, at.v + 16 * half * (D / 2), v.w[half]);
+    v.s[half] = __builtin_amdgcn_raw_buffer_load_b32(rs.scales, at.vs + 16 * half * (D / 32), 0, 0);
   }
 }
 
 // A operands of a strip's keys times the queries: scores of tokens 16 kt + 4 g + i.
 template <int D, bool BF16>
-__device__ __forceinline__ void key_operand(const Codes<D>& k, int kt, uint4 x[D / 32]) {
+__device__ __forceinline__ void key_operand(const Codes<D>& k, uint32_t shift, int kt, uint4 x[D / 32]) {
+  const uint32_t bytes = k.s[kt] >> shift;
 #pragma unroll
-  for (int j = 0; j < D / 32; ++j) {
-    const uint32_t byte = D == 256 ? (j < 4 ? k.s[kt] & 0xffu : k.s[kt] >> 8) : k.s[kt];
-    x[j] = kv_values8<BF16>(k.w[kt][j], kv_scale(byte));
-  }
+  for (int j = 0; j < D / 32; ++j)
+    x[j] = kv_values8<BF16>(k.w[kt][j], kv_scale((D == 256 && j >= 4 ? bytes >> 8 : bytes) & 0xffu));
 }
 
 // Two values of token TOK (of four) of a half's codes: channels 2 JP and 2 JP + 1 of the run.
@@ -218,20 +268,23 @@ __device__ __forceinline__ void add_values(const Codes<D>& v, const float s[2][4
   }
 }
 
+// Mask of a strip's tokens: lane l reads token t0 + l % 32's byte.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t mask_rsrc(const AttendArgs& a, int s, int h) {
+  const uint8_t* p = static_cast<const uint8_t*>(a.mask.p_dev) + s * a.mask.seq_stride + h * a.mask.head_stride;
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), (short)0, a.mask.cols, 0x00020000);
+}
+
+__device__ __forceinline__ uint32_t load_mask(__amdgpu_buffer_rsrc_t rs, int t0) {
+  return (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(rs, t0 + (threadIdx.x & 31), 0, 0);
+}
+
 // Which of a strip's tokens the lane's query sees: bit 4 half + i for token t0 + 16 half + 4 g + i.
-__device__ __forceinline__ uint32_t seen_bits(const AttendArgs& a, int s, int h, int t0, int end) {
+__device__ __forceinline__ uint32_t seen_bits(bool masked, uint32_t mask_byte, int t0, int end) {
   const int g = (threadIdx.x & 63) >> 4;
-  uint32_t m = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int t = t0 + 16 * (i >> 2) + 4 * g + (i & 3);
-    bool in = t < end;
-    if (a.mask.p_dev)
-      in = in && t < a.mask.cols &&
-           static_cast<const uint8_t*>(a.mask.p_dev)[s * a.mask.seq_stride + h * a.mask.head_stride + t] != 0;
-    m |= (in ? 1u : 0u) << i;
-  }
-  return m;
+  const uint32_t all = masked ? (uint32_t)__ballot(mask_byte != 0) : 0xffffffffu;
+  const int n = min(max(end - t0, 0), 32);
+  const uint32_t in = (all & (n == 32 ? 0xffffffffu : (1u << n) - 1u)) >> (4 * g);
+  return (in & 0xfu) | ((in >> 12) & 0xf0u);
 }
 
 __device__ __forceinline__ uint32_t pack_half(float x, float y) {
@@ -244,54 +297,54 @@ __device__ __forceinline__ uint16_t to_out(float x, bool bf16) {
   return __builtin_bit_cast(uint16_t, (_Float16)x);
 }
 
-template <int D, bool BF16>
-__global__ __launch_bounds__(kAttThreads) void k_kv_attend(AttendArgs a) {
-  constexpr int kRun = D / 16;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
-  int64_t id = blockIdx.x;
-  const int split = (int)(id % a.splits);
-  id /= a.splits;
-  const int h = (int)(id % a.c.heads);
-  const TileRows w = tile_rows(a, id / a.c.heads);
-  if (w.s < 0) return;
-  const int T = 1 << a.c.page_shift;
-  const int64_t head_bytes = KvLayout<D>::head_bytes(T);
+__device__ __forceinline__ float log_sum(float M, float sum) {
+  return sum == 0.0f ? -__builtin_inff() : M + __builtin_amdgcn_logf(sum);
+}
 
-  uint4 q[D / 32];
-  load_q<D>(a, w, h, w.r0, q);
-  const int end = pair_end(a, w, min(w.r0 + c, w.pairs - 1));
-  const int end_first = pair_end(a, w, w.r0), end_last = pair_end(a, w, min(w.r0 + kAttRows, w.pairs) - 1);
+// A strip of a page outside the pool: no scores.
+__device__ __forceinline__ void keep_nothing(float* scores) {
+  const int g = (threadIdx.x & 63) >> 4;
+  const float no = -__builtin_inff();
+  *reinterpret_cast<kv_f4*>(scores + 4 * g) = kv_f4{no, no, no, no};
+  *reinterpret_cast<kv_f4*>(scores + 4 * g + 16) = kv_f4{no, no, no, no};
+}
 
+// The running softmax of 16 query rows over the strips a wave takes.
+template <int D, bool BF16, bool MASK>
+struct Running {
+  static constexpr int kRun = D / 16;
   kv_f4 o[kRun];
+  float m, l;
+
+  __device__ __forceinline__ Running() : m(kNoMax), l(0.0f) {
 #pragma unroll
-  for (int j = 0; j < kRun; ++j) o[j] = kv_f4{0, 0, 0, 0};
-  float m = kNoMax, l = 0.0f;
+    for (int j = 0; j < kRun; ++j) o[j] = kv_f4{0, 0, 0, 0};
+  }
 
-  const int from = split * a.part, to = (int)min((int64_t)from + a.part, (int64_t)end_last);
-  for (int t0 = from + wave * kKvStrip; t0 < to; t0 += kKvStrip * kAttWaves) {
-    const int64_t page = a.c.page(w.s, t0 >> a.c.page_shift);
-    if (page < 0) continue;
-    const uint8_t* base = a.c.head_page(page, h, head_bytes);
-    Codes<D> k, v;
-    load_keys<D>(base, T, t0 & (T - 1), k);
-    load_vals<D>(base, T, t0 & (T - 1), v);
-
+  // One strip at t0; whole: every query sees all of its tokens.  scores: where
+  // the query's scores are kept (null: nowhere), slot by slot.
+  __device__ __forceinline__ void add(const AttendArgs& a, int len, int t0, bool whole, int end, uint32_t mask_byte,
+                                      float* scores, uint32_t shift, const uint4 q[D / 32], const Codes<D>& k, Codes<D>& v) {
+    const int g = (threadIdx.x & 63) >> 4;
     float x[8];
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
       uint4 y[D / 32];
-      key_operand<D, BF16>(k, kt, y);
+      key_operand<D, BF16>(k, shift, kt, y);
       kv_f4 sc{0, 0, 0, 0};
 #pragma unroll
       for (int j = 0; j < D / 32; ++j) sc = mfma<BF16>(y[j], q[j], sc);
 #pragma unroll
       for (int i = 0; i < 4; ++i) x[4 * kt + i] = sc[i] * a.scale2;
     }
-    const bool edge = t0 + kKvStrip > end_first || a.mask.p_dev != nullptr;
-    if (edge) {
-      const uint32_t in = seen_bits(a, w.s, h, t0, end);
+    if (!whole) {
+      const uint32_t in = seen_bits(MASK, mask_byte, t0, end);
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] = (in >> i) & 1u ? x[i] : -__builtin_inff();
+    }
+    if (scores) {
+      *reinterpret_cast<kv_f4*>(scores + t0 + 4 * g) = kv_f4{x[0], x[1], x[2], x[3]};
+      *reinterpret_cast<kv_f4*>(scores + t0 + 4 * g + 16) = kv_f4{x[4], x[5], x[6], x[7]};
     }
     float top = x[0];
 #pragma unroll
@@ -318,12 +371,12 @@ __global__ __launch_bounds__(kAttThreads) void k_kv_attend(AttendArgs a) {
     for (int half = 0; half < 2; ++half)
 #pragma unroll
       for (int i = 0; i < 4; ++i) s[half][i] = kv_scale((v.s[half] >> (8 * i)) & 0xffu);
-    if (t0 + kKvStrip > w.len) {   // memory past the last token may hold anything: 0 times it must be 0
+    if (t0 + kKvStrip > len) {   // memory past the last token may hold anything: 0 times it must be 0
 #pragma unroll
       for (int half = 0; half < 2; ++half)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (t0 + 16 * half + 4 * g + i >= w.len) {
+          if (t0 + 16 * half + 4 * g + i >= len) {
             s[half][i] = 1.0f;
 #pragma unroll
             for (int b = i * (D / 32); b < (i + 1) * (D / 32); ++b) v.w[half][b >> 2] &= ~(0xffu << (8 * (b & 3)));
@@ -331,6 +384,76 @@ __global__ __launch_bounds__(kAttThreads) void k_kv_attend(AttendArgs a) {
     }
     add_values<D, 0>(v, s, pb, o);
   }
+};
+
+template <int D, bool BF16, bool MASK>
+__global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : 3) void k_kv_attend(AttendArgs a) {
+  constexpr int kRun = D / 16;
+  const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t id = blockIdx.x / (uint32_t)a.splits;
+  const int split = (int)(blockIdx.x % (uint32_t)a.splits);
+  const int h = (int)(id % (uint32_t)a.c.heads);
+  const TileRows w = tile_rows(a, id / (uint32_t)a.c.heads);
+  if (w.s < 0) return;
+  const int T = 1 << a.c.page_shift;
+  const int64_t head_bytes = KvLayout<D>::head_bytes(T);
+
+  const int end = pair_end(a, w, min(w.r0 + c, w.pairs - 1));
+  const int end_first = pair_end(a, w, w.r0), end_last = pair_end(a, w, min(w.r0 + kAttRows, w.pairs) - 1);
+  const int from = split * a.part, to = (int)min((int64_t)from + a.part, (int64_t)end_last);
+  const int whole_to = MASK ? -1 : end_first - kKvStrip;   // strips up to here are seen whole
+
+  // Strips at t0, t0 + 128, ...: kAhead strips' codes are on their way while one
+  // is taken in, and the page of the next to load is read from the table before.
+  constexpr int kStep = kKvStrip * kAttWaves, kAhead = D == 256 ? 1 : 2, kBufs = kAhead + 1;
+  const LaneAt<D> at(T);
+  Codes<D> k[kBufs], v[kBufs];
+  uint32_t mb[kBufs] = {};
+  bool ok[kBufs];
+  const __amdgpu_buffer_rsrc_t mrs = mask_rsrc(a, w.s, h);
+  // Entries of the table are scalar loads, held as they come until they are
+  // needed: a vector load, or a test of one at once, would wait for every strip
+  // that is on its way.
+  const kv_const_i32 entries = kv_const(a.c.table + (int64_t)w.s * a.c.table_stride);
+  const int last_col = max(a.c.table_cols - 1, 0);
+  auto entry = [&](int t) { return entries[min(t >> a.c.page_shift, last_col)]; };
+  auto load = [&](int b, int32_t page, int t) {
+    ok[b] = t < to && page >= 0 && page < a.c.n_pages;
+    const StripRsrc rs = strip_rsrc<D>(a.c.head_page(ok[b] ? page : 0, h, head_bytes), T, t & (T - 1), ok[b]);
+    load_keys<D>(rs, at, k[b]);
+    load_vals<D>(rs, at, v[b]);
+    if constexpr (MASK) mb[b] = load_mask(mrs, t);   // (a byte load's result is moved, so waited for, each round)
+  };
+  uint4 q[D / 32];
+  load_q<D>(a, w, h, w.r0, q);
+  int t0 = from + wave * kKvStrip;
+  int32_t pages[kAhead + 1];
+#pragma unroll
+  for (int i = 0; i <= kAhead; ++i) pages[i] = entry(t0 + i * kStep);
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) load(i, pages[i], t0 + i * kStep);
+  int32_t next = pages[kAhead];
+  float* scores = nullptr;
+  if (a.kept && w.r0 + c < w.pairs) {
+    const int r = w.r0 + c;
+    scores = a.kept + ((w.first + r / a.group) * a.q_heads + h * a.group + r % a.group) * a.kept_cols;
+  }
+  Running<D, BF16, MASK> r;
+  while (t0 < to) {
+#pragma unroll
+    for (int i = 0; i < kBufs; ++i) {
+      if (t0 >= to) break;
+      const int32_t page = next;
+      next = entry(t0 + (kAhead + 1) * kStep);
+      load((i + kAhead) % kBufs, page, t0 + kAhead * kStep);
+      if (ok[i]) r.add(a, w.len, t0, t0 <= whole_to, end, mb[i], scores, at.shift, q, k[i], v[i]);
+      else if (scores) keep_nothing(scores + t0);
+      t0 += kStep;
+    }
+  }
+  float m = r.m, l = r.l;
+  kv_f4(&o)[kRun] = r.o;
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
 
@@ -349,8 +472,8 @@ __global__ __launch_bounds__(kAttThreads) void k_kv_attend(AttendArgs a) {
           kv_f4{o[j][i], o[j + 1][i], o[j + 2][i], o[j + 3][i]};
   __syncthreads();
   const int col = threadIdx.x >> 4, run = threadIdx.x & 15;
-  const int r = w.r0 + col;
-  if (r >= w.pairs) return;
+  const int pair = w.r0 + col;
+  if (pair >= w.pairs) return;
   float M = sm[0][col];
 #pragma unroll
   for (int i = 1; i < kAttWaves; ++i) M = fmaxf(M, sm[i][col]);
@@ -367,9 +490,9 @@ __global__ __launch_bounds__(kAttThreads) void k_kv_attend(AttendArgs a) {
 #pragma unroll
     for (int i = 0; i < kAttWaves; ++i) acc[j] += f[i] * so[i][col][run * kRun + j];
   }
-  const int64_t at = (w.first + r / a.group) * a.q_heads + h * a.group + r % a.group;
+  const int64_t row = (w.first + pair / a.group) * a.q_heads + h * a.group + pair % a.group;
   if (a.splits > 1) {
-    const int64_t p = at * a.splits + split;
+    const int64_t p = row * a.splits + split;
     if (run == 0) {
       a.part_m[p] = M;
       a.part_l[p] = sum;
@@ -380,7 +503,7 @@ __global__ __launch_bounds__(kAttThreads) void k_kv_attend(AttendArgs a) {
     return;
   }
   const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-  uint16_t* d = a.out + at * D + run * kRun;
+  uint16_t* d = a.out + row * D + run * kRun;
 #pragma unroll
   for (int j = 0; j < kRun; j += 4) {
     uint2 u;
@@ -389,41 +512,104 @@ __global__ __launch_bounds__(kAttThreads) void k_kv_attend(AttendArgs a) {
     *reinterpret_cast<uint2*>(d + j) = u;
   }
   if (run == 0) {
-    const float e = sum == 0.0f ? -__builtin_inff() : M + __builtin_amdgcn_logf(sum);
-    if (a.lse2) a.lse2[at] = e;
-    if (a.lse) a.lse[at] = e * 0.6931471805599453f;
+    const float e = log_sum(M, sum);
+    if (a.lse2) a.lse2[row] = e;
+    if (a.lse) a.lse[row] = e * 0.6931471805599453f;
   }
+}
+
+// Maximum and sum of a row over the parts of the length: f, 2^(m - M) of part i.
+__device__ __forceinline__ float joined(const AttendArgs& a, int64_t at, float* sum) {
+  const float* pm = a.part_m + at * a.splits;
+  const float* pl = a.part_l + at * a.splits;
+  float M = kNoMax, total = 0.0f;
+  for (int i = 0; i < a.splits; ++i) M = fmaxf(M, pm[i]);
+  for (int i = 0; i < a.splits; ++i) total += __builtin_amdgcn_exp2f(pm[i] - M) * pl[i];
+  *sum = total;
+  return M;
 }
 
 // Joins the parts of the length: D/4 lanes per query row and head.
 template <int D, bool BF16>
-__global__ __launch_bounds__(kAttThreads) void k_kv_join(AttendArgs a) {
+__device__ __forceinline__ void join_rows(const AttendArgs& a, uint32_t block) {
   constexpr int kLanes = D / 4;
-  const int64_t at = (int64_t)blockIdx.x * (kAttThreads / kLanes) + threadIdx.x / kLanes;
+  const int64_t at = (int64_t)block * (kAttThreads / kLanes) + threadIdx.x / kLanes;
   const int sub = threadIdx.x % kLanes;
   if (at >= a.c.rows * a.q_heads) return;
-  if (a.c.starts && a.c.seq_of(at / a.q_heads) < 0) return;   // a row of no sequence: no part was written
-  const float* pm = a.part_m + at * a.splits;
-  const float* pl = a.part_l + at * a.splits;
-  float M = kNoMax;
-  for (int i = 0; i < a.splits; ++i) M = fmaxf(M, pm[i]);
-  float sum = 0.0f;
-  kv_f4 acc{0, 0, 0, 0};
-  for (int i = 0; i < a.splits; ++i) {
-    const float f = __builtin_amdgcn_exp2f(pm[i] - M);
-    sum += f * pl[i];
-    acc += f * *reinterpret_cast<const kv_f4*>(a.part_o + (at * a.splits + i) * D + 4 * sub);
+  if (a.c.starts) {   // a row of no sequence: no part was written
+    const int64_t row = at / a.q_heads;
+    if (row < a.c.start(0) || row >= a.c.start(a.c.n_seqs)) return;
   }
+  float sum;
+  const float M = joined(a, at, &sum);
+  kv_f4 acc{0, 0, 0, 0};
+  for (int i = 0; i < a.splits; ++i)
+    acc += __builtin_amdgcn_exp2f(a.part_m[at * a.splits + i] - M) *
+           *reinterpret_cast<const kv_f4*>(a.part_o + (at * a.splits + i) * D + 4 * sub);
   const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
   uint2 u;
   u.x = (uint32_t)to_out(acc[0] * inv, BF16) | ((uint32_t)to_out(acc[1] * inv, BF16) << 16);
   u.y = (uint32_t)to_out(acc[2] * inv, BF16) | ((uint32_t)to_out(acc[3] * inv, BF16) << 16);
   *reinterpret_cast<uint2*>(a.out + at * D + 4 * sub) = u;
   if (sub == 0) {
-    const float e = sum == 0.0f ? -__builtin_inff() : M + __builtin_amdgcn_logf(sum);
+    const float e = log_sum(M, sum);
     if (a.lse2) a.lse2[at] = e;
     if (a.lse) a.lse[at] = e * 0.6931471805599453f;
   }
+}
+
+// Weights from the scores that the attention kept: a workgroup takes 1,024 tokens of one
+// head, four a thread, and sums p = 2^(s - lse) over the sequence's rows in their order.
+constexpr int kKeptTokens = 4 * kAttThreads;
+
+__device__ __forceinline__ void add_kept(const AttendArgs& a, uint32_t block) {
+  const uint32_t chunks = (uint32_t)(a.kept_cols / kKeptTokens);
+  const int t = (int)(block % chunks) * kKeptTokens + 4 * (int)threadIdx.x;
+  const int h = (int)(block / chunks % (uint32_t)a.c.heads), s = (int)(block / chunks / (uint32_t)a.c.heads);
+  const int64_t first = a.c.start(s);
+  const int n = (int)max((int64_t)0, a.c.start(s + 1) - first), full = a.c.length(s);
+  const int len = (int)min((int64_t)full, a.cut), pairs = n * a.group;
+  __shared__ float lse[kAttRows];
+  kv_f4 w{0, 0, 0, 0};
+  for (int r0 = 0; r0 < pairs; r0 += kAttRows) {
+    const int rows = min(pairs - r0, kAttRows);
+    __syncthreads();
+    if ((int)threadIdx.x < rows) {
+      const int r = r0 + (int)threadIdx.x;
+      const int64_t at = (first + r / a.group) * a.q_heads + h * a.group + r % a.group;
+      float e;
+      if (a.splits > 1) {
+        float sum;
+        const float M = joined(a, at, &sum);
+        e = log_sum(M, sum);
+      } else {
+        e = a.lse2[at];
+      }
+      lse[threadIdx.x] = e == -__builtin_inff() ? __builtin_inff() : e;   // no token: 2^(-inf) each
+    }
+    __syncthreads();
+    for (int j = 0; j < rows; ++j) {
+      // whole strips up to the row's last token were kept, others not
+      const int i = (r0 + j) / a.group, last = a.causal ? min(len, full - n + i + 1) : len;
+      if (t >= last) continue;
+      const int64_t at = (first + i) * a.q_heads + h * a.group + (r0 + j) % a.group;
+      const kv_f4 x = *reinterpret_cast<const kv_f4*>(a.kept + at * a.kept_cols + t);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] += __builtin_amdgcn_exp2f(x[e] - lse[j]);
+    }
+  }
+  float* d = static_cast<float*>(a.weights.p_dev) + s * a.weights.seq_stride + h * a.weights.head_stride + t;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (t + j < len && t + j < a.weights.cols) d[j] += w[j];
+}
+
+// What follows the attention, in one launch: the parts joined, the kept scores made weights.
+template <int D, bool BF16>
+__global__ __launch_bounds__(kAttThreads) void k_kv_finish(AttendArgs a, uint32_t join_blocks) {
+  const uint32_t b = blockIdx.x;
+  if (b < join_blocks) join_rows<D, BF16>(a, b);
+  else add_kept(a, b - join_blocks);
 }
 
 // Accumulated weights: a wave owns 32 tokens of one head, whose keys it converts
@@ -431,14 +617,14 @@ __global__ __launch_bounds__(kAttThreads) void k_kv_join(AttendArgs a) {
 // wave in the order of the rows, so the result does not depend on timing.
 template <int D, bool BF16>
 __global__ __launch_bounds__(kAttThreads) void k_kv_weights(AttendArgs a) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
-  int64_t id = blockIdx.x;
-  const int64_t chunks = (a.cut + kKvStrip * kAttWaves - 1) / (kKvStrip * kAttWaves);
-  const int t0 = (int)(id % chunks) * (kKvStrip * kAttWaves) + wave * kKvStrip;
-  id /= chunks;
-  const int h = (int)(id % a.c.heads);
+  const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t chunks = (uint32_t)((a.cut + kKvStrip * kAttWaves - 1) / (kKvStrip * kAttWaves));
+  const int t0 = (int)(blockIdx.x % chunks) * (kKvStrip * kAttWaves) + wave * kKvStrip;
+  const uint32_t id = blockIdx.x / chunks;
+  const int h = (int)(id % (uint32_t)a.c.heads);
   TileRows w;
-  w.s = (int)(id / a.c.heads);
+  w.s = (int)(id / (uint32_t)a.c.heads);
   w.first = a.c.start(w.s);
   w.n = (int)max((int64_t)0, a.c.start(w.s + 1) - w.first);
   w.pairs = w.n * a.group;
@@ -448,11 +634,13 @@ __global__ __launch_bounds__(kAttThreads) void k_kv_weights(AttendArgs a) {
   const int T = 1 << a.c.page_shift;
   const int64_t page = a.c.page(w.s, t0 >> a.c.page_shift);
   if (page < 0) return;
+  const LaneAt<D> at(T);
   Codes<D> k;
-  load_keys<D>(a.c.head_page(page, h, KvLayout<D>::head_bytes(T)), T, t0 & (T - 1), k);
+  load_keys<D>(strip_rsrc<D>(a.c.head_page(page, h, KvLayout<D>::head_bytes(T)), T, t0 & (T - 1), true), at, k);
+  const uint32_t mb = a.mask.p_dev ? load_mask(mask_rsrc(a, w.s, h), t0) : 0u;
   uint4 y[2][D / 32];
-  key_operand<D, BF16>(k, 0, y[0]);
-  key_operand<D, BF16>(k, 1, y[1]);
+  key_operand<D, BF16>(k, at.shift, 0, y[0]);
+  key_operand<D, BF16>(k, at.shift, 1, y[1]);
   float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
   // with a causal limit the first row that sees token t0 is row t0 - (end_full - n)
   int r0 = a.causal ? max(0, t0 - (w.end_full - w.n)) * a.group / kAttRows * kAttRows : 0;
@@ -462,7 +650,8 @@ __global__ __launch_bounds__(kAttThreads) void k_kv_weights(AttendArgs a) {
     const int r = r0 + c, rr = min(r, w.pairs - 1);
     const float e = a.lse2[(w.first + rr / a.group) * a.q_heads + h * a.group + rr % a.group];
     const int end = pair_end(a, w, rr);
-    const uint32_t in = r < w.pairs && e > -__builtin_inff() ? seen_bits(a, w.s, h, t0, end) : 0u;
+    const uint32_t bits = seen_bits(a.mask.p_dev, mb, t0, end);
+    const uint32_t in = r < w.pairs && e > -__builtin_inff() ? bits : 0u;
     const uint32_t nan = r < w.pairs && e != e ? 0xffu : 0u;
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
@@ -499,6 +688,7 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
                             const lam_kv_slots& weights, void* out, float* lse) {
   AttendArgs a{};
   a.c = KvArgs::of(v);
+  if (v.table_cols == 0) a.c.table = v.lengths_dev, a.c.table_stride = 0;   // never used, but read ahead of the length
   a.q = static_cast<const uint16_t*>(q);
   a.q_row = q_row;
   a.q_head = q_head;
@@ -509,6 +699,8 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
   a.scale2 = (float)((double)scale * 1.4426950408889634);
   a.cut = (int64_t)v.table_cols * v.page_size;
   if (max_length > 0) a.cut = std::min(a.cut, max_length);
+  if (v.n_pages == 0) a.cut = 0;
+
   a.mask = mask;
   a.weights = weights;
   a.out = static_cast<uint16_t*>(out);
@@ -525,16 +717,27 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
   // with less than a strip for each wave
   const int64_t units = tiles * v.kv_heads;
   const int64_t strips = std::max<int64_t>(1, (a.cut + kKvStrip * kAttWaves - 1) / (kKvStrip * kAttWaves));
-  const int64_t want = std::min<int64_t>(strips, std::max<int64_t>(1, 1024 / units));
+  const int64_t want = std::min<int64_t>(strips, std::max<int64_t>(1, 768 / units));
   const int64_t per = (strips + want - 1) / want;
   a.part = (int)(per * kKvStrip * kAttWaves);
   a.splits = (int)((strips + per - 1) / per);
 
+  // Weights: from scores that the attention keeps (8 bytes a row and token, written
+  // and read) where sequences have a tile of rows on average, else from a second
+  // pass over the keys.
   const int64_t pairs = v.rows * q_heads;
   const int64_t parts = a.splits > 1 ? pairs * a.splits : 0;
+  const bool keep = weights.p_dev && v.rows * a.group <= kAttRows * (int64_t)v.n_seqs && pairs * a.cut * 4 <= kKeptBytes;
+  a.kept_cols = (a.cut + kKeptTokens - 1) / kKeptTokens * kKeptTokens;
   DevBuf& buf = ctx->scratch[kScratchKv];
-  LAM_TRY(buf.ensure((size_t)(parts * (v.head_dim + 2) + (weights.p_dev ? pairs : 0)) * 4));
-  a.part_o = buf.as<float>();
+  const int64_t floats = (keep ? pairs * a.kept_cols : 0) + parts * (v.head_dim + 2) + (weights.p_dev ? pairs : 0);
+  LAM_TRY(buf.ensure((size_t)floats * 4));
+  float* at = buf.as<float>();
+  if (keep) {
+    a.kept = at;
+    at += pairs * a.kept_cols;
+  }
+  a.part_o = at;
   a.part_m = a.part_o + parts * v.head_dim;
   a.part_l = a.part_m + parts;
   if (weights.p_dev) a.lse2 = a.part_l + parts;
@@ -543,22 +746,32 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
   LAM_CHECK(blocks < (1LL << 31), LAM_EINVAL, "too many rows for one launch");
   hipEvent_t e0, e1;
   LAM_TRY(prof_launch_events(ctx, "kv_attend", &e0, &e1));
-#define LAM_GO(D, BF) \
-  hipExtLaunchKernelGGL((k_kv_attend<D, BF>), dim3((unsigned)blocks), dim3(kAttThreads), 0, ctx->stream, e0, e1, 0, a)
+#define LAM_GO(D, BF)                                                                                               \
+  do {                                                                                                              \
+    if (mask.p_dev)                                                                                                 \
+      hipExtLaunchKernelGGL((k_kv_attend<D, BF, true>), dim3((unsigned)blocks), dim3(kAttThreads), 0, ctx->stream,  \
+                            e0, e1, 0, a);                                                                          \
+    else                                                                                                            \
+      hipExtLaunchKernelGGL((k_kv_attend<D, BF, false>), dim3((unsigned)blocks), dim3(kAttThreads), 0, ctx->stream, \
+                            e0, e1, 0, a);                                                                          \
+  } while (0)
   LAM_KV_DISPATCH(v, LAM_GO);
 #undef LAM_GO
   LAM_HIP(hipGetLastError());
-  if (a.splits > 1) {
-    const int64_t per_block = kAttThreads / (v.head_dim / 4);
-    const int64_t jb = (pairs + per_block - 1) / per_block;
-    LAM_TRY(prof_launch_events(ctx, "kv_join", &e0, &e1));
-#define LAM_GO(D, BF) \
-  hipExtLaunchKernelGGL((k_kv_join<D, BF>), dim3((unsigned)jb), dim3(kAttThreads), 0, ctx->stream, e0, e1, 0, a)
+  const int64_t per_block = kAttThreads / (v.head_dim / 4);
+  const int64_t join_blocks = a.splits > 1 ? (pairs + per_block - 1) / per_block : 0;
+  const int64_t kept_blocks = keep ? a.kept_cols / kKeptTokens * v.kv_heads * v.n_seqs : 0;
+  if (join_blocks + kept_blocks > 0) {
+    LAM_CHECK(join_blocks + kept_blocks < (1LL << 31), LAM_EINVAL, "too many rows for one launch");
+    LAM_TRY(prof_launch_events(ctx, "kv_finish", &e0, &e1));
+#define LAM_GO(D, BF)                                                                                               \
+  hipExtLaunchKernelGGL((k_kv_finish<D, BF>), dim3((unsigned)(join_blocks + kept_blocks)), dim3(kAttThreads), 0,     \
+                        ctx->stream, e0, e1, 0, a, (uint32_t)join_blocks)
     LAM_KV_DISPATCH(v, LAM_GO);
 #undef LAM_GO
     LAM_HIP(hipGetLastError());
   }
-  if (weights.p_dev && a.cut > 0) {
+  if (weights.p_dev && !keep && a.cut > 0) {
     const int64_t wb = strips * v.kv_heads * v.n_seqs;
     LAM_CHECK(wb < (1LL << 31), LAM_EINVAL, "too many sequences for one launch");
     LAM_TRY(prof_launch_events(ctx, "kv_weights", &e0, &e1));
