@@ -38,6 +38,7 @@ constexpr int kAttRows = 16;
 // within float16, and those 2^-21 below the maximum are still normal numbers.
 constexpr float kLift = 7.0f, kSpan = 15.0f;
 constexpr float kNoMax = -3.0e38f;   // no token seen yet
+constexpr int kFill = 768;            // workgroups that fill the chip: three a compute unit
 constexpr int64_t kKeptBytes = 1LL << 30;   // most scratch for kept scores
 
 struct AttendArgs {
@@ -50,41 +51,127 @@ struct AttendArgs {
   float scale2;           // scale * log2(e)
   int64_t cut;            // lengths are cut to it
   int tiles_per_seq;      // where every sequence has the same number of rows
-  int splits, part;       // parts of the length, and their tokens (a multiple of kKvStrip * kAttWaves)
+  int split_to;           // workgroups to split the lengths over, 0: none is split
   lam_kv_slots mask, weights;
   uint16_t* out;
   float* lse;             // natural logarithm, the caller's
   float* lse2;            // base 2, for the weights
   float* kept;            // scores of every row's tokens, base 2: [row * q_heads + head][kept_cols], or null
   int64_t kept_cols;
-  float* part_m;          // [row * q_heads + head][splits]
+  float* part_m;          // of workgroup b's row r of its tile: [b][rows of a tile]
   float* part_l;
-  float* part_o;          // [row * q_heads + head][splits][D]
+  float* part_o;          // [b][rows of a tile][D]
 };
 
-// The rows of a tile: tile `t` of the call, in order of sequences.
-struct TileRows {
-  int s;             // sequence, -1: an empty tile
-  int64_t first;     // its first row of the call
-  int n;             // its rows
-  int r0;            // first of the tile's 16 (row, head of the group) pairs, row-major
-  int pairs;         // pairs of the sequence
-  int len, end_full; // cached tokens, cut and not
+// What a workgroup does: a part of the length for a tile of R (row, head of the
+// group) pairs of a sequence and a key/value head.
+struct Work {
+  int s;               // sequence, -1: nothing to do
+  int64_t first;       // its first row of the call
+  int n;               // its rows
+  int pairs;           // its pairs, row-major
+  int len, end_full;   // cached tokens, cut and not
+  int parts, tokens;   // parts of its length, and the tokens of one
+  uint32_t base;       // its first workgroup
+  int h, r0, part;     // head, first pair of the tile, part
 };
 
-__device__ __forceinline__ TileRows tile_rows(const AttendArgs& a, uint32_t t) {
-  TileRows w;
+__device__ __forceinline__ int tiles_of(int pairs, int R) { return (pairs + R - 1) / R; }
+
+// A lane's sequence: its rows, tiles and length.
+struct LaneSeq {
+  int64_t first;
+  int n, tiles, full, len;
+  __device__ __forceinline__ LaneSeq(const AttendArgs& a, int s, int R) {
+    const bool in = s < a.c.n_seqs;
+    const int q = min(s, a.c.n_seqs - 1);
+    first = a.c.start(q);
+    n = in ? (int)max((int64_t)0, a.c.start(q + 1) - first) : 0;
+    full = a.c.length(q);
+    len = (int)min((int64_t)full, a.cut);
+    tiles = tiles_of(n * a.group, R);
+  }
+};
+
+// The workgroups of a call whose lengths are split: every sequence's length is cut
+// into parts of the same number of tokens, chosen from the lengths on the
+// device so that about split_to workgroups with equal parts cover them all
+// (equal parts of the longest length had left a ragged batch's short sequences
+// with empty ones).  The last part of a tile is half full on average, so the parts are for
+// split_to less half the tiles.  All lanes of a wave look at a sequence each.
+// id: a workgroup, or (by_seq) a sequence whose plan is wanted.
+template <int R>
+__device__ __forceinline__ Work plan(const AttendArgs& a, uint32_t id, bool by_seq) {
+  const int lane = threadIdx.x & 63;
+  double tokens = 0.0, units = 0.0;
+  for (int b = 0; b < a.c.n_seqs; b += 64) {
+    const LaneSeq q(a, b + lane, R);
+    tokens += (double)q.tiles * q.len;
+    units += (double)q.tiles;
+  }
+  const float all = (float)wave_sum_f64(tokens) * a.c.heads, half = 0.5f * (float)wave_sum_f64(units) * a.c.heads;
+  constexpr int kGrain = kKvStrip * kAttWaves;
+  const float want = all / fmaxf((float)a.split_to - half, 0.5f * a.split_to) * 1.0001f;
+  Work w;
+  w.s = -1;
+  w.tokens = (int)fminf(floorf(want / kGrain) * kGrain + kGrain, 2147483520.0f);
+  uint32_t before = 0;
+  for (int b = 0; b < a.c.n_seqs; b += 64) {
+    const LaneSeq q(a, b + lane, R);
+    const int parts = max(1, (q.len + w.tokens - 1) / w.tokens);
+    const int even = ((q.len + parts - 1) / parts + kGrain - 1) / kGrain * kGrain;   // its parts made equal
+    const uint32_t mine = (uint32_t)(q.tiles * a.c.heads * parts);
+    uint32_t upto = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const uint32_t o = __shfl_up(upto, d);
+      if (lane >= d) upto += o;
+    }
+    upto += before;
+    const unsigned long long hit =
+        by_seq ? ((uint32_t)b <= id && id < (uint32_t)b + 64u ? 1ull << (id - b) : 0ull) : __ballot(upto > id);
+    if (hit) {
+      const int l = (int)__builtin_ctzll(hit);
+      w.s = b + l;
+      w.first = (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)q.first, l);
+      w.n = __builtin_amdgcn_readlane(q.n, l);
+      w.len = __builtin_amdgcn_readlane(q.len, l);
+      w.end_full = __builtin_amdgcn_readlane(q.full, l);
+      w.parts = __builtin_amdgcn_readlane(parts, l);
+      w.tokens = __builtin_amdgcn_readlane(even, l);
+      w.base = (uint32_t)__builtin_amdgcn_readlane((int)(upto - mine), l);
+      w.pairs = w.n * a.group;
+      const uint32_t in = id - w.base, unit = in / (uint32_t)w.parts;
+      w.part = (int)(in % (uint32_t)w.parts);
+      w.h = (int)(unit % (uint32_t)a.c.heads);
+      w.r0 = (int)(unit / (uint32_t)a.c.heads) * R;
+      break;
+    }
+    before = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+  }
+  return w;
+}
+
+// The workgroup's work where no length is split: heads innermost, then tiles.
+template <int R>
+__device__ __forceinline__ Work tile_work(const AttendArgs& a, uint32_t id) {
+  Work w;
+  w.h = (int)(id % (uint32_t)a.c.heads);
+  w.part = 0;
+  w.parts = 1;
+  w.tokens = 0x7fffffff;
+  w.base = 0;
+  const uint32_t t = id / (uint32_t)a.c.heads;
   int64_t next;
-  int length;
   if (!a.c.starts) {
     const uint32_t per = (uint32_t)a.tiles_per_seq;
     w.s = (int)(t / per);
-    w.r0 = (int)(t % per) * kAttRows;
+    w.r0 = (int)(t % per) * R;
     w.first = (int64_t)w.s * a.c.per_seq;
     next = w.first + a.c.per_seq;
-    length = a.c.length(w.s);
+    w.end_full = a.c.length(w.s);
   } else {
-    // Sequence s has its tiles from floor(start(s) * group / 16) + s on, a bound that
+    // Sequence s has its tiles from floor(start(s) * group / R) + s on, a bound that
     // leaves room for every partial tile and rises with s: the last s whose bound
     // is at most t is found by all lanes at once, 64 sequences a step, each lane
     // with its sequence's rows and length in hand (a search by halves had cost a
@@ -93,33 +180,37 @@ __device__ __forceinline__ TileRows tile_rows(const AttendArgs& a, uint32_t t) {
     w.s = 0;
     w.r0 = -1;
     w.first = next = 0;
-    length = 0;
+    w.end_full = 0;
     for (int b = 0; b < a.c.n_seqs; b += 64) {
       const int s = min(b + lane, a.c.n_seqs - 1);
       const int64_t s0 = a.c.start(s), s1 = a.c.start(s + 1);
       const int l = a.c.length(s);
-      const uint32_t at = (uint32_t)(s0 * a.group / kAttRows) + (uint32_t)s;
+      const uint32_t at = (uint32_t)(s0 * a.group / R) + (uint32_t)s;
       const unsigned long long in = __ballot(b + lane < a.c.n_seqs && at <= t);
       if (in == 0) break;
       const int last = (int)__popcll(in) - 1;
       w.s = b + last;
       w.first = (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)s0, last);
       next = (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)s1, last);
-      length = __builtin_amdgcn_readlane(l, last);
-      w.r0 = (int)min((t - (uint32_t)__builtin_amdgcn_readlane((int)at, last)) * (uint32_t)kAttRows, 0x7fffff00u);
+      w.end_full = __builtin_amdgcn_readlane(l, last);
+      w.r0 = (int)min((t - (uint32_t)__builtin_amdgcn_readlane((int)at, last)) * (uint32_t)R, 0x7fffff00u);
       if (last < 63) break;
     }
   }
   w.n = (int)max((int64_t)0, next - w.first);
   w.pairs = w.n * a.group;
-  w.end_full = length;
-  w.len = (int)min((int64_t)length, a.cut);
+  w.len = (int)min((int64_t)w.end_full, a.cut);
   if (w.r0 < 0 || w.r0 >= w.pairs) w.s = -1;
   return w;
 }
 
+template <int R>
+__device__ __forceinline__ Work work_of(const AttendArgs& a, uint32_t id) {
+  return a.split_to ? plan<R>(a, id, false) : tile_work<R>(a, id);
+}
+
 // Tokens that pair r of the sequence sees: those below this.
-__device__ __forceinline__ int pair_end(const AttendArgs& a, const TileRows& w, int r) {
+__device__ __forceinline__ int pair_end(const AttendArgs& a, const Work& w, int r) {
   if (!a.causal) return w.len;
   return max(0, min(w.len, w.end_full - w.n + r / a.group + 1));
 }
@@ -128,7 +219,7 @@ __device__ __forceinline__ int pair_end(const AttendArgs& a, const TileRows& w, 
 // of pair r0 + c as step j.  Columns past the last pair repeat it; nothing of
 // theirs is written.
 template <int D>
-__device__ __forceinline__ void load_q(const AttendArgs& a, const TileRows& w, int h, int r0, uint4 q[D / 32]) {
+__device__ __forceinline__ void load_q(const AttendArgs& a, const Work& w, int h, int r0, uint4 q[D / 32]) {
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
   const int r = r0 + c;
   const int rr = min(r, w.pairs - 1);
@@ -301,6 +392,27 @@ __device__ __forceinline__ float log_sum(float M, float sum) {
   return sum == 0.0f ? -__builtin_inff() : M + __builtin_amdgcn_logf(sum);
 }
 
+// A lane's channels of a finished row, and the row's log sums.
+template <int D, bool BF16>
+__device__ __forceinline__ void write_row(const AttendArgs& a, int64_t row, int run, const float acc[D / 16], float M,
+                                          float sum) {
+  constexpr int kRun = D / 16;
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  uint16_t* d = a.out + row * D + run * kRun;
+#pragma unroll
+  for (int j = 0; j < kRun; j += 4) {
+    uint2 u;
+    u.x = (uint32_t)to_out(acc[j] * inv, BF16) | ((uint32_t)to_out(acc[j + 1] * inv, BF16) << 16);
+    u.y = (uint32_t)to_out(acc[j + 2] * inv, BF16) | ((uint32_t)to_out(acc[j + 3] * inv, BF16) << 16);
+    *reinterpret_cast<uint2*>(d + j) = u;
+  }
+  if (run == 0) {
+    const float e = log_sum(M, sum);
+    if (a.lse2) a.lse2[row] = e;
+    if (a.lse) a.lse[row] = e * 0.6931471805599453f;
+  }
+}
+
 // A strip of a page outside the pool: no scores.
 __device__ __forceinline__ void keep_nothing(float* scores) {
   const int g = (threadIdx.x & 63) >> 4;
@@ -391,17 +503,16 @@ __global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : 3) void k_kv_attend(Att
   constexpr int kRun = D / 16;
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t id = blockIdx.x / (uint32_t)a.splits;
-  const int split = (int)(blockIdx.x % (uint32_t)a.splits);
-  const int h = (int)(id % (uint32_t)a.c.heads);
-  const TileRows w = tile_rows(a, id / (uint32_t)a.c.heads);
+  const Work w = work_of<kAttRows>(a, blockIdx.x);
   if (w.s < 0) return;
+  const int h = w.h;
   const int T = 1 << a.c.page_shift;
   const int64_t head_bytes = KvLayout<D>::head_bytes(T);
 
   const int end = pair_end(a, w, min(w.r0 + c, w.pairs - 1));
   const int end_first = pair_end(a, w, w.r0), end_last = pair_end(a, w, min(w.r0 + kAttRows, w.pairs) - 1);
-  const int from = split * a.part, to = (int)min((int64_t)from + a.part, (int64_t)end_last);
+  const int64_t part_at = (int64_t)w.part * w.tokens;
+  const int from = (int)min(part_at, (int64_t)w.len), to = (int)min(part_at + w.tokens, (int64_t)end_last);
   const int whole_to = MASK ? -1 : end_first - kKvStrip;   // strips up to here are seen whole
 
   // Strips at t0, t0 + 128, ...: kAhead strips' codes are on their way while one
@@ -491,8 +602,8 @@ __global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : 3) void k_kv_attend(Att
     for (int i = 0; i < kAttWaves; ++i) acc[j] += f[i] * so[i][col][run * kRun + j];
   }
   const int64_t row = (w.first + pair / a.group) * a.q_heads + h * a.group + pair % a.group;
-  if (a.splits > 1) {
-    const int64_t p = row * a.splits + split;
+  if (w.parts > 1) {
+    const int64_t p = (int64_t)blockIdx.x * kAttRows + col;
     if (run == 0) {
       a.part_m[p] = M;
       a.part_l[p] = sum;
@@ -502,59 +613,46 @@ __global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : 3) void k_kv_attend(Att
     for (int j = 0; j < kRun; j += 4) *reinterpret_cast<kv_f4*>(d + j) = kv_f4{acc[j], acc[j + 1], acc[j + 2], acc[j + 3]};
     return;
   }
-  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-  uint16_t* d = a.out + row * D + run * kRun;
-#pragma unroll
-  for (int j = 0; j < kRun; j += 4) {
-    uint2 u;
-    u.x = (uint32_t)to_out(acc[j] * inv, BF16) | ((uint32_t)to_out(acc[j + 1] * inv, BF16) << 16);
-    u.y = (uint32_t)to_out(acc[j + 2] * inv, BF16) | ((uint32_t)to_out(acc[j + 3] * inv, BF16) << 16);
-    *reinterpret_cast<uint2*>(d + j) = u;
-  }
-  if (run == 0) {
-    const float e = log_sum(M, sum);
-    if (a.lse2) a.lse2[row] = e;
-    if (a.lse) a.lse[row] = e * 0.6931471805599453f;
-  }
+  write_row<D, BF16>(a, row, run, acc, M, sum);
 }
 
-// Maximum and sum of a row over the parts of the length: f, 2^(m - M) of part i.
-__device__ __forceinline__ float joined(const AttendArgs& a, int64_t at, float* sum) {
-  const float* pm = a.part_m + at * a.splits;
-  const float* pl = a.part_l + at * a.splits;
+// Maximum and sum of row `col` of a tile over its parts, the first of which is workgroup `at`'s.
+template <int R>
+__device__ __forceinline__ float joined(const AttendArgs& a, uint32_t at, int col, int parts, float* sum) {
+  const float* pm = a.part_m + (int64_t)at * R + col;
+  const float* pl = a.part_l + (int64_t)at * R + col;
   float M = kNoMax, total = 0.0f;
-  for (int i = 0; i < a.splits; ++i) M = fmaxf(M, pm[i]);
-  for (int i = 0; i < a.splits; ++i) total += __builtin_amdgcn_exp2f(pm[i] - M) * pl[i];
+#pragma unroll 4
+  for (int i = 0; i < parts; ++i) M = fmaxf(M, pm[i * R]);
+#pragma unroll 4
+  for (int i = 0; i < parts; ++i) total += __builtin_amdgcn_exp2f(pm[i * R] - M) * pl[i * R];
   *sum = total;
   return M;
 }
 
-// Joins the parts of the length: D/4 lanes per query row and head.
-template <int D, bool BF16>
+// Joins the parts of a tile: the workgroup that has the place of the tile's first
+// one in the attention; 16 lanes a row, D/16 channels a lane.
+template <int D, bool BF16, int R>
 __device__ __forceinline__ void join_rows(const AttendArgs& a, uint32_t block) {
-  constexpr int kLanes = D / 4;
-  const int64_t at = (int64_t)block * (kAttThreads / kLanes) + threadIdx.x / kLanes;
-  const int sub = threadIdx.x % kLanes;
-  if (at >= a.c.rows * a.q_heads) return;
-  if (a.c.starts) {   // a row of no sequence: no part was written
-    const int64_t row = at / a.q_heads;
-    if (row < a.c.start(0) || row >= a.c.start(a.c.n_seqs)) return;
-  }
-  float sum;
-  const float M = joined(a, at, &sum);
-  kv_f4 acc{0, 0, 0, 0};
-  for (int i = 0; i < a.splits; ++i)
-    acc += __builtin_amdgcn_exp2f(a.part_m[at * a.splits + i] - M) *
-           *reinterpret_cast<const kv_f4*>(a.part_o + (at * a.splits + i) * D + 4 * sub);
-  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-  uint2 u;
-  u.x = (uint32_t)to_out(acc[0] * inv, BF16) | ((uint32_t)to_out(acc[1] * inv, BF16) << 16);
-  u.y = (uint32_t)to_out(acc[2] * inv, BF16) | ((uint32_t)to_out(acc[3] * inv, BF16) << 16);
-  *reinterpret_cast<uint2*>(a.out + at * D + 4 * sub) = u;
-  if (sub == 0) {
-    const float e = log_sum(M, sum);
-    if (a.lse2) a.lse2[at] = e;
-    if (a.lse) a.lse[at] = e * 0.6931471805599453f;
+  constexpr int kRun = D / 16;
+  const Work w = plan<R>(a, block, false);
+  if (w.s < 0 || w.part != 0 || w.parts == 1) return;
+  const int run = threadIdx.x & 15;
+  for (int col = threadIdx.x >> 4; col < R; col += kAttThreads / 16) {
+    const int pair = w.r0 + col;
+    if (pair >= w.pairs) return;
+    float sum;
+    const float M = joined<R>(a, block, col, w.parts, &sum);
+    float acc[kRun] = {};
+    const float* po = a.part_o + ((int64_t)block * R + col) * D + run * kRun;
+#pragma unroll 4
+    for (int i = 0; i < w.parts; ++i) {
+      const float f = __builtin_amdgcn_exp2f(a.part_m[((int64_t)block + i) * R + col] - M);
+#pragma unroll
+      for (int j = 0; j < kRun; ++j) acc[j] += f * po[(int64_t)i * R * D + j];
+    }
+    const int64_t row = (w.first + pair / a.group) * a.q_heads + w.h * a.group + pair % a.group;
+    write_row<D, BF16>(a, row, run, acc, M, sum);
   }
 }
 
@@ -569,46 +667,62 @@ __device__ __forceinline__ void add_kept(const AttendArgs& a, uint32_t block) {
   const int64_t first = a.c.start(s);
   const int n = (int)max((int64_t)0, a.c.start(s + 1) - first), full = a.c.length(s);
   const int len = (int)min((int64_t)full, a.cut), pairs = n * a.group;
+  if ((int)(block % chunks) * kKeptTokens >= len) return;
+  Work q;
+  q.parts = 1;
+  if (a.split_to) q = plan<kAttRows>(a, (uint32_t)s, true);
+  float* d = static_cast<float*>(a.weights.p_dev) + s * a.weights.seq_stride + h * a.weights.head_stride + t;
+  float w[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) w[j] = t + j < min(len, a.weights.cols) ? d[j] : 0.0f;
   __shared__ float lse[kAttRows];
-  kv_f4 w{0, 0, 0, 0};
   for (int r0 = 0; r0 < pairs; r0 += kAttRows) {
-    const int rows = min(pairs - r0, kAttRows);
     __syncthreads();
-    if ((int)threadIdx.x < rows) {
+    if ((int)threadIdx.x < min(pairs - r0, kAttRows)) {
       const int r = r0 + (int)threadIdx.x;
       const int64_t at = (first + r / a.group) * a.q_heads + h * a.group + r % a.group;
       float e;
-      if (a.splits > 1) {
+      if (q.parts > 1) {
         float sum;
-        const float M = joined(a, at, &sum);
+        const uint32_t unit = (uint32_t)(r0 / kAttRows * a.c.heads + h);
+        const float M = joined<kAttRows>(a, q.base + unit * q.parts, threadIdx.x, q.parts, &sum);
         e = log_sum(M, sum);
       } else {
         e = a.lse2[at];
       }
       lse[threadIdx.x] = e == -__builtin_inff() ? __builtin_inff() : e;   // no token: 2^(-inf) each
     }
-    __syncthreads();
-    for (int j = 0; j < rows; ++j) {
-      // whole strips up to the row's last token were kept, others not
-      const int i = (r0 + j) / a.group, last = a.causal ? min(len, full - n + i + 1) : len;
-      if (t >= last) continue;
-      const int64_t at = (first + i) * a.q_heads + h * a.group + (r0 + j) % a.group;
-      const kv_f4 x = *reinterpret_cast<const kv_f4*>(a.kept + at * a.kept_cols + t);
+    // four rows' scores at a time, on their way before the sums are known
+    for (int r = r0; r < min(pairs, r0 + kAttRows); r += 4) {
+      kv_f4 x[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] += __builtin_amdgcn_exp2f(x[e] - lse[j]);
+      for (int j = 0; j < 4; ++j) {
+        // whole strips up to the row's last token were kept, others not
+        const int i = (r + j) / a.group, last = a.causal ? min(len, full - n + i + 1) : len;
+        const int64_t at = (first + i) * a.q_heads + h * a.group + (r + j) % a.group;
+        const float no = -__builtin_inff();
+        x[j] = r + j < pairs && t < last ? *reinterpret_cast<const kv_f4*>(a.kept + at * a.kept_cols + t)
+                                         : kv_f4{no, no, no, no};
+      }
+      if (r == r0) __syncthreads();
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float e = r + j < pairs ? lse[r + j - r0] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] += __builtin_amdgcn_exp2f(x[j][i] - e);
+      }
     }
   }
-  float* d = static_cast<float*>(a.weights.p_dev) + s * a.weights.seq_stride + h * a.weights.head_stride + t;
 #pragma unroll
   for (int j = 0; j < 4; ++j)
-    if (t + j < len && t + j < a.weights.cols) d[j] += w[j];
+    if (t + j < min(len, a.weights.cols)) d[j] = w[j];
 }
 
 // What follows the attention, in one launch: the parts joined, the kept scores made weights.
 template <int D, bool BF16>
 __global__ __launch_bounds__(kAttThreads) void k_kv_finish(AttendArgs a, uint32_t join_blocks) {
   const uint32_t b = blockIdx.x;
-  if (b < join_blocks) join_rows<D, BF16>(a, b);
+  if (b < join_blocks) join_rows<D, BF16, kAttRows>(a, b);
   else add_kept(a, b - join_blocks);
 }
 
@@ -623,7 +737,7 @@ __global__ __launch_bounds__(kAttThreads) void k_kv_weights(AttendArgs a) {
   const int t0 = (int)(blockIdx.x % chunks) * (kKvStrip * kAttWaves) + wave * kKvStrip;
   const uint32_t id = blockIdx.x / chunks;
   const int h = (int)(id % (uint32_t)a.c.heads);
-  TileRows w;
+  Work w;
   w.s = (int)(id / (uint32_t)a.c.heads);
   w.first = a.c.start(w.s);
   w.n = (int)max((int64_t)0, a.c.start(w.s + 1) - w.first);
@@ -713,20 +827,20 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
     a.tiles_per_seq = (int)((v.rows / v.n_seqs * a.group + kAttRows - 1) / kAttRows);
     tiles = (int64_t)a.tiles_per_seq * v.n_seqs;
   }
-  // parts of the length: enough workgroups for four on every compute unit, none
-  // with less than a strip for each wave
+  // Lengths are split where the tiles do not fill the chip: three workgroups of
+  // 256 threads a compute unit.
   const int64_t units = tiles * v.kv_heads;
-  const int64_t strips = std::max<int64_t>(1, (a.cut + kKvStrip * kAttWaves - 1) / (kKvStrip * kAttWaves));
-  const int64_t want = std::min<int64_t>(strips, std::max<int64_t>(1, 768 / units));
-  const int64_t per = (strips + want - 1) / want;
-  a.part = (int)(per * kKvStrip * kAttWaves);
-  a.splits = (int)((strips + per - 1) / per);
+  int64_t blocks = units;
+  if (units < kFill && a.cut > kKvStrip * kAttWaves) {
+    a.split_to = kFill;
+    blocks = kFill + units;   // see plan(): at most split_to - units / 2 (or split_to / 2) full parts, and one more a tile
+  }
 
   // Weights: from scores that the attention keeps (8 bytes a row and token, written
   // and read) where sequences have a tile of rows on average, else from a second
   // pass over the keys.
   const int64_t pairs = v.rows * q_heads;
-  const int64_t parts = a.splits > 1 ? pairs * a.splits : 0;
+  const int64_t parts = a.split_to ? blocks * kAttRows : 0;
   const bool keep = weights.p_dev && v.rows * a.group <= kAttRows * (int64_t)v.n_seqs && pairs * a.cut * 4 <= kKeptBytes;
   a.kept_cols = (a.cut + kKeptTokens - 1) / kKeptTokens * kKeptTokens;
   DevBuf& buf = ctx->scratch[kScratchKv];
@@ -742,7 +856,6 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
   a.part_l = a.part_m + parts;
   if (weights.p_dev) a.lse2 = a.part_l + parts;
 
-  const int64_t blocks = units * a.splits;
   LAM_CHECK(blocks < (1LL << 31), LAM_EINVAL, "too many rows for one launch");
   hipEvent_t e0, e1;
   LAM_TRY(prof_launch_events(ctx, "kv_attend", &e0, &e1));
@@ -758,8 +871,7 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
   LAM_KV_DISPATCH(v, LAM_GO);
 #undef LAM_GO
   LAM_HIP(hipGetLastError());
-  const int64_t per_block = kAttThreads / (v.head_dim / 4);
-  const int64_t join_blocks = a.splits > 1 ? (pairs + per_block - 1) / per_block : 0;
+  const int64_t join_blocks = a.split_to ? blocks : 0;
   const int64_t kept_blocks = keep ? a.kept_cols / kKeptTokens * v.kv_heads * v.n_seqs : 0;
   if (join_blocks + kept_blocks > 0) {
     LAM_CHECK(join_blocks + kept_blocks < (1LL << 31), LAM_EINVAL, "too many rows for one launch");
@@ -772,7 +884,7 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
     LAM_HIP(hipGetLastError());
   }
   if (weights.p_dev && !keep && a.cut > 0) {
-    const int64_t wb = strips * v.kv_heads * v.n_seqs;
+    const int64_t wb = (a.cut + kKvStrip * kAttWaves - 1) / (kKvStrip * kAttWaves) * v.kv_heads * v.n_seqs;
     LAM_CHECK(wb < (1LL << 31), LAM_EINVAL, "too many sequences for one launch");
     LAM_TRY(prof_launch_events(ctx, "kv_weights", &e0, &e1));
 #define LAM_GO(D, BF) \
