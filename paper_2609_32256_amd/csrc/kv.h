@@ -127,4 +127,13 @@ __device__ __forceinline__ uint4 kv_values8(uint32_t word, float scale) {
                kv_values<BF16, 3>(word, scale)};
 }
 
+// Calls LAUNCH with the head size and the type as constants.
+#define LAM_KV_DISPATCH(v, LAUNCH)                                                          \
+  do {                                                                                      \
+    const bool bf_ = (v).dtype == LAM_BF16;                                                 \
+    if ((v).head_dim == 64) { if (bf_) LAUNCH(64, true); else LAUNCH(64, false); }          \
+    else if ((v).head_dim == 128) { if (bf_) LAUNCH(128, true); else LAUNCH(128, false); }  \
+    else { if (bf_) LAUNCH(256, true); else LAUNCH(256, false); }                           \
+  } while (0)
+
 }  // namespace lam

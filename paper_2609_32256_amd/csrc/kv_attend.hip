@@ -21,397 +21,12 @@
 #include <hip/hip_ext.h>
 
 #include <algorithm>
+#include <cmath>
 
-#include "kv.h"
-#include "lam_internal.h"
-#include "wave.h"
+#include "kv_attend.h"
 
 namespace lam {
 namespace {
-
-constexpr int kAttThreads = 256;
-constexpr int kAttWaves = kAttThreads / 64;
-constexpr int kAttRows = 16;
-
-// The reference of a row's exponentials is at least its maximum so far less
-// 2^kSpan and at most 2^-kLift of it when it was set: the weights reach 2^15,
-// within float16, and those 2^-21 below the maximum are still normal numbers.
-constexpr float kLift = 7.0f, kSpan = 15.0f;
-constexpr float kNoMax = -3.0e38f;   // no token seen yet
-constexpr int kFill = 768;            // workgroups that fill the chip: three a compute unit
-constexpr int64_t kKeptBytes = 1LL << 30;   // most scratch for kept scores
-
-struct AttendArgs {
-  KvArgs c;
-  const uint16_t* q;
-  int64_t q_row, q_head;
-  int q_wide;             // every eight channels of q are a 16-byte load
-  int q_heads, group;
-  int causal;
-  float scale2;           // scale * log2(e)
-  int64_t cut;            // lengths are cut to it
-  int tiles_per_seq;      // where every sequence has the same number of rows
-  int split_to;           // workgroups to split the lengths over, 0: none is split
-  lam_kv_slots mask, weights;
-  uint16_t* out;
-  float* lse;             // natural logarithm, the caller's
-  float* lse2;            // base 2, for the weights
-  float* kept;            // scores of every row's tokens, base 2: [row * q_heads + head][kept_cols], or null
-  int64_t kept_cols;
-  float* part_m;          // of workgroup b's row r of its tile: [b][rows of a tile]
-  float* part_l;
-  float* part_o;          // [b][rows of a tile][D]
-};
-
-// What a workgroup does: a part of the length for a tile of R (row, head of the
-// group) pairs of a sequence and a key/value head.
-struct Work {
-  int s;               // sequence, -1: nothing to do
-  int64_t first;       // its first row of the call
-  int n;               // its rows
-  int pairs;           // its pairs, row-major
-  int len, end_full;   // cached tokens, cut and not
-  int parts, tokens;   // parts of its length, and the tokens of one
-  uint32_t base;       // its first workgroup
-  int h, r0, part;     // head, first pair of the tile, part
-};
-
-__device__ __forceinline__ int tiles_of(int pairs, int R) { return (pairs + R - 1) / R; }
-
-// A lane's sequence: its rows, tiles and length.
-struct LaneSeq {
-  int64_t first;
-  int n, tiles, full, len;
-  __device__ __forceinline__ LaneSeq(const AttendArgs& a, int s, int R) {
-    const bool in = s < a.c.n_seqs;
-    const int q = min(s, a.c.n_seqs - 1);
-    first = a.c.start(q);
-    n = in ? (int)max((int64_t)0, a.c.start(q + 1) - first) : 0;
-    full = a.c.length(q);
-    len = (int)min((int64_t)full, a.cut);
-    tiles = tiles_of(n * a.group, R);
-  }
-};
-
-// The workgroups of a call whose lengths are split: every sequence's length is cut
-// into parts of the same number of tokens, chosen from the lengths on the
-// device so that about split_to workgroups with equal parts cover them all
-// (equal parts of the longest length had left a ragged batch's short sequences
-// with empty ones).  The last part of a tile is half full on average, so the parts are for
-// split_to less half the tiles.  All lanes of a wave look at a sequence each.
-// id: a workgroup, or (by_seq) a sequence whose plan is wanted.
-template <int R>
-__device__ __forceinline__ Work plan(const AttendArgs& a, uint32_t id, bool by_seq) {
-  const int lane = threadIdx.x & 63;
-  double tokens = 0.0, units = 0.0;
-  for (int b = 0; b < a.c.n_seqs; b += 64) {
-    const LaneSeq q(a, b + lane, R);
-    tokens += (double)q.tiles * q.len;
-    units += (double)q.tiles;
-  }
-  const float all = (float)wave_sum_f64(tokens) * a.c.heads, half = 0.5f * (float)wave_sum_f64(units) * a.c.heads;
-  constexpr int kGrain = kKvStrip * kAttWaves;
-  const float want = all / fmaxf((float)a.split_to - half, 0.5f * a.split_to) * 1.0001f;
-  Work w;
-  w.s = -1;
-  w.tokens = (int)fminf(floorf(want / kGrain) * kGrain + kGrain, 2147483520.0f);
-  uint32_t before = 0;
-  for (int b = 0; b < a.c.n_seqs; b += 64) {
-    const LaneSeq q(a, b + lane, R);
-    const int parts = max(1, (q.len + w.tokens - 1) / w.tokens);
-    const int even = ((q.len + parts - 1) / parts + kGrain - 1) / kGrain * kGrain;   // its parts made equal
-    const uint32_t mine = (uint32_t)(q.tiles * a.c.heads * parts);
-    uint32_t upto = mine;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const uint32_t o = __shfl_up(upto, d);
-      if (lane >= d) upto += o;
-    }
-    upto += before;
-    const unsigned long long hit =
-        by_seq ? ((uint32_t)b <= id && id < (uint32_t)b + 64u ? 1ull << (id - b) : 0ull) : __ballot(upto > id);
-    if (hit) {
-      const int l = (int)__builtin_ctzll(hit);
-      w.s = b + l;
-      w.first = (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)q.first, l);
-      w.n = __builtin_amdgcn_readlane(q.n, l);
-      w.len = __builtin_amdgcn_readlane(q.len, l);
-      w.end_full = __builtin_amdgcn_readlane(q.full, l);
-      w.parts = __builtin_amdgcn_readlane(parts, l);
-      w.tokens = __builtin_amdgcn_readlane(even, l);
-      w.base = (uint32_t)__builtin_amdgcn_readlane((int)(upto - mine), l);
-      w.pairs = w.n * a.group;
-      const uint32_t in = id - w.base, unit = in / (uint32_t)w.parts;
-      w.part = (int)(in % (uint32_t)w.parts);
-      w.h = (int)(unit % (uint32_t)a.c.heads);
-      w.r0 = (int)(unit / (uint32_t)a.c.heads) * R;
-      break;
-    }
-    before = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
-  }
-  return w;
-}
-
-// The workgroup's work where no length is split: heads innermost, then tiles.
-template <int R>
-__device__ __forceinline__ Work tile_work(const AttendArgs& a, uint32_t id) {
-  Work w;
-  w.h = (int)(id % (uint32_t)a.c.heads);
-  w.part = 0;
-  w.parts = 1;
-  w.tokens = 0x7fffffff;
-  w.base = 0;
-  const uint32_t t = id / (uint32_t)a.c.heads;
-  int64_t next;
-  if (!a.c.starts) {
-    const uint32_t per = (uint32_t)a.tiles_per_seq;
-    w.s = (int)(t / per);
-    w.r0 = (int)(t % per) * R;
-    w.first = (int64_t)w.s * a.c.per_seq;
-    next = w.first + a.c.per_seq;
-    w.end_full = a.c.length(w.s);
-  } else {
-    // Sequence s has its tiles from floor(start(s) * group / R) + s on, a bound that
-    // leaves room for every partial tile and rises with s: the last s whose bound
-    // is at most t is found by all lanes at once, 64 sequences a step, each lane
-    // with its sequence's rows and length in hand (a search by halves had cost a
-    // round trip to memory for each step).
-    const int lane = threadIdx.x & 63;
-    w.s = 0;
-    w.r0 = -1;
-    w.first = next = 0;
-    w.end_full = 0;
-    for (int b = 0; b < a.c.n_seqs; b += 64) {
-      const int s = min(b + lane, a.c.n_seqs - 1);
-      const int64_t s0 = a.c.start(s), s1 = a.c.start(s + 1);
-      const int l = a.c.length(s);
-      const uint32_t at = (uint32_t)(s0 * a.group / R) + (uint32_t)s;
-      const unsigned long long in = __ballot(b + lane < a.c.n_seqs && at <= t);
-      if (in == 0) break;
-      const int last = (int)__popcll(in) - 1;
-      w.s = b + last;
-      w.first = (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)s0, last);
-      next = (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)s1, last);
-      w.end_full = __builtin_amdgcn_readlane(l, last);
-      w.r0 = (int)min((t - (uint32_t)__builtin_amdgcn_readlane((int)at, last)) * (uint32_t)R, 0x7fffff00u);
-      if (last < 63) break;
-    }
-  }
-  w.n = (int)max((int64_t)0, next - w.first);
-  w.pairs = w.n * a.group;
-  w.len = (int)min((int64_t)w.end_full, a.cut);
-  if (w.r0 < 0 || w.r0 >= w.pairs) w.s = -1;
-  return w;
-}
-
-template <int R>
-__device__ __forceinline__ Work work_of(const AttendArgs& a, uint32_t id) {
-  return a.split_to ? plan<R>(a, id, false) : tile_work<R>(a, id);
-}
-
-// Tokens that pair r of the sequence sees: those below this.
-__device__ __forceinline__ int pair_end(const AttendArgs& a, const Work& w, int r) {
-  if (!a.causal) return w.len;
-  return max(0, min(w.len, w.end_full - w.n + r / a.group + 1));
-}
-
-// B operands of the 16 query rows: lane (c, g) holds channels g D/4 + 8 j + 0..7
-// of pair r0 + c as step j.  Columns past the last pair repeat it; nothing of
-// theirs is written.
-template <int D>
-__device__ __forceinline__ void load_q(const AttendArgs& a, const Work& w, int h, int r0, uint4 q[D / 32]) {
-  const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
-  const int r = r0 + c;
-  const int rr = min(r, w.pairs - 1);
-  const uint16_t* p =
-      a.q + (w.first + rr / a.group) * a.q_row + (int64_t)(h * a.group + rr % a.group) * a.q_head + g * (D / 4);
-  if (a.q_wide) {
-#pragma unroll
-    for (int j = 0; j < D / 32; ++j) q[j] = *reinterpret_cast<const uint4*>(p + 8 * j);
-  } else {
-#pragma unroll
-    for (int j = 0; j < D / 32; ++j) {
-      uint32_t x[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = (uint32_t)p[8 * j + 2 * i] | ((uint32_t)p[8 * j + 2 * i + 1] << 16);
-      q[j] = uint4{x[0], x[1], x[2], x[3]};
-    }
-  }
-}
-
-template <bool BF16>
-__device__ __forceinline__ kv_f4 mfma(uint4 x, uint4 y, kv_f4 z) {
-  if constexpr (BF16)
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(kv_b8, x), __builtin_bit_cast(kv_b8, y), z, 0, 0, 0);
-  else
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(kv_h8, x), __builtin_bit_cast(kv_h8, y), z, 0, 0, 0);
-}
-
-// One lane's codes and scales of a strip's keys or values, as they lie in memory.
-template <int D>
-struct Codes {
-  uint32_t w[2][D / 32];
-  uint32_t s[2];
-};
-
-// Loads of a strip go through a buffer resource over its head's part of the page:
-// one of no bytes stands for a strip past the end or a page outside the pool and
-// reads as zeros without touching memory, so no load hangs on a branch and the
-// compiler can count those in flight.  Codes are read once and marked so
-// (non-temporal: 199 -> 173 us for eight sequences of 131,072 tokens, 6.6 TB/s).
-constexpr int kNonTemporal = 2;
-
-// The codes and the scales of a strip at token t of a page: resources whose base
-// is the strip's, so that what a lane adds is constant.
-struct StripRsrc {
-  __amdgpu_buffer_rsrc_t codes, scales;
-};
-
-template <int D>
-__device__ __forceinline__ StripRsrc strip_rsrc(uint8_t* head, int T, int t, bool ok) {
-  const int bytes = ok ? (int)KvLayout<D>::head_bytes(T) : 0;
-  return StripRsrc{__builtin_amdgcn_make_buffer_rsrc(head + t * (D / 2), (short)0, bytes, 0x00020000),
-                   __builtin_amdgcn_make_buffer_rsrc(head + T * D + t * (D / 32), (short)0, bytes, 0x00020000)};
-}
-
-template <int D>
-__device__ __forceinline__ void load_words(__amdgpu_buffer_rsrc_t rs, uint32_t at, uint32_t w[D / 32]) {
-  if constexpr (D == 64) {
-    const uint2 u = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(rs, at, 0, kNonTemporal));
-    w[0] = u.x, w[1] = u.y;
-  } else {
-#pragma unroll
-    for (int j = 0; j < D / 128; ++j) {
-      const uint4 u = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rs, at + 16 * j, 0, kNonTemporal));
-      w[4 * j] = u.x, w[4 * j + 1] = u.y, w[4 * j + 2] = u.z, w[4 * j + 3] = u.w;
-    }
-  }
-}
-
-// Where a lane's codes and scales lie from a strip's bases on.
-template <int D>
-struct LaneAt {
-  uint32_t k, ks, shift, v, vs;
-  __device__ __forceinline__ explicit LaneAt(int T) {
-    const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
-    k = c * (D / 2) + g * (D / 8);
-    // the word that holds the lane's scale bytes, and their place in it
-    const int b = c * (D / 32) + (D == 64 ? g >> 1 : D == 128 ? g : 2 * g);
-    ks = b & ~3;
-    shift = (b & 3) * 8;
-    v = T * (D / 2) + (g * 16 + c) * (D / 8);
-    vs = T * (D / 32) + (g * (D / 32) + c * (D / 16) / kKvBlock) * 4;
-  }
-};
-
-// Keys: tile kt of a strip, token 16 kt + c, the lane's quarter of the channels.
-template <int D>
-__device__ __forceinline__ void load_keys(const StripRsrc& rs, const LaneAt<D>& at, Codes<D>& k) {
-#pragma unroll
-  for (int kt = 0; kt < 2; ++kt) {
-    load_words<D>(rs.codes, at.k + 16 * kt * (D / 2), k.w[kt]);
-    k.s[kt] = __builtin_amdgcn_raw_buffer_load_b32(rs.scales, at.ks + 16 * kt * (D / 32), 0, 0);
-  }
-}
-
-// Values: half `half` of a strip, tokens 16 half + 4 g + 0..3, run c of the channels.
-template <int D>
-__device__ __forceinline__ void load_vals(const StripRsrc& rs, const LaneAt<D>& at, Codes<D>& v) {
-#pragma unroll
-  for (int half = 0; half < 2; ++half) {
-    load_words<D>(rs.codes, at.v + 16 * half * (D / 2), v.w[half]);
-    v.s[half] = __builtin_amdgcn_raw_buffer_load_b32(rs.scales, at.vs + 16 * half * (D / 32), 0, 0);
-  }
-}
-
-// A operands of a strip's keys times the queries: scores of tokens 16 kt + 4 g + i.
-template <int D, bool BF16>
-__device__ __forceinline__ void key_operand(const Codes<D>& k, uint32_t shift, int kt, uint4 x[D / 32]) {
-  const uint32_t bytes = k.s[kt] >> shift;
-#pragma unroll
-  for (int j = 0; j < D / 32; ++j)
-    x[j] = kv_values8<BF16>(k.w[kt][j], kv_scale((D == 256 && j >= 4 ? bytes >> 8 : bytes) & 0xffu));
-}
-
-// Two values of token TOK (of four) of a half's codes: channels 2 JP and 2 JP + 1 of the run.
-template <int D, int TOK, int JP>
-__device__ __forceinline__ uint32_t val_pair(const uint32_t w[D / 32], float s) {
-  constexpr int byte = TOK * (D / 32) + JP;
-  return kv_values<false, byte % 4>(w[byte / 4], s);
-}
-
-// O^T += V^T P^T of a strip: one product per channel of the lane's run.
-template <int D, int JP>
-__device__ __forceinline__ void add_values(const Codes<D>& v, const float s[2][4], uint4 p, kv_f4* o) {
-  if constexpr (JP < D / 32) {
-    uint4 even, odd;
-    const uint32_t a0 = val_pair<D, 0, JP>(v.w[0], s[0][0]), a1 = val_pair<D, 1, JP>(v.w[0], s[0][1]);
-    const uint32_t a2 = val_pair<D, 2, JP>(v.w[0], s[0][2]), a3 = val_pair<D, 3, JP>(v.w[0], s[0][3]);
-    const uint32_t b0 = val_pair<D, 0, JP>(v.w[1], s[1][0]), b1 = val_pair<D, 1, JP>(v.w[1], s[1][1]);
-    const uint32_t b2 = val_pair<D, 2, JP>(v.w[1], s[1][2]), b3 = val_pair<D, 3, JP>(v.w[1], s[1][3]);
-    even = uint4{__builtin_amdgcn_perm(a1, a0, 0x05040100u), __builtin_amdgcn_perm(a3, a2, 0x05040100u),
-                 __builtin_amdgcn_perm(b1, b0, 0x05040100u), __builtin_amdgcn_perm(b3, b2, 0x05040100u)};
-    odd = uint4{__builtin_amdgcn_perm(a1, a0, 0x07060302u), __builtin_amdgcn_perm(a3, a2, 0x07060302u),
-                __builtin_amdgcn_perm(b1, b0, 0x07060302u), __builtin_amdgcn_perm(b3, b2, 0x07060302u)};
-    o[2 * JP] = mfma<false>(even, p, o[2 * JP]);
-    o[2 * JP + 1] = mfma<false>(odd, p, o[2 * JP + 1]);
-    add_values<D, JP + 1>(v, s, p, o);
-  }
-}
-
-// Mask of a strip's tokens: lane l reads token t0 + l % 32's byte.
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t mask_rsrc(const AttendArgs& a, int s, int h) {
-  const uint8_t* p = static_cast<const uint8_t*>(a.mask.p_dev) + s * a.mask.seq_stride + h * a.mask.head_stride;
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), (short)0, a.mask.cols, 0x00020000);
-}
-
-__device__ __forceinline__ uint32_t load_mask(__amdgpu_buffer_rsrc_t rs, int t0) {
-  return (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(rs, t0 + (threadIdx.x & 31), 0, 0);
-}
-
-// Which of a strip's tokens the lane's query sees: bit 4 half + i for token t0 + 16 half + 4 g + i.
-__device__ __forceinline__ uint32_t seen_bits(bool masked, uint32_t mask_byte, int t0, int end) {
-  const int g = (threadIdx.x & 63) >> 4;
-  const uint32_t all = masked ? (uint32_t)__ballot(mask_byte != 0) : 0xffffffffu;
-  const int n = min(max(end - t0, 0), 32);
-  const uint32_t in = (all & (n == 32 ? 0xffffffffu : (1u << n) - 1u)) >> (4 * g);
-  return (in & 0xfu) | ((in >> 12) & 0xf0u);
-}
-
-__device__ __forceinline__ uint32_t pack_half(float x, float y) {
-  const kv_h2 v{(_Float16)x, (_Float16)y};
-  return __builtin_bit_cast(uint32_t, v);
-}
-
-__device__ __forceinline__ uint16_t to_out(float x, bool bf16) {
-  if (bf16) return __builtin_bit_cast(uint16_t, (__bf16)x);
-  return __builtin_bit_cast(uint16_t, (_Float16)x);
-}
-
-__device__ __forceinline__ float log_sum(float M, float sum) {
-  return sum == 0.0f ? -__builtin_inff() : M + __builtin_amdgcn_logf(sum);
-}
-
-// A lane's channels of a finished row, and the row's log sums.
-template <int D, bool BF16>
-__device__ __forceinline__ void write_row(const AttendArgs& a, int64_t row, int run, const float acc[D / 16], float M,
-                                          float sum) {
-  constexpr int kRun = D / 16;
-  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-  uint16_t* d = a.out + row * D + run * kRun;
-#pragma unroll
-  for (int j = 0; j < kRun; j += 4) {
-    uint2 u;
-    u.x = (uint32_t)to_out(acc[j] * inv, BF16) | ((uint32_t)to_out(acc[j + 1] * inv, BF16) << 16);
-    u.y = (uint32_t)to_out(acc[j + 2] * inv, BF16) | ((uint32_t)to_out(acc[j + 3] * inv, BF16) << 16);
-    *reinterpret_cast<uint2*>(d + j) = u;
-  }
-  if (run == 0) {
-    const float e = log_sum(M, sum);
-    if (a.lse2) a.lse2[row] = e;
-    if (a.lse) a.lse[row] = e * 0.6931471805599453f;
-  }
-}
 
 // A strip of a page outside the pool: no scores.
 __device__ __forceinline__ void keep_nothing(float* scores) {
@@ -447,7 +62,7 @@ struct Running {
 #pragma unroll
       for (int j = 0; j < D / 32; ++j) sc = mfma<BF16>(y[j], q[j], sc);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[4 * kt + i] = sc[i] * a.scale2;
+      for (int i = 0; i < 4; ++i) x[4 * kt + i] = sc[i];
     }
     if (!whole) {
       const uint32_t in = seen_bits(MASK, mask_byte, t0, end);
@@ -455,12 +70,13 @@ struct Running {
       for (int i = 0; i < 8; ++i) x[i] = (in >> i) & 1u ? x[i] : -__builtin_inff();
     }
     if (scores) {
-      *reinterpret_cast<kv_f4*>(scores + t0 + 4 * g) = kv_f4{x[0], x[1], x[2], x[3]};
-      *reinterpret_cast<kv_f4*>(scores + t0 + 4 * g + 16) = kv_f4{x[4], x[5], x[6], x[7]};
+      *reinterpret_cast<kv_f4*>(scores + t0 + 4 * g) = kv_f4{x[0], x[1], x[2], x[3]} * a.scale2;
+      *reinterpret_cast<kv_f4*>(scores + t0 + 4 * g + 16) = kv_f4{x[4], x[5], x[6], x[7]} * a.scale2;
     }
     float top = x[0];
 #pragma unroll
     for (int i = 1; i < 8; ++i) top = fmaxf(top, x[i]);
+    top *= a.scale2;
     if (__any(top > m + kSpan)) {
       top = fmaxf(top, __shfl_xor(top, 16));
       top = fmaxf(top, __shfl_xor(top, 32));
@@ -474,27 +90,13 @@ struct Running {
     float p[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      p[i] = __builtin_amdgcn_exp2f(x[i] - m);
+      p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale2, -m));
       l += p[i];
     }
     const uint4 pb{pack_half(p[0], p[1]), pack_half(p[2], p[3]), pack_half(p[4], p[5]), pack_half(p[6], p[7])};
     float s[2][4];
-#pragma unroll
-    for (int half = 0; half < 2; ++half)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) s[half][i] = kv_scale((v.s[half] >> (8 * i)) & 0xffu);
-    if (t0 + kKvStrip > len) {   // memory past the last token may hold anything: 0 times it must be 0
-#pragma unroll
-      for (int half = 0; half < 2; ++half)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (t0 + 16 * half + 4 * g + i >= len) {
-            s[half][i] = 1.0f;
-#pragma unroll
-            for (int b = i * (D / 32); b < (i + 1) * (D / 32); ++b) v.w[half][b >> 2] &= ~(0xffu << (8 * (b & 3)));
-          }
-    }
-    add_values<D, 0>(v, s, pb, o);
+    value_scales<D>(v, t0, len, s);
+    add_values<D, 1, 0>(v, s, &pb, &o);
   }
 };
 
@@ -719,10 +321,10 @@ __device__ __forceinline__ void add_kept(const AttendArgs& a, uint32_t block) {
 }
 
 // What follows the attention, in one launch: the parts joined, the kept scores made weights.
-template <int D, bool BF16>
+template <int D, bool BF16, int R>
 __global__ __launch_bounds__(kAttThreads) void k_kv_finish(AttendArgs a, uint32_t join_blocks) {
   const uint32_t b = blockIdx.x;
-  if (b < join_blocks) join_rows<D, BF16, kAttRows>(a, b);
+  if (b < join_blocks) join_rows<D, BF16, R>(a, b);
   else add_kept(a, b - join_blocks);
 }
 
@@ -789,14 +391,6 @@ __global__ __launch_bounds__(kAttThreads) void k_kv_weights(AttendArgs a) {
 
 }  // namespace
 
-#define LAM_KV_DISPATCH(v, LAUNCH)                                   \
-  do {                                                               \
-    const bool bf_ = (v).dtype == LAM_BF16;                          \
-    if ((v).head_dim == 64) { if (bf_) LAUNCH(64, true); else LAUNCH(64, false); }           \
-    else if ((v).head_dim == 128) { if (bf_) LAUNCH(128, true); else LAUNCH(128, false); }   \
-    else { if (bf_) LAUNCH(256, true); else LAUNCH(256, false); }    \
-  } while (0)
-
 lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, int64_t q_row, int64_t q_head,
                             int32_t q_heads, float scale, bool causal, int64_t max_length, const lam_kv_slots& mask,
                             const lam_kv_slots& weights, void* out, float* lse) {
@@ -810,7 +404,9 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
   a.q_heads = q_heads;
   a.group = q_heads / v.kv_heads;
   a.causal = causal;
-  a.scale2 = (float)((double)scale * 1.4426950408889634);
+  // a scale of 0 becomes one that no score survives, and masked ones (-inf) stay what they are
+  a.scale2 = std::max((float)(std::fabs((double)scale) * 1.4426950408889634), 1e-37f);
+  a.flip = scale < 0.0f;
   a.cut = (int64_t)v.table_cols * v.page_size;
   if (max_length > 0) a.cut = std::min(a.cut, max_length);
   if (v.n_pages == 0) a.cut = 0;
@@ -820,28 +416,32 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
   a.out = static_cast<uint16_t*>(out);
   a.lse = lse;
 
+  // The kernel for chunks where sequences have more than a tile of the other's rows on average.
+  const bool chunk = v.rows * a.group > kAttRows * (int64_t)v.n_seqs;
+  const int rows = chunk ? chunk_rows(v.head_dim) : kAttRows;
+  const int fill = chunk ? kFillWaves : kFill;
   int64_t tiles;
   if (v.starts_dev) {
-    tiles = v.rows * a.group / kAttRows + v.n_seqs;
+    tiles = v.rows * a.group / rows + v.n_seqs;
   } else {
-    a.tiles_per_seq = (int)((v.rows / v.n_seqs * a.group + kAttRows - 1) / kAttRows);
+    a.tiles_per_seq = (int)((v.rows / v.n_seqs * a.group + rows - 1) / rows);
     tiles = (int64_t)a.tiles_per_seq * v.n_seqs;
   }
-  // Lengths are split where the tiles do not fill the chip: three workgroups of
-  // 256 threads a compute unit.
+  // Lengths are split where the tiles do not fill the chip.
   const int64_t units = tiles * v.kv_heads;
   int64_t blocks = units;
-  if (units < kFill && a.cut > kKvStrip * kAttWaves) {
-    a.split_to = kFill;
-    blocks = kFill + units;   // see plan(): at most split_to - units / 2 (or split_to / 2) full parts, and one more a tile
+  if (units < fill && a.cut > kKvStrip * kAttWaves) {
+    a.split_to = fill;
+    blocks = fill + units;   // see plan(): at most split_to - units / 2 (or split_to / 2) full parts, and one more a tile
   }
+  LAM_CHECK(blocks < (1LL << 31), LAM_EINVAL, "too many rows for one launch");
 
   // Weights: from scores that the attention keeps (8 bytes a row and token, written
   // and read) where sequences have a tile of rows on average, else from a second
   // pass over the keys.
   const int64_t pairs = v.rows * q_heads;
-  const int64_t parts = a.split_to ? blocks * kAttRows : 0;
-  const bool keep = weights.p_dev && v.rows * a.group <= kAttRows * (int64_t)v.n_seqs && pairs * a.cut * 4 <= kKeptBytes;
+  const int64_t parts = a.split_to ? blocks * rows : 0;
+  const bool keep = weights.p_dev && !chunk && pairs * a.cut * 4 <= kKeptBytes;
   a.kept_cols = (a.cut + kKeptTokens - 1) / kKeptTokens * kKeptTokens;
   DevBuf& buf = ctx->scratch[kScratchKv];
   const int64_t floats = (keep ? pairs * a.kept_cols : 0) + parts * (v.head_dim + 2) + (weights.p_dev ? pairs : 0);
@@ -856,8 +456,10 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
   a.part_l = a.part_m + parts;
   if (weights.p_dev) a.lse2 = a.part_l + parts;
 
-  LAM_CHECK(blocks < (1LL << 31), LAM_EINVAL, "too many rows for one launch");
   hipEvent_t e0, e1;
+  if (chunk) {
+    LAM_TRY(launch_kv_chunk(ctx, v, a, blocks, mask.p_dev != nullptr));
+  } else {
   LAM_TRY(prof_launch_events(ctx, "kv_attend", &e0, &e1));
 #define LAM_GO(D, BF)                                                                                               \
   do {                                                                                                              \
@@ -871,14 +473,21 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
   LAM_KV_DISPATCH(v, LAM_GO);
 #undef LAM_GO
   LAM_HIP(hipGetLastError());
+  }
   const int64_t join_blocks = a.split_to ? blocks : 0;
   const int64_t kept_blocks = keep ? a.kept_cols / kKeptTokens * v.kv_heads * v.n_seqs : 0;
   if (join_blocks + kept_blocks > 0) {
     LAM_CHECK(join_blocks + kept_blocks < (1LL << 31), LAM_EINVAL, "too many rows for one launch");
     LAM_TRY(prof_launch_events(ctx, "kv_finish", &e0, &e1));
 #define LAM_GO(D, BF)                                                                                               \
-  hipExtLaunchKernelGGL((k_kv_finish<D, BF>), dim3((unsigned)(join_blocks + kept_blocks)), dim3(kAttThreads), 0,     \
-                        ctx->stream, e0, e1, 0, a, (uint32_t)join_blocks)
+  do {                                                                                                              \
+    if (chunk)                                                                                                      \
+      hipExtLaunchKernelGGL((k_kv_finish<D, BF, chunk_rows(D)>), dim3((unsigned)join_blocks), dim3(kAttThreads), 0, \
+                            ctx->stream, e0, e1, 0, a, (uint32_t)join_blocks);                                      \
+    else                                                                                                            \
+      hipExtLaunchKernelGGL((k_kv_finish<D, BF, kAttRows>), dim3((unsigned)(join_blocks + kept_blocks)),            \
+                            dim3(kAttThreads), 0, ctx->stream, e0, e1, 0, a, (uint32_t)join_blocks);                \
+  } while (0)
     LAM_KV_DISPATCH(v, LAM_GO);
 #undef LAM_GO
     LAM_HIP(hipGetLastError());

@@ -382,15 +382,6 @@ lam_status row_grid(const lam_kv_view& v, unsigned* grid) {
 
 }  // namespace
 
-// Calls f with D and the type as constants.
-#define LAM_KV_DISPATCH(v, LAUNCH)                                   \
-  do {                                                               \
-    const bool bf_ = (v).dtype == LAM_BF16;                          \
-    if ((v).head_dim == 64) { if (bf_) LAUNCH(64, true); else LAUNCH(64, false); }           \
-    else if ((v).head_dim == 128) { if (bf_) LAUNCH(128, true); else LAUNCH(128, false); }   \
-    else { if (bf_) LAUNCH(256, true); else LAUNCH(256, false); }    \
-  } while (0)
-
 lam_status launch_kv_append(lam_ctx* ctx, const lam_kv_view& v, const void* k, int64_t k_row, int64_t k_head,
                             const void* val, int64_t v_row, int64_t v_head, const lam_kv_slots& weights,
                             const lam_kv_slots& positions, const int32_t* first, uint32_t* status) {
