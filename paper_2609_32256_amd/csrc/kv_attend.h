@@ -394,9 +394,70 @@ __device__ __forceinline__ uint32_t seen_bits(bool masked, uint32_t mask_byte, i
   return (in & 0xfu) | ((in >> 12) & 0xf0u);
 }
 
-__device__ __forceinline__ uint32_t pack_half(float x, float y) {
-  const kv_h2 v{(_Float16)x, (_Float16)y};
-  return __builtin_bit_cast(uint32_t, v);
+// The softmax of a lane's query over the strips so far.  Four lanes (g) share a
+// query: m and seen are the same in them, l counts each lane's own tokens.
+struct Row {
+  float m = 0.0f;      // reference of the exponentials, base 2
+  float l = 0.0f;
+  bool seen = false;   // m is a score's
+
+  // top: the largest score of a strip less m
+  __device__ __forceinline__ bool rises(float top) const { return top > kSpan || (!seen && top > -__builtin_inff()); }
+
+  // A new reference for the rows that need one; x becomes relative to it.  The
+  // factor for what was summed relative to the old one.
+  __device__ __forceinline__ float raise(float top, kv_f4 x[2]) {
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const float by = rises(top) ? top - kLift : 0.0f;
+    x[0] -= by;
+    x[1] -= by;
+    m += by;
+    const float f = seen ? __builtin_amdgcn_exp2f(-by) : 0.0f;   // (nothing summed yet: by may be anything)
+    seen = seen || top > -__builtin_inff();
+    l *= f;
+    return f;
+  }
+
+  // 2^x of the strip as the B operand of the values' product.  There they are
+  // float16: 11 bits of each, an error that averages out below the result's own
+  // rounding (bfloat16) or about at it (float16).  Their sum keeps them in float32,
+  // since the log sums and the accumulated weights come from it.
+  __device__ __forceinline__ uint4 weights(const kv_f4 x[2]) {
+    uint32_t p[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float a = __builtin_amdgcn_exp2f(x[i >> 1][2 * (i & 1)]), b = __builtin_amdgcn_exp2f(x[i >> 1][2 * (i & 1) + 1]);
+      const kv_h2 h{(_Float16)a, (_Float16)b};
+      l += a;
+      l += b;
+      p[i] = __builtin_bit_cast(uint32_t, h);
+    }
+    return uint4{p[0], p[1], p[2], p[3]};
+  }
+
+  __device__ __forceinline__ float sum() const {
+    const float s = l + __shfl_xor(l, 16);
+    return s + __shfl_xor(s, 32);
+  }
+  __device__ __forceinline__ float reference() const { return seen ? m : kNoMax; }
+};
+
+__device__ __forceinline__ void less_reference(kv_f4 x[2], float scale2, const Row& r) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i >> 2][i & 3] = __builtin_fmaf(x[i >> 2][i & 3], scale2, -r.m);
+}
+
+__device__ __forceinline__ void hide(kv_f4 x[2], uint32_t seen) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i >> 2][i & 3] = (seen >> i) & 1u ? x[i >> 2][i & 3] : -__builtin_inff();
+}
+
+__device__ __forceinline__ float top_of(const kv_f4 x[2]) {
+  float z = fmaxf(x[0][0], x[1][0]);
+#pragma unroll
+  for (int i = 1; i < 4; ++i) z = fmaxf(fmaxf(z, x[0][i]), x[1][i]);
+  return z;
 }
 
 __device__ __forceinline__ uint16_t to_out(float x, bool bf16) {

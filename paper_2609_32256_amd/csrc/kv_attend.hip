@@ -41,9 +41,9 @@ template <int D, bool BF16, bool MASK>
 struct Running {
   static constexpr int kRun = D / 16;
   kv_f4 o[kRun];
-  float m, l;
+  Row row;
 
-  __device__ __forceinline__ Running() : m(kNoMax), l(0.0f) {
+  __device__ __forceinline__ Running() {
 #pragma unroll
     for (int j = 0; j < kRun; ++j) o[j] = kv_f4{0, 0, 0, 0};
   }
@@ -51,52 +51,34 @@ struct Running {
   // One strip at t0; whole: every query sees all of its tokens.  scores: where
   // the query's scores are kept (null: nowhere), slot by slot.
   __device__ __forceinline__ void add(const AttendArgs& a, int len, int t0, bool whole, int end, uint32_t mask_byte,
-                                      float* scores, uint32_t shift, const uint4 q[D / 32], const Codes<D>& k, Codes<D>& v) {
-    const int g = (threadIdx.x & 63) >> 4;
-    float x[8];
+                                      float* scores, uint32_t shift, const uint4 q[D / 32], const Codes<D>& k,
+                                      Codes<D>& v) {
+    kv_f4 x[2];
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
       uint4 y[D / 32];
       key_operand<D, BF16>(k, shift, kt, y);
-      kv_f4 sc{0, 0, 0, 0};
+      x[kt] = kv_f4{0, 0, 0, 0};
 #pragma unroll
-      for (int j = 0; j < D / 32; ++j) sc = mfma<BF16>(y[j], q[j], sc);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[4 * kt + i] = sc[i];
+      for (int j = 0; j < D / 32; ++j) x[kt] = mfma<BF16>(y[j], q[j], x[kt]);
     }
-    if (!whole) {
-      const uint32_t in = seen_bits(MASK, mask_byte, t0, end);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = (in >> i) & 1u ? x[i] : -__builtin_inff();
-    }
+    less_reference(x, a.scale2, row);
+    if (!whole) hide(x, seen_bits(MASK, mask_byte, t0, end));
     if (scores) {
-      *reinterpret_cast<kv_f4*>(scores + t0 + 4 * g) = kv_f4{x[0], x[1], x[2], x[3]} * a.scale2;
-      *reinterpret_cast<kv_f4*>(scores + t0 + 4 * g + 16) = kv_f4{x[4], x[5], x[6], x[7]} * a.scale2;
+      const int g = (threadIdx.x & 63) >> 4;
+      *reinterpret_cast<kv_f4*>(scores + t0 + 4 * g) = x[0] + row.m;
+      *reinterpret_cast<kv_f4*>(scores + t0 + 4 * g + 16) = x[1] + row.m;
     }
-    float top = x[0];
-#pragma unroll
-    for (int i = 1; i < 8; ++i) top = fmaxf(top, x[i]);
-    top *= a.scale2;
-    if (__any(top > m + kSpan)) {
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
-      const float next = top > m + kSpan ? top - kLift : m;
-      const float f = __builtin_amdgcn_exp2f(m - next);
-      m = next;
-      l *= f;
+    const float top = top_of(x);
+    if (__any(row.rises(top))) {
+      const float f = row.raise(top, x);
 #pragma unroll
       for (int j = 0; j < kRun; ++j) o[j] *= f;
     }
-    float p[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale2, -m));
-      l += p[i];
-    }
-    const uint4 pb{pack_half(p[0], p[1]), pack_half(p[2], p[3]), pack_half(p[4], p[5]), pack_half(p[6], p[7])};
+    const uint4 p = row.weights(x);
     float s[2][4];
     value_scales<D>(v, t0, len, s);
-    add_values<D, 1, 0>(v, s, &pb, &o);
+    add_values<D, 1, 0>(v, s, &p, &o);
   }
 };
 
@@ -165,10 +147,8 @@ __global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : 3) void k_kv_attend(Att
       t0 += kStep;
     }
   }
-  float m = r.m, l = r.l;
   kv_f4(&o)[kRun] = r.o;
-  l += __shfl_xor(l, 16);
-  l += __shfl_xor(l, 32);
+  const float m = r.row.reference(), l = r.row.sum();
 
   // the waves' parts: every wave's sums relative to the largest maximum
   __shared__ float sm[kAttWaves][kAttRows], sl[kAttWaves][kAttRows];

@@ -37,123 +37,111 @@ __global__ __launch_bounds__(64, D == 256 ? 1 : 2) void k_kv_chunk(AttendArgs a)
   const int whole_to = MASK ? -1 : end_first - kKvStrip;
 
   kv_f4 o[kTiles][kRun];
-  float m[kTiles], l[kTiles];
+  Row row[kTiles];
 #pragma unroll
-  for (int t = 0; t < kTiles; ++t) {
-    m[t] = kNoMax;
-    l[t] = 0.0f;
+  for (int t = 0; t < kTiles; ++t)
 #pragma unroll
     for (int j = 0; j < kRun; ++j) o[t][j] = kv_f4{0, 0, 0, 0};
-  }
 
+  // One strip's codes in registers: the next one's keys are loaded as soon as the
+  // keys are converted, its values when the values are.
   const LaneAt<D> at(T);
-  Codes<D> k[2], v[2];
-  uint32_t mb[2] = {};
-  bool ok[2];
+  Codes<D> k, v;
+  uint32_t mb = 0;
   const __amdgpu_buffer_rsrc_t mrs = mask_rsrc(a, w.s, w.h);
   const kv_const_i32 entries = kv_const(a.c.table + (int64_t)w.s * a.c.table_stride);
   const int last_col = max(a.c.table_cols - 1, 0);
   auto entry = [&](int t) { return entries[min(t >> a.c.page_shift, last_col)]; };
-  auto load = [&](int b, int32_t page, int t) {
-    ok[b] = t < to && page >= 0 && page < a.c.n_pages;
-    const StripRsrc rs = strip_rsrc<D>(a.c.head_page(ok[b] ? page : 0, w.h, head_bytes), T, t & (T - 1), ok[b]);
-    load_keys<D>(rs, at, k[b]);
-    load_vals<D>(rs, at, v[b]);
-    if constexpr (MASK) mb[b] = load_mask(mrs, t);
+  const uint32_t n_pages = (uint32_t)a.c.n_pages;
+  // the strip to load next: its page's address is worked out once a page
+  uint8_t* head;
+  bool ok_page;
+  auto turn = [&](int32_t page) {
+    ok_page = (uint32_t)page < n_pages;
+    head = a.c.head_page(ok_page ? page : 0, w.h, head_bytes);
   };
-
-  auto add = [&](int b, int t0) {
-    // scores of 32 tokens for every tile of queries
-    kv_f4 x[kTiles][2];
-    {
-      uint4 y[2][kSteps];
-      key_operand<D, BF16>(k[b], at.shift, 0, y[0]);
-      key_operand<D, BF16>(k[b], at.shift, 1, y[1]);
+  int t0 = from;
+  int32_t next = entry(t0 - (t0 & (T - 1)) + T);
+  turn(entry(t0));
+  bool ok = t0 < to && ok_page;
+  {
+    const StripRsrc rs = strip_rsrc<D>(head, T, t0 & (T - 1), ok);
+    load_keys<D>(rs, at, k);
+    load_vals<D>(rs, at, v);
+    if constexpr (MASK) mb = load_mask(mrs, t0);
+  }
+  for (; t0 < to; t0 += kKvStrip) {
+    uint4 y[2][kSteps];
+    key_operand<D, BF16>(k, at.shift, 0, y[0]);
+    key_operand<D, BF16>(k, at.shift, 1, y[1]);
+    const int t1 = t0 + kKvStrip;
+    if ((t1 & (T - 1)) == 0) {
+      turn(next);
+      next = entry(t1 + T);
+    }
+    const bool ok_next = t1 < to && ok_page;
+    const StripRsrc rs = strip_rsrc<D>(head, T, t1 & (T - 1), ok_next);
+    load_keys<D>(rs, at, k);
+    if (ok) {
+      // scores of 32 tokens for every tile of queries, less the row's reference
+      kv_f4 x[kTiles][2];
+      uint4 q = sq[0][0][lane];
 #pragma unroll
       for (int t = 0; t < kTiles; ++t) {
         x[t][0] = x[t][1] = kv_f4{0, 0, 0, 0};
 #pragma unroll
         for (int j = 0; j < kSteps; ++j) {
-          const uint4 q = sq[t][j][lane];
+          const int n = t * kSteps + j + 1;
+          uint4 q_next = q;
+          if (n < kTiles * kSteps) q_next = sq[n / kSteps][n % kSteps][lane];
           x[t][0] = mfma<BF16>(y[0][j], q, x[t][0]);
           x[t][1] = mfma<BF16>(y[1][j], q, x[t][1]);
+          q = q_next;
         }
       }
-    }
-    if (t0 > whole_to) {
+      float s[2][4];
+      value_scales<D>(v, t0, w.len, s);
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t) less_reference(x[t], a.scale2, row[t]);
+      if (t0 > whole_to) {
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t)
+          hide(x[t], seen_bits(MASK, mb, t0, pair_end(a, w, min(w.r0 + 16 * t + c, w.pairs - 1))));
+      }
+      bool up = false;
+      float top[kTiles];
 #pragma unroll
       for (int t = 0; t < kTiles; ++t) {
-        const int end = pair_end(a, w, min(w.r0 + 16 * t + c, w.pairs - 1));
-        const uint32_t in = seen_bits(MASK, mb[b], t0, end);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[t][i >> 2][i & 3] = (in >> i) & 1u ? x[t][i >> 2][i & 3] : -__builtin_inff();
+        top[t] = top_of(x[t]);
+        up |= row[t].rises(top[t]);
       }
-    }
-    float top[kTiles];
-    bool up = false;
+      if (__any(up)) {
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) {
-      float z = fmaxf(x[t][0][0], x[t][1][0]);
+        for (int t = 0; t < kTiles; ++t) {
+          const float f = row[t].raise(top[t], x[t]);
 #pragma unroll
-      for (int i = 1; i < 4; ++i) z = fmaxf(z, fmaxf(x[t][0][i], x[t][1][i]));
-      top[t] = z * a.scale2;
-      up |= top[t] > m[t] + kSpan;
-    }
-    if (__any(up)) {
-#pragma unroll
-      for (int t = 0; t < kTiles; ++t) {
-        float z = fmaxf(top[t], __shfl_xor(top[t], 16));
-        z = fmaxf(z, __shfl_xor(z, 32));
-        const float next = z > m[t] + kSpan ? z - kLift : m[t];
-        const float f = __builtin_amdgcn_exp2f(m[t] - next);
-        m[t] = next;
-        l[t] *= f;
-#pragma unroll
-        for (int j = 0; j < kRun; ++j) o[t][j] *= f;
+          for (int j = 0; j < kRun; ++j) o[t][j] *= f;
+        }
       }
-    }
-    uint4 p[kTiles];
+      uint4 p[kTiles];
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) {
-      float e[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][i >> 2][i & 3], a.scale2, -m[t]));
-        l[t] += e[i];
-      }
-      p[t] = uint4{pack_half(e[0], e[1]), pack_half(e[2], e[3]), pack_half(e[4], e[5]), pack_half(e[6], e[7])};
+      for (int t = 0; t < kTiles; ++t) p[t] = row[t].weights(x[t]);
+      add_values<D, kTiles, 0>(v, s, p, o);
     }
-    float s[2][4];
-    value_scales<D>(v[b], t0, w.len, s);
-    add_values<D, kTiles, 0>(v[b], s, p, o);
-  };
-
-  int t0 = from;
-  int32_t page = entry(t0), next = entry(t0 + kKvStrip);
-  load(0, page, t0);
-  while (t0 < to) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      if (t0 >= to) break;
-      page = next;
-      next = entry(t0 + 2 * kKvStrip);
-      load(1 - i, page, t0 + kKvStrip);
-      if (ok[i]) add(i, t0);
-      t0 += kKvStrip;
-    }
+    load_vals<D>(rs, at, v);
+    if constexpr (MASK) mb = load_mask(mrs, t1);
+    ok = ok_next;
   }
 
 #pragma unroll
   for (int t = 0; t < kTiles; ++t) {
-    float sum = l[t];
-    sum += __shfl_xor(sum, 16);
-    sum += __shfl_xor(sum, 32);
+    const float sum = row[t].sum(), m = row[t].reference();
     const int pair = w.r0 + 16 * t + c;
     if (pair >= w.pairs) continue;
     if (w.parts > 1) {
       const int64_t p = (int64_t)blockIdx.x * kRows + 16 * t + c;
       if (g == 0) {
-        a.part_m[p] = m[t];
+        a.part_m[p] = m;
         a.part_l[p] = sum;
       }
       float* d = a.part_o + p * D + 4 * g * kRun;
@@ -163,13 +151,13 @@ __global__ __launch_bounds__(64, D == 256 ? 1 : 2) void k_kv_chunk(AttendArgs a)
         for (int j = 0; j < kRun; j += 4)
           *reinterpret_cast<kv_f4*>(d + i * kRun + j) = kv_f4{o[t][j][i], o[t][j + 1][i], o[t][j + 2][i], o[t][j + 3][i]};
     } else {
-      const int64_t row = (w.first + pair / a.group) * a.q_heads + w.h * a.group + pair % a.group;
+      const int64_t at = (w.first + pair / a.group) * a.q_heads + w.h * a.group + pair % a.group;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         float acc[kRun];
 #pragma unroll
         for (int j = 0; j < kRun; ++j) acc[j] = o[t][j][i];
-        write_row<D, BF16>(a, row, 4 * g + i, acc, m[t], sum);
+        write_row<D, BF16>(a, at, 4 * g + i, acc, m, sum);
       }
     }
   }
