@@ -199,17 +199,11 @@ __device__ __forceinline__ int pair_end(const AttendArgs& a, const Work& w, int 
   return max(0, min(w.len, w.end_full - w.n + r / a.group + 1));
 }
 
-// B operands of the 16 query rows: lane (c, g) holds channels g D/4 + 8 j + 0..7
-// of pair r0 + c as step j.  Columns past the last pair repeat it; nothing of
-// theirs is written.
+// B operand of a query row and head: lane (c, g) holds channels g D/4 + 8 j + 0..7
+// of column c as step j.  p: where its channels begin.
 template <int D>
-__device__ __forceinline__ void load_q(const AttendArgs& a, const Work& w, int h, int r0, uint4 q[D / 32]) {
-  const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
-  const int r = r0 + c;
-  const int rr = min(r, w.pairs - 1);
-  const uint16_t* p =
-      a.q + (w.first + rr / a.group) * a.q_row + (int64_t)(h * a.group + rr % a.group) * a.q_head + g * (D / 4);
-  if (a.q_wide) {
+__device__ __forceinline__ void load_row(const uint16_t* p, bool wide, uint4 q[D / 32]) {
+  if (wide) {
 #pragma unroll
     for (int j = 0; j < D / 32; ++j) q[j] = *reinterpret_cast<const uint4*>(p + 8 * j);
   } else {
@@ -221,11 +215,25 @@ __device__ __forceinline__ void load_q(const AttendArgs& a, const Work& w, int h
       q[j] = uint4{x[0], x[1], x[2], x[3]};
     }
   }
-  if (a.flip) {   // a negative scale: scale2 is its size, the queries take its sign
+}
+
+// A negative scale: scale2 is its size, the queries (or the keys) take its sign.
+template <int N>
+__device__ __forceinline__ void flip_signs(uint4 x[N]) {
 #pragma unroll
-    for (int j = 0; j < D / 32; ++j)
-      q[j] = uint4{q[j].x ^ 0x80008000u, q[j].y ^ 0x80008000u, q[j].z ^ 0x80008000u, q[j].w ^ 0x80008000u};
-  }
+  for (int j = 0; j < N; ++j)
+    x[j] = uint4{x[j].x ^ 0x80008000u, x[j].y ^ 0x80008000u, x[j].z ^ 0x80008000u, x[j].w ^ 0x80008000u};
+}
+
+// The 16 pairs from r0 on.  Columns past the last pair repeat it; nothing of theirs
+// is written.
+template <int D>
+__device__ __forceinline__ void load_q(const AttendArgs& a, const Work& w, int h, int r0, uint4 q[D / 32]) {
+  const int r = min(r0 + (int)(threadIdx.x & 15), w.pairs - 1);
+  const int g = (threadIdx.x & 63) >> 4;
+  load_row<D>(a.q + (w.first + r / a.group) * a.q_row + (int64_t)(h * a.group + r % a.group) * a.q_head + g * (D / 4),
+              a.q_wide, q);
+  if (a.flip) flip_signs<D / 32>(q);
 }
 
 template <bool BF16>

@@ -308,15 +308,21 @@ __global__ __launch_bounds__(kAttThreads) void k_kv_finish(AttendArgs a, uint32_
   else add_kept(a, b - join_blocks);
 }
 
-// Accumulated weights: a wave owns 32 tokens of one head, whose keys it converts
-// once, and walks the call's rows; p = 2^(s - lse).  Every token is summed by one
-// wave in the order of the rows, so the result does not depend on timing.
+// Accumulated weights: a workgroup owns 64 tokens of one head (32 of 256 channels),
+// whose keys each wave converts once; its waves share the call's rows, 16 at a
+// time, the next 16 on their way; p = 2^(s - lse).  The waves' sums are added in
+// their order, so the result does not depend on timing.  (With 32 tokens a wave
+// and all rows to each, addresses and loads were two thirds of the instructions.)
+template <int D>
+constexpr int weight_strips() { return D == 256 ? 1 : 2; }
+
 template <int D, bool BF16>
-__global__ __launch_bounds__(kAttThreads) void k_kv_weights(AttendArgs a) {
+__global__ __launch_bounds__(kAttThreads, D == 64 ? 4 : D == 128 ? 3 : 2) void k_kv_weights(AttendArgs a) {
+  constexpr int kSteps = D / 32, kStrips = weight_strips<D>(), kTokens = kStrips * kKvStrip;
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t chunks = (uint32_t)((a.cut + kKvStrip * kAttWaves - 1) / (kKvStrip * kAttWaves));
-  const int t0 = (int)(blockIdx.x % chunks) * (kKvStrip * kAttWaves) + wave * kKvStrip;
+  const uint32_t chunks = (uint32_t)((a.cut + kTokens - 1) / kTokens);
+  const int t0 = (int)(blockIdx.x % chunks) * kTokens;
   const uint32_t id = blockIdx.x / chunks;
   const int h = (int)(id % (uint32_t)a.c.heads);
   Work w;
@@ -328,44 +334,110 @@ __global__ __launch_bounds__(kAttThreads) void k_kv_weights(AttendArgs a) {
   w.len = (int)min((int64_t)w.end_full, a.cut);
   if (t0 >= w.len || w.pairs == 0) return;
   const int T = 1 << a.c.page_shift;
-  const int64_t page = a.c.page(w.s, t0 >> a.c.page_shift);
-  if (page < 0) return;
   const LaneAt<D> at(T);
-  Codes<D> k;
-  load_keys<D>(strip_rsrc<D>(a.c.head_page(page, h, KvLayout<D>::head_bytes(T)), T, t0 & (T - 1), true), at, k);
-  const uint32_t mb = a.mask.p_dev ? load_mask(mask_rsrc(a, w.s, h), t0) : 0u;
-  uint4 y[2][D / 32];
-  key_operand<D, BF16>(k, at.shift, 0, y[0]);
-  key_operand<D, BF16>(k, at.shift, 1, y[1]);
-  float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-  // with a causal limit the first row that sees token t0 is row t0 - (end_full - n)
-  int r0 = a.causal ? max(0, t0 - (w.end_full - w.n)) * a.group / kAttRows * kAttRows : 0;
-  for (; r0 < w.pairs; r0 += kAttRows) {
-    uint4 q[D / 32];
-    load_q<D>(a, w, h, r0, q);
-    const int r = r0 + c, rr = min(r, w.pairs - 1);
-    const float e = a.lse2[(w.first + rr / a.group) * a.q_heads + h * a.group + rr % a.group];
-    const int end = pair_end(a, w, rr);
-    const uint32_t bits = seen_bits(a.mask.p_dev, mb, t0, end);
-    const uint32_t in = r < w.pairs && e > -__builtin_inff() ? bits : 0u;
-    const uint32_t nan = r < w.pairs && e != e ? 0xffu : 0u;
+  uint4 y[2 * kStrips][kSteps];
+  uint32_t mb[kStrips] = {};
+  bool ok[kStrips];   // the strip's page is there
+#pragma unroll
+  for (int n = 0; n < kStrips; ++n) {
+    const int t = t0 + n * kKvStrip;
+    const int64_t page = t < w.len ? a.c.page(w.s, t >> a.c.page_shift) : -1;
+    ok[n] = page >= 0;
+    Codes<D> k;
+    load_keys<D>(strip_rsrc<D>(a.c.head_page(ok[n] ? page : 0, h, KvLayout<D>::head_bytes(T)), T, t & (T - 1), ok[n]), at, k);
+    if (a.mask.p_dev) mb[n] = load_mask(mask_rsrc(a, w.s, h), t);
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
-      kv_f4 sc{0, 0, 0, 0};
-#pragma unroll
-      for (int j = 0; j < D / 32; ++j) sc = mfma<BF16>(y[kt][j], q[j], sc);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        sum[4 * kt + i] += ((in | nan) >> (4 * kt + i)) & 1u ? __builtin_amdgcn_exp2f(sc[i] * a.scale2 - e) : 0.0f;
+      key_operand<D, BF16>(k, at.shift, kt, y[2 * n + kt]);
+      if (a.flip) flip_signs<kSteps>(y[2 * n + kt]);
     }
   }
+  float sum[kStrips][8] = {};
+
+  // with a causal limit the first row that sees token t0 is row t0 - (end_full - n)
+  const int hidden = w.end_full - w.n;
+  const int first = a.causal ? (int)min((int64_t)max(0, t0 - hidden) * a.group, (int64_t)w.pairs) / 16 * 16 : 0;
+  int r0 = first + 16 * wave;
+  // The lane's pair of the next tile: row i of the sequence, head j of the group, and
+  // where its query and its log sum lie; the last pair's stand in past the end.
+  constexpr int kStep = 16 * kAttWaves;
+  int i = (r0 + c) / a.group, j = (r0 + c) % a.group;
+  const int di = kStep / a.group, dj = kStep % a.group;
+  const int64_t q_step = di * a.q_row + dj * a.q_head, q_turn = a.q_row - a.group * a.q_head;
+  const int l_step = di * a.q_heads + dj, l_turn = a.q_heads - a.group;
+  auto q_of = [&](int i, int j) { return a.q + (w.first + i) * a.q_row + (int64_t)(h * a.group + j) * a.q_head + g * (D / 4); };
+  auto l_of = [&](int i, int j) { return a.lse2 + (w.first + i) * a.q_heads + h * a.group + j; };
+  const uint16_t* qp = q_of(i, j);
+  const float* lp = l_of(i, j);
+  const uint16_t* const q_end = q_of(w.n - 1, a.group - 1);
+  const float* const l_end = l_of(w.n - 1, a.group - 1);
+  uint4 q[2][kSteps];
+  float e[2];
+  int row[2];
+  auto load = [&](int b, int r) {
+    const bool in = r + c < w.pairs;
+    row[b] = i;
+    load_row<D>(in ? qp : q_end, a.q_wide, q[b]);
+    e[b] = *(in ? lp : l_end);   // (as it comes: a test here would wait for all that is on its way)
+    i += di;
+    j += dj;
+    qp += q_step;
+    lp += l_step;
+    const bool turn = j >= a.group;
+    j -= turn ? a.group : 0;
+    i += turn ? 1 : 0;
+    qp += turn ? q_turn : 0;
+    lp += turn ? l_turn : 0;
+  };
+  auto add = [&](int b, int r) {
+    const bool whole = !a.mask.p_dev && t0 + kTokens <= (a.causal ? min(w.len, hidden + r / a.group + 1) : w.len);
+    const bool out = r + c >= w.pairs || e[b] == -__builtin_inff();
+    const float less = out ? __builtin_inff() : e[b];   // no row, or one that sees no token: 2^(-inf) each
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+    for (int n = 0; n < kStrips; ++n) {
+      kv_f4 x[2];
+      x[0] = x[1] = kv_f4{0, 0, 0, 0};
 #pragma unroll
-    for (int d = 1; d < 16; d <<= 1) sum[i] += __shfl_xor(sum[i], d);
-    const int t = t0 + 16 * (i >> 2) + 4 * g + (i & 3);
-    if (c == 0 && t < w.len && t < a.weights.cols)
-      static_cast<float*>(a.weights.p_dev)[w.s * a.weights.seq_stride + h * a.weights.head_stride + t] += sum[i];
+      for (int s = 0; s < kSteps; ++s) {
+        x[0] = mfma<BF16>(y[2 * n][s], q[b][s], x[0]);
+        x[1] = mfma<BF16>(y[2 * n + 1][s], q[b][s], x[1]);
+      }
+#pragma unroll
+      for (int v = 0; v < 8; ++v) x[v >> 2][v & 3] = __builtin_fmaf(x[v >> 2][v & 3], a.scale2, -less);
+      if (!whole) {
+        const int end = a.causal ? min(w.len, hidden + row[b] + 1) : w.len;
+        hide(x, seen_bits(a.mask.p_dev, mb[n], t0 + n * kKvStrip, end));
+      }
+#pragma unroll
+      for (int v = 0; v < 8; ++v) sum[n][v] += __builtin_amdgcn_exp2f(x[v >> 2][v & 3]);
+    }
+  };
+  load(0, r0);
+  while (r0 < w.pairs) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      if (r0 >= w.pairs) break;
+      load(1 - b, r0 + kStep);
+      add(b, r0);
+      r0 += kStep;
+    }
+  }
+  __shared__ float total[kAttWaves][kTokens];
+#pragma unroll
+  for (int n = 0; n < kStrips; ++n)
+#pragma unroll
+    for (int v = 0; v < 8; ++v) {
+#pragma unroll
+      for (int d = 1; d < 16; d <<= 1) sum[n][v] += __shfl_xor(sum[n][v], d);
+      if (c == 0) total[wave][n * kKvStrip + 16 * (v >> 2) + 4 * g + (v & 3)] = ok[n] ? sum[n][v] : 0.0f;
+    }
+  __syncthreads();
+  const int t = t0 + (int)threadIdx.x;
+  if ((int)threadIdx.x < kTokens && t < w.len && t < a.weights.cols) {
+    float all = 0.0f;
+#pragma unroll
+    for (int n = 0; n < kAttWaves; ++n) all += total[n][threadIdx.x];
+    static_cast<float*>(a.weights.p_dev)[w.s * a.weights.seq_stride + h * a.weights.head_stride + t] += all;
   }
 }
 
@@ -473,7 +545,8 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
     LAM_HIP(hipGetLastError());
   }
   if (weights.p_dev && !keep && a.cut > 0) {
-    const int64_t wb = (a.cut + kKvStrip * kAttWaves - 1) / (kKvStrip * kAttWaves) * v.kv_heads * v.n_seqs;
+    const int tokens = (v.head_dim == 256 ? weight_strips<256>() : weight_strips<128>()) * kKvStrip;
+    const int64_t wb = (a.cut + tokens - 1) / tokens * v.kv_heads * v.n_seqs;
     LAM_CHECK(wb < (1LL << 31), LAM_EINVAL, "too many sequences for one launch");
     LAM_TRY(prof_launch_events(ctx, "kv_weights", &e0, &e1));
 #define LAM_GO(D, BF) \
