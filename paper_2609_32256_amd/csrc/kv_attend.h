@@ -20,8 +20,11 @@ constexpr int kAttRows = 16;        // rows of a tile of the kernel for single t
 // within float16, and those 2^-21 below the maximum are still normal numbers.
 constexpr float kLift = 7.0f, kSpan = 15.0f;
 constexpr float kNoMax = -3.0e38f;   // no token seen yet
-constexpr int kFill = 768;            // workgroups that fill the chip: three of four waves a compute unit
-constexpr int kFillWaves = 2048;      // and of one wave: two a SIMD
+// Workgroups (of four waves) that a call is split over where its tiles are fewer:
+// three a compute unit for single tokens, which is as many as run at once; for
+// chunks twice the two that do, so that unequal parts even out.
+constexpr int kFill = 768, kFillChunk = 1024;
+constexpr int kChunkGrain = 512;      // least tokens of a part of a chunk's tile: its sums are 64 rows
 constexpr int64_t kKeptBytes = 1LL << 30;   // most scratch for kept scores
 
 struct AttendArgs {
@@ -35,6 +38,7 @@ struct AttendArgs {
   int flip;               // the scale is negative
   int64_t cut;            // lengths are cut to it
   int tiles_per_seq;      // where every sequence has the same number of rows
+  int join_rows;          // rows a wave joins
   int split_to;           // workgroups to split the lengths over, 0: none is split
   lam_kv_slots mask, weights;
   uint16_t* out;
@@ -83,9 +87,11 @@ struct LaneSeq {
 // (equal parts of the longest length had left a ragged batch's short sequences
 // with empty ones).  The last part of a tile is half full on average, so the parts are for
 // split_to less half the tiles.  All lanes of a wave look at a sequence each.
-// id: a workgroup, or (by_seq) a sequence whose plan is wanted.
-template <int R>
-__device__ __forceinline__ Work plan(const AttendArgs& a, uint32_t id, bool by_seq) {
+// id: a workgroup; or a sequence, or a unit (a tile of a head), whose plan is wanted.
+enum class PlanOf { kWorkgroup, kSequence, kUnit };
+
+template <int R, PlanOf OF>
+__device__ __forceinline__ Work plan(const AttendArgs& a, uint32_t id) {
   const int lane = threadIdx.x & 63;
   double tokens = 0.0, units = 0.0;
   for (int b = 0; b < a.c.n_seqs; b += 64) {
@@ -94,26 +100,28 @@ __device__ __forceinline__ Work plan(const AttendArgs& a, uint32_t id, bool by_s
     units += (double)q.tiles;
   }
   const float all = (float)wave_sum_f64(tokens) * a.c.heads, half = 0.5f * (float)wave_sum_f64(units) * a.c.heads;
-  constexpr int kGrain = kKvStrip * kAttWaves;
+  constexpr int kStrips = kKvStrip * kAttWaves, kGrain = R == kAttRows ? kStrips : kChunkGrain;
   const float want = all / fmaxf((float)a.split_to - half, 0.5f * a.split_to) * 1.0001f;
   Work w;
   w.s = -1;
   w.tokens = (int)fminf(floorf(want / kGrain) * kGrain + kGrain, 2147483520.0f);
-  uint32_t before = 0;
+  uint32_t before = 0, units_before = 0;
   for (int b = 0; b < a.c.n_seqs; b += 64) {
     const LaneSeq q(a, b + lane, R);
     const int parts = max(1, (q.len + w.tokens - 1) / w.tokens);
-    const int even = ((q.len + parts - 1) / parts + kGrain - 1) / kGrain * kGrain;   // its parts made equal
-    const uint32_t mine = (uint32_t)(q.tiles * a.c.heads * parts);
-    uint32_t upto = mine;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const uint32_t o = __shfl_up(upto, d);
-      if (lane >= d) upto += o;
+    const int even = ((q.len + parts - 1) / parts + kStrips - 1) / kStrips * kStrips;   // its parts made equal
+    const uint32_t my_units = (uint32_t)(q.tiles * a.c.heads), mine = my_units * parts;
+    const uint32_t upto = wave_scan_u32(mine) + before;
+    unsigned long long hit;
+    uint32_t units_upto = 0;
+    if constexpr (OF == PlanOf::kWorkgroup) {
+      hit = __ballot(upto > id);
+    } else if constexpr (OF == PlanOf::kSequence) {
+      hit = (uint32_t)b <= id && id < (uint32_t)b + 64u ? 1ull << (id - b) : 0ull;
+    } else {
+      units_upto = wave_scan_u32(my_units) + units_before;
+      hit = __ballot(units_upto > id);
     }
-    upto += before;
-    const unsigned long long hit =
-        by_seq ? ((uint32_t)b <= id && id < (uint32_t)b + 64u ? 1ull << (id - b) : 0ull) : __ballot(upto > id);
     if (hit) {
       const int l = (int)__builtin_ctzll(hit);
       w.s = b + l;
@@ -125,13 +133,23 @@ __device__ __forceinline__ Work plan(const AttendArgs& a, uint32_t id, bool by_s
       w.tokens = __builtin_amdgcn_readlane(even, l);
       w.base = (uint32_t)__builtin_amdgcn_readlane((int)(upto - mine), l);
       w.pairs = w.n * a.group;
-      const uint32_t in = id - w.base, unit = in / (uint32_t)w.parts;
-      w.part = (int)(in % (uint32_t)w.parts);
-      w.h = (int)(unit % (uint32_t)a.c.heads);
-      w.r0 = (int)(unit / (uint32_t)a.c.heads) * R;
+      if constexpr (OF != PlanOf::kSequence) {
+        uint32_t unit = id - (uint32_t)__builtin_amdgcn_readlane((int)(units_upto - my_units), l);
+        w.part = 0;
+        if constexpr (OF == PlanOf::kWorkgroup) {
+          const uint32_t in = id - w.base;
+          unit = in / (uint32_t)w.parts;
+          w.part = (int)(in % (uint32_t)w.parts);
+        } else {
+          w.base += unit * w.parts;   // the unit's own first workgroup
+        }
+        w.h = (int)(unit % (uint32_t)a.c.heads);
+        w.r0 = (int)(unit / (uint32_t)a.c.heads) * R;
+      }
       break;
     }
     before = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+    if constexpr (OF == PlanOf::kUnit) units_before = (uint32_t)__builtin_amdgcn_readlane((int)units_upto, 63);
   }
   return w;
 }
@@ -190,7 +208,7 @@ __device__ __forceinline__ Work tile_work(const AttendArgs& a, uint32_t id) {
 
 template <int R>
 __device__ __forceinline__ Work work_of(const AttendArgs& a, uint32_t id) {
-  return a.split_to ? plan<R>(a, id, false) : tile_work<R>(a, id);
+  return a.split_to ? plan<R, PlanOf::kWorkgroup>(a, id) : tile_work<R>(a, id);
 }
 
 // Tokens that pair r of the sequence sees: those below this.
@@ -498,6 +516,66 @@ __device__ __forceinline__ void write_row(const AttendArgs& a, int64_t row, int 
   }
 }
 
+
+// Where the waves of a workgroup put their sums of 16 rows to be joined.
+template <int D>
+struct JoinSpace {
+  float m[kAttWaves][kAttRows], l[kAttWaves][kAttRows];
+  __align__(16) float o[kAttWaves][kAttRows][D + 4];
+};
+
+// Joins the waves' sums of the 16 rows from r0 on, relative to the largest
+// maximum; 16 lanes a row write them out, or as the part's.  slot: where the
+// first row's partial results go.
+template <int D, bool BF16>
+__device__ __forceinline__ void join_waves(const AttendArgs& a, const Work& w, int r0, int64_t slot, const Row& row,
+                                           const kv_f4 o[D / 16], JoinSpace<D>& js) {
+  constexpr int kRun = D / 16;
+  const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4, wave = threadIdx.x >> 6;
+  const float m = row.reference(), l = row.sum();
+  if (g == 0) {
+    js.m[wave][c] = m;
+    js.l[wave][c] = l;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < kRun; j += 4)
+      *reinterpret_cast<kv_f4*>(&js.o[wave][c][(4 * g + i) * kRun + j]) =
+          kv_f4{o[j][i], o[j + 1][i], o[j + 2][i], o[j + 3][i]};
+  __syncthreads();
+  const int col = threadIdx.x >> 4, run = threadIdx.x & 15;
+  const int pair = r0 + col;
+  if (pair >= w.pairs) return;
+  float M = js.m[0][col];
+#pragma unroll
+  for (int i = 1; i < kAttWaves; ++i) M = fmaxf(M, js.m[i][col]);
+  float f[kAttWaves], sum = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kAttWaves; ++i) {
+    f[i] = __builtin_amdgcn_exp2f(js.m[i][col] - M);
+    sum += f[i] * js.l[i][col];
+  }
+  float acc[kRun];
+#pragma unroll
+  for (int j = 0; j < kRun; ++j) {
+    acc[j] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kAttWaves; ++i) acc[j] += f[i] * js.o[i][col][run * kRun + j];
+  }
+  if (w.parts > 1) {
+    if (run == 0) {
+      a.part_m[slot + col] = M;
+      a.part_l[slot + col] = sum;
+    }
+    float* d = a.part_o + (slot + col) * D + run * kRun;
+#pragma unroll
+    for (int j = 0; j < kRun; j += 4) *reinterpret_cast<kv_f4*>(d + j) = kv_f4{acc[j], acc[j + 1], acc[j + 2], acc[j + 3]};
+  } else {
+    const int64_t at = (w.first + pair / a.group) * a.q_heads + w.h * a.group + pair % a.group;
+    write_row<D, BF16>(a, at, run, acc, M, sum);
+  }
+}
 
 // Rows of a tile of the kernel for chunks (kv_chunk.hip), and its launch.
 __host__ __device__ constexpr int chunk_rows(int D) { return D == 256 ? 32 : 64; }

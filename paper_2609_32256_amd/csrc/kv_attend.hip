@@ -148,54 +148,8 @@ __global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : 3) void k_kv_attend(Att
     }
   }
   kv_f4(&o)[kRun] = r.o;
-  const float m = r.row.reference(), l = r.row.sum();
-
-  // the waves' parts: every wave's sums relative to the largest maximum
-  __shared__ float sm[kAttWaves][kAttRows], sl[kAttWaves][kAttRows];
-  __shared__ __align__(16) float so[kAttWaves][kAttRows][D + 4];
-  if (g == 0) {
-    sm[wave][c] = m;
-    sl[wave][c] = l;
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < kRun; j += 4)
-      *reinterpret_cast<kv_f4*>(&so[wave][c][(4 * g + i) * kRun + j]) =
-          kv_f4{o[j][i], o[j + 1][i], o[j + 2][i], o[j + 3][i]};
-  __syncthreads();
-  const int col = threadIdx.x >> 4, run = threadIdx.x & 15;
-  const int pair = w.r0 + col;
-  if (pair >= w.pairs) return;
-  float M = sm[0][col];
-#pragma unroll
-  for (int i = 1; i < kAttWaves; ++i) M = fmaxf(M, sm[i][col]);
-  float f[kAttWaves], sum = 0.0f;
-#pragma unroll
-  for (int i = 0; i < kAttWaves; ++i) {
-    f[i] = __builtin_amdgcn_exp2f(sm[i][col] - M);
-    sum += f[i] * sl[i][col];
-  }
-  float acc[kRun];
-#pragma unroll
-  for (int j = 0; j < kRun; ++j) {
-    acc[j] = 0.0f;
-#pragma unroll
-    for (int i = 0; i < kAttWaves; ++i) acc[j] += f[i] * so[i][col][run * kRun + j];
-  }
-  const int64_t row = (w.first + pair / a.group) * a.q_heads + h * a.group + pair % a.group;
-  if (w.parts > 1) {
-    const int64_t p = (int64_t)blockIdx.x * kAttRows + col;
-    if (run == 0) {
-      a.part_m[p] = M;
-      a.part_l[p] = sum;
-    }
-    float* d = a.part_o + p * D + run * kRun;
-#pragma unroll
-    for (int j = 0; j < kRun; j += 4) *reinterpret_cast<kv_f4*>(d + j) = kv_f4{acc[j], acc[j + 1], acc[j + 2], acc[j + 3]};
-    return;
-  }
-  write_row<D, BF16>(a, row, run, acc, M, sum);
+  __shared__ JoinSpace<D> js;
+  join_waves<D, BF16>(a, w, w.r0, (int64_t)blockIdx.x * kAttRows, r.row, r.o, js);
 }
 
 // Maximum and sum of row `col` of a tile over its parts, the first of which is workgroup `at`'s.
@@ -204,40 +158,59 @@ __device__ __forceinline__ float joined(const AttendArgs& a, uint32_t at, int co
   const float* pm = a.part_m + (int64_t)at * R + col;
   const float* pl = a.part_l + (int64_t)at * R + col;
   float M = kNoMax, total = 0.0f;
-#pragma unroll 4
+#pragma unroll 8
   for (int i = 0; i < parts; ++i) M = fmaxf(M, pm[i * R]);
-#pragma unroll 4
+#pragma unroll 8
   for (int i = 0; i < parts; ++i) total += __builtin_amdgcn_exp2f(pm[i * R] - M) * pl[i * R];
   *sum = total;
   return M;
 }
 
-// Joins the parts of a tile: the workgroup that has the place of the tile's first
-// one in the attention; 16 lanes a row, D/16 channels a lane.
+// One row of a unit, by a wave.
 template <int D, bool BF16, int R>
-__device__ __forceinline__ void join_rows(const AttendArgs& a, uint32_t block) {
-  constexpr int kRun = D / 16;
-  const Work w = plan<R>(a, block, false);
-  if (w.s < 0 || w.part != 0 || w.parts == 1) return;
-  const int run = threadIdx.x & 15;
-  for (int col = threadIdx.x >> 4; col < R; col += kAttThreads / 16) {
-    const int pair = w.r0 + col;
-    if (pair >= w.pairs) return;
-    float sum;
-    const float M = joined<R>(a, block, col, w.parts, &sum);
-    float acc[kRun] = {};
-    const float* po = a.part_o + ((int64_t)block * R + col) * D + run * kRun;
+__device__ __forceinline__ void join_row(const AttendArgs& a, const Work& w, int col) {
+  constexpr int kLanes = D / 4, kGroups = 64 / kLanes;
+  const int pair = w.r0 + col;
+  const int lane = threadIdx.x & 63, sub = lane % kLanes, group = lane / kLanes;
+  const int64_t slot = (int64_t)w.base * R + col;
+  float sum;
+  const float M = joined<R>(a, w.base, col, w.parts, &sum);
+  kv_f4 acc{0, 0, 0, 0};
+  const float* po = a.part_o + slot * D + 4 * sub;
 #pragma unroll 4
-    for (int i = 0; i < w.parts; ++i) {
-      const float f = __builtin_amdgcn_exp2f(a.part_m[((int64_t)block + i) * R + col] - M);
+  for (int i = group; i < w.parts; i += kGroups)
+    acc += __builtin_amdgcn_exp2f(a.part_m[slot + (int64_t)i * R] - M) * *reinterpret_cast<const kv_f4*>(po + (int64_t)i * R * D);
 #pragma unroll
-      for (int j = 0; j < kRun; ++j) acc[j] += f * po[(int64_t)i * R * D + j];
-    }
-    const int64_t row = (w.first + pair / a.group) * a.q_heads + w.h * a.group + pair % a.group;
-    write_row<D, BF16>(a, row, run, acc, M, sum);
+  for (int d = kLanes; d < 64; d <<= 1)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[j] += __shfl_xor(acc[j], d);
+  if (group != 0) return;
+  const int64_t at = (w.first + pair / a.group) * a.q_heads + w.h * a.group + pair % a.group;
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  uint2 u;
+  u.x = (uint32_t)to_out(acc[0] * inv, BF16) | ((uint32_t)to_out(acc[1] * inv, BF16) << 16);
+  u.y = (uint32_t)to_out(acc[2] * inv, BF16) | ((uint32_t)to_out(acc[3] * inv, BF16) << 16);
+  *reinterpret_cast<uint2*>(a.out + at * D + 4 * sub) = u;
+  if (sub == 0) {
+    const float e = log_sum(M, sum);
+    if (a.lse2) a.lse2[at] = e;
+    if (a.lse) a.lse[at] = e * 0.6931471805599453f;
   }
 }
 
+// Joins the parts of some rows of a unit (a.join_rows for each wave): D/4 lanes hold
+// a part's channels, the wave's groups of them every other (or fourth) part.
+template <int D, bool BF16, int R>
+__device__ __forceinline__ void join_rows(const AttendArgs& a, uint32_t block) {
+  const uint32_t blocks = R / (kAttWaves * (uint32_t)a.join_rows);   // of a unit
+  const Work w = plan<R, PlanOf::kUnit>(a, block / blocks);
+  if (w.s < 0 || w.parts == 1) return;
+  for (int n = 0; n < a.join_rows; ++n) {
+    const int col = ((int)(block % blocks) * a.join_rows + n) * kAttWaves + (int)(threadIdx.x >> 6);
+    if (w.r0 + col >= w.pairs) return;
+    join_row<D, BF16, R>(a, w, col);
+  }
+}
 // Weights from the scores that the attention kept: a workgroup takes 1,024 tokens of one
 // head, four a thread, and sums p = 2^(s - lse) over the sequence's rows in their order.
 constexpr int kKeptTokens = 4 * kAttThreads;
@@ -252,7 +225,7 @@ __device__ __forceinline__ void add_kept(const AttendArgs& a, uint32_t block) {
   if ((int)(block % chunks) * kKeptTokens >= len) return;
   Work q;
   q.parts = 1;
-  if (a.split_to) q = plan<kAttRows>(a, (uint32_t)s, true);
+  if (a.split_to) q = plan<kAttRows, PlanOf::kSequence>(a, (uint32_t)s);
   float* d = static_cast<float*>(a.weights.p_dev) + s * a.weights.seq_stride + h * a.weights.head_stride + t;
   float w[4];
 #pragma unroll
@@ -471,7 +444,7 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
   // The kernel for chunks where sequences have more than a tile of the other's rows on average.
   const bool chunk = v.rows * a.group > kAttRows * (int64_t)v.n_seqs;
   const int rows = chunk ? chunk_rows(v.head_dim) : kAttRows;
-  const int fill = chunk ? kFillWaves : kFill;
+  const int fill = chunk ? kFillChunk : kFill;
   int64_t tiles;
   if (v.starts_dev) {
     tiles = v.rows * a.group / rows + v.n_seqs;
@@ -482,7 +455,7 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
   // Lengths are split where the tiles do not fill the chip.
   const int64_t units = tiles * v.kv_heads;
   int64_t blocks = units;
-  if (units < fill && a.cut > kKvStrip * kAttWaves) {
+  if (units < fill && a.cut > (chunk ? kChunkGrain : kKvStrip * kAttWaves)) {
     a.split_to = fill;
     blocks = fill + units;   // see plan(): at most split_to - units / 2 (or split_to / 2) full parts, and one more a tile
   }
@@ -526,7 +499,8 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
 #undef LAM_GO
   LAM_HIP(hipGetLastError());
   }
-  const int64_t join_blocks = a.split_to ? blocks : 0;
+  a.join_rows = units * rows >= 8192 ? 4 : 1;   // few rows: each its own wave, many: four, and a quarter of the plans
+  const int64_t join_blocks = a.split_to ? units * (rows / (kAttWaves * a.join_rows)) : 0;
   const int64_t kept_blocks = keep ? a.kept_cols / kKeptTokens * v.kv_heads * v.n_seqs : 0;
   if (join_blocks + kept_blocks > 0) {
     LAM_CHECK(join_blocks + kept_blocks < (1LL << 31), LAM_EINVAL, "too many rows for one launch");

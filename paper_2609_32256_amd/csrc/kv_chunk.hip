@@ -1,10 +1,11 @@
 // Attention of chunks of queries over the 4-bit cache (lam_kv_attend where a
 // sequence has more than a few rows).
 //
-// As in kv_attend.hip a wave walks strips of 32 tokens and keeps everything but
-// the queries in registers; here it takes 64 query rows (32 for heads of 256
-// channels), so that a strip's conversions serve four products instead of one.
-// One wave is a workgroup: nothing is shared, nothing waits at a barrier.
+// As in kv_attend.hip the waves of a workgroup walk strips of 32 tokens and keep
+// everything but the queries in registers; here they take 64 query rows (32 for
+// heads of 256 channels), so that a strip's conversions serve four products instead of
+// one.  The queries lie in LDS for all of them; they meet only at the end, when
+// their sums are joined.
 #include <hip/hip_ext.h>
 
 #include "kv_attend.h"
@@ -13,9 +14,10 @@ namespace lam {
 namespace {
 
 template <int D, bool BF16, bool MASK>
-__global__ __launch_bounds__(64, D == 256 ? 1 : 2) void k_kv_chunk(AttendArgs a) {
+__global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) void k_kv_chunk(AttendArgs a) {
   constexpr int kRun = D / 16, kRows = chunk_rows(D), kTiles = kRows / 16, kSteps = D / 32;
-  const int lane = threadIdx.x, c = lane & 15, g = lane >> 4;
+  const int lane = threadIdx.x & 63, c = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Work w = work_of<kRows>(a, blockIdx.x);
   if (w.s < 0) return;
   const int T = 1 << a.c.page_shift;
@@ -23,13 +25,14 @@ __global__ __launch_bounds__(64, D == 256 ? 1 : 2) void k_kv_chunk(AttendArgs a)
 
   // the queries, as B operands, for the whole walk
   __shared__ uint4 sq[kTiles][kSteps][64];
-#pragma unroll
-  for (int t = 0; t < kTiles; ++t) {
+  for (int t = wave; t < kTiles; t += kAttWaves) {
     uint4 q[kSteps];
     load_q<D>(a, w, w.h, w.r0 + 16 * t, q);
 #pragma unroll
     for (int j = 0; j < kSteps; ++j) sq[t][j][lane] = q[j];
   }
+
+  __syncthreads();
 
   const int end_first = pair_end(a, w, w.r0), end_last = pair_end(a, w, min(w.r0 + kRows, w.pairs) - 1);
   const int64_t part_at = (int64_t)w.part * w.tokens;
@@ -53,15 +56,16 @@ __global__ __launch_bounds__(64, D == 256 ? 1 : 2) void k_kv_chunk(AttendArgs a)
   const int last_col = max(a.c.table_cols - 1, 0);
   auto entry = [&](int t) { return entries[min(t >> a.c.page_shift, last_col)]; };
   const uint32_t n_pages = (uint32_t)a.c.n_pages;
-  // the strip to load next: its page's address is worked out once a page
+  // the page of the strip to load next
   uint8_t* head;
   bool ok_page;
   auto turn = [&](int32_t page) {
     ok_page = (uint32_t)page < n_pages;
     head = a.c.head_page(ok_page ? page : 0, w.h, head_bytes);
   };
-  int t0 = from;
-  int32_t next = entry(t0 - (t0 & (T - 1)) + T);
+  constexpr int kStep = kKvStrip * kAttWaves;
+  int t0 = from + wave * kKvStrip;
+  int32_t next = entry(t0 + kStep);
   turn(entry(t0));
   bool ok = t0 < to && ok_page;
   {
@@ -70,15 +74,13 @@ __global__ __launch_bounds__(64, D == 256 ? 1 : 2) void k_kv_chunk(AttendArgs a)
     load_vals<D>(rs, at, v);
     if constexpr (MASK) mb = load_mask(mrs, t0);
   }
-  for (; t0 < to; t0 += kKvStrip) {
+  for (; t0 < to; t0 += kStep) {
     uint4 y[2][kSteps];
     key_operand<D, BF16>(k, at.shift, 0, y[0]);
     key_operand<D, BF16>(k, at.shift, 1, y[1]);
-    const int t1 = t0 + kKvStrip;
-    if ((t1 & (T - 1)) == 0) {
-      turn(next);
-      next = entry(t1 + T);
-    }
+    const int t1 = t0 + kStep;
+    turn(next);
+    next = entry(t1 + kStep);
     const bool ok_next = t1 < to && ok_page;
     const StripRsrc rs = strip_rsrc<D>(head, T, t1 & (T - 1), ok_next);
     load_keys<D>(rs, at, k);
@@ -133,33 +135,11 @@ __global__ __launch_bounds__(64, D == 256 ? 1 : 2) void k_kv_chunk(AttendArgs a)
     ok = ok_next;
   }
 
+  __shared__ JoinSpace<D> js;
 #pragma unroll
   for (int t = 0; t < kTiles; ++t) {
-    const float sum = row[t].sum(), m = row[t].reference();
-    const int pair = w.r0 + 16 * t + c;
-    if (pair >= w.pairs) continue;
-    if (w.parts > 1) {
-      const int64_t p = (int64_t)blockIdx.x * kRows + 16 * t + c;
-      if (g == 0) {
-        a.part_m[p] = m;
-        a.part_l[p] = sum;
-      }
-      float* d = a.part_o + p * D + 4 * g * kRun;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < kRun; j += 4)
-          *reinterpret_cast<kv_f4*>(d + i * kRun + j) = kv_f4{o[t][j][i], o[t][j + 1][i], o[t][j + 2][i], o[t][j + 3][i]};
-    } else {
-      const int64_t at = (w.first + pair / a.group) * a.q_heads + w.h * a.group + pair % a.group;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float acc[kRun];
-#pragma unroll
-        for (int j = 0; j < kRun; ++j) acc[j] = o[t][j][i];
-        write_row<D, BF16>(a, at, 4 * g + i, acc, m, sum);
-      }
-    }
+    if (t > 0) __syncthreads();   // (all 256 threads get here for every tile)
+    join_waves<D, BF16>(a, w, w.r0 + 16 * t, (int64_t)blockIdx.x * kRows + 16 * t, row[t], o[t], js);
   }
 }
 
@@ -171,10 +151,10 @@ lam_status launch_kv_chunk(lam_ctx* ctx, const lam_kv_view& v, const AttendArgs&
 #define LAM_GO(D, BF)                                                                                            \
   do {                                                                                                           \
     if (masked)                                                                                                  \
-      hipExtLaunchKernelGGL((k_kv_chunk<D, BF, true>), dim3((unsigned)blocks), dim3(64), 0, ctx->stream, e0, e1, \
+      hipExtLaunchKernelGGL((k_kv_chunk<D, BF, true>), dim3((unsigned)blocks), dim3(kAttThreads), 0, ctx->stream, e0, e1, \
                             0, a);                                                                               \
     else                                                                                                         \
-      hipExtLaunchKernelGGL((k_kv_chunk<D, BF, false>), dim3((unsigned)blocks), dim3(64), 0, ctx->stream, e0,    \
+      hipExtLaunchKernelGGL((k_kv_chunk<D, BF, false>), dim3((unsigned)blocks), dim3(kAttThreads), 0, ctx->stream, e0,    \
                             e1, 0, a);                                                                           \
   } while (0)
   LAM_KV_DISPATCH(v, LAM_GO);

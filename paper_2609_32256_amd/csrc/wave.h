@@ -56,6 +56,19 @@ __device__ __forceinline__ double wave_sum_f64(double v) {
   return __longlong_as_double((long long)(((unsigned long long)rhi << 32) | rlo));
 }
 
+// Inclusive sums over the lanes of a wave, in lane order: within rows of 16 by
+// shifts of 1, 2, 4 and 8 lanes (a lane past the row's edge gets 0), then the ends
+// of rows 0 and 2 into rows 1 and 3, then lane 31's into rows 2 and 3.
+__device__ __forceinline__ uint32_t wave_scan_u32(uint32_t v) {
+  v += (uint32_t)LAM_DPP_MOVE(0, v, 0x111, 0xf);
+  v += (uint32_t)LAM_DPP_MOVE(0, v, 0x112, 0xf);
+  v += (uint32_t)LAM_DPP_MOVE(0, v, 0x114, 0xf);
+  v += (uint32_t)LAM_DPP_MOVE(0, v, 0x118, 0xf);
+  v += (uint32_t)LAM_DPP_MOVE(0, v, 0x142, 0xa);
+  v += (uint32_t)LAM_DPP_MOVE(0, v, 0x143, 0xc);
+  return v;
+}
+
 // The largest of each quad's four values, in all four lanes (which must be active together).
 __device__ __forceinline__ float quad_max_f32(float v) {
   v = fmaxf(v, __int_as_float(LAM_DPP_MOVE(__float_as_int(v), __float_as_int(v), 0xb1, 0xf)));
