@@ -3,6 +3,7 @@
 #include <hip/hip_ext.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "kv.h"
 #include "lam_internal.h"
@@ -200,9 +201,48 @@ struct EvictArgs {
   int32_t moves;                          // most moves of a sequence's head
   int32_t* kept;
   int32_t* lengths_out;
-  int32_t* holes;    // [seq][head][moves]
-  int32_t* extras;
-  int32_t* n_moves;  // [seq][head]
+  int32_t* lists;   // of a long cache's holes and extra slots: [seq][head][2][moves]
+};
+
+// What one sequence's head selects from and writes to.
+struct EvictHead {
+  const float* sc;
+  const int32_t* ps;   // or null: the slot
+  float* so;
+  int32_t* po;         // or null
+  int32_t* kept;
+  int len, newest;
+
+  __device__ __forceinline__ EvictHead(const KvArgs& a, const EvictArgs& e, int bh) {
+    const int s = bh / a.heads, h = bh % a.heads;
+    auto at = [&](const lam_kv_slots& x) -> int64_t { return s * x.seq_stride + h * x.head_stride; };
+    len = min(a.length(s), e.bound);
+    sc = static_cast<const float*>(e.scores.p_dev) + at(e.scores);
+    ps = e.positions.p_dev ? static_cast<const int32_t*>(e.positions.p_dev) + at(e.positions) : nullptr;
+    so = static_cast<float*>(e.scores_out.p_dev) + at(e.scores_out);
+    po = e.positions_out.p_dev ? static_cast<int32_t*>(e.positions_out.p_dev) + at(e.positions_out) : nullptr;
+    kept = e.kept + (int64_t)bh * e.budget;
+    newest = len > 0 ? (ps ? ps[len - 1] : len - 1) : 0;
+  }
+  __device__ __forceinline__ int pos(int t) const { return ps ? ps[t] : t; }
+  // new slot t holds what old slot `from` held
+  __device__ __forceinline__ void keep(int t, int from) const {
+    kept[t] = from;
+    so[t] = sc[from];
+    if (po) po[t] = pos(from);
+  }
+  // nothing to evict: the tokens stay as they are
+  __device__ __forceinline__ void keep_all(int budget) const {
+    for (int t = threadIdx.x; t < budget; t += blockDim.x) {
+      if (t < len) {
+        keep(t, t);
+      } else {
+        kept[t] = -1;
+        so[t] = 0.0f;
+        if (po) po[t] = -1;
+      }
+    }
+  }
 };
 
 // Order of the scores as unsigned integers: protected slots above all, NaN below all.
@@ -213,48 +253,200 @@ __device__ __forceinline__ uint32_t evict_key(float s, int pos, int newest, int 
   return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
 }
 
-// One workgroup per sequence and head.  The budget-th largest key is found digit
-// by digit (four histograms of 256 counts); then one pass over the slots in order
-// marks those that stay (ties by slot) and lists the holes below budget and the
-// kept slots beyond it.
+// Digits of a key, from the top: sign, exponent and two bits of the fraction
+// spread weights over the counters of a histogram.
+constexpr int kDigits = 3, kDigitBits[kDigits] = {11, 11, 10}, kDigitShift[kDigits] = {21, 10, 0};
+constexpr int kBins = 1 << 11;
+
+// One workgroup per sequence and head, the keys of up to 1,024 KPT slots in its
+// registers (thread i has slots i, i + 1024, ...).  The budget-th largest key is
+// found digit by digit with histograms in LDS; a wave whose digits are all the same
+// (weights of 0, say) adds them at once; it ends as soon as a digit's keys all stay.
+// Then holes below budget and slots kept beyond it are ranked by their place, and the i-th hole
+// takes the i-th such slot.  Bound by its one reading of scores and positions.
+// (A search bit by bit, each a count of all keys, took 25 us more for 32,768 slots.)
+template <int KPT>
 __global__ __launch_bounds__(kSelThreads) void k_kv_select(KvArgs a, EvictArgs e) {
-  const int bh = blockIdx.x;
-  const int s = bh / a.heads, h = bh % a.heads;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int len = min(a.length(s), e.bound);
-  const float* sc = static_cast<const float*>(e.scores.p_dev) + s * e.scores.seq_stride + h * e.scores.head_stride;
-  const int32_t* ps = e.positions.p_dev ? static_cast<const int32_t*>(e.positions.p_dev) + s * e.positions.seq_stride +
-                                              h * e.positions.head_stride
-                                        : nullptr;
-  float* so = static_cast<float*>(e.scores_out.p_dev) + s * e.scores_out.seq_stride + h * e.scores_out.head_stride;
-  int32_t* po = e.positions_out.p_dev ? static_cast<int32_t*>(e.positions_out.p_dev) +
-                                            s * e.positions_out.seq_stride + h * e.positions_out.head_stride
-                                      : nullptr;
-  int32_t* kept = e.kept + (int64_t)bh * e.budget;
-  int32_t* holes = e.holes + (int64_t)bh * e.moves;
-  int32_t* extras = e.extras + (int64_t)bh * e.moves;
-  if (len <= e.budget) {
-    for (int t = tid; t < e.budget; t += kSelThreads) {
-      const bool in = t < len;
-      kept[t] = in ? t : -1;
-      so[t] = in ? sc[t] : 0.0f;
-      if (po) po[t] = in ? (ps ? ps[t] : t) : -1;
-    }
-    if (tid == 0) e.n_moves[bh] = 0;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const EvictHead d(a, e, blockIdx.x);
+  if (d.len <= e.budget) {
+    d.keep_all(e.budget);
     return;
   }
+  constexpr int kCounts = KPT * kSelWaves;   // of 64 slots each, in the order of the slots
+  __shared__ uint32_t hist[kBins], found[3];
+  __shared__ uint32_t hole_at[kCounts], extra_at[kCounts], sums[2][kSelWaves];
+  __shared__ uint16_t extras[KPT * kSelThreads / 2];
+
+  // in batches whose loads are all on their way before the first is used
+  constexpr int kBatch = KPT < 16 ? KPT : 16;
+  uint32_t key[KPT];
+  auto fill = [&](auto has_positions) {
+#pragma unroll
+    for (int k0 = 0; k0 < KPT; k0 += kBatch) {
+      float s[kBatch];
+      int p[kBatch];
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        const uint32_t t = min((k0 + j) * kSelThreads + tid, d.len - 1);
+        s[j] = d.sc[t];
+        p[j] = has_positions ? d.ps[t] : (int)t;
+      }
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j)
+        key[k0 + j] = (k0 + j) * kSelThreads + tid < d.len ? evict_key(s[j], p[j], d.newest, e.recent, e.sinks) : 0u;
+    }
+  };
+  if (d.ps) fill(std::true_type{}); else fill(std::false_type{});
+  // the budget-th largest key: the digits found so far, and how many slots of theirs stay
+  uint32_t least = 0;
+  int ties = e.budget;
+  bool exact = false;   // all of them do
+#pragma unroll
+  for (int n = 0; n < kDigits; ++n) {
+    if (exact) break;
+    const int shift = kDigitShift[n];
+    const uint32_t above = n == 0 ? 0u : 0xffffffffu << kDigitShift[n == 0 ? 0 : n - 1];
+    for (int i = tid; i < kBins; i += kSelThreads) hist[i] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < KPT; ++k) {
+      const bool in = k * kSelThreads + tid < d.len && (key[k] & above) == least;
+      const unsigned long long m = __ballot(in);
+      if (m == 0) continue;
+      const uint32_t digit = (key[k] >> shift) & (kBins - 1);
+      const uint32_t one = (uint32_t)__builtin_amdgcn_readlane((int)digit, (int)__builtin_ctzll(m));
+      if (__ballot(in && digit != one) == 0) {
+        if (lane == 0) atomicAdd(&hist[one], (uint32_t)__popcll(m));
+      } else if (in) {
+        atomicAdd(&hist[digit], 1u);
+      }
+    }
+    __syncthreads();
+    // thread i holds bins kBins - 1 - 2 i and the one below; sums from the top
+    const uint32_t c0 = hist[kBins - 1 - 2 * tid], c1 = hist[kBins - 2 - 2 * tid];
+    const uint32_t upto = wave_scan_u32(c0 + c1);
+    if (lane == 63) sums[0][wave] = upto;
+    __syncthreads();
+    uint32_t before = upto - c0 - c1;
+    for (int w = 0; w < wave; ++w) before += sums[0][w];
+    const uint32_t need = (uint32_t)ties;
+    if (before < need && before + c0 + c1 >= need) {
+      const bool first = before + c0 >= need;
+      found[0] = (uint32_t)(kBins - 1 - 2 * tid - (first ? 0 : 1));
+      found[1] = need - before - (first ? 0u : c0);
+      found[2] = first ? c0 : c1;
+    }
+    __syncthreads();
+    least |= found[0] << shift;
+    ties = (int)found[1];
+    exact = found[1] == found[2];
+  }
+  const unsigned long long low = (1ull << lane) - 1;
+  // sums of the counts before each group of 64 slots
+  auto scan = [&](uint32_t* c, uint32_t* s) {
+    const uint32_t mine = tid < kCounts ? c[tid] : 0u;
+    const uint32_t upto = wave_scan_u32(mine);
+    if (lane == 63) s[wave] = upto;
+    __syncthreads();
+    uint32_t before = 0;
+    for (int w = 0; w < wave; ++w) before += s[w];
+    if (tid < kCounts) c[tid] = before + upto - mine;
+  };
+  if (!exact) {   // (hole_at for the ranks of equal keys)
+#pragma unroll
+    for (int k = 0; k < KPT; ++k) {
+      const unsigned long long m = __ballot(key[k] == least && k * kSelThreads + tid < d.len);
+      if (lane == 0) hole_at[k * kSelWaves + wave] = (uint32_t)__popcll(m);
+    }
+    __syncthreads();
+    scan(hole_at, sums[0]);
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < KPT; ++k) {
+      const bool eq = key[k] == least && k * kSelThreads + tid < d.len;
+      const int rank = (int)(hole_at[k * kSelWaves + wave] + __popcll(__ballot(eq) & low));
+      if (eq && rank >= ties) key[k] = 0;              // evicted
+      else if (eq && least == 0) key[k] = 1;           // (a key of 0 that stays)
+    }
+    __syncthreads();
+  }
+  least = max(least, 1u);   // (not exact: keys of 0 that stay are 1 now; slots past the length have 0)
+#pragma unroll
+  for (int k = 0; k < KPT; ++k) {
+    const int t = k * kSelThreads + tid;
+    const unsigned long long mh = __ballot(t < e.budget && key[k] < least), mx = __ballot(t >= e.budget && key[k] >= least);
+    if (lane == 0) {
+      hole_at[k * kSelWaves + wave] = (uint32_t)__popcll(mh);
+      extra_at[k * kSelWaves + wave] = (uint32_t)__popcll(mx);
+    }
+  }
+  __syncthreads();
+  scan(hole_at, sums[0]);
+  scan(extra_at, sums[1]);
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < KPT; ++k) {
+    const int t = k * kSelThreads + tid;
+    const bool extra = t >= e.budget && key[k] >= least;
+    const unsigned long long m = __ballot(extra);
+    if (extra) extras[extra_at[k * kSelWaves + wave] + (uint32_t)__popcll(m & low)] = (uint16_t)(t - e.budget);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k0 = 0; k0 < KPT; k0 += kBatch) {
+    if (k0 * kSelThreads >= e.budget) break;
+    int from[kBatch], p[kBatch];
+    float s[kBatch];
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      const int k = k0 + j, t = k * kSelThreads + tid;
+      const bool hole = t < e.budget && key[k] < least;
+      const uint32_t rank = hole_at[k * kSelWaves + wave] + (uint32_t)__popcll(__ballot(hole) & low);
+      from[j] = hole ? e.budget + (int)extras[rank] : min(t, e.budget - 1);
+    }
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) s[j] = d.sc[(uint32_t)from[j]];
+    if (d.po) {
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) p[j] = d.pos(from[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      const int t = (k0 + j) * kSelThreads + tid;
+      if (t < e.budget) {
+        d.kept[t] = from[j];
+        d.so[t] = s[j];
+        if (d.po) d.po[t] = p[j];
+      }
+    }
+  }
+}
+
+// The same for longer caches, whose keys are made from memory each time: the
+// budget-th largest key digit by digit (four histograms of 256 counts), then one pass over the
+// slots in order, and lists in memory.
+__global__ __launch_bounds__(kSelThreads) void k_kv_select_long(KvArgs a, EvictArgs e) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const EvictHead d(a, e, blockIdx.x);
+  if (d.len <= e.budget) {
+    d.keep_all(e.budget);
+    return;
+  }
+  int32_t* holes = e.lists + (int64_t)blockIdx.x * 2 * e.moves;
+  int32_t* extras = holes + e.moves;
   __shared__ uint32_t hist[256];
   __shared__ uint32_t found[2];
   __shared__ int32_t cnt[2][3][kSelWaves];
-  const int newest = ps ? ps[len - 1] : len - 1;
-  auto key_of = [&](int t) { return evict_key(sc[t], ps ? ps[t] : t, newest, e.recent, e.sinks); };
+  auto key_of = [&](int t) { return evict_key(d.sc[t], d.pos(t), d.newest, e.recent, e.sinks); };
 
   uint32_t prefix = 0, need = (uint32_t)e.budget;
   for (int shift = 24; shift >= 0; shift -= 8) {
     if (tid < 256) hist[tid] = 0;
     __syncthreads();
     const uint32_t above = shift == 24 ? 0u : 0xffffffffu << (shift + 8);
-    for (int t = tid; t < len; t += kSelThreads) {
+    for (int t = tid; t < d.len; t += kSelThreads) {
       const uint32_t k = key_of(t);
       if ((k & above) == prefix) atomicAdd(&hist[(k >> shift) & 255u], 1u);
     }
@@ -264,12 +456,7 @@ __global__ __launch_bounds__(kSelThreads) void k_kv_select(KvArgs a, EvictArgs e
       uint32_t c[4], sum = 0;
 #pragma unroll
       for (int j = 0; j < 4; ++j) sum += c[j] = hist[255 - 4 * lane - j];
-      uint32_t upto = sum;
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const uint32_t o = __shfl_up(upto, d);
-        if (lane >= d) upto += o;
-      }
+      const uint32_t upto = wave_scan_u32(sum);
       uint32_t before = upto - sum;
       if (before < need && upto >= need) {
 #pragma unroll
@@ -289,10 +476,10 @@ __global__ __launch_bounds__(kSelThreads) void k_kv_select(KvArgs a, EvictArgs e
 
   // need: how many slots of the threshold's key stay, the lowest ones
   int ties = 0, n_holes = 0, n_extras = 0, buf = 0;
-  for (int t0 = 0; t0 < len; t0 += kSelThreads, buf ^= 1) {
+  for (int t0 = 0; t0 < d.len; t0 += kSelThreads, buf ^= 1) {
     const int t = t0 + tid;
-    const uint32_t k = t < len ? key_of(t) : 0u;
-    const bool eq = t < len && k == prefix;
+    const uint32_t k = t < d.len ? key_of(t) : 0u;
+    const bool eq = t < d.len && k == prefix;
     const unsigned long long me = __ballot(eq), low = (1ull << lane) - 1;
     if (lane == 0) cnt[buf][0][wave] = (int)__popcll(me);
     __syncthreads();
@@ -301,7 +488,7 @@ __global__ __launch_bounds__(kSelThreads) void k_kv_select(KvArgs a, EvictArgs e
       if (w < wave) rank += cnt[buf][0][w];
       ties += cnt[buf][0][w];
     }
-    const bool stays = t < len && (k > prefix || (eq && rank < (int)need));
+    const bool stays = t < d.len && (k > prefix || (eq && rank < (int)need));
     const bool hole = t < e.budget && !stays, extra = t >= e.budget && stays;
     const unsigned long long mh = __ballot(hole), mx = __ballot(extra);
     if (lane == 0) {
@@ -320,50 +507,106 @@ __global__ __launch_bounds__(kSelThreads) void k_kv_select(KvArgs a, EvictArgs e
     }
     if (hole) holes[ih] = t;
     if (extra) extras[ix] = t;
-    if (t < e.budget && stays) {
-      kept[t] = t;
-      so[t] = sc[t];
-      if (po) po[t] = ps ? ps[t] : t;
-    }
+    if (t < e.budget && stays) d.keep(t, t);
   }
   __syncthreads();
-  for (int i = tid; i < n_holes; i += kSelThreads) {
-    const int to = holes[i], from = extras[i];
-    kept[to] = from;
-    so[to] = sc[from];
-    if (po) po[to] = ps ? ps[from] : from;
-  }
-  if (tid == 0) e.n_moves[bh] = n_holes;
+  for (int i = tid; i < n_holes; i += kSelThreads) d.keep(holes[i], extras[i]);
 }
 
-// Moves the listed tokens' codes and scales: D/8 lanes a token.  Sources lie at
-// or beyond budget and destinations below it, so no move reads what another wrote.
+// Moves the tokens that have a new slot: D/8 lanes take kMoveQuads times four slots,
+// the units in which value codes lie.  Sources lie at or beyond budget and
+// destinations below it, so no move reads what another wrote.  A chain of dependent loads (slot, page, codes): every step of all
+// the lane's tokens is on its way at once, and a token that stays reads its own
+// place instead of branching.
+constexpr int kMoveQuads = 2;
+
 template <int D>
 __global__ __launch_bounds__(kKvThreads) void k_kv_move(KvArgs a, EvictArgs e) {
   using L = KvLayout<D>;
-  constexpr int kLanes = D / 8;
+  constexpr int kLanes = D / 8, kGroups = kKvThreads / kLanes, N = 4 * kMoveQuads;
   const int bh = blockIdx.y;
   const int s = bh / a.heads, h = bh % a.heads;
   if (blockIdx.x == 0 && h == 0 && threadIdx.x == 0)
     e.lengths_out[s] = min(min(a.length(s), e.bound), e.budget);
   const int T = 1 << a.page_shift;
-  const int i = blockIdx.x * (kKvThreads / kLanes) + threadIdx.x / kLanes;
   const int sub = threadIdx.x % kLanes;
-  if (i >= e.n_moves[bh]) return;
-  const int to = e.holes[(int64_t)bh * e.moves + i], from = e.extras[(int64_t)bh * e.moves + i];
-  const int64_t pd = a.page(s, to >> a.page_shift), pf = a.page(s, from >> a.page_shift);
-  if (pd < 0 || pf < 0) return;
-  uint8_t* d = a.head_page(pd, h, L::head_bytes(T));
-  const uint8_t* f = a.head_page(pf, h, L::head_bytes(T));
-  const int td = to & (T - 1), tf = from & (T - 1);
-  const uint32_t kw = *reinterpret_cast<const uint32_t*>(f + L::k_codes(tf) + 4 * sub);
-  const uint32_t vw = get_v_word<D>(f, T, tf, sub);
-  *reinterpret_cast<uint32_t*>(d + L::k_codes(td) + 4 * sub) = kw;
-  put_v_word<D>(d, T, td, sub, vw);
-  if ((sub & 3) == 0) {
-    const int b = sub >> 2;
-    d[L::k_scales(T, td) + b] = f[L::k_scales(T, tf) + b];
-    d[L::v_scales(T, td, b)] = f[L::v_scales(T, tf, b)];
+  const int quad0 = (int)(blockIdx.x * kGroups * kMoveQuads + threadIdx.x / kLanes);   // and kGroups further on
+  const int32_t* kept = e.kept + (int64_t)bh * e.budget;
+  const int32_t* entries = a.table + s * a.table_stride;
+  auto slot = [&](int n) { return 4 * (quad0 + n / 4 * kGroups) + n % 4; };
+
+  int from[N];
+#pragma unroll
+  for (int n = 0; n < N; ++n) from[n] = slot(n) < e.budget ? kept[slot(n)] : -1;
+  bool move[N], any = false;
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    move[n] = from[n] >= 0 && from[n] != slot(n);
+    any |= move[n];
+  }
+  if (!any || a.n_pages == 0) return;
+  const int last = a.table_cols - 1;
+  int32_t pf[N], pd[kMoveQuads];
+#pragma unroll
+  for (int n = 0; n < N; ++n) pf[n] = entries[min(max(from[n], 0) >> a.page_shift, last)];
+#pragma unroll
+  for (int q = 0; q < kMoveQuads; ++q) pd[q] = entries[min(slot(4 * q) >> a.page_shift, last)];
+  uint8_t* d[kMoveQuads];
+  const uint8_t* f[N];
+  int tf[N], td[kMoveQuads];
+#pragma unroll
+  for (int q = 0; q < kMoveQuads; ++q) {
+    const bool ok = pd[q] >= 0 && pd[q] < a.n_pages;
+    d[q] = a.head_page(ok ? pd[q] : 0, h, L::head_bytes(T));
+    td[q] = slot(4 * q) & (T - 1);
+#pragma unroll
+    for (int n = 4 * q; n < 4 * q + 4; ++n) {
+      move[n] = move[n] && ok && pf[n] >= 0 && pf[n] < a.n_pages;
+      f[n] = move[n] ? a.head_page(pf[n], h, L::head_bytes(T)) : d[q];
+      tf[n] = move[n] ? from[n] & (T - 1) : td[q] + n % 4;
+    }
+  }
+  uint32_t kw[N], vw[N];
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    kw[n] = *reinterpret_cast<const uint32_t*>(f[n] + L::k_codes(tf[n]) + 4 * sub);
+    vw[n] = get_v_word<D>(f[n], T, tf[n], sub);
+  }
+  // the lane's scales: block b of token i of each quad
+  const int i = sub / (D / 32), b = sub % (D / 32);
+  uint8_t ks[kMoveQuads], vs[kMoveQuads];
+  bool ms[kMoveQuads];
+#pragma unroll
+  for (int q = 0; q < kMoveQuads; ++q) {
+    const uint8_t* fi = f[4 * q];
+    int ti = tf[4 * q];
+    ms[q] = move[4 * q];
+#pragma unroll
+    for (int n = 1; n < 4; ++n) {
+      fi = i == n ? f[4 * q + n] : fi;
+      ti = i == n ? tf[4 * q + n] : ti;
+      ms[q] = i == n ? move[4 * q + n] : ms[q];
+    }
+    ks[q] = fi[L::k_scales(T, ti) + b];
+    vs[q] = fi[L::v_scales(T, ti, b)];
+  }
+#pragma unroll
+  for (int q = 0; q < kMoveQuads; ++q) {
+    const bool* m = move + 4 * q;
+    if (D == 128 && m[0] && m[1] && m[2] && m[3]) {
+      *reinterpret_cast<uint4*>(d[q] + L::v_codes(T, td[q], sub)) = uint4{vw[4 * q], vw[4 * q + 1], vw[4 * q + 2], vw[4 * q + 3]};
+    } else {
+#pragma unroll
+      for (int n = 0; n < 4; ++n)
+        if (m[n]) put_v_word<D>(d[q], T, td[q] + n, sub, vw[4 * q + n]);
+    }
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
+      if (m[n]) *reinterpret_cast<uint32_t*>(d[q] + L::k_codes(td[q] + n) + 4 * sub) = kw[4 * q + n];
+    if (ms[q]) {
+      d[q][L::k_scales(T, td[q] + i) + b] = ks[q];
+      d[q][L::v_scales(T, td[q] + i, b)] = vs[q];
+    }
   }
 }
 
@@ -429,21 +672,27 @@ lam_status launch_kv_evict(lam_ctx* ctx, const lam_kv_view& v, const lam_kv_slot
   e.moves = std::max(0, std::min(budget, e.bound - budget));
   e.kept = kept;
   e.lengths_out = lengths_out;
-  DevBuf& buf = ctx->scratch[kScratchKv];
-  LAM_TRY(buf.ensure((size_t)pairs * (2 * (size_t)e.moves + 1) * 4));
-  e.n_moves = buf.as<int32_t>();
-  e.holes = e.n_moves + pairs;
-  e.extras = e.holes + pairs * e.moves;
   hipEvent_t e0, e1;
   LAM_TRY(prof_launch_events(ctx, "kv_select", &e0, &e1));
-  hipExtLaunchKernelGGL(k_kv_select, dim3((unsigned)pairs), dim3(kSelThreads), 0, ctx->stream, e0, e1, 0, a, e);
+#define LAM_GO(KPT)                                                                                                  \
+  hipExtLaunchKernelGGL((k_kv_select<KPT>), dim3((unsigned)pairs), dim3(kSelThreads), 0, ctx->stream, e0, e1, 0, a, e)
+  if (e.bound <= 2 * kSelThreads) LAM_GO(2);
+  else if (e.bound <= 8 * kSelThreads) LAM_GO(8);
+  else if (e.bound <= 32 * kSelThreads) LAM_GO(32);
+  else if (e.bound <= 64 * kSelThreads) LAM_GO(64);
+#undef LAM_GO
+  else {
+    DevBuf& buf = ctx->scratch[kScratchKv];
+    LAM_TRY(buf.ensure((size_t)pairs * 2 * (size_t)e.moves * 4));
+    e.lists = buf.as<int32_t>();
+    hipExtLaunchKernelGGL(k_kv_select_long, dim3((unsigned)pairs), dim3(kSelThreads), 0, ctx->stream, e0, e1, 0, a, e);
+  }
   LAM_HIP(hipGetLastError());
   LAM_TRY(prof_launch_events(ctx, "kv_move", &e0, &e1));
-  const int per = kKvThreads / (v.head_dim / 8);
-  const dim3 grid((unsigned)std::max(1, (e.moves + per - 1) / per), (unsigned)pairs);
-#define LAM_GO(D, BF) \
-  hipExtLaunchKernelGGL((k_kv_move<D>), grid, dim3(kKvThreads), 0, ctx->stream, e0, e1, 0, a, e)
-  if (v.head_dim == 64) LAM_GO(64, 0); else if (v.head_dim == 128) LAM_GO(128, 0); else LAM_GO(256, 0);
+  const int per = kKvThreads / (v.head_dim / 8) * 4 * kMoveQuads;   // slots a workgroup
+  const dim3 grid((unsigned)((std::min(budget, std::max(e.bound, 1)) + per - 1) / per), (unsigned)pairs);
+#define LAM_GO(D) hipExtLaunchKernelGGL((k_kv_move<D>), grid, dim3(kKvThreads), 0, ctx->stream, e0, e1, 0, a, e)
+  if (v.head_dim == 64) LAM_GO(64); else if (v.head_dim == 128) LAM_GO(128); else LAM_GO(256);
 #undef LAM_GO
   LAM_HIP(hipGetLastError());
   return LAM_OK;
