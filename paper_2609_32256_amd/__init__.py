@@ -255,7 +255,7 @@ _default_ctx: dict = {}
 
 def default_context() -> Context:
     dev = torch.cuda.current_device()
-    key = (dev, torch.cuda.current_stream(dev).cuda_stream)
+    key = (dev, torch._C._cuda_getCurrentRawStream(dev))   # the handle of current_stream(dev), without the object
     c = _default_ctx.get(key)
     if c is None:
         c = _default_ctx[key] = Context(dev)
@@ -354,39 +354,37 @@ def kv_pages(n_pages: int, kv_heads: int, head_dim: int, page_size: int = 64, de
     return torch.zeros((int(n_pages), int(kv_heads), size), dtype=torch.uint8, device=device or "cuda")
 
 
-def _kv_tensor(t, dtype, dims, name, device):
+def _kv_tensor(t, dtype, dims, name, dev):
+    """Checks of a tensor argument (dev: the device's index)."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA (HIP) tensor")
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, the cache on {device}")
-    if t.dtype != dtype:
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, the context on cuda:{dev}")
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
     if t.dim() != dims:
         raise ValueError(f"{name} must have {dims} dimensions")
     return t
 
 
-def _kv_view(ctx, pages, table, lengths, starts, rows, head_dim, dtype):
-    """The C view of a call.  Tensors whose last axis is not contiguous are
-    copied where the library only reads them, refused where it writes."""
-    if not isinstance(pages, torch.Tensor) or not pages.is_cuda:
-        raise TypeError("pages must be a CUDA (HIP) tensor")
-    dev = pages.device
-    if dev.index != ctx.device:
-        raise ValueError(f"pages are on {dev}, the context on cuda:{ctx.device}")
+def _kv_view(dev, pages, table, lengths, starts, rows, head_dim, dtype):
+    """The C view of a call.  Index tensors whose last axis is not contiguous are
+    copied; the copies are returned to be held until the launch is queued."""
     _kv_tensor(pages, torch.uint8, 3, "pages", dev)
     if not pages.is_contiguous():
         raise ValueError("pages must be contiguous")
-    size, per = pages.shape[2], head_dim + head_dim // 16
-    if per <= 0 or size % per or _lib.lam_kv_page_bytes(head_dim, size // per) != size:
+    n_pages, heads, size = pages.shape
+    page_size, rest = divmod(size, head_dim + head_dim // 16) if head_dim > 0 else (0, 1)
+    if rest or _lib.lam_kv_page_bytes(head_dim, page_size) != size:
         raise ValueError(f"pages of {size} bytes a head do not hold heads of {head_dim} channels")
     _kv_tensor(table, torch.int32, 2, "table", dev)
     _kv_tensor(lengths, torch.int32, 1, "lengths", dev)
-    if table.stride(1) != 1 and table.shape[1] > 1 or table.stride(0) < table.shape[1]:
+    (n, cols), (stride, step) = table.shape, table.stride()
+    if step != 1 and cols > 1 or stride < cols:
         table = table.contiguous()
+        stride = table.stride(0)
     lengths = lengths.contiguous()
-    n = lengths.shape[0]
-    if table.shape[0] != n:
+    if lengths.shape[0] != n:
         raise ValueError("table and lengths must have a row for each sequence")
     if starts is not None:
         starts = _kv_tensor(starts, torch.int32, 1, "starts", dev).contiguous()
@@ -394,35 +392,38 @@ def _kv_view(ctx, pages, table, lengths, starts, rows, head_dim, dtype):
             raise ValueError("starts must have an entry for each sequence and one more")
     elif rows and (n == 0 or rows % n):
         raise ValueError("without starts every sequence has the same number of rows")
-    v = KvView(pages.data_ptr(), pages.shape[0], table.data_ptr(), table.stride(0), lengths.data_ptr(),
-               None if starts is None else starts.data_ptr(), rows, n, table.shape[1], pages.shape[1], head_dim,
-               size // per, _KV_DTYPES[dtype])
-    return v, (table, lengths, starts)   # kept until the launch is queued
+    v = KvView(pages.data_ptr(), n_pages, table.data_ptr(), stride, lengths.data_ptr(),
+               None if starts is None else starts.data_ptr(), rows, n, cols, heads, head_dim, page_size,
+               _KV_DTYPES[dtype])
+    return v, (table, lengths, starts)
 
 
-def _kv_rows(t, heads, name, device):
+def _kv_rows(t, heads, name, dev):
     """(rows, heads, head_dim) in float16 or bfloat16, channels contiguous."""
     if not isinstance(t, torch.Tensor) or t.dtype not in _KV_DTYPES:
         raise TypeError(f"{name} must be a float16 or bfloat16 tensor")
-    _kv_tensor(t, t.dtype, 3, name, device)
+    _kv_tensor(t, t.dtype, 3, name, dev)
     if heads is not None and t.shape[1] != heads:
         raise ValueError(f"{name} must have {heads} heads")
-    return t if t.stride(2) == 1 and min(t.stride()) > 0 else t.contiguous()
+    strides = t.stride()
+    return t if strides[2] == 1 and strides[0] > 0 and strides[1] > 0 else t.contiguous()
 
 
-def _kv_slots(t, dtype, view, name, device, shared=False, copy=False):
-    """A value per cached token: (sequences, heads or 1 where shared, slots)."""
+def _kv_slots(t, dtype, view, name, dev, shared=False, copy=False):
+    """A value per cached token: (sequences, heads or 1 where shared, slots).  A tensor
+    whose slots are not contiguous is copied where the library only reads it."""
     if t is None:
         return None, None
-    _kv_tensor(t, dtype, 3, name, device)
-    if t.shape[0] != view.n_seqs or not (t.shape[1] == view.kv_heads or (shared and t.shape[1] == 1)):
+    _kv_tensor(t, dtype, 3, name, dev)
+    n, heads, cols = t.shape
+    if n != view.n_seqs or not (heads == view.kv_heads or (shared and heads == 1)):
         raise ValueError(f"{name} must be (sequences, heads, slots)")
-    if t.stride(2) != 1 and t.shape[2] > 1:
+    if cols > 1 and t.stride(2) != 1:
         if not copy:
             raise ValueError(f"the slots of {name} must be contiguous")
         t = t.contiguous()
-    head = 0 if t.shape[1] == 1 else t.stride(1)
-    return KvSlots(t.data_ptr(), t.stride(0), head, t.shape[2]), t
+    seq, head, _ = t.stride()
+    return KvSlots(t.data_ptr(), seq, 0 if heads == 1 else head, cols), t
 
 
 def _ref(s):
@@ -439,12 +440,12 @@ def kv_append(k: torch.Tensor, v: torch.Tensor, pages: torch.Tensor, table: torc
     new tokens become 0, positions first[s], first[s] + 1, ...; status: int32
     tensor of 3, counts of non-finite, out-of-range and misplaced input."""
     ctx = ctx or default_context()
-    dev = pages.device if isinstance(pages, torch.Tensor) else None
+    dev = ctx.device
     k = _kv_rows(k, None, "k", dev)
     v = _kv_rows(v, k.shape[1], "v", dev)
     if v.shape != k.shape or v.dtype != k.dtype:
         raise ValueError("k and v must have the same shape and dtype")
-    view, hold = _kv_view(ctx, pages, table, lengths, starts, k.shape[0], k.shape[2], k.dtype)
+    view, hold = _kv_view(dev, pages, table, lengths, starts, k.shape[0], k.shape[2], k.dtype)
     if k.shape[1] != view.kv_heads:
         raise ValueError(f"k must have {view.kv_heads} heads")
     w, _ = _kv_slots(weights, torch.float32, view, "weights", dev)
@@ -468,8 +469,9 @@ def kv_read(pages: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, row
     ctx = ctx or default_context()
     if dtype not in _KV_DTYPES:
         raise TypeError("dtype must be float16 or bfloat16")
-    view, hold = _kv_view(ctx, pages, table, lengths, starts, int(rows), int(head_dim), dtype)
-    k, v = (torch.empty((int(rows), view.kv_heads, int(head_dim)), dtype=dtype, device=pages.device) for _ in range(2))
+    view, hold = _kv_view(ctx.device, pages, table, lengths, starts, int(rows), int(head_dim), dtype)
+    k = torch.empty((int(rows), view.kv_heads, int(head_dim)), dtype=dtype, device=pages.device)
+    v = torch.empty_like(k)
     _check(_lib.lam_kv_read(ctx.handle, ctypes.byref(view), k.data_ptr(), v.data_ptr()))
     return k, v
 
@@ -486,15 +488,15 @@ def kv_attend(q: torch.Tensor, pages: torch.Tensor, table: torch.Tensor, lengths
     each token received; lse (float32: rows, q_heads) receives the scores' log
     sums.  max_length, where the caller knows a bound of lengths, sizes the launch."""
     ctx = ctx or default_context()
-    dev = pages.device if isinstance(pages, torch.Tensor) else None
+    dev = ctx.device
     q = _kv_rows(q, None, "q", dev)
-    view, hold = _kv_view(ctx, pages, table, lengths, starts, q.shape[0], q.shape[2], q.dtype)
+    view, hold = _kv_view(dev, pages, table, lengths, starts, q.shape[0], q.shape[2], q.dtype)
     if mask is not None and mask.dtype == torch.bool:
         mask = mask.view(torch.uint8)
     m, hold_mask = _kv_slots(mask, torch.uint8, view, "mask", dev, shared=True, copy=True)
     w, _ = _kv_slots(weights, torch.float32, view, "weights", dev)
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
     elif _kv_tensor(out, q.dtype, 3, "out", dev).shape != q.shape or not out.is_contiguous():
         raise ValueError("out must be contiguous and of q's shape")
     if lse is not None and (_kv_tensor(lse, torch.float32, 2, "lse", dev).shape != q.shape[:2] or not lse.is_contiguous()):
@@ -517,21 +519,19 @@ def kv_evict(pages: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, sc
     (scores, positions or None, lengths) to write to, which may be the inputs
     (only their first budget slots are written)."""
     ctx = ctx or default_context()
-    dev = pages.device if isinstance(pages, torch.Tensor) else None
-    view, hold = _kv_view(ctx, pages, table, lengths, None, 0, int(head_dim), torch.float16)
+    dev = ctx.device
+    view, hold = _kv_view(dev, pages, table, lengths, None, 0, int(head_dim), torch.float16)
     s, hold_s = _kv_slots(scores, torch.float32, view, "scores", dev, copy=True)
     p, hold_p = _kv_slots(positions, torch.int32, view, "positions", dev, copy=True)
     if s is None:
         raise TypeError("scores must be a CUDA (HIP) tensor")
-    shape = (view.n_seqs, view.kv_heads, int(budget))
+    kept = torch.empty((view.n_seqs, view.kv_heads, int(budget)), dtype=torch.int32, device=pages.device)
     if out is None:
-        out = (torch.empty(shape, dtype=torch.float32, device=dev), torch.empty(shape, dtype=torch.int32, device=dev),
-               torch.empty(view.n_seqs, dtype=torch.int32, device=dev))
+        out = (torch.empty_like(kept, dtype=torch.float32), torch.empty_like(kept), torch.empty_like(hold[1]))
     so, _ = _kv_slots(out[0], torch.float32, view, "out scores", dev)
     po, _ = _kv_slots(out[1], torch.int32, view, "out positions", dev)
     if _kv_tensor(out[2], torch.int32, 1, "out lengths", dev).shape[0] != view.n_seqs or not out[2].is_contiguous():
         raise ValueError("out lengths must be contiguous, an entry for each sequence")
-    kept = torch.empty(shape, dtype=torch.int32, device=dev)
     _check(_lib.lam_kv_evict(ctx.handle, ctypes.byref(view), _ref(s), _ref(p), int(budget), int(recent), int(sinks),
                              kept.data_ptr(), _ref(so), _ref(po), out[2].data_ptr()))
     return kept, out[0], out[1], out[2]
