@@ -105,90 +105,173 @@ struct RowArgs {   // rows of keys or values: strides in elements
   int wide;        // every eight channels are a 16-byte load
 };
 
-// One lane per eight channels of a row's head.
+// Four consecutive slots of a head, the unit in which value codes lie, of which the
+// call's rows take some.  Units go by sequence: with the same number of rows each, a.quads of
+// them a sequence; else those of sequence s begin at floor(start(s) / 4) + 2 s, a
+// bound that leaves room for the partial ones at both ends.
+struct Quad {
+  int s = -1;           // sequence, -1: nothing
+  int64_t row = 0;      // row of its first slot (which may be none of the call's)
+  int64_t slot = 0;     // its first slot
+  int64_t first_row = 0;
+  uint32_t rows = 0;    // bit i: slot i is one of the call's rows
+  uint8_t* base = nullptr;   // the head's page, null: no place
+};
+
+template <int D>
+__device__ __forceinline__ Quad quad_at(const KvArgs& a, int quads, uint32_t unit, int h) {
+  Quad q;
+  uint32_t local;
+  if (!a.starts) {
+    q.s = (int)(unit / (uint32_t)quads);
+    local = unit % (uint32_t)quads;
+    if (q.s >= a.n_seqs) q.s = -1;
+  } else {
+    int lo = 0, hi = a.n_seqs;
+    while (hi - lo > 1) {
+      const int m = (lo + hi) >> 1;
+      if (a.start(m) / 4 + 2 * (int64_t)m <= unit) lo = m; else hi = m;
+    }
+    const int64_t at = (int64_t)unit - (a.start(lo) / 4 + 2 * (int64_t)lo);
+    q.s = at >= 0 && a.n_seqs > 0 ? lo : -1;
+    local = (uint32_t)at;
+  }
+  if (q.s < 0) return q;
+  q.first_row = a.start(q.s);
+  const int64_t n = a.start(q.s + 1) - q.first_row;
+  const int64_t slot0 = (int64_t)a.lengths[q.s] - n;   // of the first row
+  q.slot = (slot0 >> 2) * 4 + 4 * (int64_t)local;
+  q.row = q.first_row + (q.slot - slot0);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (q.slot + i >= slot0 && q.slot + i < slot0 + n) q.rows |= 1u << i;
+  if (q.rows && q.slot >= 0 && (q.slot >> a.page_shift) < a.table_cols) {
+    const int64_t page = a.page(q.s, (int)(q.slot >> a.page_shift));
+    if (page >= 0) q.base = a.head_page(page, h, KvLayout<D>::head_bytes(1 << a.page_shift));
+  }
+  return q;
+}
+
+// A lane quantizes eight channels of a quad's four rows: its value codes are then
+// one store (of 16 bytes for 128 channels) where all four are the call's, its scales
+// of the values one word.  Bound by memory: two rows read and 17/32 of a byte a
+// channel written.  (A lane for each row, 4-byte stores 16 bytes apart, wrote every
+// line in four parts: 175 us for 131,072 rows of 8 heads of 128 channels.)
 template <int D, bool BF16>
-__global__ __launch_bounds__(kKvThreads) void k_kv_append(KvArgs a, RowArgs k, RowArgs v, lam_kv_slots weights,
-                                                          lam_kv_slots positions, const int32_t* first,
-                                                          uint32_t* status) {
+__global__ __launch_bounds__(kKvThreads) void k_kv_append(KvArgs a, int quads, RowArgs k, RowArgs v,
+                                                          lam_kv_slots weights, lam_kv_slots positions,
+                                                          const int32_t* first, uint32_t* status) {
   using L = KvLayout<D>;
   constexpr int kLanes = D / 8;
-  const int64_t item = (int64_t)blockIdx.x * kKvThreads + threadIdx.x;
-  const int64_t unit = item / kLanes;
-  const int sub = (int)(item % kLanes);
-  const int64_t row = unit / a.heads;
-  const int h = (int)(unit % a.heads);
-  bool bad = false, over = false, lost = false;
-  if (row < a.rows) {
-    const int s = a.seq_of(row);
-    const int T = 1 << a.page_shift;
-    int64_t page = -1, slot = -1;
-    int64_t i = 0;
-    if (s >= 0) {
-      const int64_t r0 = a.start(s), n = a.start(s + 1) - r0;
-      i = row - r0;
-      slot = (int64_t)a.lengths[s] - n + i;
-      if (slot >= 0 && (slot >> a.page_shift) < a.table_cols) page = a.page(s, (int)(slot >> a.page_shift));
+  const uint32_t item = blockIdx.x * (kKvThreads / kLanes) + threadIdx.x / kLanes;
+  const int sub = threadIdx.x % kLanes;
+  const int h = (int)(item % (uint32_t)a.heads);
+  const Quad q = quad_at<D>(a, quads, item / (uint32_t)a.heads, h);
+  const int T = 1 << a.page_shift;
+  bool bad = false, over = false;
+  if (q.base) {
+    float x[4][8], y[4][8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      // a slot that is not the call's repeats one that is
+      const int64_t row = q.row + ((q.rows >> i) & 1u ? i : __builtin_ctz(q.rows));
+      load8<BF16>(k.p, row * k.row + h * k.head + 8 * sub, k.wide, x[i]);
+      load8<BF16>(v.p, row * v.row + h * v.head + 8 * sub, v.wide, y[i]);
     }
-    lost = page < 0 && sub == 0;
-    if (page >= 0) {
-      float x[8], y[8];
-      load8<BF16>(k.p, row * k.row + h * k.head + 8 * sub, k.wide, x);
-      load8<BF16>(v.p, row * v.row + h * v.head + 8 * sub, v.wide, y);
-      uint32_t kb, vb;
-      const uint32_t kw = quantize8(x, &kb, &bad, &over), vw = quantize8(y, &vb, &bad, &over);
-      uint8_t* base = a.head_page(page, h, L::head_bytes(T));
-      const int t = (int)(slot & (T - 1));
-      *reinterpret_cast<uint32_t*>(base + L::k_codes(t) + 4 * sub) = kw;
-      put_v_word<D>(base, T, t, sub, vw);
-      if ((sub & 3) == 0) {
-        base[L::k_scales(T, t) + (sub >> 2)] = (uint8_t)kb;
-        base[L::v_scales(T, t, sub >> 2)] = (uint8_t)vb;
+    uint32_t kw[4], vw[4], kb[4], vb[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      kw[i] = quantize8(x[i], &kb[i], &bad, &over);
+      vw[i] = quantize8(y[i], &vb[i], &bad, &over);
+    }
+    const int t = (int)(q.slot & (T - 1));
+    uint32_t* vs = reinterpret_cast<uint32_t*>(q.base + L::v_scales(T, t, sub >> 2));
+    if (q.rows == 0xfu) {
+      if constexpr (D == 128) {
+        *reinterpret_cast<uint4*>(q.base + L::v_codes(T, t, sub)) = uint4{vw[0], vw[1], vw[2], vw[3]};
+      } else if constexpr (D == 64) {   // two runs of four channels: halves of the words
+        *reinterpret_cast<uint4*>(q.base + L::v_codes(T, t, 2 * sub)) =
+            uint4{__builtin_amdgcn_perm(vw[1], vw[0], 0x05040100u), __builtin_amdgcn_perm(vw[3], vw[2], 0x05040100u),
+                  __builtin_amdgcn_perm(vw[1], vw[0], 0x07060302u), __builtin_amdgcn_perm(vw[3], vw[2], 0x07060302u)};
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) put_v_word<D>(q.base, T, t + i, sub, vw[i]);
       }
-      if (sub == 0) {
-        if (weights.p_dev && slot < weights.cols)
-          static_cast<float*>(weights.p_dev)[s * weights.seq_stride + h * weights.head_stride + slot] = 0.0f;
-        if (positions.p_dev && slot < positions.cols)
-          static_cast<int32_t*>(positions.p_dev)[s * positions.seq_stride + h * positions.head_stride + slot] =
-              (int32_t)(first[s] + i);
+      if ((sub & 3) == 0) *vs = vb[0] | (vb[1] << 8) | (vb[2] << 16) | (vb[3] << 24);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if ((q.rows >> i) & 1u) {
+          put_v_word<D>(q.base, T, t + i, sub, vw[i]);
+          if ((sub & 3) == 0) reinterpret_cast<uint8_t*>(vs)[i] = (uint8_t)vb[i];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if ((q.rows >> i) & 1u) {
+        *reinterpret_cast<uint32_t*>(q.base + L::k_codes(t + i) + 4 * sub) = kw[i];
+        if ((sub & 3) == 0) q.base[L::k_scales(T, t + i) + (sub >> 2)] = (uint8_t)kb[i];
       }
+    if (sub < 4 && (q.rows >> sub) & 1u) {   // lane i: token i's weight and position
+      const int64_t slot = q.slot + sub;
+      if (weights.p_dev && slot < weights.cols)
+        static_cast<float*>(weights.p_dev)[q.s * weights.seq_stride + h * weights.head_stride + slot] = 0.0f;
+      if (positions.p_dev && slot < positions.cols)
+        static_cast<int32_t*>(positions.p_dev)[q.s * positions.seq_stride + h * positions.head_stride + slot] =
+            (int32_t)(first[q.s] + (q.row + sub - q.first_row));
     }
   }
   if (status) {
     count_in(status, 0, bad);
     count_in(status, 1, over);
-    count_in(status, 2, lost);
+    // rows without a place: of this quad, and (once) those of no sequence
+    uint32_t lost = !q.base && sub == 0 ? (uint32_t)__popc(q.rows) : 0u;
+    if (a.starts && blockIdx.x == 0 && threadIdx.x == 0)
+      lost += (uint32_t)(a.start(0) + a.rows - a.start(a.n_seqs)) * (uint32_t)a.heads;
+    if (lost) atomicAdd(status + 2, lost);
   }
 }
 
 template <int D, bool BF16>
-__global__ __launch_bounds__(kKvThreads) void k_kv_read(KvArgs a, uint4* k, uint4* v) {
+__global__ __launch_bounds__(kKvThreads) void k_kv_read(KvArgs a, int quads, uint4* k, uint4* v) {
   using L = KvLayout<D>;
   constexpr int kLanes = D / 8;
-  const int64_t item = (int64_t)blockIdx.x * kKvThreads + threadIdx.x;
-  const int64_t unit = item / kLanes;
-  const int sub = (int)(item % kLanes);
-  const int64_t row = unit / a.heads;
-  const int h = (int)(unit % a.heads);
-  if (row >= a.rows) return;
-  const int s = a.seq_of(row);
+  const uint32_t item = blockIdx.x * (kKvThreads / kLanes) + threadIdx.x / kLanes;
+  const int sub = threadIdx.x % kLanes;
+  const int h = (int)(item % (uint32_t)a.heads);
+  const Quad q = quad_at<D>(a, quads, item / (uint32_t)a.heads, h);
   const int T = 1 << a.page_shift;
-  uint4 x{0, 0, 0, 0}, y{0, 0, 0, 0};
-  if (s >= 0) {
-    const int64_t r0 = a.start(s), n = a.start(s + 1) - r0;
-    const int64_t slot = (int64_t)a.lengths[s] - n + (row - r0);
-    if (slot >= 0 && (slot >> a.page_shift) < a.table_cols) {
-      const int64_t page = a.page(s, (int)(slot >> a.page_shift));
-      if (page >= 0) {
-        const uint8_t* base = a.head_page(page, h, L::head_bytes(T));
-        const int t = (int)(slot & (T - 1));
-        x = kv_values8<BF16>(*reinterpret_cast<const uint32_t*>(base + L::k_codes(t) + 4 * sub),
-                             kv_scale(base[L::k_scales(T, t) + (sub >> 2)]));
-        y = kv_values8<BF16>(get_v_word<D>(base, T, t, sub), kv_scale(base[L::v_scales(T, t, sub >> 2)]));
-      }
+  uint4 x[4] = {}, y[4] = {};
+  if (q.base) {
+    const int t = (int)(q.slot & (T - 1));
+    uint32_t kw[4], vw[4], kb[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      kw[i] = *reinterpret_cast<const uint32_t*>(q.base + L::k_codes(t + i) + 4 * sub);
+      vw[i] = get_v_word<D>(q.base, T, t + i, sub);   // (of 128 channels: one load)
+      kb[i] = q.base[L::k_scales(T, t + i) + (sub >> 2)];
+    }
+    const uint32_t vb = *reinterpret_cast<const uint32_t*>(q.base + L::v_scales(T, t, sub >> 2));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[i] = kv_values8<BF16>(kw[i], kv_scale(kb[i]));
+      y[i] = kv_values8<BF16>(vw[i], kv_scale((vb >> (8 * i)) & 0xffu));
     }
   }
-  k[item] = x;
-  v[item] = y;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if ((q.rows >> i) & 1u) {
+      const int64_t at = ((q.row + i) * a.heads + h) * kLanes + sub;
+      k[at] = x[i];
+      v[at] = y[i];
+    }
+  if (a.starts) {   // rows of no sequence
+    const int64_t before = a.start(0), after = a.start(a.n_seqs), row_size = (int64_t)a.heads * kLanes;
+    for (int64_t r = blockIdx.x; r < before + a.rows - after; r += gridDim.x) {
+      const int64_t row = r < before ? r : after + r - before;
+      for (int64_t i = threadIdx.x; i < row_size; i += kKvThreads) k[row * row_size + i] = v[row * row_size + i] = uint4{0, 0, 0, 0};
+    }
+  }
 }
 
 // ------------------------------------------------------------------ eviction
@@ -614,12 +697,20 @@ bool wide_rows(const void* p, int64_t row, int64_t head) {
   return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && row % 8 == 0 && head % 8 == 0;
 }
 
-// blocks of kKvThreads lanes, D/8 lanes per row and head
-lam_status row_grid(const lam_kv_view& v, unsigned* grid) {
-  const int64_t items = v.rows * v.kv_heads * (v.head_dim / 8);
-  const int64_t g = (items + kKvThreads - 1) / kKvThreads;
-  LAM_CHECK(g < (1LL << 31), LAM_EINVAL, "too many rows for one launch");
-  *grid = (unsigned)g;
+// workgroups of kKvThreads lanes, D/8 lanes a quad and head; quads: of a sequence, where all have as many rows
+lam_status quad_grid(const lam_kv_view& v, int* quads, unsigned* grid) {
+  int64_t units;
+  *quads = 0;
+  if (v.starts_dev) {
+    units = v.rows / 4 + 2 * (int64_t)v.n_seqs;
+  } else {
+    const int64_t n = v.rows / v.n_seqs;
+    *quads = (int)(n / 4 + (n % 4 > 1 ? 2 : 1));   // n rows from any slot on touch no more
+    units = *quads * (int64_t)v.n_seqs;
+  }
+  const int64_t per = kKvThreads / (v.head_dim / 8), items = units * v.kv_heads;
+  LAM_CHECK(items < (1LL << 31), LAM_EINVAL, "too many rows for one launch");
+  *grid = (unsigned)((items + per - 1) / per);
   return LAM_OK;
 }
 
@@ -629,13 +720,14 @@ lam_status launch_kv_append(lam_ctx* ctx, const lam_kv_view& v, const void* k, i
                             const void* val, int64_t v_row, int64_t v_head, const lam_kv_slots& weights,
                             const lam_kv_slots& positions, const int32_t* first, uint32_t* status) {
   unsigned grid;
-  LAM_TRY(row_grid(v, &grid));
+  int quads;
+  LAM_TRY(quad_grid(v, &quads, &grid));
   const KvArgs a = KvArgs::of(v);
   const RowArgs ka{k, k_row, k_head, wide_rows(k, k_row, k_head)}, va{val, v_row, v_head, wide_rows(val, v_row, v_head)};
   hipEvent_t e0, e1;
   LAM_TRY(prof_launch_events(ctx, "kv_append", &e0, &e1));
 #define LAM_GO(D, BF)                                                                                              \
-  hipExtLaunchKernelGGL((k_kv_append<D, BF>), dim3(grid), dim3(kKvThreads), 0, ctx->stream, e0, e1, 0, a, ka, va,   \
+  hipExtLaunchKernelGGL((k_kv_append<D, BF>), dim3(grid), dim3(kKvThreads), 0, ctx->stream, e0, e1, 0, a, quads, ka, va,  \
                         weights, positions, first, status)
   LAM_KV_DISPATCH(v, LAM_GO);
 #undef LAM_GO
@@ -645,12 +737,13 @@ lam_status launch_kv_append(lam_ctx* ctx, const lam_kv_view& v, const void* k, i
 
 lam_status launch_kv_read(lam_ctx* ctx, const lam_kv_view& v, void* k, void* val) {
   unsigned grid;
-  LAM_TRY(row_grid(v, &grid));
+  int quads;
+  LAM_TRY(quad_grid(v, &quads, &grid));
   const KvArgs a = KvArgs::of(v);
   hipEvent_t e0, e1;
   LAM_TRY(prof_launch_events(ctx, "kv_read", &e0, &e1));
 #define LAM_GO(D, BF)                                                                                            \
-  hipExtLaunchKernelGGL((k_kv_read<D, BF>), dim3(grid), dim3(kKvThreads), 0, ctx->stream, e0, e1, 0, a,           \
+  hipExtLaunchKernelGGL((k_kv_read<D, BF>), dim3(grid), dim3(kKvThreads), 0, ctx->stream, e0, e1, 0, a, quads,    \
                         static_cast<uint4*>(k), static_cast<uint4*>(val))
   LAM_KV_DISPATCH(v, LAM_GO);
 #undef LAM_GO
