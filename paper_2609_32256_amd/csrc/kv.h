@@ -105,6 +105,7 @@ typedef _Float16 kv_h2 __attribute__((ext_vector_type(2)));
 typedef _Float16 kv_h8 __attribute__((ext_vector_type(8)));
 typedef __bf16 kv_b2 __attribute__((ext_vector_type(2)));
 typedef __bf16 kv_b8 __attribute__((ext_vector_type(8)));
+typedef uint32_t kv_u4 __attribute__((ext_vector_type(4)));
 typedef float kv_f4 __attribute__((ext_vector_type(4)));
 
 // scale byte -> 2^e as a float32 (a byte of a block never written may be anything)

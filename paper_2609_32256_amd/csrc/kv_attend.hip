@@ -223,13 +223,28 @@ __device__ __forceinline__ void add_kept(const AttendArgs& a, uint32_t block) {
   const int n = (int)max((int64_t)0, a.c.start(s + 1) - first), full = a.c.length(s);
   const int len = (int)min((int64_t)full, a.cut), pairs = n * a.group;
   if ((int)(block % chunks) * kKeptTokens >= len) return;
-  Work q;
-  q.parts = 1;
-  if (a.split_to) q = plan<kAttRows, PlanOf::kSequence>(a, (uint32_t)s);
+  // Four rows' scores at a time, the first four on their way before the plan and the
+  // sums are known.
+  kv_f4 x[4];
+  auto load = [&](int r) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      // whole strips up to the row's last token were kept, others not
+      const int i = (r + j) / a.group, last = a.causal ? min(len, full - n + i + 1) : len;
+      const int64_t at = (first + i) * a.q_heads + h * a.group + (r + j) % a.group;
+      const float no = -__builtin_inff();
+      x[j] = r + j < pairs && t < last ? *reinterpret_cast<const kv_f4*>(a.kept + at * a.kept_cols + t)
+                                       : kv_f4{no, no, no, no};
+    }
+  };
+  load(0);
   float* d = static_cast<float*>(a.weights.p_dev) + s * a.weights.seq_stride + h * a.weights.head_stride + t;
   float w[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) w[j] = t + j < min(len, a.weights.cols) ? d[j] : 0.0f;
+  Work q;
+  q.parts = 1;
+  if (a.split_to) q = plan<kAttRows, PlanOf::kSequence>(a, (uint32_t)s);
   __shared__ float lse[kAttRows];
   for (int r0 = 0; r0 < pairs; r0 += kAttRows) {
     __syncthreads();
@@ -247,25 +262,15 @@ __device__ __forceinline__ void add_kept(const AttendArgs& a, uint32_t block) {
       }
       lse[threadIdx.x] = e == -__builtin_inff() ? __builtin_inff() : e;   // no token: 2^(-inf) each
     }
-    // four rows' scores at a time, on their way before the sums are known
+    __syncthreads();
     for (int r = r0; r < min(pairs, r0 + kAttRows); r += 4) {
-      kv_f4 x[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        // whole strips up to the row's last token were kept, others not
-        const int i = (r + j) / a.group, last = a.causal ? min(len, full - n + i + 1) : len;
-        const int64_t at = (first + i) * a.q_heads + h * a.group + (r + j) % a.group;
-        const float no = -__builtin_inff();
-        x[j] = r + j < pairs && t < last ? *reinterpret_cast<const kv_f4*>(a.kept + at * a.kept_cols + t)
-                                         : kv_f4{no, no, no, no};
-      }
-      if (r == r0) __syncthreads();
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const float e = r + j < pairs ? lse[r + j - r0] : 0.0f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] += __builtin_amdgcn_exp2f(x[j][i] - e);
       }
+      load(r + 4);
     }
   }
 #pragma unroll
