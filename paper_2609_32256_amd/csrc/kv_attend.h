@@ -21,9 +21,10 @@ constexpr int kAttRows = 16;        // rows of a tile of the kernel for single t
 constexpr float kLift = 7.0f, kSpan = 15.0f;
 constexpr float kNoMax = -3.0e38f;   // no token seen yet
 // Workgroups (of four waves) that a call is split over where its tiles are fewer:
-// three a compute unit for single tokens, which is as many as run at once; for
-// chunks twice the two that do, so that unequal parts even out.
-constexpr int kFill = 768, kFillChunk = 1024;
+// as many as run at once, three a compute unit for single tokens and two for chunks.
+// (Chunks of 2,400 to 8,192 pairs were 8 to 30 % slower at twice as many, where the
+// sums written for the join outweigh the evener parts.)
+constexpr int kFill = 768, kFillChunk = 512;
 constexpr int kChunkGrain = 512;      // least tokens of a part of a chunk's tile: its sums are 64 rows
 constexpr int64_t kKeptBytes = 1LL << 30;   // most scratch for kept scores
 
