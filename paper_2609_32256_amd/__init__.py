@@ -27,6 +27,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 import torch  # noqa: F401  (loads the HIP runtime that liblam then shares)
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -86,15 +87,10 @@ class BlockStats(ctypes.Structure):
         return {f: getattr(self, f) for f, _ in self._fields_ if f != "pad"}
 
 
-class KvView(ctypes.Structure):
-    _fields_ = [("pages", _P), ("n_pages", _I64), ("table", _P), ("table_stride", _I64), ("lengths", _P),
-                ("starts", _P), ("rows", _I64), ("n_seqs", ctypes.c_int32), ("table_cols", ctypes.c_int32),
-                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32),
-                ("dtype", ctypes.c_int32)]
-
-
-class KvSlots(ctypes.Structure):
-    _fields_ = [("p", _P), ("seq_stride", _I64), ("head_stride", _I64), ("cols", ctypes.c_int32)]
+# lam_kv_view and lam_kv_slots as the bytes of the C structs: packing them takes a
+# third of the time that filling a ctypes.Structure does, on calls of some microseconds.
+_KV_VIEW = struct.Struct("@PqPqPPqiiiiii")
+_KV_SLOTS = struct.Struct("@Pqqi4x")
 
 
 class CeilingStats(ctypes.Structure):
@@ -147,13 +143,13 @@ _SIGS = {
     "lam_score_topk": ([_P, _P, _P, _I64, ctypes.c_int32, _P, _P, _P], ctypes.c_int),
     "lam_score_topk_noalloc": ([_P, _P, _P, _I64, ctypes.c_int32, _P, _P, _P], ctypes.c_int),
     "lam_kv_page_bytes": ([ctypes.c_int32, ctypes.c_int32], _I64),
-    "lam_kv_append": ([_P, ctypes.POINTER(KvView), _P, _I64, _I64, _P, _I64, _I64, ctypes.POINTER(KvSlots),
-                       ctypes.POINTER(KvSlots), _P, _P], ctypes.c_int),
-    "lam_kv_read": ([_P, ctypes.POINTER(KvView), _P, _P], ctypes.c_int),
-    "lam_kv_attend": ([_P, ctypes.POINTER(KvView), _P, _I64, _I64, ctypes.c_int32, ctypes.c_double, ctypes.c_int, _I64,
-                       ctypes.POINTER(KvSlots), ctypes.POINTER(KvSlots), _P, _P], ctypes.c_int),
-    "lam_kv_evict": ([_P, ctypes.POINTER(KvView), ctypes.POINTER(KvSlots), ctypes.POINTER(KvSlots), ctypes.c_int32,
-                      ctypes.c_int32, ctypes.c_int32, _P, ctypes.POINTER(KvSlots), ctypes.POINTER(KvSlots), _P],
+    "lam_kv_append": ([_P, _P, _P, _I64, _I64, _P, _I64, _I64, _P,
+                       _P, _P, _P], ctypes.c_int),
+    "lam_kv_read": ([_P, _P, _P, _P], ctypes.c_int),
+    "lam_kv_attend": ([_P, _P, _P, _I64, _I64, ctypes.c_int32, ctypes.c_double, ctypes.c_int, _I64,
+                       _P, _P, _P, _P], ctypes.c_int),
+    "lam_kv_evict": ([_P, _P, _P, _P, ctypes.c_int32,
+                      ctypes.c_int32, ctypes.c_int32, _P, _P, _P, _P],
                      ctypes.c_int),
     "lam_triad": ([_P, _P, _P, _P, _I64, ctypes.c_float], ctypes.c_int),
 }
@@ -343,6 +339,8 @@ def triad(a: torch.Tensor, b: torch.Tensor, c: torch.Tensor, s: float = 3.0, ctx
 
 # ---------------------------------------------------------------- 4-bit key/value cache
 _KV_DTYPES = {torch.float16: 0, torch.bfloat16: 1}
+_KV_HEADS = (64, 128, 256)
+_KV_PAGES = (32, 64, 128, 256, 512, 1024)
 
 
 def kv_pages(n_pages: int, kv_heads: int, head_dim: int, page_size: int = 64, device=None) -> torch.Tensor:
@@ -364,18 +362,17 @@ def _kv_tensor(t, dtype, dims, name, dev):
         raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
     if t.dim() != dims:
         raise ValueError(f"{name} must have {dims} dimensions")
-    return t
 
 
 def _kv_view(dev, pages, table, lengths, starts, rows, head_dim, dtype):
-    """The C view of a call.  Index tensors whose last axis is not contiguous are
-    copied; the copies are returned to be held until the launch is queued."""
+    """(lam_kv_view, sequences, kv_heads, tensors to hold until the launch is queued)
+    of a call.  Index tensors whose last axis is not contiguous are copied."""
     _kv_tensor(pages, torch.uint8, 3, "pages", dev)
     if not pages.is_contiguous():
         raise ValueError("pages must be contiguous")
     n_pages, heads, size = pages.shape
     page_size, rest = divmod(size, head_dim + head_dim // 16) if head_dim > 0 else (0, 1)
-    if rest or _lib.lam_kv_page_bytes(head_dim, page_size) != size:
+    if rest or head_dim not in _KV_HEADS or page_size not in _KV_PAGES:
         raise ValueError(f"pages of {size} bytes a head do not hold heads of {head_dim} channels")
     _kv_tensor(table, torch.int32, 2, "table", dev)
     _kv_tensor(lengths, torch.int32, 1, "lengths", dev)
@@ -384,18 +381,19 @@ def _kv_view(dev, pages, table, lengths, starts, rows, head_dim, dtype):
         table = table.contiguous()
         stride = table.stride(0)
     lengths = lengths.contiguous()
-    if lengths.shape[0] != n:
+    if len(lengths) != n:
         raise ValueError("table and lengths must have a row for each sequence")
     if starts is not None:
-        starts = _kv_tensor(starts, torch.int32, 1, "starts", dev).contiguous()
-        if starts.shape[0] != n + 1:
+        _kv_tensor(starts, torch.int32, 1, "starts", dev)
+        starts = starts.contiguous()
+        if len(starts) != n + 1:
             raise ValueError("starts must have an entry for each sequence and one more")
     elif rows and (n == 0 or rows % n):
         raise ValueError("without starts every sequence has the same number of rows")
-    v = KvView(pages.data_ptr(), n_pages, table.data_ptr(), stride, lengths.data_ptr(),
-               None if starts is None else starts.data_ptr(), rows, n, cols, heads, head_dim, page_size,
-               _KV_DTYPES[dtype])
-    return v, (table, lengths, starts)
+    v = _KV_VIEW.pack(pages.data_ptr(), n_pages, table.data_ptr(), stride, lengths.data_ptr(),
+                      0 if starts is None else starts.data_ptr(), rows, n, cols, heads, head_dim, page_size,
+                      _KV_DTYPES[dtype])
+    return v, n, heads, (table, lengths, starts)
 
 
 def _kv_rows(t, heads, name, dev):
@@ -405,29 +403,26 @@ def _kv_rows(t, heads, name, dev):
     _kv_tensor(t, t.dtype, 3, name, dev)
     if heads is not None and t.shape[1] != heads:
         raise ValueError(f"{name} must have {heads} heads")
-    strides = t.stride()
-    return t if strides[2] == 1 and strides[0] > 0 and strides[1] > 0 else t.contiguous()
+    row, head, step = t.stride()
+    return t if step == 1 and row > 0 and head > 0 else t.contiguous()
 
 
-def _kv_slots(t, dtype, view, name, dev, shared=False, copy=False):
-    """A value per cached token: (sequences, heads or 1 where shared, slots).  A tensor
-    whose slots are not contiguous is copied where the library only reads it."""
+def _kv_slots(t, dtype, n, heads, name, dev, shared=False, copy=False):
+    """(lam_kv_slots, tensor to hold) of a value per cached token: (sequences, heads or
+    1 where shared, slots).  A tensor whose slots are not contiguous is copied where
+    the library only reads it."""
     if t is None:
         return None, None
     _kv_tensor(t, dtype, 3, name, dev)
-    n, heads, cols = t.shape
-    if n != view.n_seqs or not (heads == view.kv_heads or (shared and heads == 1)):
+    seqs, own, cols = t.shape
+    if seqs != n or not (own == heads or (shared and own == 1)):
         raise ValueError(f"{name} must be (sequences, heads, slots)")
     if cols > 1 and t.stride(2) != 1:
         if not copy:
             raise ValueError(f"the slots of {name} must be contiguous")
         t = t.contiguous()
     seq, head, _ = t.stride()
-    return KvSlots(t.data_ptr(), seq, 0 if heads == 1 else head, cols), t
-
-
-def _ref(s):
-    return ctypes.byref(s) if s is not None else None
+    return _KV_SLOTS.pack(t.data_ptr(), seq, 0 if own == 1 else head, cols), t
 
 
 def kv_append(k: torch.Tensor, v: torch.Tensor, pages: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor,
@@ -445,21 +440,24 @@ def kv_append(k: torch.Tensor, v: torch.Tensor, pages: torch.Tensor, table: torc
     v = _kv_rows(v, k.shape[1], "v", dev)
     if v.shape != k.shape or v.dtype != k.dtype:
         raise ValueError("k and v must have the same shape and dtype")
-    view, hold = _kv_view(dev, pages, table, lengths, starts, k.shape[0], k.shape[2], k.dtype)
-    if k.shape[1] != view.kv_heads:
-        raise ValueError(f"k must have {view.kv_heads} heads")
-    w, _ = _kv_slots(weights, torch.float32, view, "weights", dev)
-    p, _ = _kv_slots(positions, torch.int32, view, "positions", dev)
+    rows, own, head_dim = k.shape
+    view, n, heads, hold = _kv_view(dev, pages, table, lengths, starts, rows, head_dim, k.dtype)
+    if own != heads:
+        raise ValueError(f"k must have {heads} heads")
+    w, _ = _kv_slots(weights, torch.float32, n, heads, "weights", dev)
+    p, _ = _kv_slots(positions, torch.int32, n, heads, "positions", dev)
     if first is not None:
-        first = _kv_tensor(first, torch.int32, 1, "first", dev).contiguous()
-        if first.shape[0] != view.n_seqs:
+        _kv_tensor(first, torch.int32, 1, "first", dev)
+        first = first.contiguous()
+        if len(first) != n:
             raise ValueError("first must have an entry for each sequence")
     if status is not None:
         _kv_tensor(status, torch.int32, 1, "status", dev)
         if not status.is_contiguous() or status.numel() < 3:
             raise ValueError("status must be a contiguous int32 tensor of at least 3 entries")
-    _check(_lib.lam_kv_append(ctx.handle, ctypes.byref(view), k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(),
-                              v.stride(0), v.stride(1), _ref(w), _ref(p), _ptr(first), _ptr(status)))
+    _check(_lib.lam_kv_append(ctx.handle, view, k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0),
+                              v.stride(1), w, p, None if first is None else first.data_ptr(),
+                              None if status is None else status.data_ptr()))
 
 
 def kv_read(pages: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, rows: int, head_dim: int,
@@ -469,10 +467,10 @@ def kv_read(pages: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, row
     ctx = ctx or default_context()
     if dtype not in _KV_DTYPES:
         raise TypeError("dtype must be float16 or bfloat16")
-    view, hold = _kv_view(ctx.device, pages, table, lengths, starts, int(rows), int(head_dim), dtype)
-    k = torch.empty((int(rows), view.kv_heads, int(head_dim)), dtype=dtype, device=pages.device)
+    view, _, heads, hold = _kv_view(ctx.device, pages, table, lengths, starts, int(rows), int(head_dim), dtype)
+    k = torch.empty((int(rows), heads, int(head_dim)), dtype=dtype, device=pages.device)
     v = torch.empty_like(k)
-    _check(_lib.lam_kv_read(ctx.handle, ctypes.byref(view), k.data_ptr(), v.data_ptr()))
+    _check(_lib.lam_kv_read(ctx.handle, view, k.data_ptr(), v.data_ptr()))
     return k, v
 
 
@@ -490,21 +488,26 @@ def kv_attend(q: torch.Tensor, pages: torch.Tensor, table: torch.Tensor, lengths
     ctx = ctx or default_context()
     dev = ctx.device
     q = _kv_rows(q, None, "q", dev)
-    view, hold = _kv_view(dev, pages, table, lengths, starts, q.shape[0], q.shape[2], q.dtype)
+    rows, q_heads, head_dim = q.shape
+    view, n, heads, hold = _kv_view(dev, pages, table, lengths, starts, rows, head_dim, q.dtype)
     if mask is not None and mask.dtype == torch.bool:
         mask = mask.view(torch.uint8)
-    m, hold_mask = _kv_slots(mask, torch.uint8, view, "mask", dev, shared=True, copy=True)
-    w, _ = _kv_slots(weights, torch.float32, view, "weights", dev)
+    m, hold_mask = _kv_slots(mask, torch.uint8, n, heads, "mask", dev, shared=True, copy=True)
+    w, _ = _kv_slots(weights, torch.float32, n, heads, "weights", dev)
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
-    elif _kv_tensor(out, q.dtype, 3, "out", dev).shape != q.shape or not out.is_contiguous():
-        raise ValueError("out must be contiguous and of q's shape")
-    if lse is not None and (_kv_tensor(lse, torch.float32, 2, "lse", dev).shape != q.shape[:2] or not lse.is_contiguous()):
-        raise ValueError("lse must be contiguous and (rows, q_heads)")
-    _check(_lib.lam_kv_attend(ctx.handle, ctypes.byref(view), q.data_ptr(), q.stride(0), q.stride(1), q.shape[1],
-                              q.shape[2] ** -0.5 if scale is None else float(scale), int(bool(causal)),
-                              0 if max_length is None else max(1, int(max_length)), _ref(m), _ref(w), out.data_ptr(),
-                              _ptr(lse)))
+    else:
+        _kv_tensor(out, q.dtype, 3, "out", dev)
+        if out.shape != q.shape or not out.is_contiguous():
+            raise ValueError("out must be contiguous and of q's shape")
+    if lse is not None:
+        _kv_tensor(lse, torch.float32, 2, "lse", dev)
+        if lse.shape != q.shape[:2] or not lse.is_contiguous():
+            raise ValueError("lse must be contiguous and (rows, q_heads)")
+    _check(_lib.lam_kv_attend(ctx.handle, view, q.data_ptr(), q.stride(0), q.stride(1), q_heads,
+                              head_dim ** -0.5 if scale is None else float(scale), 1 if causal else 0,
+                              0 if max_length is None else max(1, int(max_length)), m, w, out.data_ptr(),
+                              None if lse is None else lse.data_ptr()))
     return out
 
 
@@ -520,20 +523,23 @@ def kv_evict(pages: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, sc
     (only their first budget slots are written)."""
     ctx = ctx or default_context()
     dev = ctx.device
-    view, hold = _kv_view(dev, pages, table, lengths, None, 0, int(head_dim), torch.float16)
-    s, hold_s = _kv_slots(scores, torch.float32, view, "scores", dev, copy=True)
-    p, hold_p = _kv_slots(positions, torch.int32, view, "positions", dev, copy=True)
+    view, n, heads, hold = _kv_view(dev, pages, table, lengths, None, 0, int(head_dim), torch.float16)
+    s, hold_s = _kv_slots(scores, torch.float32, n, heads, "scores", dev, copy=True)
+    p, hold_p = _kv_slots(positions, torch.int32, n, heads, "positions", dev, copy=True)
     if s is None:
         raise TypeError("scores must be a CUDA (HIP) tensor")
-    kept = torch.empty((view.n_seqs, view.kv_heads, int(budget)), dtype=torch.int32, device=pages.device)
+    kept = torch.empty((n, heads, int(budget)), dtype=torch.int32, device=pages.device)
     if out is None:
         out = (torch.empty_like(kept, dtype=torch.float32), torch.empty_like(kept), torch.empty_like(hold[1]))
-    so, _ = _kv_slots(out[0], torch.float32, view, "out scores", dev)
-    po, _ = _kv_slots(out[1], torch.int32, view, "out positions", dev)
-    if _kv_tensor(out[2], torch.int32, 1, "out lengths", dev).shape[0] != view.n_seqs or not out[2].is_contiguous():
-        raise ValueError("out lengths must be contiguous, an entry for each sequence")
-    _check(_lib.lam_kv_evict(ctx.handle, ctypes.byref(view), _ref(s), _ref(p), int(budget), int(recent), int(sinks),
-                             kept.data_ptr(), _ref(so), _ref(po), out[2].data_ptr()))
+        so, po = (_KV_SLOTS.pack(t.data_ptr(), heads * int(budget), int(budget), int(budget)) for t in out[:2])
+    else:
+        so, _ = _kv_slots(out[0], torch.float32, n, heads, "out scores", dev)
+        po, _ = _kv_slots(out[1], torch.int32, n, heads, "out positions", dev)
+        _kv_tensor(out[2], torch.int32, 1, "out lengths", dev)
+        if len(out[2]) != n or not out[2].is_contiguous():
+            raise ValueError("out lengths must be contiguous, an entry for each sequence")
+    _check(_lib.lam_kv_evict(ctx.handle, view, s, p, int(budget), int(recent), int(sinks), kept.data_ptr(), so, po,
+                             out[2].data_ptr()))
     return kept, out[0], out[1], out[2]
 
 

@@ -18,8 +18,6 @@
 //
 // Conversions are one instruction per two values with the scale applied; values
 // of two tokens are then paired by one move each.
-#include <hip/hip_ext.h>
-
 #include <algorithm>
 #include <cmath>
 
@@ -490,19 +488,15 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
   if (chunk) {
     LAM_TRY(launch_kv_chunk(ctx, v, a, blocks, mask.p_dev != nullptr));
   } else {
-  LAM_TRY(prof_launch_events(ctx, "kv_attend", &e0, &e1));
-#define LAM_GO(D, BF)                                                                                               \
-  do {                                                                                                              \
-    if (mask.p_dev)                                                                                                 \
-      hipExtLaunchKernelGGL((k_kv_attend<D, BF, true>), dim3((unsigned)blocks), dim3(kAttThreads), 0, ctx->stream,  \
-                            e0, e1, 0, a);                                                                          \
-    else                                                                                                            \
-      hipExtLaunchKernelGGL((k_kv_attend<D, BF, false>), dim3((unsigned)blocks), dim3(kAttThreads), 0, ctx->stream, \
-                            e0, e1, 0, a);                                                                          \
+    LAM_TRY(prof_launch_events(ctx, "kv_attend", &e0, &e1));
+#define LAM_GO(D, BF)                                                                                          \
+  do {                                                                                                         \
+    if (mask.p_dev) launch(k_kv_attend<D, BF, true>, dim3((unsigned)blocks), kAttThreads, ctx->stream, e0, e1, a); \
+    else launch(k_kv_attend<D, BF, false>, dim3((unsigned)blocks), kAttThreads, ctx->stream, e0, e1, a);       \
   } while (0)
-  LAM_KV_DISPATCH(v, LAM_GO);
+    LAM_KV_DISPATCH(v, LAM_GO);
 #undef LAM_GO
-  LAM_HIP(hipGetLastError());
+    LAM_HIP(hipGetLastError());
   }
   a.join_rows = units * rows >= 8192 ? 4 : 1;   // few rows: each its own wave, many: four, and a quarter of the plans
   const int64_t join_blocks = a.split_to ? units * (rows / (kAttWaves * a.join_rows)) : 0;
@@ -510,14 +504,12 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
   if (join_blocks + kept_blocks > 0) {
     LAM_CHECK(join_blocks + kept_blocks < (1LL << 31), LAM_EINVAL, "too many rows for one launch");
     LAM_TRY(prof_launch_events(ctx, "kv_finish", &e0, &e1));
-#define LAM_GO(D, BF)                                                                                               \
-  do {                                                                                                              \
-    if (chunk)                                                                                                      \
-      hipExtLaunchKernelGGL((k_kv_finish<D, BF, chunk_rows(D)>), dim3((unsigned)join_blocks), dim3(kAttThreads), 0, \
-                            ctx->stream, e0, e1, 0, a, (uint32_t)join_blocks);                                      \
-    else                                                                                                            \
-      hipExtLaunchKernelGGL((k_kv_finish<D, BF, kAttRows>), dim3((unsigned)(join_blocks + kept_blocks)),            \
-                            dim3(kAttThreads), 0, ctx->stream, e0, e1, 0, a, (uint32_t)join_blocks);                \
+    const dim3 grid((unsigned)(join_blocks + kept_blocks));
+    const uint32_t jb = (uint32_t)join_blocks;
+#define LAM_GO(D, BF)                                                                                 \
+  do {                                                                                                \
+    if (chunk) launch(k_kv_finish<D, BF, chunk_rows(D)>, grid, kAttThreads, ctx->stream, e0, e1, a, jb); \
+    else launch(k_kv_finish<D, BF, kAttRows>, grid, kAttThreads, ctx->stream, e0, e1, a, jb);         \
   } while (0)
     LAM_KV_DISPATCH(v, LAM_GO);
 #undef LAM_GO
@@ -528,8 +520,7 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
     const int64_t wb = (a.cut + tokens - 1) / tokens * v.kv_heads * v.n_seqs;
     LAM_CHECK(wb < (1LL << 31), LAM_EINVAL, "too many sequences for one launch");
     LAM_TRY(prof_launch_events(ctx, "kv_weights", &e0, &e1));
-#define LAM_GO(D, BF) \
-  hipExtLaunchKernelGGL((k_kv_weights<D, BF>), dim3((unsigned)wb), dim3(kAttThreads), 0, ctx->stream, e0, e1, 0, a)
+#define LAM_GO(D, BF) launch(k_kv_weights<D, BF>, dim3((unsigned)wb), kAttThreads, ctx->stream, e0, e1, a)
     LAM_KV_DISPATCH(v, LAM_GO);
 #undef LAM_GO
     LAM_HIP(hipGetLastError());

@@ -1,7 +1,5 @@
 // The 4-bit key/value cache's own memory: rows quantized into it, values read
 // back, and tokens evicted from it (include/lam.h, lam_kv_*).
-#include <hip/hip_ext.h>
-
 #include <algorithm>
 #include <type_traits>
 
@@ -602,7 +600,7 @@ __global__ __launch_bounds__(kSelThreads) void k_kv_select_long(KvArgs a, EvictA
 // destinations below it, so no move reads what another wrote.  A chain of dependent loads (slot, page, codes): every step of all
 // the lane's tokens is on its way at once, and a token that stays reads its own
 // place instead of branching.
-constexpr int kMoveQuads = 2;
+constexpr int kMoveQuads = 1;
 
 template <int D>
 __global__ __launch_bounds__(kKvThreads) void k_kv_move(KvArgs a, EvictArgs e) {
@@ -727,9 +725,9 @@ lam_status launch_kv_append(lam_ctx* ctx, const lam_kv_view& v, const void* k, i
   const RowArgs ka{k, k_row, k_head, wide_rows(k, k_row, k_head)}, va{val, v_row, v_head, wide_rows(val, v_row, v_head)};
   hipEvent_t e0, e1;
   LAM_TRY(prof_launch_events(ctx, "kv_append", &e0, &e1));
-#define LAM_GO(D, BF)                                                                                              \
-  hipExtLaunchKernelGGL((k_kv_append<D, BF>), dim3(grid), dim3(kKvThreads), 0, ctx->stream, e0, e1, 0, a, quads, ka, va,  \
-                        weights, positions, first, status)
+#define LAM_GO(D, BF)                                                                                             \
+  launch(k_kv_append<D, BF>, dim3(grid), kKvThreads, ctx->stream, e0, e1, a, quads, ka, va, weights, positions, first, \
+         status)
   LAM_KV_DISPATCH(v, LAM_GO);
 #undef LAM_GO
   LAM_HIP(hipGetLastError());
@@ -743,9 +741,9 @@ lam_status launch_kv_read(lam_ctx* ctx, const lam_kv_view& v, void* k, void* val
   const KvArgs a = KvArgs::of(v);
   hipEvent_t e0, e1;
   LAM_TRY(prof_launch_events(ctx, "kv_read", &e0, &e1));
-#define LAM_GO(D, BF)                                                                                            \
-  hipExtLaunchKernelGGL((k_kv_read<D, BF>), dim3(grid), dim3(kKvThreads), 0, ctx->stream, e0, e1, 0, a, quads,    \
-                        static_cast<uint4*>(k), static_cast<uint4*>(val))
+#define LAM_GO(D, BF)                                                                          \
+  launch(k_kv_read<D, BF>, dim3(grid), kKvThreads, ctx->stream, e0, e1, a, quads, static_cast<uint4*>(k), \
+         static_cast<uint4*>(val))
   LAM_KV_DISPATCH(v, LAM_GO);
 #undef LAM_GO
   LAM_HIP(hipGetLastError());
@@ -768,8 +766,7 @@ lam_status launch_kv_evict(lam_ctx* ctx, const lam_kv_view& v, const lam_kv_slot
   e.lengths_out = lengths_out;
   hipEvent_t e0, e1;
   LAM_TRY(prof_launch_events(ctx, "kv_select", &e0, &e1));
-#define LAM_GO(KPT)                                                                                                  \
-  hipExtLaunchKernelGGL((k_kv_select<KPT>), dim3((unsigned)pairs), dim3(kSelThreads), 0, ctx->stream, e0, e1, 0, a, e)
+#define LAM_GO(KPT) launch(k_kv_select<KPT>, dim3((unsigned)pairs), kSelThreads, ctx->stream, e0, e1, a, e)
   if (e.bound <= 2 * kSelThreads) LAM_GO(2);
   else if (e.bound <= 8 * kSelThreads) LAM_GO(8);
   else if (e.bound <= 32 * kSelThreads) LAM_GO(32);
@@ -779,13 +776,13 @@ lam_status launch_kv_evict(lam_ctx* ctx, const lam_kv_view& v, const lam_kv_slot
     DevBuf& buf = ctx->scratch[kScratchKv];
     LAM_TRY(buf.ensure((size_t)pairs * 2 * (size_t)e.moves * 4));
     e.lists = buf.as<int32_t>();
-    hipExtLaunchKernelGGL(k_kv_select_long, dim3((unsigned)pairs), dim3(kSelThreads), 0, ctx->stream, e0, e1, 0, a, e);
+    launch(k_kv_select_long, dim3((unsigned)pairs), kSelThreads, ctx->stream, e0, e1, a, e);
   }
   LAM_HIP(hipGetLastError());
   LAM_TRY(prof_launch_events(ctx, "kv_move", &e0, &e1));
   const int per = kKvThreads / (v.head_dim / 8) * 4 * kMoveQuads;   // slots a workgroup
   const dim3 grid((unsigned)((std::min(budget, std::max(e.bound, 1)) + per - 1) / per), (unsigned)pairs);
-#define LAM_GO(D) hipExtLaunchKernelGGL((k_kv_move<D>), grid, dim3(kKvThreads), 0, ctx->stream, e0, e1, 0, a, e)
+#define LAM_GO(D) launch(k_kv_move<D>, grid, kKvThreads, ctx->stream, e0, e1, a, e)
   if (v.head_dim == 64) LAM_GO(64); else if (v.head_dim == 128) LAM_GO(128); else LAM_GO(256);
 #undef LAM_GO
   LAM_HIP(hipGetLastError());

@@ -6,8 +6,6 @@
 // heads of 256 channels), so that a strip's conversions serve four products instead of
 // one.  The queries lie in LDS for all of them; they meet only at the end, when
 // their sums are joined.
-#include <hip/hip_ext.h>
-
 #include "kv_attend.h"
 
 namespace lam {
@@ -148,14 +146,10 @@ __global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) void k_kv_chunk(Atte
 lam_status launch_kv_chunk(lam_ctx* ctx, const lam_kv_view& v, const AttendArgs& a, int64_t blocks, bool masked) {
   hipEvent_t e0, e1;
   LAM_TRY(prof_launch_events(ctx, "kv_chunk", &e0, &e1));
-#define LAM_GO(D, BF)                                                                                            \
-  do {                                                                                                           \
-    if (masked)                                                                                                  \
-      hipExtLaunchKernelGGL((k_kv_chunk<D, BF, true>), dim3((unsigned)blocks), dim3(kAttThreads), 0, ctx->stream, e0, e1, \
-                            0, a);                                                                               \
-    else                                                                                                         \
-      hipExtLaunchKernelGGL((k_kv_chunk<D, BF, false>), dim3((unsigned)blocks), dim3(kAttThreads), 0, ctx->stream, e0,    \
-                            e1, 0, a);                                                                           \
+#define LAM_GO(D, BF)                                                                                             \
+  do {                                                                                                            \
+    if (masked) launch(k_kv_chunk<D, BF, true>, dim3((unsigned)blocks), kAttThreads, ctx->stream, e0, e1, a);     \
+    else launch(k_kv_chunk<D, BF, false>, dim3((unsigned)blocks), kAttThreads, ctx->stream, e0, e1, a);           \
   } while (0)
   LAM_KV_DISPATCH(v, LAM_GO);
 #undef LAM_GO
