@@ -95,11 +95,15 @@ template <int R, PlanOf OF>
 __device__ __forceinline__ Work plan(const AttendArgs& a, uint32_t id) {
   const int lane = threadIdx.x & 63;
   double tokens = 0.0, units = 0.0;
-  for (int b = 0; b < a.c.n_seqs; b += 64) {
-    const LaneSeq q(a, b + lane, R);
+  LaneSeq q(a, lane, R);
+  for (int b = 0;;) {
     tokens += (double)q.tiles * q.len;
     units += (double)q.tiles;
+    b += 64;
+    if (b >= a.c.n_seqs) break;
+    q = LaneSeq(a, b + lane, R);
   }
+  if (a.c.n_seqs > 64) q = LaneSeq(a, lane, R);
   const float all = (float)wave_sum_f64(tokens) * a.c.heads, half = 0.5f * (float)wave_sum_f64(units) * a.c.heads;
   constexpr int kStrips = kKvStrip * kAttWaves, kGrain = R == kAttRows ? kStrips : kChunkGrain;
   const float want = all / fmaxf((float)a.split_to - half, 0.5f * a.split_to) * 1.0001f;
@@ -108,7 +112,7 @@ __device__ __forceinline__ Work plan(const AttendArgs& a, uint32_t id) {
   w.tokens = (int)fminf(floorf(want / kGrain) * kGrain + kGrain, 2147483520.0f);
   uint32_t before = 0, units_before = 0;
   for (int b = 0; b < a.c.n_seqs; b += 64) {
-    const LaneSeq q(a, b + lane, R);
+    if (b > 0) q = LaneSeq(a, b + lane, R);
     const int parts = max(1, (q.len + w.tokens - 1) / w.tokens);
     const int even = ((q.len + parts - 1) / parts + kStrips - 1) / kStrips * kStrips;   // its parts made equal
     const uint32_t my_units = (uint32_t)(q.tiles * a.c.heads), mine = my_units * parts;
