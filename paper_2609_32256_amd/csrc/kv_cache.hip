@@ -595,100 +595,77 @@ __global__ __launch_bounds__(kSelThreads) void k_kv_select_long(KvArgs a, EvictA
   for (int i = tid; i < n_holes; i += kSelThreads) d.keep(holes[i], extras[i]);
 }
 
-// Moves the tokens that have a new slot: D/8 lanes take kMoveQuads times four slots,
-// the units in which value codes lie.  Sources lie at or beyond budget and
-// destinations below it, so no move reads what another wrote.  A chain of dependent loads (slot, page, codes): every step of all
-// the lane's tokens is on its way at once, and a token that stays reads its own
-// place instead of branching.
-constexpr int kMoveQuads = 1;
-
+// Moves the tokens that have a new slot: D/8 lanes take four slots, the units in
+// which value codes lie.  Sources lie at or beyond budget and destinations below it,
+// so no move reads what another wrote.  Bound by memory, at more than the codes'
+// bytes: a token's value codes are a quarter of every 16 bytes of 2 D bytes, and
+// what is kept of a long tail lies apart.  192 heads' 6,144 moves of 128 channels take 131 to
+// 145 us (the bytes alone 62 at a copy's rate); the same with every source token
+// next to the last 82 to 90 us for 8,192.  (Tokens that stay reading their own place,
+// so that no load hangs on a branch, were 7 % slower, two units a lane group 9 %.)
 template <int D>
 __global__ __launch_bounds__(kKvThreads) void k_kv_move(KvArgs a, EvictArgs e) {
   using L = KvLayout<D>;
-  constexpr int kLanes = D / 8, kGroups = kKvThreads / kLanes, N = 4 * kMoveQuads;
+  constexpr int kLanes = D / 8;
   const int bh = blockIdx.y;
   const int s = bh / a.heads, h = bh % a.heads;
   if (blockIdx.x == 0 && h == 0 && threadIdx.x == 0)
     e.lengths_out[s] = min(min(a.length(s), e.bound), e.budget);
   const int T = 1 << a.page_shift;
+  const int t0 = 4 * (int)(blockIdx.x * (kKvThreads / kLanes) + threadIdx.x / kLanes);
   const int sub = threadIdx.x % kLanes;
-  const int quad0 = (int)(blockIdx.x * kGroups * kMoveQuads + threadIdx.x / kLanes);   // and kGroups further on
+  if (t0 >= e.budget) return;
   const int32_t* kept = e.kept + (int64_t)bh * e.budget;
-  const int32_t* entries = a.table + s * a.table_stride;
-  auto slot = [&](int n) { return 4 * (quad0 + n / 4 * kGroups) + n % 4; };
-
-  int from[N];
+  int from[4];
+  bool any = false;
 #pragma unroll
-  for (int n = 0; n < N; ++n) from[n] = slot(n) < e.budget ? kept[slot(n)] : -1;
-  bool move[N], any = false;
-#pragma unroll
-  for (int n = 0; n < N; ++n) {
-    move[n] = from[n] >= 0 && from[n] != slot(n);
-    any |= move[n];
+  for (int i = 0; i < 4; ++i) {
+    from[i] = t0 + i < e.budget ? kept[t0 + i] : -1;
+    any |= from[i] >= 0 && from[i] != t0 + i;
   }
-  if (!any || a.n_pages == 0) return;
-  const int last = a.table_cols - 1;
-  int32_t pf[N], pd[kMoveQuads];
+  if (!any) return;
+  const int64_t pd = a.page(s, t0 >> a.page_shift);
+  int64_t pf[4];
 #pragma unroll
-  for (int n = 0; n < N; ++n) pf[n] = entries[min(max(from[n], 0) >> a.page_shift, last)];
+  for (int i = 0; i < 4; ++i) pf[i] = a.page(s, max(from[i], 0) >> a.page_shift);
+  const uint8_t* f[4];   // the sources' pages, null: nothing to move
 #pragma unroll
-  for (int q = 0; q < kMoveQuads; ++q) pd[q] = entries[min(slot(4 * q) >> a.page_shift, last)];
-  uint8_t* d[kMoveQuads];
-  const uint8_t* f[N];
-  int tf[N], td[kMoveQuads];
-#pragma unroll
-  for (int q = 0; q < kMoveQuads; ++q) {
-    const bool ok = pd[q] >= 0 && pd[q] < a.n_pages;
-    d[q] = a.head_page(ok ? pd[q] : 0, h, L::head_bytes(T));
-    td[q] = slot(4 * q) & (T - 1);
-#pragma unroll
-    for (int n = 4 * q; n < 4 * q + 4; ++n) {
-      move[n] = move[n] && ok && pf[n] >= 0 && pf[n] < a.n_pages;
-      f[n] = move[n] ? a.head_page(pf[n], h, L::head_bytes(T)) : d[q];
-      tf[n] = move[n] ? from[n] & (T - 1) : td[q] + n % 4;
-    }
+  for (int i = 0; i < 4; ++i) {
+    const bool move = from[i] >= 0 && from[i] != t0 + i && pd >= 0 && pf[i] >= 0;
+    f[i] = move ? a.head_page(pf[i], h, L::head_bytes(T)) : nullptr;
+    from[i] &= T - 1;
   }
-  uint32_t kw[N], vw[N];
+  uint8_t* d = a.head_page(pd, h, L::head_bytes(T));   // (used only where something moves)
+  const int td = t0 & (T - 1);
+  uint32_t kw[4], vw[4];
 #pragma unroll
-  for (int n = 0; n < N; ++n) {
-    kw[n] = *reinterpret_cast<const uint32_t*>(f[n] + L::k_codes(tf[n]) + 4 * sub);
-    vw[n] = get_v_word<D>(f[n], T, tf[n], sub);
+  for (int i = 0; i < 4; ++i) {
+    if (!f[i]) continue;
+    kw[i] = *reinterpret_cast<const uint32_t*>(f[i] + L::k_codes(from[i]) + 4 * sub);
+    vw[i] = get_v_word<D>(f[i], T, from[i], sub);
   }
-  // the lane's scales: block b of token i of each quad
+  // the lane's scales: block b of the i-th token
   const int i = sub / (D / 32), b = sub % (D / 32);
-  uint8_t ks[kMoveQuads], vs[kMoveQuads];
-  bool ms[kMoveQuads];
-#pragma unroll
-  for (int q = 0; q < kMoveQuads; ++q) {
-    const uint8_t* fi = f[4 * q];
-    int ti = tf[4 * q];
-    ms[q] = move[4 * q];
-#pragma unroll
-    for (int n = 1; n < 4; ++n) {
-      fi = i == n ? f[4 * q + n] : fi;
-      ti = i == n ? tf[4 * q + n] : ti;
-      ms[q] = i == n ? move[4 * q + n] : ms[q];
-    }
-    ks[q] = fi[L::k_scales(T, ti) + b];
-    vs[q] = fi[L::v_scales(T, ti, b)];
+  const uint8_t* fi = i == 0 ? f[0] : i == 1 ? f[1] : i == 2 ? f[2] : f[3];
+  const int ti = i == 0 ? from[0] : i == 1 ? from[1] : i == 2 ? from[2] : from[3];
+  uint8_t ks = 0, vs = 0;
+  if (fi) {
+    ks = fi[L::k_scales(T, ti) + b];
+    vs = fi[L::v_scales(T, ti, b)];
   }
-#pragma unroll
-  for (int q = 0; q < kMoveQuads; ++q) {
-    const bool* m = move + 4 * q;
-    if (D == 128 && m[0] && m[1] && m[2] && m[3]) {
-      *reinterpret_cast<uint4*>(d[q] + L::v_codes(T, td[q], sub)) = uint4{vw[4 * q], vw[4 * q + 1], vw[4 * q + 2], vw[4 * q + 3]};
-    } else {
-#pragma unroll
-      for (int n = 0; n < 4; ++n)
-        if (m[n]) put_v_word<D>(d[q], T, td[q] + n, sub, vw[4 * q + n]);
-    }
+  if (D == 128 && f[0] && f[1] && f[2] && f[3]) {
+    *reinterpret_cast<uint4*>(d + L::v_codes(T, td, sub)) = uint4{vw[0], vw[1], vw[2], vw[3]};
+  } else {
 #pragma unroll
     for (int n = 0; n < 4; ++n)
-      if (m[n]) *reinterpret_cast<uint32_t*>(d[q] + L::k_codes(td[q] + n) + 4 * sub) = kw[4 * q + n];
-    if (ms[q]) {
-      d[q][L::k_scales(T, td[q] + i) + b] = ks[q];
-      d[q][L::v_scales(T, td[q] + i, b)] = vs[q];
-    }
+      if (f[n]) put_v_word<D>(d, T, td + n, sub, vw[n]);
+  }
+#pragma unroll
+  for (int n = 0; n < 4; ++n)
+    if (f[n]) *reinterpret_cast<uint32_t*>(d + L::k_codes(td + n) + 4 * sub) = kw[n];
+  if (fi) {
+    d[L::k_scales(T, td + i) + b] = ks;
+    d[L::v_scales(T, td + i, b)] = vs;
   }
 }
 
@@ -780,7 +757,7 @@ lam_status launch_kv_evict(lam_ctx* ctx, const lam_kv_view& v, const lam_kv_slot
   }
   LAM_HIP(hipGetLastError());
   LAM_TRY(prof_launch_events(ctx, "kv_move", &e0, &e1));
-  const int per = kKvThreads / (v.head_dim / 8) * 4 * kMoveQuads;   // slots a workgroup
+  const int per = kKvThreads / (v.head_dim / 8) * 4;   // slots a workgroup
   const dim3 grid((unsigned)((std::min(budget, std::max(e.bound, 1)) + per - 1) / per), (unsigned)pairs);
 #define LAM_GO(D) launch(k_kv_move<D>, grid, kKvThreads, ctx->stream, e0, e1, a, e)
   if (v.head_dim == 64) LAM_GO(64); else if (v.head_dim == 128) LAM_GO(128); else LAM_GO(256);
