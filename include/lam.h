@@ -432,7 +432,8 @@ int64_t lam_kv_page_bytes(int32_t head_dim, int32_t page_size);
  * starts is NULL, rows / n_seqs each.  table, lengths and starts are read on the
  * device: pages outside the pool, tokens past the table's columns and rows
  * outside [0, rows) are not touched (append: counted; attend and evict: as if
- * masked, left in place). */
+ * masked, left in place).
+ * table_cols * page_size <= 2^30 (EINVAL above). */
 typedef struct lam_kv_view {
   uint8_t* pages_dev;
   int64_t n_pages;
@@ -477,15 +478,16 @@ lam_status lam_kv_read(lam_ctx* ctx, const lam_kv_view* view, void* k_dev, void*
  * are masked; head_stride 0 for one mask of all heads).  A row with no token left
  * gets 0 (lse -inf).  Scores, maxima and sums are float32; p enters the product
  * with the values as float16 relative to the row's maximum so far.  A query with
- * NaN or Inf spoils its own row only.  q [rows][q_heads][head_dim] of
+ * NaN or Inf spoils its own row only, and the weights of the tokens that it sees.  q [rows][q_heads][head_dim] of
  * view->dtype, out likewise and contiguous; lse_dev (float32[rows][q_heads], or
  * NULL): log sum_t exp(scale * q . k_hat_t).
  * weights (float32, or NULL): the sum of p over the call's rows of s and the
  * query heads of h is added to element (s, h, t); tokens past its columns are
  * left out.  max_length: an upper bound of lengths that the launch is sized by
- * (longer sequences are cut to it); <= 0 for the table's.  Context scratch: per
- * query row and part of the length 4 (head_dim + 2) bytes, where the length is
- * split.  Asynchronous. */
+ * (longer sequences are cut to it); <= 0 for the table's.  Context scratch: where
+ * lengths are split, partial results of at most 35 MB; with weights 4 bytes for each
+ * query row and head, and for up to 64 rows times heads of a group per sequence 4
+ * bytes for each of them and each token of the bound, at most 1 GiB.  Asynchronous. */
 lam_status lam_kv_attend(lam_ctx* ctx, const lam_kv_view* view, const void* q_dev, int64_t q_row_stride,
                          int64_t q_head_stride, int32_t q_heads, double scale, int causal, int64_t max_length,
                          const lam_kv_slots* mask, const lam_kv_slots* weights, void* out_dev, float* lse_dev);

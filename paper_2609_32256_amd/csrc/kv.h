@@ -88,17 +88,6 @@ struct KvArgs {
   __device__ uint8_t* head_page(int64_t page, int h, int64_t head_bytes) const {
     return pages + (page * heads + h) * head_bytes;
   }
-  // sequence of a row (-1: none): the last one that starts at or before it
-  __device__ int seq_of(int64_t row) const {
-    if (!starts) return per_seq > 0 ? (int)(row / per_seq) : -1;
-    int lo = 0, hi = n_seqs;   // start(lo) <= row < start(hi)
-    if (start(0) > row || start(n_seqs) <= row) return -1;
-    while (hi - lo > 1) {
-      const int m = (lo + hi) >> 1;
-      if (start(m) <= row) lo = m; else hi = m;
-    }
-    return lo;
-  }
 };
 
 typedef _Float16 kv_h2 __attribute__((ext_vector_type(2)));

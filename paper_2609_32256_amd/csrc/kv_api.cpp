@@ -25,8 +25,8 @@ lam_status check_view(const lam_kv_view* v) {
   LAM_CHECK(v->kv_heads >= 1 && v->kv_heads <= 4096, LAM_EINVAL, "kv_heads must be in [1, 4096]");
   LAM_CHECK(v->n_seqs >= 0 && v->n_seqs <= (1 << 20), LAM_EINVAL, "n_seqs must be in [0, 2^20]");
   LAM_CHECK(v->rows >= 0 && v->rows < (1LL << 31), LAM_EINVAL, "rows must be in [0, 2^31)");
-  LAM_CHECK(v->table_cols >= 0 && (int64_t)v->table_cols * v->page_size < (1LL << 31), LAM_EINVAL,
-            "table_cols * page_size must be in [0, 2^31)");
+  LAM_CHECK(v->table_cols >= 0 && (int64_t)v->table_cols * v->page_size <= (1LL << 30), LAM_EINVAL,
+            "table_cols * page_size must be in [0, 2^30]");   // (strips ahead of a length are still 32-bit numbers)
   LAM_CHECK(v->n_pages >= 0 && v->n_pages < (1LL << 31), LAM_EINVAL, "n_pages must be in [0, 2^31)");
   LAM_CHECK(v->dtype == LAM_F16 || v->dtype == LAM_BF16, LAM_EINVAL, "dtype %d is not LAM_F16 or LAM_BF16", v->dtype);
   LAM_CHECK(v->pages_dev != nullptr || v->n_pages == 0, LAM_EINVAL, "pages is NULL");

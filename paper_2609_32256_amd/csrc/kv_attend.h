@@ -20,12 +20,24 @@ constexpr int kAttRows = 16;        // rows of a tile of the kernel for single t
 // within float16, and those 2^-21 below the maximum are still normal numbers.
 constexpr float kLift = 7.0f, kSpan = 15.0f;
 constexpr float kNoMax = -3.0e38f;   // no token seen yet
-// Workgroups (of four waves) that a call is split over where its tiles are fewer:
-// as many as run at once, three a compute unit for single tokens and two for chunks.
-// (Chunks of 2,400 to 8,192 pairs were 8 to 30 % slower at twice as many, where the
-// sums written for the join outweigh the evener parts.)
-constexpr int kFill = 768, kFillChunk = 512;
+// Workgroups (of four waves) that run at once: three a compute unit for single tokens,
+// two for chunks, one where heads have 256 channels (by registers).  Lengths are split
+// over as many where the tiles are fewer.  (Over twice as many: chunks of 2,400 to 8,192
+// pairs 8 to 30 % slower, since the sums written for the join outweigh the evener
+// parts; 800 to 1,500 tiles of single tokens split as well: 5 to 35 % slower but
+// for a gain of 3 % at 800; 256 channels over 768 workgroups: 6 to 30 % slower than 256.)
+constexpr int kFillDecode = 768, kFillChunk = 512, kFillWide = 256;
+// No length up to these is split, since the launch that joins the parts takes as long as
+// their walk: 1,400 tokens of single tokens of 1 to 64 sequences take 11 to 20 us whole
+// and 18 to 25 split, 3,000 tokens 18 to 19 whole and 14 to 18 split; chunks at 600
+// tokens 15 to 19 whole and 19 to 41 split, at 1,500 27 whole and 23 split.
+constexpr int kWholeDecode = 2048, kWholeChunk = 1024;
 constexpr int kChunkGrain = 512;      // least tokens of a part of a chunk's tile: its sums are 64 rows
+// The kernel for chunks is taken where sequences have more (row, head) pairs than
+// this on average.  64 pairs over 10,000 tokens of 4 sequences and 8 heads of 128
+// channels: 34 us by 16 rows, 37 by 64; 96 pairs over 4,096 tokens of 20: 66 and 87 without
+// weights, but 109 and 96 with weights over 10,000 tokens of 4.
+constexpr int kChunkPairs = 64;
 constexpr int64_t kKeptBytes = 1LL << 30;   // most scratch for kept scores
 
 struct AttendArgs {
@@ -39,8 +51,9 @@ struct AttendArgs {
   int flip;               // the scale is negative
   int64_t cut;            // lengths are cut to it
   int tiles_per_seq;      // where every sequence has the same number of rows
-  int join_rows;          // rows a wave joins
+  int kept_waves;         // waves that share a token's kept scores, 1 or 4
   int split_to;           // workgroups to split the lengths over, 0: none is split
+  int64_t blocks;         // workgroups of the attention: places for partial results
   lam_kv_slots mask, weights;
   uint16_t* out;
   float* lse;             // natural logarithm, the caller's
@@ -520,7 +533,6 @@ __device__ __forceinline__ void write_row(const AttendArgs& a, int64_t row, int 
     if (a.lse) a.lse[row] = e * 0.6931471805599453f;
   }
 }
-
 
 // Where the waves of a workgroup put their sums of 16 rows to be joined.
 template <int D>

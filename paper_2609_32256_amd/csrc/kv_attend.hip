@@ -150,21 +150,24 @@ __global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : 3) void k_kv_attend(Att
   join_waves<D, BF16>(a, w, w.r0, (int64_t)blockIdx.x * kAttRows, r.row, r.o, js);
 }
 
-// Maximum and sum of row `col` of a tile over its parts, the first of which is workgroup `at`'s.
+// What the parts of a tile's row `col` have in common, by a wave: lane i reads part
+// i's maximum and sum (a lane that read them all in turn took 17 us for 96 parts).
+// at: the first part's workgroup.
 template <int R>
 __device__ __forceinline__ float joined(const AttendArgs& a, uint32_t at, int col, int parts, float* sum) {
+  const int lane = threadIdx.x & 63;
   const float* pm = a.part_m + (int64_t)at * R + col;
   const float* pl = a.part_l + (int64_t)at * R + col;
   float M = kNoMax, total = 0.0f;
-#pragma unroll 8
-  for (int i = 0; i < parts; ++i) M = fmaxf(M, pm[i * R]);
-#pragma unroll 8
-  for (int i = 0; i < parts; ++i) total += __builtin_amdgcn_exp2f(pm[i * R] - M) * pl[i * R];
-  *sum = total;
+  for (int i = lane; i < parts; i += 64) M = fmaxf(M, pm[(int64_t)i * R]);
+  M = wave_max_f32(M);
+  for (int i = lane; i < parts; i += 64) total += __builtin_amdgcn_exp2f(pm[(int64_t)i * R] - M) * pl[(int64_t)i * R];
+  *sum = (float)wave_sum_f64(total);
   return M;
 }
 
-// One row of a unit, by a wave.
+// One row of a unit, by a wave: D/4 lanes hold a part's channels, the wave's groups of
+// them every other (or fourth) part.
 template <int D, bool BF16, int R>
 __device__ __forceinline__ void join_row(const AttendArgs& a, const Work& w, int col) {
   constexpr int kLanes = D / 4, kGroups = 64 / kLanes;
@@ -175,7 +178,7 @@ __device__ __forceinline__ void join_row(const AttendArgs& a, const Work& w, int
   const float M = joined<R>(a, w.base, col, w.parts, &sum);
   kv_f4 acc{0, 0, 0, 0};
   const float* po = a.part_o + slot * D + 4 * sub;
-#pragma unroll 4
+#pragma unroll 8
   for (int i = group; i < w.parts; i += kGroups)
     acc += __builtin_amdgcn_exp2f(a.part_m[slot + (int64_t)i * R] - M) * *reinterpret_cast<const kv_f4*>(po + (int64_t)i * R * D);
 #pragma unroll
@@ -196,31 +199,38 @@ __device__ __forceinline__ void join_row(const AttendArgs& a, const Work& w, int
   }
 }
 
-// Joins the parts of some rows of a unit (a.join_rows for each wave): D/4 lanes hold
-// a part's channels, the wave's groups of them every other (or fourth) part.
+// Joins the parts of 16 rows of a unit, four a wave: with one a wave the plans of four
+// times the workgroups cost more (16 sequences of 8,192 tokens and 16 rows a head: 39 us
+// in all, 35 with four).
+constexpr int kJoinRows = 4;
 template <int D, bool BF16, int R>
 __device__ __forceinline__ void join_rows(const AttendArgs& a, uint32_t block) {
-  const uint32_t blocks = R / (kAttWaves * (uint32_t)a.join_rows);   // of a unit
+  const uint32_t blocks = R / (kAttWaves * kJoinRows);   // of a unit
   const Work w = plan<R, PlanOf::kUnit>(a, block / blocks);
-  if (w.s < 0 || w.parts == 1) return;
-  for (int n = 0; n < a.join_rows; ++n) {
-    const int col = ((int)(block % blocks) * a.join_rows + n) * kAttWaves + (int)(threadIdx.x >> 6);
+  if (w.s < 0 || w.parts == 1 || (int64_t)w.base + w.parts > a.blocks) return;   // (the last: starts that do not rise)
+  for (int n = 0; n < kJoinRows; ++n) {
+    const int col = ((int)(block % blocks) * kJoinRows + n) * kAttWaves + (int)(threadIdx.x >> 6);
     if (w.r0 + col >= w.pairs) return;
     join_row<D, BF16, R>(a, w, col);
   }
 }
-// Weights from the scores that the attention kept: a workgroup takes 1,024 tokens of one
-// head, four a thread, and sums p = 2^(s - lse) over the sequence's rows in their order.
+
+// Weights from the scores that the attention kept: p = 2^(s - lse) summed over the
+// sequence's rows.  A thread takes four tokens of one head; a workgroup 1,024 with all
+// rows to each thread, or, where those workgroups are few, 256 with a quarter of every
+// 16 rows to each wave.
 constexpr int kKeptTokens = 4 * kAttThreads;
 
 __device__ __forceinline__ void add_kept(const AttendArgs& a, uint32_t block) {
-  const uint32_t chunks = (uint32_t)(a.kept_cols / kKeptTokens);
-  const int t = (int)(block % chunks) * kKeptTokens + 4 * (int)threadIdx.x;
+  const int tokens = kKeptTokens / a.kept_waves, wave = (int)threadIdx.x >> 6, lane = (int)threadIdx.x & 63;
+  const uint32_t chunks = (uint32_t)(a.kept_cols / tokens);
+  const bool share = a.kept_waves > 1;
+  const int t = (int)(block % chunks) * tokens + 4 * (share ? lane : (int)threadIdx.x);
   const int h = (int)(block / chunks % (uint32_t)a.c.heads), s = (int)(block / chunks / (uint32_t)a.c.heads);
   const int64_t first = a.c.start(s);
   const int n = (int)max((int64_t)0, a.c.start(s + 1) - first), full = a.c.length(s);
   const int len = (int)min((int64_t)full, a.cut), pairs = n * a.group;
-  if ((int)(block % chunks) * kKeptTokens >= len) return;
+  if ((int)(block % chunks) * tokens >= len) return;
   // Four rows' scores at a time, the first four on their way before the plan and the
   // sums are known.
   kv_f4 x[4];
@@ -235,41 +245,51 @@ __device__ __forceinline__ void add_kept(const AttendArgs& a, uint32_t block) {
                                        : kv_f4{no, no, no, no};
     }
   };
-  load(0);
+  const int r_first = share ? 4 * wave : 0, r_step = share ? kAttRows : 4;
+  load(r_first);
   float* d = static_cast<float*>(a.weights.p_dev) + s * a.weights.seq_stride + h * a.weights.head_stride + t;
   float w[4];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) w[j] = t + j < min(len, a.weights.cols) ? d[j] : 0.0f;
+  for (int j = 0; j < 4; ++j) w[j] = (!share || wave == 0) && t + j < min(len, a.weights.cols) ? d[j] : 0.0f;
   Work q;
   q.parts = 1;
   if (a.split_to) q = plan<kAttRows, PlanOf::kSequence>(a, (uint32_t)s);
   __shared__ float lse[kAttRows];
   for (int r0 = 0; r0 < pairs; r0 += kAttRows) {
     __syncthreads();
-    if ((int)threadIdx.x < min(pairs - r0, kAttRows)) {
-      const int r = r0 + (int)threadIdx.x;
-      const int64_t at = (first + r / a.group) * a.q_heads + h * a.group + r % a.group;
-      float e;
-      if (q.parts > 1) {
-        float sum;
-        const uint32_t unit = (uint32_t)(r0 / kAttRows * a.c.heads + h);
-        const float M = joined<kAttRows>(a, q.base + unit * q.parts, threadIdx.x, q.parts, &sum);
-        e = log_sum(M, sum);
-      } else {
-        e = a.lse2[at];
+    if (q.parts > 1) {
+      const int64_t first_part = q.base + (int64_t)(r0 / kAttRows * a.c.heads + h) * q.parts;
+      for (int i = threadIdx.x >> 6; i < min(pairs - r0, kAttRows); i += kAttWaves) {
+        float sum = 0.0f, M = 0.0f;
+        if (first_part + q.parts <= a.blocks) M = joined<kAttRows>(a, (uint32_t)first_part, i, q.parts, &sum);
+        if ((threadIdx.x & 63) == 0) lse[i] = log_sum(M, sum);
       }
-      lse[threadIdx.x] = e == -__builtin_inff() ? __builtin_inff() : e;   // no token: 2^(-inf) each
+    } else if ((int)threadIdx.x < min(pairs - r0, kAttRows)) {
+      const int r = r0 + (int)threadIdx.x;
+      lse[threadIdx.x] = a.lse2[(first + r / a.group) * a.q_heads + h * a.group + r % a.group];
     }
     __syncthreads();
-    for (int r = r0; r < min(pairs, r0 + kAttRows); r += 4) {
+    for (int r = r0 + r_first; r < min(pairs, r0 + kAttRows); r += r_step) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float e = r + j < pairs ? lse[r + j - r0] : 0.0f;
+        float e = r + j < pairs ? lse[r + j - r0] : 0.0f;
+        e = e == -__builtin_inff() ? __builtin_inff() : e;   // no token: 2^(-inf) each
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] += __builtin_amdgcn_exp2f(x[j][i] - e);
       }
-      load(r + 4);
+      load(r + r_step);
     }
+  }
+  if (share) {   // the waves' sums, in their order
+    __shared__ float sums[kAttWaves][256];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sums[wave][4 * lane + j] = w[j];
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int i = 1; i < kAttWaves; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[j] += sums[i][4 * lane + j];
   }
 #pragma unroll
   for (int j = 0; j < 4; ++j)
@@ -444,10 +464,9 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
   a.out = static_cast<uint16_t*>(out);
   a.lse = lse;
 
-  // The kernel for chunks where sequences have more than a tile of the other's rows on average.
-  const bool chunk = v.rows * a.group > kAttRows * (int64_t)v.n_seqs;
+  const bool chunk = v.rows * a.group > kChunkPairs * (int64_t)v.n_seqs;
   const int rows = chunk ? chunk_rows(v.head_dim) : kAttRows;
-  const int fill = chunk ? kFillChunk : kFill;
+  const int fill = v.head_dim == 256 ? kFillWide : chunk ? kFillChunk : kFillDecode;
   int64_t tiles;
   if (v.starts_dev) {
     tiles = v.rows * a.group / rows + v.n_seqs;
@@ -458,15 +477,17 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
   // Lengths are split where the tiles do not fill the chip.
   const int64_t units = tiles * v.kv_heads;
   int64_t blocks = units;
-  if (units < fill && a.cut > (chunk ? kChunkGrain : kKvStrip * kAttWaves)) {
+  if (units < fill && a.cut > (chunk ? kWholeChunk : kWholeDecode)) {
     a.split_to = fill;
     blocks = fill + units;   // see plan(): at most split_to - units / 2 (or split_to / 2) full parts, and one more a tile
   }
   LAM_CHECK(blocks < (1LL << 31), LAM_EINVAL, "too many rows for one launch");
+  a.blocks = blocks;
 
   // Weights: from scores that the attention keeps (8 bytes a row and token, written
-  // and read) where sequences have a tile of rows on average, else from a second
-  // pass over the keys.
+  // and read) where it is not the kernel for chunks, else from a second pass over the
+  // keys.  (16 sequences of 8,192 tokens, 8 heads of 128 channels: 44 and 158 us for 4 pairs
+  // a head, 60 and 161 for 16.)
   const int64_t pairs = v.rows * q_heads;
   const int64_t parts = a.split_to ? blocks * rows : 0;
   const bool keep = weights.p_dev && !chunk && pairs * a.cut * 4 <= kKeptBytes;
@@ -498,9 +519,12 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
 #undef LAM_GO
     LAM_HIP(hipGetLastError());
   }
-  a.join_rows = units * rows >= 8192 ? 4 : 1;   // few rows: each its own wave, many: four, and a quarter of the plans
-  const int64_t join_blocks = a.split_to ? units * (rows / (kAttWaves * a.join_rows)) : 0;
-  const int64_t kept_blocks = keep ? a.kept_cols / kKeptTokens * v.kv_heads * v.n_seqs : 0;
+  const int64_t join_blocks = a.split_to ? units * (rows / (kAttWaves * kJoinRows)) : 0;
+  int64_t kept_blocks = keep ? a.kept_cols / kKeptTokens * v.kv_heads * v.n_seqs : 0;
+  // (4 sequences of 4,000 tokens, 64 pairs: 51 us with one wave a token, 46 with four;
+  // 4 of 8,192 and 4 pairs: 21 and 22)
+  a.kept_waves = kept_blocks < 1024 && v.rows * a.group > kAttRows * (int64_t)v.n_seqs ? 4 : 1;
+  kept_blocks *= a.kept_waves;
   if (join_blocks + kept_blocks > 0) {
     LAM_CHECK(join_blocks + kept_blocks < (1LL << 31), LAM_EINVAL, "too many rows for one launch");
     LAM_TRY(prof_launch_events(ctx, "kv_finish", &e0, &e1));

@@ -1,0 +1,131 @@
+"""Attention over the 4-bit cache where lengths are cut into parts, where a call has
+more sequences than a wave has lanes, and where the weights come by either way; eviction
+at the sizes where its kernels change.  Tolerances as in test_gpu_kv_attend.
+"""
+import numpy as np
+import pytest
+import torch
+
+from test_gpu_kv_attend import Case, _i32
+from test_gpu_kv_cache import _evict_case, _scores
+
+pytestmark = pytest.mark.gpu
+
+
+def _all(c, causal=True, mask=None, **kw):
+    """Outputs, log sums and weights of one call, and the output without them."""
+    B, cols = len(c.lens), max(1, max(c.lens))
+    lse = torch.empty(c.q.shape[:2], device="cuda")
+    w = torch.zeros((B, c.Hk, cols), device="cuda")
+    m = None if mask is None else torch.from_numpy(mask).cuda()
+    cut = None if mask is None else [mask[b][:, : c.lens[b]] for b in range(B)]
+    c.check(c.call(causal=causal, mask=m, lse=lse, weights=w, **kw), causal=causal, mask=cut, lse=lse, weights=w)
+    c.check(c.call(causal=causal, mask=m, **kw), causal=causal, mask=cut)
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("D,T,Hk,G,rows,lens", [
+    (128, 64, 2, 4, [1], [5000]),                            # few tiles, many parts
+    (128, 32, 1, 1, [1], [13000]),
+    (64, 32, 1, 16, [1, 1, 1], [9000, 2049, 0]),
+    (128, 64, 1, 4, [4, 4, 4], [2100, 70, 6000]),
+    (256, 64, 1, 2, [1, 3, 2], [4097, 3, 2600]),
+    (64, 1024, 2, 3, [11, 0, 2], [3001, 500, 2500]),         # three tiles of a sequence
+    (128, 64, 1, 8, [8], [3333]),                            # 64 pairs
+])
+def test_parts_of_single_tokens(lam, D, T, Hk, G, rows, lens, dt):
+    c = Case(lam, D, T, Hk, G, dt, rows, lens, seed=sum(lens))
+    _all(c)
+    _all(c, causal=False)
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("D,T,Hk,G,rows,lens", [
+    (128, 64, 1, 4, [20], [3000]),
+    (64, 128, 2, 2, [90, 0, 70], [2600, 900, 1500]),
+    (256, 32, 1, 8, [9, 30], [2000, 1100]),
+    (64, 64, 1, 1, [65, 65], [1025, 2303]),
+])
+def test_parts_of_chunks(lam, D, T, Hk, G, rows, lens, dt):
+    c = Case(lam, D, T, Hk, G, dt, rows, lens, seed=sum(lens))
+    _all(c)
+    _all(c, causal=False)
+
+
+@pytest.mark.parametrize("n,G", [(1, 4), (6, 8), (40, 2)])
+def test_parts_and_masks(lam, n, G):
+    lens = [2900, 64, 4100]
+    c = Case(lam, 64, 32, 1, G, "f16", [n] * 3, lens, seed=n)
+    m = np.random.default_rng(n).random((3, 1, max(lens))) > 0.3
+    m[0, 0, 640:1900] = False                                # parts of which nothing is left
+    m[1] = False
+    _all(c, mask=m)
+
+
+@pytest.mark.parametrize("longest", [60, 2700])
+@pytest.mark.parametrize("B,rows", [
+    (64, lambda s: 1), (65, lambda s: 1), (200, lambda s: 1),
+    (64, lambda s: s % 3), (129, lambda s: (s * 7) % 4),
+    (70, lambda s: 60 if s in (3, 66) else s % 2),
+    (66, lambda s: 40),                                      # chunks
+    (130, lambda s: 50 + s % 30),
+])
+def test_many_sequences(lam, B, rows, longest):
+    rng = np.random.default_rng(B)
+    n = [rows(s) for s in range(B)]
+    lens = [max(n[s], int(x)) for s, x in enumerate(rng.integers(0, 50, B))]
+    lens[B // 2] = lens[-1] = longest
+    n = [min(a, b) for a, b in zip(n, lens)] if len(set(n)) > 1 else n
+    c = Case(lam, 64, 32, 1, 2, "bf16", n, lens, seed=B)
+    _all(c)
+
+
+def test_sequences_beyond_one_step_of_the_chip(lam):
+    """More tiles than run at once: nothing is split."""
+    rng = np.random.default_rng(1)
+    lens = [int(x) for x in rng.integers(0, 40, 1100)]
+    for rows in ([1] * 1100, [min(l, s % 3) for s, l in enumerate(lens)]):
+        c = Case(lam, 64, 32, 1, 1, "f16", rows, lens, seed=2)
+        _all(c)
+
+
+def test_weights_of_a_wide_table(lam):
+    """Scores of every column would take over a GiB: the weights come from a second pass."""
+    c = Case(lam, 64, 64, 1, 16, "f16", [4, 4], [300, 2500], seed=5)
+    wide = torch.zeros((2, (1 << 15) + 1), dtype=torch.int32, device="cuda")
+    wide[:, : c.table.shape[1]] = c.table
+    c.table = wide
+    _all(c)
+
+
+def test_weights_by_both_ways_agree(lam):
+    """One row at a time (kept scores) and all rows at once (a second pass) add up to the same."""
+    c = Case(lam, 128, 64, 2, 4, "bf16", [48], [1500], seed=6)
+    w = torch.zeros((1, 2, 1500), device="cuda")
+    out = c.call(causal=False, weights=w)
+    one, q = torch.zeros_like(w), c.q
+    for i in range(48):
+        c.q = q[i:i + 1]
+        got = c.call(causal=False, weights=one)
+        # an output differs by its own rounding, and by that of the weights to float16
+        assert torch.allclose(got[0].float(), out[i].float(), rtol=2.0 ** -7, atol=2.0 ** -9)
+    # sums of 48 * 4 weights: each to 2^-20 of itself, and the additions' rounding
+    assert ((one - w).abs() <= 2.0 ** -18 * (1 + w)).all()
+
+
+def test_starts_that_do_not_rise(lam):
+    """Such rows get anything, but nothing outside the call's arrays is touched, and the next call is right."""
+    c = Case(lam, 64, 32, 2, 4, "f16", [2, 2, 2, 2], [3000, 90, 2100, 5], seed=7)
+    w = torch.zeros((4, 2, 3000), device="cuda")
+    for starts in ([0, 8, 0, 8, 0], [8, 6, 4, 2, 0], [-5, 100, -(1 << 31), (1 << 31) - 1, 3]):
+        out = lam.kv_attend(c.q, c.pool, c.table, c.lengths, starts=_i32(starts), weights=w)
+        assert out.shape == c.q.shape
+    torch.cuda.synchronize()
+    _all(c)
+
+
+@pytest.mark.parametrize("kind", ["random", "equal", "odd"])
+@pytest.mark.parametrize("L", [2048, 2049, 8192, 8193, 32768, 32769, 65536, 65537])
+def test_evict_where_kernels_change(lam, L, kind):
+    budget = L - 3 if kind == "equal" else L // 3
+    _evict_case(lam, 64, 1024, 1, [L, max(0, L - 1500)], budget, 10, 2, _scores(L, 2, 1, L, kind), None, False, seed=L)
