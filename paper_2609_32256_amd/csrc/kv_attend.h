@@ -594,8 +594,9 @@ __device__ __forceinline__ void join_waves(const AttendArgs& a, const Work& w, i
   }
 }
 
-// Rows of a tile of the kernel for chunks (kv_chunk.hip), and its launch.
-__host__ __device__ constexpr int chunk_rows(int D) { return D == 256 ? 32 : 64; }
-lam_status launch_kv_chunk(lam_ctx* ctx, const lam_kv_view& v, const AttendArgs& a, int64_t blocks, bool masked);
+// Rows of a tile of the kernel for chunks (kv_chunk.hip): 64, or 32 and 48 of 256
+// channels, and its launch.
+constexpr int kChunkRows = 64, kChunkRowsWide = 32, kChunkRowsWider = 48;
+lam_status launch_kv_chunk(lam_ctx* ctx, const lam_kv_view& v, const AttendArgs& a, int rows, int64_t blocks, bool masked);
 
 }  // namespace lam

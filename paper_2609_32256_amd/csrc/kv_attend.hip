@@ -150,69 +150,84 @@ __global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : 3) void k_kv_attend(Att
   join_waves<D, BF16>(a, w, w.r0, (int64_t)blockIdx.x * kAttRows, r.row, r.o, js);
 }
 
-// What the parts of a tile's row `col` have in common, by a wave: lane i reads part
-// i's maximum and sum (a lane that read them all in turn took 17 us for 96 parts).
-// at: the first part's workgroup.
-template <int R>
-__device__ __forceinline__ float joined(const AttendArgs& a, uint32_t at, int col, int parts, float* sum) {
-  const int lane = threadIdx.x & 63;
-  const float* pm = a.part_m + (int64_t)at * R + col;
-  const float* pl = a.part_l + (int64_t)at * R + col;
-  float M = kNoMax, total = 0.0f;
-  for (int i = lane; i < parts; i += 64) M = fmaxf(M, pm[(int64_t)i * R]);
-  M = wave_max_f32(M);
-  for (int i = lane; i < parts; i += 64) total += __builtin_amdgcn_exp2f(pm[(int64_t)i * R] - M) * pl[(int64_t)i * R];
-  *sum = (float)wave_sum_f64(total);
-  return M;
-}
-
-// One row of a unit, by a wave: D/4 lanes hold a part's channels, the wave's groups of
-// them every other (or fourth) part.
-template <int D, bool BF16, int R>
-__device__ __forceinline__ void join_row(const AttendArgs& a, const Work& w, int col) {
-  constexpr int kLanes = D / 4, kGroups = 64 / kLanes;
-  const int pair = w.r0 + col;
-  const int lane = threadIdx.x & 63, sub = lane % kLanes, group = lane / kLanes;
-  const int64_t slot = (int64_t)w.base * R + col;
-  float sum;
-  const float M = joined<R>(a, w.base, col, w.parts, &sum);
-  kv_f4 acc{0, 0, 0, 0};
-  const float* po = a.part_o + slot * D + 4 * sub;
-#pragma unroll 8
-  for (int i = group; i < w.parts; i += kGroups)
-    acc += __builtin_amdgcn_exp2f(a.part_m[slot + (int64_t)i * R] - M) * *reinterpret_cast<const kv_f4*>(po + (int64_t)i * R * D);
+// Maxima and sums of N rows over their parts, by a wave: lane i reads part i's (a lane
+// that read them all in turn took 17 us for 96 parts).  slot: where a row's first part is.
+template <int R, int N>
+__device__ __forceinline__ void joined(const AttendArgs& a, const int64_t slot[N], int parts, float M[N], float sum[N]) {
+  float m[N], l[N];
 #pragma unroll
-  for (int d = kLanes; d < 64; d <<= 1)
+  for (int n = 0; n < N; ++n) m[n] = kNoMax, l[n] = 0.0f;
+  for (int i = threadIdx.x & 63; i < parts; i += 64)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[j] += __shfl_xor(acc[j], d);
-  if (group != 0) return;
-  const int64_t at = (w.first + pair / a.group) * a.q_heads + w.h * a.group + pair % a.group;
-  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-  uint2 u;
-  u.x = (uint32_t)to_out(acc[0] * inv, BF16) | ((uint32_t)to_out(acc[1] * inv, BF16) << 16);
-  u.y = (uint32_t)to_out(acc[2] * inv, BF16) | ((uint32_t)to_out(acc[3] * inv, BF16) << 16);
-  *reinterpret_cast<uint2*>(a.out + at * D + 4 * sub) = u;
-  if (sub == 0) {
-    const float e = log_sum(M, sum);
-    if (a.lse2) a.lse2[at] = e;
-    if (a.lse) a.lse[at] = e * 0.6931471805599453f;
+    for (int n = 0; n < N; ++n) {
+      const float pm = a.part_m[slot[n] + (int64_t)i * R], pl = a.part_l[slot[n] + (int64_t)i * R];
+      const float top = fmaxf(m[n], pm);
+      l[n] = l[n] * __builtin_amdgcn_exp2f(m[n] - top) + pl * __builtin_amdgcn_exp2f(pm - top);
+      m[n] = top;
+    }
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    M[n] = wave_max_f32(m[n]);
+    sum[n] = (float)wave_sum_f64(l[n] * __builtin_amdgcn_exp2f(m[n] - M[n]));
   }
 }
 
-// Joins the parts of 16 rows of a unit, four a wave: with one a wave the plans of four
-// times the workgroups cost more (16 sequences of 8,192 tokens and 16 rows a head: 39 us
-// in all, 35 with four).
+// Joins N rows by a wave: D/4 lanes hold a part's channels, the wave's groups of them
+// every other (or fourth) part.  Rows at or past n_rows repeat the first and are not
+// written.
+template <int D, bool BF16, int R, int N>
+__device__ __forceinline__ void join_some(const AttendArgs& a, const Work& w, int col, int n_rows) {
+  constexpr int kLanes = D / 4, kGroups = 64 / kLanes;
+  const int lane = threadIdx.x & 63, sub = lane % kLanes, group = lane / kLanes;
+  int64_t slot[N];
+#pragma unroll
+  for (int n = 0; n < N; ++n) slot[n] = (int64_t)w.base * R + col + (n < n_rows ? n * kAttWaves : 0);
+  float M[N], sum[N];
+  joined<R, N>(a, slot, w.parts, M, sum);
+  kv_f4 acc[N] = {};
+#pragma unroll N == 1 ? 8 : 4
+  for (int i = group; i < w.parts; i += kGroups)
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+      acc[n] += __builtin_amdgcn_exp2f(a.part_m[slot[n] + (int64_t)i * R] - M[n]) *
+                *reinterpret_cast<const kv_f4*>(a.part_o + (slot[n] + (int64_t)i * R) * D + 4 * sub);
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+#pragma unroll
+    for (int d = kLanes; d < 64; d <<= 1)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[n][j] += __shfl_xor(acc[n][j], d);
+    if (group != 0 || n >= n_rows) continue;
+    const int pair = w.r0 + col + n * kAttWaves;
+    const int64_t at = (w.first + pair / a.group) * a.q_heads + w.h * a.group + pair % a.group;
+    const float inv = sum[n] == 0.0f ? 0.0f : 1.0f / sum[n];
+    uint2 u;
+    u.x = (uint32_t)to_out(acc[n][0] * inv, BF16) | ((uint32_t)to_out(acc[n][1] * inv, BF16) << 16);
+    u.y = (uint32_t)to_out(acc[n][2] * inv, BF16) | ((uint32_t)to_out(acc[n][3] * inv, BF16) << 16);
+    *reinterpret_cast<uint2*>(a.out + at * D + 4 * sub) = u;
+    if (sub == 0) {
+      const float e = log_sum(M[n], sum[n]);
+      if (a.lse2) a.lse2[at] = e;
+      if (a.lse) a.lse[at] = e * 0.6931471805599453f;
+    }
+  }
+}
+
+// Joins the parts of 16 rows of a unit, up to four a wave with their loads on their way
+// together (one after the other: 13 us for 20 parts, 8 so; one row a wave: the plans of four
+// times the workgroups cost more).
 constexpr int kJoinRows = 4;
+
 template <int D, bool BF16, int R>
 __device__ __forceinline__ void join_rows(const AttendArgs& a, uint32_t block) {
-  const uint32_t blocks = R / (kAttWaves * kJoinRows);   // of a unit
-  const Work w = plan<R, PlanOf::kUnit>(a, block / blocks);
+  constexpr uint32_t kBlocks = R / (kAttWaves * kJoinRows);   // of a unit
+  const Work w = plan<R, PlanOf::kUnit>(a, block / kBlocks);
   if (w.s < 0 || w.parts == 1 || (int64_t)w.base + w.parts > a.blocks) return;   // (the last: starts that do not rise)
-  for (int n = 0; n < kJoinRows; ++n) {
-    const int col = ((int)(block % blocks) * kJoinRows + n) * kAttWaves + (int)(threadIdx.x >> 6);
-    if (w.r0 + col >= w.pairs) return;
-    join_row<D, BF16, R>(a, w, col);
-  }
+  const int col = (int)(block % kBlocks) * kAttWaves * kJoinRows + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n_rows = (w.pairs - w.r0 - col + kAttWaves - 1) / kAttWaves;
+  if (n_rows <= 0) return;
+  if (n_rows == 1) join_some<D, BF16, R, 1>(a, w, col, 1);
+  else join_some<D, BF16, R, kJoinRows>(a, w, col, min(n_rows, kJoinRows));
 }
 
 // Weights from the scores that the attention kept: p = 2^(s - lse) summed over the
@@ -259,11 +274,17 @@ __device__ __forceinline__ void add_kept(const AttendArgs& a, uint32_t block) {
     __syncthreads();
     if (q.parts > 1) {
       const int64_t first_part = q.base + (int64_t)(r0 / kAttRows * a.c.heads + h) * q.parts;
-      for (int i = threadIdx.x >> 6; i < min(pairs - r0, kAttRows); i += kAttWaves) {
-        float sum = 0.0f, M = 0.0f;
-        if (first_part + q.parts <= a.blocks) M = joined<kAttRows>(a, (uint32_t)first_part, i, q.parts, &sum);
-        if ((threadIdx.x & 63) == 0) lse[i] = log_sum(M, sum);
-      }
+      float M[kJoinRows] = {}, sum[kJoinRows] = {};
+      int64_t slot[kJoinRows];
+      const int last = min(pairs - r0, kAttRows) - 1;
+#pragma unroll
+      for (int n = 0; n < kJoinRows; ++n) slot[n] = first_part * kAttRows + min(wave + n * kAttWaves, last);
+      if (first_part + q.parts > a.blocks) q.parts = 0;   // (starts that do not rise)
+      if (last < kAttWaves) joined<kAttRows, 1>(a, slot, q.parts, M, sum);
+      else joined<kAttRows, kJoinRows>(a, slot, q.parts, M, sum);
+#pragma unroll
+      for (int n = 0; n < kJoinRows; ++n)
+        if (lane == 0 && wave + n * kAttWaves <= last) lse[wave + n * kAttWaves] = log_sum(M[n], sum[n]);
     } else if ((int)threadIdx.x < min(pairs - r0, kAttRows)) {
       const int r = r0 + (int)threadIdx.x;
       lse[threadIdx.x] = a.lse2[(first + r / a.group) * a.q_heads + h * a.group + r % a.group];
@@ -304,17 +325,17 @@ __global__ __launch_bounds__(kAttThreads) void k_kv_finish(AttendArgs a, uint32_
   else add_kept(a, b - join_blocks);
 }
 
-// Accumulated weights: a workgroup owns 64 tokens of one head (32 of 256 channels),
-// whose keys each wave converts once; its waves share the call's rows, 16 at a
-// time, the next 16 on their way; p = 2^(s - lse).  The waves' sums are added in
-// their order, so the result does not depend on timing.  (With 32 tokens a wave
-// and all rows to each, addresses and loads were two thirds of the instructions.)
-template <int D>
-constexpr int weight_strips() { return D == 256 ? 1 : 2; }
+// Accumulated weights: a workgroup owns 64 tokens of one head, whose keys each wave
+// converts once; its waves share the call's rows, 16 at a time, the next 16 on their
+// way; p = 2^(s - lse).  The waves' sums are added in their order, so the result does
+// not depend on timing.  (With 32 tokens and all rows to each wave, addresses and
+// loads were two thirds of the instructions; of 256 channels 32 tokens took 415 us
+// for 405 rows of 32 heads over 17,034 tokens, 64 take 234.)
+constexpr int kWeightStrips = 2;
 
 template <int D, bool BF16>
 __global__ __launch_bounds__(kAttThreads, D == 64 ? 4 : D == 128 ? 3 : 2) void k_kv_weights(AttendArgs a) {
-  constexpr int kSteps = D / 32, kStrips = weight_strips<D>(), kTokens = kStrips * kKvStrip;
+  constexpr int kSteps = D / 32, kStrips = kWeightStrips, kTokens = kStrips * kKvStrip;
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t chunks = (uint32_t)((a.cut + kTokens - 1) / kTokens);
@@ -465,17 +486,24 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
   a.lse = lse;
 
   const bool chunk = v.rows * a.group > kChunkPairs * (int64_t)v.n_seqs;
-  const int rows = chunk ? chunk_rows(v.head_dim) : kAttRows;
   const int fill = v.head_dim == 256 ? kFillWide : chunk ? kFillChunk : kFillDecode;
-  int64_t tiles;
-  if (v.starts_dev) {
-    tiles = v.rows * a.group / rows + v.n_seqs;
-  } else {
-    a.tiles_per_seq = (int)((v.rows / v.n_seqs * a.group + rows - 1) / rows);
-    tiles = (int64_t)a.tiles_per_seq * v.n_seqs;
+  auto units_of = [&](int rows) {   // tiles of every head
+    const int64_t tiles = v.starts_dev ? v.rows * a.group / rows + v.n_seqs
+                                       : (v.rows / v.n_seqs * a.group + rows - 1) / rows * v.n_seqs;
+    return tiles * v.kv_heads;
+  };
+  int rows = chunk ? kChunkRows : kAttRows;
+  if (chunk && v.head_dim == 256) {
+    // A round of 48 rows takes 1.2 times one of 32: 48 where the rounds that the chip takes
+    // are fewer by as much.  (405 rows of 32 heads, 4 key/value heads, 17,034 tokens: two
+    // rounds of either, 514 us by 32 and 599 by 48; 100 rows of 32 and 8 heads of 3
+    // sequences of 8,000: 247 and 160; 2,048 rows over 8,192: 893 and 808.)
+    const int64_t wide = (units_of(kChunkRowsWide) + fill - 1) / fill, wider = (units_of(kChunkRowsWider) + fill - 1) / fill;
+    rows = 6 * wider <= 5 * wide ? kChunkRowsWider : kChunkRowsWide;
   }
+  if (!v.starts_dev) a.tiles_per_seq = (int)((v.rows / v.n_seqs * a.group + rows - 1) / rows);
   // Lengths are split where the tiles do not fill the chip.
-  const int64_t units = tiles * v.kv_heads;
+  const int64_t units = units_of(rows);
   int64_t blocks = units;
   if (units < fill && a.cut > (chunk ? kWholeChunk : kWholeDecode)) {
     a.split_to = fill;
@@ -507,7 +535,7 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
 
   hipEvent_t e0, e1;
   if (chunk) {
-    LAM_TRY(launch_kv_chunk(ctx, v, a, blocks, mask.p_dev != nullptr));
+    LAM_TRY(launch_kv_chunk(ctx, v, a, rows, blocks, mask.p_dev != nullptr));
   } else {
     LAM_TRY(prof_launch_events(ctx, "kv_attend", &e0, &e1));
 #define LAM_GO(D, BF)                                                                                          \
@@ -532,15 +560,18 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
     const uint32_t jb = (uint32_t)join_blocks;
 #define LAM_GO(D, BF)                                                                                 \
   do {                                                                                                \
-    if (chunk) launch(k_kv_finish<D, BF, chunk_rows(D)>, grid, kAttThreads, ctx->stream, e0, e1, a, jb); \
-    else launch(k_kv_finish<D, BF, kAttRows>, grid, kAttThreads, ctx->stream, e0, e1, a, jb);         \
+    constexpr int kMost = D == 256 ? kChunkRowsWider : kChunkRows;                                    \
+    constexpr int kLess = D == 256 ? kChunkRowsWide : kChunkRows;                                     \
+    if (!chunk) launch(k_kv_finish<D, BF, kAttRows>, grid, kAttThreads, ctx->stream, e0, e1, a, jb);  \
+    else if (rows == kMost) launch(k_kv_finish<D, BF, kMost>, grid, kAttThreads, ctx->stream, e0, e1, a, jb); \
+    else launch(k_kv_finish<D, BF, kLess>, grid, kAttThreads, ctx->stream, e0, e1, a, jb);            \
   } while (0)
     LAM_KV_DISPATCH(v, LAM_GO);
 #undef LAM_GO
     LAM_HIP(hipGetLastError());
   }
   if (weights.p_dev && !keep && a.cut > 0) {
-    const int tokens = (v.head_dim == 256 ? weight_strips<256>() : weight_strips<128>()) * kKvStrip;
+    const int tokens = kWeightStrips * kKvStrip;
     const int64_t wb = (a.cut + tokens - 1) / tokens * v.kv_heads * v.n_seqs;
     LAM_CHECK(wb < (1LL << 31), LAM_EINVAL, "too many sequences for one launch");
     LAM_TRY(prof_launch_events(ctx, "kv_weights", &e0, &e1));

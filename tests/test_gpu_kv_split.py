@@ -80,6 +80,17 @@ def test_many_sequences(lam, B, rows, longest):
     _all(c)
 
 
+@pytest.mark.parametrize("longest", [70, 1500])
+@pytest.mark.parametrize("B", [100, 60])                     # 256 channels: tiles of 48 rows, of 32
+def test_chunks_of_wide_heads(lam, B, longest):
+    lens = [25 + s % 40 for s in range(B)]
+    lens[7] = lens[-1] = longest
+    c = Case(lam, 256, 32, 1, 4, "f16", [24] * B, lens, seed=B)
+    _all(c)
+    if longest == 70:
+        _all(Case(lam, 256, 32, 1, 4, "bf16", [24 + s % 2 for s in range(B)], lens, seed=B))
+
+
 def test_sequences_beyond_one_step_of_the_chip(lam):
     """More tiles than run at once: nothing is split."""
     rng = np.random.default_rng(1)
