@@ -325,17 +325,24 @@ __global__ __launch_bounds__(kAttThreads) void k_kv_finish(AttendArgs a, uint32_
   else add_kept(a, b - join_blocks);
 }
 
-// Accumulated weights: a workgroup owns 64 tokens of one head, whose keys each wave
-// converts once; its waves share the call's rows, 16 at a time, the next 16 on their
-// way; p = 2^(s - lse).  The waves' sums are added in their order, so the result does
-// not depend on timing.  (With 32 tokens and all rows to each wave, addresses and
-// loads were two thirds of the instructions; of 256 channels 32 tokens took 415 us
-// for 405 rows of 32 heads over 17,034 tokens, 64 take 234.)
-constexpr int kWeightStrips = 2;
+// Accumulated weights: a workgroup owns 128 tokens of one head (64 of 256 channels),
+// whose keys each wave converts once; its waves share the call's rows, 16 at a time, the
+// next 16 on their way; p = 2^(s - lse).  The waves' sums are added in their order, so the
+// result does not depend on timing.  Bound by issue: an exponential, two additions or
+// multiplications a score beside the products, and the queries from the L2 for every
+// workgroup.  2,048 rows of 32 heads over 16,384 tokens, 8 key/value heads of 128 channels:
+// 267 us (64 tokens a workgroup 490, and 32 with all rows to each wave more).
+template <int D>
+constexpr int weight_strips() { return D == 256 ? 2 : 4; }
+// Where workgroups of 128 tokens are fewer than this, they take 64: 100 rows over 3,000
+// tokens of one sequence and 4 heads of 64 channels 11 us for 15, 512 rows over 8,192 24 for 31
+// (with 8 heads of 128, 512 workgroups, 75 for 45).
+constexpr int64_t kWeightBlocks = 512;
 
-template <int D, bool BF16>
-__global__ __launch_bounds__(kAttThreads, D == 64 ? 4 : D == 128 ? 3 : 2) void k_kv_weights(AttendArgs a) {
-  constexpr int kSteps = D / 32, kStrips = kWeightStrips, kTokens = kStrips * kKvStrip;
+template <int D, bool BF16, int kStrips>
+__global__ __launch_bounds__(kAttThreads, D == 256 ? 2 : D == 64 && kStrips == 2 ? 4 : D == 64 || kStrips == 2 ? 3 : 2)
+void k_kv_weights(AttendArgs a) {
+  constexpr int kSteps = D / 32, kTokens = kStrips * kKvStrip;
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t chunks = (uint32_t)((a.cut + kTokens - 1) / kTokens);
@@ -571,11 +578,17 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
     LAM_HIP(hipGetLastError());
   }
   if (weights.p_dev && !keep && a.cut > 0) {
-    const int tokens = kWeightStrips * kKvStrip;
-    const int64_t wb = (a.cut + tokens - 1) / tokens * v.kv_heads * v.n_seqs;
-    LAM_CHECK(wb < (1LL << 31), LAM_EINVAL, "too many sequences for one launch");
+    const int64_t heads = (int64_t)v.kv_heads * v.n_seqs;
+    auto blocks_of = [&](int strips) { return (a.cut + strips * kKvStrip - 1) / (strips * kKvStrip) * heads; };
+    LAM_CHECK(blocks_of(2) < (1LL << 31), LAM_EINVAL, "too many sequences for one launch");
     LAM_TRY(prof_launch_events(ctx, "kv_weights", &e0, &e1));
-#define LAM_GO(D, BF) launch(k_kv_weights<D, BF>, dim3((unsigned)wb), kAttThreads, ctx->stream, e0, e1, a)
+    const bool few = v.head_dim == 256 || blocks_of(4) < kWeightBlocks;
+    const dim3 grid((unsigned)blocks_of(few ? 2 : 4));
+#define LAM_GO(D, BF)                                                                                       \
+  do {                                                                                                      \
+    if (few) launch(k_kv_weights<D, BF, 2>, grid, kAttThreads, ctx->stream, e0, e1, a);                     \
+    else launch(k_kv_weights<D, BF, weight_strips<D>()>, grid, kAttThreads, ctx->stream, e0, e1, a);        \
+  } while (0)
     LAM_KV_DISPATCH(v, LAM_GO);
 #undef LAM_GO
     LAM_HIP(hipGetLastError());

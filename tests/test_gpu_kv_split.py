@@ -109,6 +109,18 @@ def test_weights_of_a_wide_table(lam):
     _all(c)
 
 
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_second_pass_of_many_tiles(lam, D, dt):
+    """Enough sequences and tokens that a workgroup of the second pass takes 128."""
+    rng = np.random.default_rng(D)
+    lens = [int(x) for x in rng.integers(35, 300, 40)]
+    lens[3], lens[20] = 900, 129
+    c = Case(lam, D, 64, 2, 2, dt, [35] * 40, lens, seed=D)
+    _all(c)
+    _all(c, causal=False, mask=rng.random((40, 2, 900)) > 0.3)
+
+
 def test_weights_by_both_ways_agree(lam):
     """One row at a time (kept scores) and all rows at once (a second pass) add up to the same."""
     c = Case(lam, 128, 64, 2, 4, "bf16", [48], [1500], seed=6)
