@@ -396,6 +396,12 @@ def _kv_view(dev, pages, table, lengths, starts, rows, head_dim, dtype):
     return v, n, heads, (table, lengths, starts)
 
 
+def _kv_elsewhere(ctx):
+    """Whether a context's stream is not the current one: copies and outputs of its
+    calls are then made on its own."""
+    return ctx.stream.cuda_stream != torch._C._cuda_getCurrentRawStream(ctx.device)
+
+
 def _kv_rows(t, heads, name, dev):
     """(rows, heads, head_dim) in float16 or bfloat16, channels contiguous."""
     if not isinstance(t, torch.Tensor) or t.dtype not in _KV_DTYPES:
@@ -434,7 +440,11 @@ def kv_append(k: torch.Tensor, v: torch.Tensor, pages: torch.Tensor, table: torc
     starts gives each sequence's rows, None: equally many each.  weights of the
     new tokens become 0, positions first[s], first[s] + 1, ...; status: int32
     tensor of 3, counts of non-finite, out-of-range and misplaced input."""
-    ctx = ctx or default_context()
+    if ctx is None:
+        ctx = default_context()
+    elif _kv_elsewhere(ctx):
+        with torch.cuda.stream(ctx.stream):
+            return kv_append(k, v, pages, table, lengths, starts, weights, positions, first, status, ctx)
     dev = ctx.device
     k = _kv_rows(k, None, "k", dev)
     v = _kv_rows(v, k.shape[1], "v", dev)
@@ -464,7 +474,11 @@ def kv_read(pages: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, row
             dtype: torch.dtype = torch.bfloat16, starts: torch.Tensor | None = None, ctx: Context | None = None):
     """The values the cache holds for the last tokens of the sequences, addressed
     as by kv_append: (k, v), each (rows, kv_heads, head_dim) (lam_kv_read)."""
-    ctx = ctx or default_context()
+    if ctx is None:
+        ctx = default_context()
+    elif _kv_elsewhere(ctx):
+        with torch.cuda.stream(ctx.stream):
+            return kv_read(pages, table, lengths, rows, head_dim, dtype, starts, ctx)
     if dtype not in _KV_DTYPES:
         raise TypeError("dtype must be float16 or bfloat16")
     view, _, heads, hold = _kv_view(ctx.device, pages, table, lengths, starts, int(rows), int(head_dim), dtype)
@@ -485,7 +499,11 @@ def kv_attend(q: torch.Tensor, pages: torch.Tensor, table: torch.Tensor, lengths
     tokens out; weights (float32: sequences, kv_heads, slots) is added to what
     each token received; lse (float32: rows, q_heads) receives the scores' log
     sums.  max_length, where the caller knows a bound of lengths, sizes the launch."""
-    ctx = ctx or default_context()
+    if ctx is None:
+        ctx = default_context()
+    elif _kv_elsewhere(ctx):
+        with torch.cuda.stream(ctx.stream):
+            return kv_attend(q, pages, table, lengths, starts, causal, scale, mask, weights, max_length, out, lse, ctx)
     dev = ctx.device
     q = _kv_rows(q, None, "q", dev)
     rows, q_heads, head_dim = q.shape
@@ -521,7 +539,11 @@ def kv_evict(pages: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, sc
     budget), the new slots' scores and positions, and the new lengths.  out:
     (scores, positions or None, lengths) to write to, which may be the inputs
     (only their first budget slots are written)."""
-    ctx = ctx or default_context()
+    if ctx is None:
+        ctx = default_context()
+    elif _kv_elsewhere(ctx):
+        with torch.cuda.stream(ctx.stream):
+            return kv_evict(pages, table, lengths, scores, budget, head_dim, recent, sinks, positions, out, ctx)
     dev = ctx.device
     view, n, heads, hold = _kv_view(dev, pages, table, lengths, None, 0, int(head_dim), torch.float16)
     s, hold_s = _kv_slots(scores, torch.float32, n, heads, "scores", dev, copy=True)

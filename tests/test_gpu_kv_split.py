@@ -6,6 +6,7 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import kv
 from test_gpu_kv_attend import Case, _i32
 from test_gpu_kv_cache import _evict_case, _scores
 
@@ -134,6 +135,34 @@ def test_weights_by_both_ways_agree(lam):
         assert torch.allclose(got[0].float(), out[i].float(), rtol=2.0 ** -7, atol=2.0 ** -9)
     # sums of 48 * 4 weights: each to 2^-20 of itself, and the additions' rounding
     assert ((one - w).abs() <= 2.0 ** -18 * (1 + w)).all()
+
+
+def test_a_context_of_another_stream(lam):
+    """Copies that a call makes of its arguments, and its outputs, are its context's stream's."""
+    side = torch.cuda.Stream()
+    ctx = lam.Context(stream=side)
+    c = Case(lam, 64, 32, 2, 2, "f16", [1, 1], [300, 90], seed=8)
+    wide = torch.zeros((2, 2 * c.table.shape[1]), dtype=torch.int32, device="cuda")
+    wide[:, ::2] = c.table
+    table, lengths = wide[:, ::2], torch.stack([c.lengths, c.lengths], 1)[:, 0]
+    q = torch.stack([c.q, c.q], -1)[..., 0]                  # strided: copied
+    k, v = torch.randn((2, 2, 2, 64), device="cuda").half()
+    w = torch.zeros((2, 2, 600), device="cuda")[..., :300]
+    scores = torch.rand((2, 300, 2), device="cuda").transpose(1, 2)
+    want_out = c.call()
+    busy = torch.randn((4096, 4096), device="cuda")
+    torch.cuda.synchronize()
+    for _ in range(20):                                      # the current stream has work before it
+        busy = busy @ busy * 1e-3
+    out = lam.kv_attend(q, c.pool, table, lengths, weights=w, ctx=ctx)
+    kept, so, po, lo = lam.kv_evict(c.pool, table, lengths, scores, 100, 64, ctx=ctx)
+    lam.kv_append(k, v, c.pool, table, lengths, ctx=ctx)
+    got = lam.kv_read(c.pool, table, lengths, 2, 64, torch.float16, ctx=ctx)
+    side.synchronize()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want_out) and lo.tolist() == [100, 90]
+    assert np.array_equal(got[0].double().cpu().numpy(), kv.rounded(k.double().cpu().numpy()))
+    assert np.array_equal(got[1].double().cpu().numpy(), kv.rounded(v.double().cpu().numpy()))
 
 
 def test_starts_that_do_not_rise(lam):
