@@ -40,6 +40,7 @@ class BoundedContext:
         self.weights = torch.zeros((n_seqs, kv_heads, slots), device=device)
         self.positions = torch.full((n_seqs, kv_heads, slots), -1, dtype=torch.int32, device=device)
         self.lengths = torch.zeros(n_seqs, dtype=torch.int32, device=device)   # cached tokens
+        self.lengths_next = torch.zeros_like(self.lengths)   # their own memory: a step's eviction is then one launch
         self.seen = torch.zeros(n_seqs, dtype=torch.int32, device=device)      # tokens so far: the next position
         self.status = torch.zeros(3, dtype=torch.int32, device=device)
 
@@ -56,7 +57,8 @@ class BoundedContext:
         out = lam.kv_attend(q, self.pages, self.table, self.lengths, weights=self.weights)
         lam.kv_evict(self.pages, self.table, self.lengths, self.weights, self.budget, self.head_dim,
                      recent=self.recent, sinks=self.sinks, positions=self.positions,
-                     out=(self.weights, self.positions, self.lengths))
+                     out=(self.weights, self.positions, self.lengths_next))
+        self.lengths, self.lengths_next = self.lengths_next, self.lengths
         return out
 
     def check(self) -> None:

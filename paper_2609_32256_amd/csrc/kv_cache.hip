@@ -281,6 +281,7 @@ struct EvictArgs {
   lam_kv_slots scores, positions, scores_out, positions_out;
   int32_t budget, recent, sinks, bound;   // bound: most tokens of a sequence
   int32_t moves;                          // most moves of a sequence's head
+  int32_t head_dim;                       // where the selection makes the moves itself, else 0
   int32_t* kept;
   int32_t* lengths_out;
   int32_t* lists;   // of a long cache's holes and extra slots: [seq][head][2][moves]
@@ -327,6 +328,37 @@ struct EvictHead {
   }
 };
 
+// A wave moves one token: its codes by two bytes (a run has D/32 of them), its scales
+// by one.
+__device__ __forceinline__ void move_token(const KvArgs& a, int bh, int D, int from, int to) {
+  const int s = bh / a.heads, h = bh % a.heads, T = 1 << a.page_shift, lane = threadIdx.x & 63;
+  const int64_t pf = a.page(s, from >> a.page_shift), pt = a.page(s, to >> a.page_shift);
+  if (pf < 0 || pt < 0) return;
+  const int64_t head_bytes = (int64_t)T * (D + D / 16);
+  const uint8_t* f = a.head_page(pf, h, head_bytes);
+  uint8_t* d = a.head_page(pt, h, head_bytes);
+  from &= T - 1;
+  to &= T - 1;
+  const int run = D / 32, blocks = D / kKvBlock;
+  auto code_at = [&](int t, int i) {   // of the token's i-th byte of codes, the keys' D/2 first
+    if (i < D / 2) return t * (D / 2) + i;
+    i -= D / 2;
+    return T * (D / 2) + (((t >> 2) * 16 + i / run) * 4 + (t & 3)) * run + i % run;
+  };
+  auto scale_at = [&](int t, int i) {
+    return T * D + (i < blocks ? t * blocks + i : T * blocks + ((t >> 2) * blocks + i - blocks) * 4 + (t & 3));
+  };
+  for (int i = 2 * lane; i < D; i += 128)
+    *reinterpret_cast<uint16_t*>(d + code_at(to, i)) = *reinterpret_cast<const uint16_t*>(f + code_at(from, i));
+  if (lane < 2 * blocks) d[scale_at(to, lane)] = f[scale_at(from, lane)];
+}
+
+// Most moves of a head that its selection makes itself, which saves the launch that
+// would: 24 sequences of 4,097 tokens and 8 heads of 128 channels cut to 4,096 take 18 us
+// for 26, of 4,160 tokens 22 for 30.  (Not where the new lengths replace those that the
+// other heads' selections still read.)
+constexpr int kOwnMoves = 64;
+
 // Order of the scores as unsigned integers: protected slots above all, NaN below all.
 __device__ __forceinline__ uint32_t evict_key(float s, int pos, int newest, int recent, int sinks) {
   if (pos < sinks || (int64_t)pos > (int64_t)newest - recent) return 0xffffffffu;
@@ -352,10 +384,14 @@ __global__ __launch_bounds__(kSelThreads) void k_kv_select(KvArgs a, EvictArgs e
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const EvictHead d(a, e, blockIdx.x);
+  if (e.head_dim && blockIdx.x % a.heads == 0 && tid == 0)
+    e.lengths_out[blockIdx.x / a.heads] = min(d.len, e.budget);
   if (d.len <= e.budget) {
     d.keep_all(e.budget);
     return;
   }
+  __shared__ int32_t move_to[kOwnMoves], move_from[kOwnMoves];
+  if (tid < kOwnMoves) move_to[tid] = -1;
   constexpr int kCounts = KPT * kSelWaves;   // of 64 slots each, in the order of the slots
   __shared__ uint32_t hist[kBins], found[3];
   __shared__ uint32_t hole_at[kCounts], extra_at[kCounts], sums[2][kSelWaves];
@@ -487,6 +523,10 @@ __global__ __launch_bounds__(kSelThreads) void k_kv_select(KvArgs a, EvictArgs e
       const bool hole = t < e.budget && key[k] < least;
       const uint32_t rank = hole_at[k * kSelWaves + wave] + (uint32_t)__popcll(__ballot(hole) & low);
       from[j] = hole ? e.budget + (int)extras[rank] : min(t, e.budget - 1);
+      if (hole && e.head_dim) {   // (at most e.moves of them)
+        move_to[rank] = t;
+        move_from[rank] = from[j];
+      }
     }
 #pragma unroll
     for (int j = 0; j < kBatch; ++j) s[j] = d.sc[(uint32_t)from[j]];
@@ -503,6 +543,13 @@ __global__ __launch_bounds__(kSelThreads) void k_kv_select(KvArgs a, EvictArgs e
         if (d.po) d.po[t] = p[j];
       }
     }
+  }
+  if (!e.head_dim) return;
+  __syncthreads();
+  for (int i = wave; i < e.moves; i += kSelWaves) {
+    const int to = __builtin_amdgcn_readfirstlane(move_to[i]);
+    if (to < 0) break;   // (the i-th hole is there if the one after it is)
+    move_token(a, blockIdx.x, e.head_dim, __builtin_amdgcn_readfirstlane(move_from[i]), to);
   }
 }
 
@@ -741,6 +788,7 @@ lam_status launch_kv_evict(lam_ctx* ctx, const lam_kv_view& v, const lam_kv_slot
   e.moves = std::max(0, std::min(budget, e.bound - budget));
   e.kept = kept;
   e.lengths_out = lengths_out;
+  if (e.moves <= kOwnMoves && e.bound <= 64 * kSelThreads && lengths_out != v.lengths_dev) e.head_dim = v.head_dim;
   hipEvent_t e0, e1;
   LAM_TRY(prof_launch_events(ctx, "kv_select", &e0, &e1));
 #define LAM_GO(KPT) launch(k_kv_select<KPT>, dim3((unsigned)pairs), kSelThreads, ctx->stream, e0, e1, a, e)
@@ -756,6 +804,7 @@ lam_status launch_kv_evict(lam_ctx* ctx, const lam_kv_view& v, const lam_kv_slot
     launch(k_kv_select_long, dim3((unsigned)pairs), kSelThreads, ctx->stream, e0, e1, a, e);
   }
   LAM_HIP(hipGetLastError());
+  if (e.head_dim) return LAM_OK;
   LAM_TRY(prof_launch_events(ctx, "kv_move", &e0, &e1));
   const int per = kKvThreads / (v.head_dim / 8) * 4;   // slots a workgroup
   const dim3 grid((unsigned)((std::min(budget, std::max(e.bound, 1)) + per - 1) / per), (unsigned)pairs);

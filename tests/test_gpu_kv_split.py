@@ -181,3 +181,31 @@ def test_starts_that_do_not_rise(lam):
 def test_evict_where_kernels_change(lam, L, kind):
     budget = L - 3 if kind == "equal" else L // 3
     _evict_case(lam, 64, 1024, 1, [L, max(0, L - 1500)], budget, 10, 2, _scores(L, 2, 1, L, kind), None, False, seed=L)
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("D,T", [(64, 32), (128, 64), (256, 256)])
+@pytest.mark.parametrize("lens,budget", [
+    ([1060, 1001, 1000, 3, 1037], 1000),
+    ([1064, 1064], 1000),                                    # as many moves as a selection makes itself
+    ([1065, 999], 1000),                                     # and one more
+    ([70], 6), ([71], 6), ([64, 0, 1], 1), ([3000, 2999], 2990),
+])
+def test_evict_few(lam, lens, budget, D, T, in_place):
+    """A cache a little over its budget, as after every decode step."""
+    heads, L = 3, max(lens)
+    g = torch.Generator(device="cuda").manual_seed(L + D)
+    pos = torch.argsort(torch.rand((len(lens), heads, L), generator=g, device="cuda"), dim=-1).to(torch.int32)
+    kind = "ties" if D == 128 else "random"
+    _evict_case(lam, D, T, heads, lens, budget, budget // 10, min(2, budget - budget // 10),
+                _scores(L, len(lens), heads, L, kind), pos, in_place, seed=L)
+
+
+def test_evict_few_and_bad_pages(lam):
+    pool = torch.randint(0, 256, (2, 1, kv.page_bytes(64, 32)), device="cuda", dtype=torch.int32).to(torch.uint8)
+    before = pool.clone()
+    w = torch.arange(64.0, device="cuda").view(1, 1, 64)
+    kept, _, _, lo = lam.kv_evict(pool, _i32([[0, 99]]), _i32([64]), w, 63, 64)
+    assert lo.tolist() == [63] and kept[0, 0].tolist() == [63] + list(range(1, 63)) and torch.equal(pool, before)
+    lam.kv_evict(pool, _i32([[-1, 1]]), _i32([64]), w, 63, 64)
+    assert torch.equal(pool, before)
