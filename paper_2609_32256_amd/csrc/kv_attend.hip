@@ -18,6 +18,14 @@
 //
 // Conversions are one instruction per two values with the scale applied; values
 // of two tokens are then paired by one move each.
+//
+// Bound by reading the cache once: 8 sequences of 131,072 tokens, 32 query heads over 8
+// key/value heads of 128 channels, bfloat16, take 172 us, 6.6 TB/s; 37 sequences of 3,000
+// to 6,000 and 28 over 4 heads 20 to 22 us, 4.3 TB/s, of which 5 are the start and the plan.
+// Sixteen rows fill the products' columns where four or seven are there: the matrix
+// units have the time.  Lengths are split where the tiles are fewer than the workgroups
+// that run at once, and joined by a second launch (5 us; a join by the last workgroup of each
+// unit took 2 to 30 us more, since its parts have to leave the caches of the XCDs).
 #include <algorithm>
 #include <cmath>
 
@@ -318,6 +326,8 @@ __device__ __forceinline__ void add_kept(const AttendArgs& a, uint32_t block) {
 }
 
 // What follows the attention, in one launch: the parts joined, the kept scores made weights.
+// Bound by latency (two dependent loads for the plan, two for a row): 5 to 7 us for parts
+// alone; with the scores of 16 sequences of 8,192 to 16,383 tokens and 32 heads 17 us.
 template <int D, bool BF16, int R>
 __global__ __launch_bounds__(kAttThreads) void k_kv_finish(AttendArgs a, uint32_t join_blocks) {
   const uint32_t b = blockIdx.x;
