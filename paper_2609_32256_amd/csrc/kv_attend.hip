@@ -390,7 +390,7 @@ void k_kv_weights(AttendArgs a) {
 
   // with a causal limit the first row that sees token t0 is row t0 - (end_full - n)
   const int hidden = w.end_full - w.n;
-  const int first = a.causal ? (int)min((int64_t)max(0, t0 - hidden) * a.group, (int64_t)w.pairs) / 16 * 16 : 0;
+  const int first = a.causal ? (int)min(max((int64_t)0, (int64_t)t0 - hidden) * a.group, (int64_t)w.pairs) / 16 * 16 : 0;
   int r0 = first + 16 * wave;
   // The lane's pair of the next tile: row i of the sequence, head j of the group, and
   // where its query and its log sum lie; the last pair's stand in past the end.
@@ -535,8 +535,8 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
   // a head, 60 and 161 for 16.)
   const int64_t pairs = v.rows * q_heads;
   const int64_t parts = a.split_to ? blocks * rows : 0;
-  const bool keep = weights.p_dev && !chunk && pairs * a.cut * 4 <= kKeptBytes;
   a.kept_cols = (a.cut + kKeptTokens - 1) / kKeptTokens * kKeptTokens;
+  const bool keep = weights.p_dev && !chunk && pairs * a.kept_cols * 4 <= kKeptBytes;
   DevBuf& buf = ctx->scratch[kScratchKv];
   const int64_t floats = (keep ? pairs * a.kept_cols : 0) + parts * (v.head_dim + 2) + (weights.p_dev ? pairs : 0);
   LAM_TRY(buf.ensure((size_t)floats * 4));
