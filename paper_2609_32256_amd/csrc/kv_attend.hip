@@ -34,7 +34,7 @@
 namespace lam {
 namespace {
 
-// A strip of a page outside the pool: no scores.
+// A strip of a page outside the pool, or all masked: no scores.
 __device__ __forceinline__ void keep_nothing(float* scores) {
   const int g = (threadIdx.x & 63) >> 4;
   const float no = -__builtin_inff();
@@ -56,7 +56,7 @@ struct Running {
 
   // One strip at t0; whole: every query sees all of its tokens.  scores: where
   // the query's scores are kept (null: nowhere), slot by slot.
-  __device__ __forceinline__ void add(const AttendArgs& a, int len, int t0, bool whole, int end, uint32_t mask_byte,
+  __device__ __forceinline__ void add(const AttendArgs& a, int len, int t0, bool whole, int end, uint32_t bits,
                                       float* scores, uint32_t shift, const uint4 q[D / 32], const Codes<D>& k,
                                       Codes<D>& v) {
     kv_f4 x[2];
@@ -69,7 +69,7 @@ struct Running {
       for (int j = 0; j < D / 32; ++j) x[kt] = mfma<BF16>(y[j], q[j], x[kt]);
     }
     less_reference(x, a.scale2, row);
-    if (!whole) hide(x, seen_bits(MASK, mask_byte, t0, end));
+    if (!whole) hide(x, seen_bits(bits, t0, end));
     if (scores) {
       const int g = (threadIdx.x & 63) >> 4;
       *reinterpret_cast<kv_f4*>(scores + t0 + 4 * g) = x[0] + row.m;
@@ -103,7 +103,7 @@ __global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : 3) void k_kv_attend(Att
   const int end_first = pair_end(a, w, w.r0), end_last = pair_end(a, w, min(w.r0 + kAttRows, w.pairs) - 1);
   const int64_t part_at = (int64_t)w.part * w.tokens;
   const int from = (int)min(part_at, (int64_t)w.len), to = (int)min(part_at + w.tokens, (int64_t)end_last);
-  const int whole_to = MASK ? -1 : end_first - kKvStrip;   // strips up to here are seen whole
+  const int whole_to = end_first - kKvStrip;   // strips up to here are seen whole
 
   // Strips at t0, t0 + 128, ...: kAhead strips' codes are on their way while one
   // is taken in, and the page of the next to load is read from the table before.
@@ -148,7 +148,9 @@ __global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : 3) void k_kv_attend(Att
       const int32_t page = next;
       next = entry(t0 + (kAhead + 1) * kStep);
       load((i + kAhead) % kBufs, page, t0 + kAhead * kStep);
-      if (ok[i]) r.add(a, w.len, t0, t0 <= whole_to, end, mb[i], scores, at.shift, q, k[i], v[i]);
+      const uint32_t bits = mask_bits<MASK>(mb[i]);
+      if (ok[i] && bits != 0)
+        r.add(a, w.len, t0, t0 <= whole_to && bits == kAllTokens, end, bits, scores, at.shift, q, k[i], v[i]);
       else if (scores) keep_nothing(scores + t0);
       t0 += kStep;
     }
@@ -370,7 +372,7 @@ void k_kv_weights(AttendArgs a) {
   const int T = 1 << a.c.page_shift;
   const LaneAt<D> at(T);
   uint4 y[2 * kStrips][kSteps];
-  uint32_t mb[kStrips] = {};
+  uint32_t bits[kStrips], any = 0, all = kAllTokens;
   bool ok[kStrips];   // the strip's page is there
 #pragma unroll
   for (int n = 0; n < kStrips; ++n) {
@@ -379,13 +381,16 @@ void k_kv_weights(AttendArgs a) {
     ok[n] = page >= 0;
     Codes<D> k;
     load_keys<D>(strip_rsrc<D>(a.c.head_page(ok[n] ? page : 0, h, KvLayout<D>::head_bytes(T)), T, t & (T - 1), ok[n]), at, k);
-    if (a.mask.p_dev) mb[n] = load_mask(mask_rsrc(a, w.s, h), t);
+    bits[n] = a.mask.p_dev ? mask_bits<true>(load_mask(mask_rsrc(a, w.s, h), t)) : kAllTokens;
+    any |= ok[n] ? bits[n] : 0u;
+    all &= bits[n];
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
       key_operand<D, BF16>(k, at.shift, kt, y[2 * n + kt]);
       if (a.flip) flip_signs<kSteps>(y[2 * n + kt]);
     }
   }
+  if (any == 0) return;   // no token gets anything
   float sum[kStrips][8] = {};
 
   // with a causal limit the first row that sees token t0 is row t0 - (end_full - n)
@@ -424,7 +429,7 @@ void k_kv_weights(AttendArgs a) {
     lp += turn ? l_turn : 0;
   };
   auto add = [&](int b, int r) {
-    const bool whole = !a.mask.p_dev && t0 + kTokens <= (a.causal ? min(w.len, hidden + r / a.group + 1) : w.len);
+    const bool whole = all == kAllTokens && t0 + kTokens <= (a.causal ? min(w.len, hidden + r / a.group + 1) : w.len);
     const bool out = r + c >= w.pairs || e[b] == -__builtin_inff();
     const float less = out ? __builtin_inff() : e[b];   // no row, or one that sees no token: 2^(-inf) each
 #pragma unroll
@@ -440,7 +445,7 @@ void k_kv_weights(AttendArgs a) {
       for (int v = 0; v < 8; ++v) x[v >> 2][v & 3] = __builtin_fmaf(x[v >> 2][v & 3], a.scale2, -less);
       if (!whole) {
         const int end = a.causal ? min(w.len, hidden + row[b] + 1) : w.len;
-        hide(x, seen_bits(a.mask.p_dev, mb[n], t0 + n * kKvStrip, end));
+        hide(x, seen_bits(bits[n], t0 + n * kKvStrip, end));
       }
 #pragma unroll
       for (int v = 0; v < 8; ++v) sum[n][v] += __builtin_amdgcn_exp2f(x[v >> 2][v & 3]);

@@ -17,7 +17,7 @@ namespace lam {
 namespace {
 
 template <int D, bool BF16, bool MASK, int kRows>
-__global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) void k_kv_chunk(AttendArgs a) {
+__global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : D == 64 ? 3 : 2) void k_kv_chunk(AttendArgs a) {
   constexpr int kRun = D / 16, kTiles = kRows / 16, kSteps = D / 32;
   const int lane = threadIdx.x & 63, c = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -40,7 +40,7 @@ __global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) void k_kv_chunk(Atte
   const int end_first = pair_end(a, w, w.r0), end_last = pair_end(a, w, min(w.r0 + kRows, w.pairs) - 1);
   const int64_t part_at = (int64_t)w.part * w.tokens;
   const int from = (int)min(part_at, (int64_t)w.len), to = (int)min(part_at + w.tokens, (int64_t)end_last);
-  const int whole_to = MASK ? -1 : end_first - kKvStrip;
+  const int whole_to = end_first - kKvStrip;
 
   kv_f4 o[kTiles][kRun];
   Row row[kTiles];
@@ -87,7 +87,8 @@ __global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) void k_kv_chunk(Atte
     const bool ok_next = t1 < to && ok_page;
     const StripRsrc rs = strip_rsrc<D>(head, T, t1 & (T - 1), ok_next);
     load_keys<D>(rs, at, k);
-    if (ok) {
+    const uint32_t bits = mask_bits<MASK>(mb);
+    if (ok && bits != 0) {
       // scores of 32 tokens for every tile of queries, less the row's reference
       kv_f4 x[kTiles][2];
       uint4 q = sq[0][0][lane];
@@ -108,10 +109,10 @@ __global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) void k_kv_chunk(Atte
       value_scales<D>(v, t0, w.len, s);
 #pragma unroll
       for (int t = 0; t < kTiles; ++t) less_reference(x[t], a.scale2, row[t]);
-      if (t0 > whole_to) {
+      if (t0 > whole_to || bits != kAllTokens) {
 #pragma unroll
         for (int t = 0; t < kTiles; ++t)
-          hide(x[t], seen_bits(MASK, mb, t0, pair_end(a, w, min(w.r0 + 16 * t + c, w.pairs - 1))));
+          hide(x[t], seen_bits(bits, t0, pair_end(a, w, min(w.r0 + 16 * t + c, w.pairs - 1))));
       }
       bool up = false;
       float top[kTiles];

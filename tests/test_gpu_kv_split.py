@@ -63,6 +63,24 @@ def test_parts_and_masks(lam, n, G):
     _all(c, mask=m)
 
 
+@pytest.mark.parametrize("D,n,G", [(64, 1, 4), (128, 3, 8), (128, 40, 2), (256, 30, 4)])
+def test_masks_of_whole_strips(lam, D, n, G):
+    """Strips that a mask leaves whole or takes out, beside some that it cuts."""
+    lens = [700, 333, 2500]
+    c = Case(lam, D, 64, 2, G, "f16", [n] * 3, lens, seed=n)
+    m = (np.random.default_rng(n).random((3, 2, 40)) > 0.4).repeat(64, axis=2)[..., : max(lens)]
+    m[:, :, 300:310] ^= True
+    m[1, 1] = True
+    m[2, 0, 1024:] = False
+    _all(c, mask=m)
+    _all(c, causal=False, mask=m)
+    c.table[0, 2] = -1                                       # and a page that is not there
+    m[0, :, 128:192] = True
+    left = m.copy()
+    left[0, :, 128:192] = False
+    c.check(c.call(mask=torch.from_numpy(m).cuda()), mask=[left[b][:, : lens[b]] for b in range(3)])
+
+
 @pytest.mark.parametrize("longest", [60, 2700])
 @pytest.mark.parametrize("B,rows", [
     (64, lambda s: 1), (65, lambda s: 1), (200, lambda s: 1),
