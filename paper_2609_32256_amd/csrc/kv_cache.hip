@@ -675,8 +675,8 @@ __global__ __launch_bounds__(kSelThreads) void k_kv_select_long(KvArgs a, EvictA
 // which value codes lie.  Sources lie at or beyond budget and destinations below it,
 // so no move reads what another wrote.  Bound by memory, at more than the codes'
 // bytes: a token's value codes are a quarter of every 16 bytes of 2 D bytes, and
-// what is kept of a long tail lies apart.  192 heads' 6,144 moves of 128 channels take 131 to
-// 145 us (the bytes alone 62 at a copy's rate); the same with every source token
+// what is kept of a long tail lies apart.  192 heads' 6,144 moves of 128 channels take 127 to
+// 145 us (the bytes alone 62 at a copy's rate, with the lines' other tokens 102); the same with every source token
 // next to the last 82 to 90 us for 8,192.  (Tokens that stay reading their own place,
 // so that no load hangs on a branch, were 7 % slower, two units a lane group 9 %.)
 template <int D>
