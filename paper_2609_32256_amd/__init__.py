@@ -354,14 +354,15 @@ def kv_pages(n_pages: int, kv_heads: int, head_dim: int, page_size: int = 64, de
 
 def _kv_tensor(t, dtype, dims, name, dev):
     """Checks of a tensor argument (dev: the device's index)."""
+    if isinstance(t, torch.Tensor) and t.get_device() == dev and t.dtype is dtype and t.dim() == dims:
+        return
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA (HIP) tensor")
     if t.get_device() != dev:
         raise ValueError(f"{name} is on {t.device}, the context on cuda:{dev}")
     if t.dtype is not dtype:
         raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
-    if t.dim() != dims:
-        raise ValueError(f"{name} must have {dims} dimensions")
+    raise ValueError(f"{name} must have {dims} dimensions")
 
 
 def _kv_view(dev, pages, table, lengths, starts, rows, head_dim, dtype):
@@ -381,12 +382,12 @@ def _kv_view(dev, pages, table, lengths, starts, rows, head_dim, dtype):
         table = table.contiguous()
         stride = table.stride(0)
     lengths = lengths.contiguous()
-    if len(lengths) != n:
+    if lengths.numel() != n:
         raise ValueError("table and lengths must have a row for each sequence")
     if starts is not None:
         _kv_tensor(starts, torch.int32, 1, "starts", dev)
         starts = starts.contiguous()
-        if len(starts) != n + 1:
+        if starts.numel() != n + 1:
             raise ValueError("starts must have an entry for each sequence and one more")
     elif rows and (n == 0 or rows % n):
         raise ValueError("without starts every sequence has the same number of rows")
@@ -459,7 +460,7 @@ def kv_append(k: torch.Tensor, v: torch.Tensor, pages: torch.Tensor, table: torc
     if first is not None:
         _kv_tensor(first, torch.int32, 1, "first", dev)
         first = first.contiguous()
-        if len(first) != n:
+        if first.numel() != n:
             raise ValueError("first must have an entry for each sequence")
     if status is not None:
         _kv_tensor(status, torch.int32, 1, "status", dev)
@@ -482,7 +483,7 @@ def kv_read(pages: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, row
     if dtype not in _KV_DTYPES:
         raise TypeError("dtype must be float16 or bfloat16")
     view, _, heads, hold = _kv_view(ctx.device, pages, table, lengths, starts, int(rows), int(head_dim), dtype)
-    k = torch.empty((int(rows), heads, int(head_dim)), dtype=dtype, device=pages.device)
+    k = pages.new_empty((int(rows), heads, int(head_dim)), dtype=dtype)
     v = torch.empty_like(k)
     _check(_lib.lam_kv_read(ctx.handle, view, k.data_ptr(), v.data_ptr()))
     return k, v
@@ -513,7 +514,7 @@ def kv_attend(q: torch.Tensor, pages: torch.Tensor, table: torch.Tensor, lengths
     m, hold_mask = _kv_slots(mask, torch.uint8, n, heads, "mask", dev, shared=True, copy=True)
     w, _ = _kv_slots(weights, torch.float32, n, heads, "weights", dev)
     if out is None:
-        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        out = torch.empty_like(q) if q.is_contiguous() else torch.empty_like(q, memory_format=torch.contiguous_format)
     else:
         _kv_tensor(out, q.dtype, 3, "out", dev)
         if out.shape != q.shape or not out.is_contiguous():
@@ -550,7 +551,7 @@ def kv_evict(pages: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, sc
     p, hold_p = _kv_slots(positions, torch.int32, n, heads, "positions", dev, copy=True)
     if s is None:
         raise TypeError("scores must be a CUDA (HIP) tensor")
-    kept = torch.empty((n, heads, int(budget)), dtype=torch.int32, device=pages.device)
+    kept = lengths.new_empty((n, heads, int(budget)))
     if out is None:
         out = (torch.empty_like(kept, dtype=torch.float32), torch.empty_like(kept), torch.empty_like(hold[1]))
         so, po = (_KV_SLOTS.pack(t.data_ptr(), heads * int(budget), int(budget), int(budget)) for t in out[:2])
@@ -558,7 +559,7 @@ def kv_evict(pages: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, sc
         so, _ = _kv_slots(out[0], torch.float32, n, heads, "out scores", dev)
         po, _ = _kv_slots(out[1], torch.int32, n, heads, "out positions", dev)
         _kv_tensor(out[2], torch.int32, 1, "out lengths", dev)
-        if len(out[2]) != n or not out[2].is_contiguous():
+        if out[2].numel() != n or not out[2].is_contiguous():
             raise ValueError("out lengths must be contiguous, an entry for each sequence")
     _check(_lib.lam_kv_evict(ctx.handle, view, s, p, int(budget), int(recent), int(sinks), kept.data_ptr(), so, po,
                              out[2].data_ptr()))
