@@ -250,7 +250,8 @@ _default_ctx: dict = {}
 
 
 def default_context() -> Context:
-    dev = torch.cuda.current_device()
+    # (current_device() without its test that the GPU is initialised, which the first context did)
+    dev = torch._C._cuda_getDevice() if _default_ctx else torch.cuda.current_device()
     key = (dev, torch._C._cuda_getCurrentRawStream(dev))   # the handle of current_stream(dev), without the object
     c = _default_ctx.get(key)
     if c is None:
