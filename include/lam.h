@@ -485,7 +485,7 @@ lam_status lam_kv_read(lam_ctx* ctx, const lam_kv_view* view, void* k_dev, void*
  * query heads of h is added to element (s, h, t); tokens past its columns are
  * left out.  max_length: an upper bound of lengths that the launch is sized by
  * (longer sequences are cut to it); <= 0 for the table's.  Context scratch: where
- * lengths are split, partial results of at most 35 MB; with weights 4 bytes for each
+ * lengths are split, partial results of at most 45 MB; with weights 4 bytes for each
  * query row and head, and for up to 64 rows times heads of a group per sequence 4
  * bytes for each of them and each token of the bound, at most 1 GiB.  Asynchronous. */
 lam_status lam_kv_attend(lam_ctx* ctx, const lam_kv_view* view, const void* q_dev, int64_t q_row_stride,

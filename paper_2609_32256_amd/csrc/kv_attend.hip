@@ -358,8 +358,12 @@ void k_kv_weights(AttendArgs a) {
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t chunks = (uint32_t)((a.cut + kTokens - 1) / kTokens);
-  const int t0 = (int)(blockIdx.x % chunks) * kTokens;
-  const uint32_t id = blockIdx.x / chunks;
+  // Workgroups of a head, which read the same queries, go to one XCD (they are dealt out
+  // in turn to eight) and find them in its L2: 1 to 15 % less.
+  const uint32_t each = gridDim.x / 8;
+  const uint32_t block = blockIdx.x < 8 * each ? blockIdx.x % 8 * each + blockIdx.x / 8 : blockIdx.x;
+  const int t0 = (int)(block % chunks) * kTokens;
+  const uint32_t id = block / chunks;
   const int h = (int)(id % (uint32_t)a.c.heads);
   Work w;
   w.s = (int)(id / (uint32_t)a.c.heads);
@@ -524,12 +528,16 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
     rows = 6 * wider <= 5 * wide ? kChunkRowsWider : kChunkRowsWide;
   }
   if (!v.starts_dev) a.tiles_per_seq = (int)((v.rows / v.n_seqs * a.group + rows - 1) / rows);
-  // Lengths are split where the tiles do not fill the chip.
+  // Lengths are split where the tiles do not fill the chip; of 256 channels, whose
+  // workgroups have a compute unit each, over two rounds where the tiles fill a little more
+  // than one (1.06 to 1.31 times: 10 to 19 % less, 36 sequences of 30,000 tokens 598 us to
+  // 487; 1.4 times: 2 % more; of 128 channels 1.04 times: 3 % less to 14 % more).
   const int64_t units = units_of(rows);
+  const int split_to = v.head_dim == 256 && units >= fill && 8 * units < 11 * fill ? 2 * fill : fill;
   int64_t blocks = units;
-  if (units < fill && a.cut > (chunk ? kWholeChunk : kWholeDecode)) {
-    a.split_to = fill;
-    blocks = fill + units;   // see plan(): at most split_to - units / 2 (or split_to / 2) full parts, and one more a tile
+  if (units < split_to && a.cut > (chunk ? kWholeChunk : kWholeDecode)) {
+    a.split_to = split_to;
+    blocks = split_to + units;   // see plan(): at most split_to - units / 2 (or split_to / 2) full parts, and one more a tile
   }
   LAM_CHECK(blocks < (1LL << 31), LAM_EINVAL, "too many rows for one launch");
   a.blocks = blocks;

@@ -110,6 +110,15 @@ def test_chunks_of_wide_heads(lam, B, longest):
         _all(Case(lam, 256, 32, 1, 4, "bf16", [24 + s % 2 for s in range(B)], lens, seed=B))
 
 
+def test_wide_heads_over_two_rounds(lam):
+    """A few more tiles of 256 channels than run at once: lengths are split all the same."""
+    rng = np.random.default_rng(3)
+    lens = [int(x) for x in rng.integers(0, 60, 300)]
+    lens[5], lens[299] = 2500, 2100
+    c = Case(lam, 256, 32, 1, 2, "bf16", [1] * 300, lens, seed=3)
+    _all(c)
+
+
 def test_sequences_beyond_one_step_of_the_chip(lam):
     """More tiles than run at once: nothing is split."""
     rng = np.random.default_rng(1)
