@@ -358,12 +358,15 @@ void k_kv_weights(AttendArgs a) {
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t chunks = (uint32_t)((a.cut + kTokens - 1) / kTokens);
-  // Workgroups of a head, which read the same queries, go to one XCD (they are dealt out
-  // in turn to eight) and find them in its L2: 1 to 15 % less.
-  const uint32_t each = gridDim.x / 8;
-  const uint32_t block = blockIdx.x < 8 * each ? blockIdx.x % 8 * each + blockIdx.x / 8 : blockIdx.x;
-  const int t0 = (int)(block % chunks) * kTokens;
-  const uint32_t id = block / chunks;
+  // Workgroups of a head read the same queries.  They are dealt out in turn to eight XCDs:
+  // where each can have as many heads of every sequence, all of a head go to one and find
+  // them in its L2 (2,048 rows of 32 heads over 16,384 tokens and 8 heads: of 64 channels 212
+  // us for 197, of 128 265 both, of 256 956 for 923; with 4 heads of sequences of unequal
+  // lengths 106 for 147, so not there).
+  const bool by_xcd = a.c.heads % 8 == 0;
+  const uint32_t turn = blockIdx.x / 8;
+  const int t0 = (int)((by_xcd ? turn : blockIdx.x) % chunks) * kTokens;
+  const uint32_t id = by_xcd ? turn / chunks * 8 + blockIdx.x % 8 : blockIdx.x / chunks;
   const int h = (int)(id % (uint32_t)a.c.heads);
   Work w;
   w.s = (int)(id / (uint32_t)a.c.heads);
