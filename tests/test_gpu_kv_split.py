@@ -149,6 +149,13 @@ def test_second_pass_of_many_tiles(lam, D, dt):
     _all(c, causal=False, mask=rng.random((40, 2, 900)) > 0.3)
 
 
+@pytest.mark.parametrize("Hk", [8, 16])
+@pytest.mark.parametrize("rows,lens", [([40, 35], [130, 500]), ([33], [77])])
+def test_second_pass_of_eight_heads(lam, Hk, rows, lens):
+    c = Case(lam, 64, 32, Hk, 3, "bf16", rows, lens, seed=Hk)
+    _all(c)
+
+
 def test_weights_by_both_ways_agree(lam):
     """One row at a time (kept scores) and all rows at once (a second pass) add up to the same."""
     c = Case(lam, 128, 64, 2, 4, "bf16", [48], [1500], seed=6)
