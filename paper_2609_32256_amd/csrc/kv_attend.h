@@ -32,7 +32,10 @@ constexpr int kFillDecode = 768, kFillChunk = 512, kFillWide = 256;
 // and 18 to 25 split, 3,000 tokens 18 to 19 whole and 14 to 18 split; chunks at 600
 // tokens 15 to 19 whole and 19 to 41 split, at 1,500 27 whole and 23 split.
 constexpr int kWholeDecode = 2048, kWholeChunk = 1024;
-constexpr int kChunkGrain = 512;      // least tokens of a part of a chunk's tile: its sums are 64 rows
+// Least tokens of a part, whose results are written and read again: with 128 for single
+// tokens 24,066 tokens of one head and 8 rows took 17.6 us for 12.5, 20,000 of four heads 20.9 for
+// 14.2.  A chunk's part is of as many tokens or a multiple (its sums are 64 rows).
+constexpr int kLeastDecode = 512, kLeastChunk = 512;
 // The kernel for chunks is taken where sequences have more (row, head) pairs than
 // this on average.  64 pairs over 10,000 tokens of 4 sequences and 8 heads of 128
 // channels: 34 us by 16 rows, 37 by 64; 96 pairs over 4,096 tokens of 20: 66 and 87 without
@@ -51,6 +54,7 @@ struct AttendArgs {
   int flip;               // the scale is negative
   int64_t cut;            // lengths are cut to it
   int tiles_per_seq;      // where every sequence has the same number of rows
+  int join_rows;          // rows a wave joins, 1 or 4
   int kept_waves;         // waves that share a token's kept scores, 1 or 4
   int split_to;           // workgroups to split the lengths over, 0: none is split
   int64_t blocks;         // workgroups of the attention: places for partial results
@@ -118,11 +122,12 @@ __device__ __forceinline__ Work plan(const AttendArgs& a, uint32_t id) {
   }
   if (a.c.n_seqs > 64) q = LaneSeq(a, lane, R);
   const float all = (float)wave_sum_f64(tokens) * a.c.heads, half = 0.5f * (float)wave_sum_f64(units) * a.c.heads;
-  constexpr int kStrips = kKvStrip * kAttWaves, kGrain = R == kAttRows ? kStrips : kChunkGrain;
+  constexpr int kStrips = kKvStrip * kAttWaves, kGrain = R == kAttRows ? kStrips : kLeastChunk;
+  constexpr int kLeast = R == kAttRows ? kLeastDecode : kLeastChunk;
   const float want = all / fmaxf((float)a.split_to - half, 0.5f * a.split_to) * 1.0001f;
   Work w;
   w.s = -1;
-  w.tokens = (int)fminf(floorf(want / kGrain) * kGrain + kGrain, 2147483520.0f);
+  w.tokens = (int)fminf(fmaxf(floorf(want / kGrain) * kGrain + kGrain, (float)kLeast), 2147483520.0f);
   uint32_t before = 0, units_before = 0;
   for (int b = 0; b < a.c.n_seqs; b += 64) {
     if (b > 0) q = LaneSeq(a, b + lane, R);

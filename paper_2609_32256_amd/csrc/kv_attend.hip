@@ -223,21 +223,24 @@ __device__ __forceinline__ void join_some(const AttendArgs& a, const Work& w, in
   }
 }
 
-// Joins the parts of 16 rows of a unit, up to four a wave with their loads on their way
-// together (one after the other: 13 us for 20 parts, 8 so; one row a wave: the plans of four
-// times the workgroups cost more).
+// Joins the parts of 16 rows of a unit, four a wave with their loads on their way together
+// (one after the other: 13 us for 20 parts, 8 so), or, where the units' rows are up to
+// kJoinFew, one: 24,066 tokens of a head and 8 rows take 18 us for 33, 4 sequences of 8,000 with 8
+// heads and 16 rows 19 for 22; with 5,120 rows the plans of four times the workgroups cost
+// 45 us for 43.6.
 constexpr int kJoinRows = 4;
+constexpr int kJoinFew = 2048;
 
 template <int D, bool BF16, int R>
 __device__ __forceinline__ void join_rows(const AttendArgs& a, uint32_t block) {
-  constexpr uint32_t kBlocks = R / (kAttWaves * kJoinRows);   // of a unit
-  const Work w = plan<R, PlanOf::kUnit>(a, block / kBlocks);
+  const uint32_t per = kAttWaves * (uint32_t)a.join_rows, blocks = R / per;   // rows of a workgroup, workgroups of a unit
+  const Work w = plan<R, PlanOf::kUnit>(a, block / blocks);
   if (w.s < 0 || w.parts == 1 || (int64_t)w.base + w.parts > a.blocks) return;   // (the last: starts that do not rise)
-  const int col = (int)(block % kBlocks) * kAttWaves * kJoinRows + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int n_rows = (w.pairs - w.r0 - col + kAttWaves - 1) / kAttWaves;
+  const int col = (int)(block % blocks * per) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n_rows = min((w.pairs - w.r0 - col + kAttWaves - 1) / kAttWaves, a.join_rows);
   if (n_rows <= 0) return;
   if (n_rows == 1) join_some<D, BF16, R, 1>(a, w, col, 1);
-  else join_some<D, BF16, R, kJoinRows>(a, w, col, min(n_rows, kJoinRows));
+  else join_some<D, BF16, R, kJoinRows>(a, w, col, n_rows);
 }
 
 // Weights from the scores that the attention kept: p = 2^(s - lse) summed over the
@@ -580,7 +583,8 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
 #undef LAM_GO
     LAM_HIP(hipGetLastError());
   }
-  const int64_t join_blocks = a.split_to ? units * (rows / (kAttWaves * kJoinRows)) : 0;
+  a.join_rows = units * rows <= kJoinFew ? 1 : kJoinRows;
+  const int64_t join_blocks = a.split_to ? units * (rows / (kAttWaves * a.join_rows)) : 0;
   int64_t kept_blocks = keep ? a.kept_cols / kKeptTokens * v.kv_heads * v.n_seqs : 0;
   // (4 sequences of 4,000 tokens, 64 pairs: 51 us with one wave a token, 46 with four;
   // 4 of 8,192 and 4 pairs: 21 and 22)
