@@ -378,28 +378,6 @@ __device__ __forceinline__ uint32_t val_pair(const uint32_t w[D / 32], float s) 
   return kv_values<false, byte % 4>(w[byte / 4], s);
 }
 
-// The scales of the lane's eight tokens of a strip at t0.  Memory past the last
-// token may hold anything, and 0 times it must be 0: its codes become 0.
-template <int D>
-__device__ __forceinline__ void value_scales(Codes<D>& v, int t0, int len, float s[2][4]) {
-  const int g = (threadIdx.x & 63) >> 4;
-#pragma unroll
-  for (int half = 0; half < 2; ++half)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) s[half][i] = kv_scale((v.s[half] >> (8 * i)) & 0xffu);
-  if (t0 + kKvStrip > len) {
-#pragma unroll
-    for (int half = 0; half < 2; ++half)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (t0 + 16 * half + 4 * g + i >= len) {
-          s[half][i] = 1.0f;
-#pragma unroll
-          for (int b = i * (D / 32); b < (i + 1) * (D / 32); ++b) v.w[half][b >> 2] &= ~(0xffu << (8 * (b & 3)));
-        }
-  }
-}
-
 // O^T += V^T P^T of a strip for TILES tiles of queries: one product per channel of
 // the lane's run and tile.
 template <int D, int TILES, int JP>
@@ -450,6 +428,29 @@ __device__ __forceinline__ uint32_t seen_bits(uint32_t all, int t0, int end) {
   const int n = min(max(end - t0, 0), 32);
   const uint32_t in = (all & (n == 32 ? 0xffffffffu : (1u << n) - 1u)) >> (4 * g);
   return (in & 0xfu) | ((in >> 12) & 0xf0u);
+}
+
+// The scales of the lane's eight tokens of a strip at t0.  Memory past the last
+// token, or of a token that the mask takes out (bits), may hold anything, and 0 times it
+// must be 0: its codes become 0.
+template <int D>
+__device__ __forceinline__ void value_scales(Codes<D>& v, int t0, int len, uint32_t bits, float s[2][4]) {
+#pragma unroll
+  for (int half = 0; half < 2; ++half)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[half][i] = kv_scale((v.s[half] >> (8 * i)) & 0xffu);
+  if (t0 + kKvStrip > len || bits != kAllTokens) {
+    const uint32_t in = seen_bits(bits, t0, len);
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (!((in >> (4 * half + i)) & 1u)) {
+          s[half][i] = 1.0f;
+#pragma unroll
+          for (int b = i * (D / 32); b < (i + 1) * (D / 32); ++b) v.w[half][b >> 2] &= ~(0xffu << (8 * (b & 3)));
+        }
+  }
 }
 
 // The softmax of a lane's query over the strips so far.  Four lanes (g) share a

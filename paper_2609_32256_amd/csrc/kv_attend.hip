@@ -83,7 +83,7 @@ struct Running {
     }
     const uint4 p = row.weights(x);
     float s[2][4];
-    value_scales<D>(v, t0, len, s);
+    value_scales<D>(v, t0, len, bits, s);
     add_values<D, 1, 0>(v, s, &p, &o);
   }
 };

@@ -106,7 +106,7 @@ __global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : D == 64 ? 3 : 2) void k
         }
       }
       float s[2][4];
-      value_scales<D>(v, t0, w.len, s);
+      value_scales<D>(v, t0, w.len, bits, s);
 #pragma unroll
       for (int t = 0; t < kTiles; ++t) less_reference(x[t], a.scale2, row[t]);
       if (t0 > whole_to || bits != kAllTokens) {

@@ -243,3 +243,21 @@ def test_evict_few_and_bad_pages(lam):
     assert lo.tolist() == [63] and kept[0, 0].tolist() == [63] + list(range(1, 63)) and torch.equal(pool, before)
     lam.kv_evict(pool, _i32([[-1, 1]]), _i32([64]), w, 63, 64)
     assert torch.equal(pool, before)
+
+
+@pytest.mark.parametrize("D,n,G", [(64, 1, 4), (128, 2, 7), (128, 40, 2), (256, 1, 2), (256, 30, 4)])
+def test_masked_tokens_may_hold_anything(lam, D, n, G):
+    """Slots that the mask takes out were never written: scales that are not numbers."""
+    T, lens, Hk = 64, [500, 97, 2300], 2
+    c = Case(lam, D, T, Hk, G, "bf16", [n] * 3, lens, seed=D + n)
+    m = np.random.default_rng(n).random((3, Hk, max(lens))) > 0.3
+    m[1, 0] = False
+    table, blocks = c.table.cpu().numpy(), D // 32
+    s, h, t = np.nonzero(~m & (np.arange(max(lens)) < np.array(lens)[:, None, None]))
+    page, t = torch.from_numpy(table[s, t // T]).long().cuda(), t % T
+    head, b = torch.from_numpy(h).cuda(), np.arange(blocks)
+    at = np.concatenate([T * D + t[:, None] * blocks + b,
+                         T * D + T * blocks + (t[:, None] // 4 * blocks + b) * 4 + t[:, None] % 4], axis=1)
+    c.pool[page[:, None], head[:, None], torch.from_numpy(at).cuda()] = 255
+    _all(c, mask=m)
+    _all(c, causal=False, mask=m)
