@@ -487,7 +487,11 @@ lam_status lam_kv_read(lam_ctx* ctx, const lam_kv_view* view, void* k_dev, void*
  * (longer sequences are cut to it); <= 0 for the table's.  Context scratch: where
  * lengths are split, partial results of at most 45 MB; with weights 4 bytes for each
  * query row and head, and for up to 64 rows times heads of a group per sequence 4
- * bytes for each of them and each token of the bound, at most 1 GiB.  Asynchronous. */
+ * bytes for each of them and each token of the bound, at most 1 GiB.  It is kept for later
+ * calls, grows to twice its size at least, and is freed with the context, also what a larger one
+ * replaced: a graph that recorded the call stays valid while the context lives (its replays
+ * and the context's other calls must not overlap, since they share it).  A call that would
+ * grow it cannot be recorded; the same call made once before has grown it.  Asynchronous. */
 lam_status lam_kv_attend(lam_ctx* ctx, const lam_kv_view* view, const void* q_dev, int64_t q_row_stride,
                          int64_t q_head_stride, int32_t q_heads, double scale, int causal, int64_t max_length,
                          const lam_kv_slots* mask, const lam_kv_slots* weights, void* out_dev, float* lse_dev);

@@ -249,6 +249,7 @@ void lam_ctx_destroy(lam_ctx* ctx) {
   DeviceGuard g(ctx->device);
   (void)hipStreamSynchronize(ctx->stream);
   for (auto& b : ctx->scratch) b.release();
+  for (auto& b : ctx->kv_old) b.release();
   for (auto& r : ctx->prof) {
     (void)hipEventDestroy(r.a);
     (void)hipEventDestroy(r.b);

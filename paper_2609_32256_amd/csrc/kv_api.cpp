@@ -2,6 +2,7 @@
 // The kernels are in kv_cache.hip and kv_attend.hip.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "lam_internal.h"
@@ -9,6 +10,8 @@
 using namespace lam;
 
 namespace {
+
+constexpr size_t kKvLeastScratch = 1 << 20;
 
 bool sizes_ok(int32_t head_dim, int32_t page_size) {
   return (head_dim == 64 || head_dim == 128 || head_dim == 256) && page_size >= 32 && page_size <= 1024 &&
@@ -70,6 +73,28 @@ lam_status check_own(const lam_kv_slots& s, const lam_kv_view* v, const char* na
 }
 
 }  // namespace
+
+namespace lam {
+
+lam_status kv_scratch(lam_ctx* ctx, size_t need, void** out) {
+  DevBuf& b = ctx->scratch[kScratchKv];
+  if (need > b.bytes || b.p == nullptr) {
+    DevBuf grown;
+    LAM_TRY(grown.ensure(std::max({need, 2 * b.bytes, kKvLeastScratch})));
+    if (b.p) {
+      DevBuf* const end = ctx->kv_old + kKvOld;
+      DevBuf* const slot = std::find_if(ctx->kv_old, end, [](const DevBuf& o) { return o.p == nullptr; });
+      if (slot == end) grown.release();
+      LAM_CHECK(slot != end, LAM_ENOMEM, "the context's scratch has grown too often");   // (31 doublings)
+      *slot = b;
+    }
+    b = grown;
+  }
+  *out = b.p;
+  return LAM_OK;
+}
+
+}  // namespace lam
 
 extern "C" {
 

@@ -556,10 +556,10 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
   const int64_t parts = a.split_to ? blocks * rows : 0;
   a.kept_cols = (a.cut + kKeptTokens - 1) / kKeptTokens * kKeptTokens;
   const bool keep = weights.p_dev && !chunk && pairs * a.kept_cols * 4 <= kKeptBytes;
-  DevBuf& buf = ctx->scratch[kScratchKv];
   const int64_t floats = (keep ? pairs * a.kept_cols : 0) + parts * (v.head_dim + 2) + (weights.p_dev ? pairs : 0);
-  LAM_TRY(buf.ensure((size_t)floats * 4));
-  float* at = buf.as<float>();
+  void* scratch = nullptr;
+  if (floats > 0) LAM_TRY(kv_scratch(ctx, (size_t)floats * 4, &scratch));
+  float* at = static_cast<float*>(scratch);
   if (keep) {
     a.kept = at;
     at += pairs * a.kept_cols;

@@ -828,9 +828,9 @@ lam_status launch_kv_evict(lam_ctx* ctx, const lam_kv_view& v, const lam_kv_slot
   else if (e.bound <= 64 * kSelThreads) LAM_GO(64);
 #undef LAM_GO
   else {
-    DevBuf& buf = ctx->scratch[kScratchKv];
-    LAM_TRY(buf.ensure((size_t)pairs * 2 * (size_t)e.moves * 4));
-    e.lists = buf.as<int32_t>();
+    void* lists;
+    LAM_TRY(kv_scratch(ctx, (size_t)pairs * 2 * (size_t)e.moves * 4, &lists));
+    e.lists = static_cast<int32_t*>(lists);
     launch(k_kv_select_long, dim3((unsigned)pairs), kSelThreads, ctx->stream, e0, e1, a, e);
   }
   LAM_HIP(hipGetLastError());

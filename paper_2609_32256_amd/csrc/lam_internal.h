@@ -69,6 +69,7 @@ constexpr int kScratchExpand = 15;       // block codec: codes expanded back to 
 constexpr int kScratchLsh = 16;          // banded candidates: chunk keys and the chunk's own index
 constexpr int kScratchKv = 17;           // 4-bit cache: partial results of split attention; eviction's lists
 constexpr int kScratchSlots = 18;
+constexpr int kKvOld = 32;
 
 struct DevBuf {
   void* p = nullptr;
@@ -112,6 +113,7 @@ struct lam_ctx {
   bool flags_zero = false;              // flags_dev known to hold zeros
   // scratch arena, grown on demand
   lam::DevBuf scratch[lam::kScratchSlots];
+  lam::DevBuf kv_old[lam::kKvOld];      // 4-bit cache: scratch that was outgrown, see kv_scratch
   // profiling
   uint32_t pair_cap = 1u << 20;         // ambiguous-pair list capacity (grows on overflow)
   int screen_tile = 0;                  // LAM_SCREEN_TILE_*
@@ -240,6 +242,10 @@ lam_status block_encode(lam_ctx* ctx, lam_store* st, lam_block_stats* out);
 lam_status block_decode(lam_ctx* ctx, const lam_store* st, float* xhat, uint32_t* codes_out);
 
 // ------------------------------------------------------------------ 4-bit cache (kv_cache.hip, kv_attend.hip)
+// The 4-bit cache's scratch, of at least `need` bytes.  Its calls are recorded into graphs,
+// which hold the address: what a larger need replaces is freed with the context only.  It
+// grows to twice its size at least, so all that was replaced is no more than what is used.
+lam_status kv_scratch(lam_ctx* ctx, size_t need, void** out);
 lam_status launch_kv_append(lam_ctx* ctx, const lam_kv_view& v, const void* k, int64_t k_row, int64_t k_head,
                             const void* val, int64_t v_row, int64_t v_head, const lam_kv_slots& weights,
                             const lam_kv_slots& positions, const int32_t* first, uint32_t* status);

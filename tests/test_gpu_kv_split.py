@@ -261,3 +261,31 @@ def test_masked_tokens_may_hold_anything(lam, D, n, G):
     c.pool[page[:, None], head[:, None], torch.from_numpy(at).cuda()] = 255
     _all(c, mask=m)
     _all(c, causal=False, mask=m)
+
+
+def test_a_graph_outlives_larger_scratch(lam):
+    """A recorded call keeps its scratch where later calls of the context need more."""
+    c = Case(lam, 128, 64, 2, 4, "bf16", [1, 1], [4100, 2900], seed=3)
+    big = Case(lam, 128, 64, 2, 4, "bf16", [8] * 8, [9000] * 8, seed=4)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    w = torch.zeros((2, 2, 4100), device="cuda")
+    with torch.cuda.stream(s):
+        ctx = lam.Context(stream=s)
+        want = c.call(weights=w, ctx=ctx)
+        want_w = w.clone()
+        s.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            out = c.call(weights=w, ctx=ctx)
+        wide = torch.zeros((8, 2, 9000), device="cuda")
+        big.check(big.call(weights=wide, ctx=ctx), weights=wide)
+    junk = torch.full((1 << 24,), float("nan"), device="cuda")
+    for _ in range(3):
+        w.zero_()
+        out.zero_()
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(w, want_w)
+        assert junk.isnan().all()
