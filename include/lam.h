@@ -501,7 +501,8 @@ lam_status lam_kv_attend(lam_ctx* ctx, const lam_kv_view* view, const void* q_de
  * head by itself: the tokens that stay are those protected, then those of the
  * largest score, equal ones in the order of their slots.  With position(s, h, t)
  * (int32, or NULL: t), protected are positions below `sinks` and the `recent`
- * positions up to that of the last slot; sinks + recent <= budget.  A NaN score
+ * positions up to the largest of the head's tokens (which need not be the last slot's,
+ * since an eviction moves tokens); sinks + recent <= budget.  A NaN score
  * is below every other.  Kept slots below budget stay where they are; the i-th slot
  * given up below budget takes the i-th one kept beyond it, so keys, values,
  * scores and positions of as few tokens as possible move.  Outputs: kept_dev

@@ -110,11 +110,12 @@ def attend(q, k, v, scale, causal=True, mask=None):
 
 # ------------------------------------------------------------------ eviction
 def evict(scores, positions, budget, recent, sinks):
-    """The old slot of each new one, for one head: scores and positions of its tokens."""
+    """The old slot of each new one, for one head: scores and positions of its tokens.
+    The newest is the largest position, whichever slot has it."""
     n = len(scores)
     if n <= budget:
         return list(range(n)) + [-1] * (budget - n)
-    newest = int(positions[-1])
+    newest = max(int(p) for p in positions)
 
     def rank(t):
         safe = positions[t] < sinks or positions[t] > newest - recent

@@ -535,8 +535,8 @@ def kv_evict(pages: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, sc
              head_dim: int, recent: int = 0, sinks: int = 0, positions: torch.Tensor | None = None, out=None,
              ctx: Context | None = None):
     """Bring sequences of more than `budget` tokens back to budget tokens
-    (lam_kv_evict): those of the largest scores stay, the `recent` newest and the
-    `sinks` first positions whatever their scores.  Returns (kept, scores,
+    (lam_kv_evict): those of the largest scores stay, the `recent` newest (by position,
+    whichever slots hold them) and the `sinks` first positions whatever their scores.  Returns (kept, scores,
     positions, lengths): the old slot of each new one (sequences, kv_heads,
     budget), the new slots' scores and positions, and the new lengths.  out:
     (scores, positions or None, lengths) to write to, which may be the inputs

@@ -322,7 +322,7 @@ struct EvictHead {
   float* so;
   int32_t* po;         // or null
   int32_t* kept;
-  int len, newest;
+  int len;
 
   __device__ __forceinline__ EvictHead(const KvArgs& a, const EvictArgs& e, int bh) {
     const int s = bh / a.heads, h = bh % a.heads;
@@ -333,7 +333,6 @@ struct EvictHead {
     so = static_cast<float*>(e.scores_out.p_dev) + at(e.scores_out);
     po = e.positions_out.p_dev ? static_cast<int32_t*>(e.positions_out.p_dev) + at(e.positions_out) : nullptr;
     kept = e.kept + (int64_t)bh * e.budget;
-    newest = len > 0 ? (ps ? ps[len - 1] : len - 1) : 0;
   }
   __device__ __forceinline__ int pos(int t) const { return ps ? ps[t] : t; }
   // new slot t holds what old slot `from` held
@@ -387,7 +386,20 @@ __device__ __forceinline__ void move_token(const KvArgs& a, int bh, int D, int f
 // other heads' selections still read.)
 constexpr int kOwnMoves = 64;
 
+// The largest of the threads' values (one barrier; tops: of the workgroup's own).
+__device__ __forceinline__ int largest(int v, uint32_t* tops) {
+  const uint32_t top = wave_max_u32((uint32_t)v ^ 0x80000000u);   // the order of signed numbers
+  if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+  __syncthreads();
+  uint32_t m = tops[0];
+#pragma unroll
+  for (int w = 1; w < kSelWaves; ++w) m = max(m, tops[w]);
+  return __builtin_amdgcn_readfirstlane((int)(m ^ 0x80000000u));
+}
+
 // Order of the scores as unsigned integers: protected slots above all, NaN below all.
+// newest: the largest position (an eviction fills holes from the tail, so the last slot
+// need not have it).
 __device__ __forceinline__ uint32_t evict_key(float s, int pos, int newest, int recent, int sinks) {
   if (pos < sinks || (int64_t)pos > (int64_t)newest - recent) return 0xffffffffu;
   if (s != s) return 0u;
@@ -405,8 +417,9 @@ constexpr int kBins = 1 << 11;
 // found digit by digit with histograms in LDS; a wave whose digits are all the same
 // (weights of 0, say) adds them at once; it ends as soon as a digit's keys all stay.
 // Then holes below budget and slots kept beyond it are ranked by their place, and the i-th hole
-// takes the i-th such slot.  Bound by its one reading of scores and positions (17 of 41
-// us for 192 heads of 32,768 slots) and by instructions of the workgroup's one compute unit.
+// takes the i-th such slot.  Bound by its reading of scores and positions (the newest position is
+// found first, so positions come from memory once and then from the caches) and by
+// instructions of the workgroup's one compute unit.
 // (A search bit by bit, each a count of all keys, took 25 us more for 32,768 slots.)
 template <int KPT>
 __global__ __launch_bounds__(kSelThreads) void k_kv_select(KvArgs a, EvictArgs e) {
@@ -431,7 +444,20 @@ __global__ __launch_bounds__(kSelThreads) void k_kv_select(KvArgs a, EvictArgs e
   __shared__ uint16_t extras[KPT * kSelThreads / 2];
 
   // in batches whose loads are all on their way before the first is used
-  constexpr int kBatch = KPT < 16 ? KPT : 16;
+  constexpr int kBatch = KPT < 16 ? KPT : KPT > 32 ? 8 : 16;   // (16 of 64 spill)
+  int newest = len - 1;
+  if (d.ps) {   // (read twice, the second time from the caches: held in registers, they spill)
+    int top = (int)0x80000000u;
+#pragma unroll 1
+    for (int t0 = tid; t0 < len; t0 += kBatch * kSelThreads) {
+      int p[kBatch];
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) p[j] = d.ps[(uint32_t)min(t0 + j * kSelThreads, len - 1)];
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) top = max(top, p[j]);
+    }
+    newest = largest(top, sums[0]);
+  }
   uint32_t key[KPT];
   auto fill = [&](auto has_positions) {
 #pragma unroll
@@ -451,7 +477,7 @@ __global__ __launch_bounds__(kSelThreads) void k_kv_select(KvArgs a, EvictArgs e
       }
 #pragma unroll
       for (int j = 0; j < kBatch; ++j)
-        key[k0 + j] = (k0 + j) * kSelThreads + tid < len ? evict_key(s[j], p[j], d.newest, e.recent, e.sinks) : 0u;
+        key[k0 + j] = (k0 + j) * kSelThreads + tid < len ? evict_key(s[j], p[j], newest, e.recent, e.sinks) : 0u;
     }
   };
   if (d.ps) fill(std::true_type{}); else fill(std::false_type{});
@@ -611,7 +637,14 @@ __global__ __launch_bounds__(kSelThreads) void k_kv_select_long(KvArgs a, EvictA
   __shared__ uint32_t hist[256];
   __shared__ uint32_t found[2];
   __shared__ int32_t cnt[2][3][kSelWaves];
-  auto key_of = [&](int t) { return evict_key(d.sc[t], d.pos(t), d.newest, e.recent, e.sinks); };
+  __shared__ uint32_t tops[kSelWaves];
+  int newest = d.len - 1;
+  if (d.ps) {
+    int top = (int)0x80000000u;
+    for (int t = tid; t < d.len; t += kSelThreads) top = max(top, d.ps[t]);
+    newest = largest(top, tops);
+  }
+  auto key_of = [&](int t) { return evict_key(d.sc[t], d.pos(t), newest, e.recent, e.sinks); };
 
   uint32_t prefix = 0, need = (uint32_t)e.budget;
   for (int shift = 24; shift >= 0; shift -= 8) {

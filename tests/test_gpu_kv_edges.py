@@ -1,0 +1,45 @@
+"""The 4-bit key/value cache on the GPU at the edges of its contract: evictions that
+follow each other.  Against the binary64 oracle; tolerances as in test_gpu_kv_attend.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import kv
+from test_gpu_kv_cache import _evict_case, _i32, _scores
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------ eviction
+@pytest.mark.parametrize("L,cuts", [
+    (100, (64, 32)), (2100, (2080, 2070, 300)), (5000, (4990, 1000)), (30000, (20000, 19990)), (40000, (30000, 7)),
+    (66000, (65990, 65800, 400)),
+])
+def test_evictions_without_new_tokens_keep_the_newest(lam, L, cuts):
+    """After an eviction the last slot holds any token; the newest positions stay all the same."""
+    D, T, heads, recent, sinks = 64, 256, 2, 5, 2
+    table = torch.arange(-(-L // T), dtype=torch.int32, device="cuda").view(1, -1)
+    pool = lam.kv_pages(table.shape[1], heads, D, T)
+    pos = torch.arange(L, dtype=torch.int32, device="cuda").expand(1, heads, L).contiguous()
+    lengths = _i32([L])
+    moved = False
+    for i, budget in enumerate(cuts):
+        w = _scores(L + i, 1, heads, pos.shape[-1], "random")
+        want = [kv.evict(w[0, h].tolist(), pos[0, h].tolist(), budget, recent, sinks) for h in range(heads)]
+        kept, _, pos, lengths = lam.kv_evict(pool, table, lengths, w, budget, D, recent=recent, sinks=sinks, positions=pos)
+        assert kept[0].tolist() == want
+        for h in range(heads):
+            assert set(pos[0, h].tolist()) >= set(range(L - recent, L)) | set(range(sinks))
+        moved |= bool((pos[0, :, -1] != L - 1).any())
+    assert moved
+
+
+@pytest.mark.parametrize("newest", [0, 17, 1023, 1500, 2999])
+def test_the_newest_position_in_any_slot(lam, newest):
+    """The largest position in a slot of its own choice, negative ones (below every sink) among the others."""
+    L = 3000
+    pos = torch.arange(-500, L - 500, dtype=torch.int32, device="cuda").flip(0).repeat(1, 2, 1)
+    pos[:, :, newest] = (1 << 31) - 1
+    pos[:, 1, newest] = 2600
+    _evict_case(lam, 64, 32, 2, [L], 1000, 300, 0, _scores(newest, 1, 2, L, "random"), pos, False)

@@ -105,3 +105,24 @@ def test_eviction_by_hand():
     assert kv.evict([math.nan, 1.0, -2.0, -0.0, 0.0], pos[:5], 2, 0, 0) == [3, 1]
     assert kv.evict([1.0, 2.0], pos[:2], 4, 1, 1) == [0, 1, -1, -1]
     assert kv.evict([1.0, 2.0, 3.0, 4.0], [9, 3, 7, 10], 2, 2, 0) == [0, 3]
+
+
+def test_eviction_twice_keeps_the_newest():
+    """An eviction puts tokens of the tail into holes, so the last slot then holds an older
+    one; the next eviction protects the newest positions all the same."""
+    # token 4 takes the place of token 0; then it is the newest, in slot 0
+    assert kv.evict([0.0, 5.0, 5.0, 5.0, 1.0], list(range(5)), 4, 1, 0) == [4, 1, 2, 3]
+    assert kv.evict([0.0, 1.0, 2.0, 3.0], [4, 1, 2, 3], 2, 1, 0) == [0, 3]
+    assert kv.evict([9.0, 1.0, 8.0, 7.0], [9, 8, 2, 1], 2, 2, 0) == [0, 1]
+    rng = np.random.default_rng(0)
+    moved = 0
+    for _ in range(50):
+        n, mid, budget, recent, sinks = 100, 64, 32, 16, 2
+        w = rng.random(n)
+        first = kv.evict(w, list(range(n)), mid, recent, sinks)
+        moved += first[-1] != n - 1
+        w2 = rng.random(mid)
+        second = kv.evict(w2, first, budget, recent, sinks)
+        kept = {first[t] for t in second}
+        assert set(range(n - recent, n)) <= kept and set(range(sinks)) <= kept
+    assert moved > 0
