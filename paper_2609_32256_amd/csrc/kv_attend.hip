@@ -276,9 +276,11 @@ __device__ __forceinline__ void add_kept(const AttendArgs& a, uint32_t block) {
   const int r_first = share ? 4 * wave : 0, r_step = share ? kAttRows : 4;
   load(r_first);
   float* d = static_cast<float*>(a.weights.p_dev) + s * a.weights.seq_stride + h * a.weights.head_stride + t;
-  float w[4];
+  // The call's sum starts at 0 and is added to what was there once: added one by one, each
+  // small p would be rounded at the size of the running total.
+  float w[4] = {}, had[4];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) w[j] = (!share || wave == 0) && t + j < min(len, a.weights.cols) ? d[j] : 0.0f;
+  for (int j = 0; j < 4; ++j) had[j] = (!share || wave == 0) && t + j < min(len, a.weights.cols) ? d[j] : 0.0f;
   Work q;
   q.parts = 1;
   if (a.split_to) q = plan<kAttRows, PlanOf::kSequence>(a, (uint32_t)s);
@@ -327,7 +329,7 @@ __device__ __forceinline__ void add_kept(const AttendArgs& a, uint32_t block) {
   }
 #pragma unroll
   for (int j = 0; j < 4; ++j)
-    if (t + j < min(len, a.weights.cols)) d[j] = w[j];
+    if (t + j < min(len, a.weights.cols)) d[j] = had[j] + w[j];
 }
 
 // What follows the attention, in one launch: the parts joined, the kept scores made weights.

@@ -1,11 +1,12 @@
 """The 4-bit key/value cache on the GPU at the edges of its contract: evictions that
-follow each other.  Against the binary64 oracle; tolerances as in test_gpu_kv_attend.
+follow each other, and weights added to large ones.  Against the binary64 oracle; tolerances as in test_gpu_kv_attend.
 """
 import numpy as np
 import pytest
 import torch
 
 from oracle import kv
+from test_gpu_kv_attend import Case, _np
 from test_gpu_kv_cache import _evict_case, _i32, _scores
 
 pytestmark = pytest.mark.gpu
@@ -43,3 +44,26 @@ def test_the_newest_position_in_any_slot(lam, newest):
     pos[:, :, newest] = (1 << 31) - 1
     pos[:, 1, newest] = 2600
     _evict_case(lam, 64, 32, 2, [L], 1000, 300, 0, _scores(newest, 1, 2, L, "random"), pos, False)
+
+
+# ------------------------------------------------------------------ weights
+@pytest.mark.parametrize("prior", [2048.0, 1e5])
+@pytest.mark.parametrize("n", [1, 4, 5])                     # scores kept, a wave a token and four; a second pass
+def test_small_weights_are_added_to_large_ones_once(lam, n, prior):
+    """Flat rows over many tokens, whose every p is below the rounding of the total so far:
+    the call's sum is added with one rounding (2^-24 of the total), and is itself right to
+    the scores' errors (test_gpu_kv_attend) and 2^-20 for its additions."""
+    L, G, D = 16384, 16, 64
+    c = Case(lam, D, 64, 1, G, "f16", [n], [L], seed=n, spread=1e-2)
+    g = torch.Generator(device="cuda").manual_seed(n)
+    before = prior * (1 + torch.rand((1, 1, L), generator=g, device="cuda"))
+    w = before.clone()
+    c.call(causal=False, weights=w)
+    want, tol = np.zeros(L), np.zeros(L)
+    for j in range(G):
+        r = kv.attend(_np(c.q)[:, j], c.k[0][:, 0], c.v[0][:, 0], D ** -0.5, False)
+        want += r["p"].sum(0)
+        tol += ((2 * (r["slack"] * (D + 8) * 2.0 ** -24) + 2.0 ** -19)[:, None] * r["p"]).sum(0)
+    total = before[0, 0].cpu().numpy().astype(np.float64) + want
+    got = w[0, 0].cpu().numpy().astype(np.float64)
+    assert (np.abs(got - total) <= 2.0 ** -24 * total + tol).all()
