@@ -476,7 +476,7 @@ lam_status lam_kv_read(lam_ctx* ctx, const lam_kv_view* view, void* k_dev, void*
  * over the tokens t < lengths[s], with causal != 0 only t <= lengths[s] - n_s + i,
  * with a mask only those with mask(s, h, t) != 0 (uint8; tokens past its columns
  * are masked; head_stride 0 for one mask of all heads; what masked tokens hold in
- * the cache does not matter).  A row with no token left
+ * the cache does not matter).  A row with no token left, or of no sequence,
  * gets 0 (lse -inf).  Scores, maxima and sums are float32; p enters the product
  * with the values as float16 relative to the row's maximum so far.  A query with
  * NaN or Inf spoils its own row only, and the weights of the tokens that it sees.  q [rows][q_heads][head_dim] of

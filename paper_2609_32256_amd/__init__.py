@@ -500,7 +500,8 @@ def kv_attend(q: torch.Tensor, pages: torch.Tensor, table: torch.Tensor, lengths
     default.  mask (bool or uint8: sequences, kv_heads or 1, slots) leaves cached
     tokens out; weights (float32: sequences, kv_heads, slots) is added to what
     each token received; lse (float32: rows, q_heads) receives the scores' log
-    sums.  max_length, where the caller knows a bound of lengths, sizes the launch."""
+    sums.  Rows that see no token, those of no sequence among them, get 0 (lse -inf).
+    max_length, where the caller knows a bound of lengths, sizes the launch."""
     if ctx is None:
         ctx = default_context()
     elif _kv_elsewhere(ctx):

@@ -234,6 +234,23 @@ __device__ __forceinline__ Work work_of(const AttendArgs& a, uint32_t id) {
   return a.split_to ? plan<R, PlanOf::kWorkgroup>(a, id) : tile_work<R>(a, id);
 }
 
+// Rows of no sequence see no token: 0, and a log sum of -inf.  (Read after the workgroup's
+// work is known, which has brought starts into the caches.)
+template <int D>
+__device__ __forceinline__ void clear_rows(const AttendArgs& a) {
+  if (!a.c.starts) return;
+  const int64_t rows = a.c.rows;
+  auto clipped = [&](int s) { return min(max((int64_t)kv_const(a.c.starts)[s], (int64_t)0), rows); };
+  const int64_t before = clipped(0), after = clipped(a.c.n_seqs), row_size = (int64_t)a.q_heads * (D / 8);
+  for (int64_t r = blockIdx.x; r < before + rows - after; r += gridDim.x) {
+    const int64_t row = r < before ? r : after + r - before;
+    for (int64_t i = threadIdx.x; i < row_size; i += kAttThreads)
+      *reinterpret_cast<uint4*>(a.out + (row * row_size + i) * 8) = uint4{0, 0, 0, 0};
+    if (a.lse)
+      for (int j = threadIdx.x; j < a.q_heads; j += kAttThreads) a.lse[row * a.q_heads + j] = -__builtin_inff();
+  }
+}
+
 // Tokens that pair r of the sequence sees: those below this.
 __device__ __forceinline__ int pair_end(const AttendArgs& a, const Work& w, int r) {
   if (!a.causal) return w.len;

@@ -94,6 +94,7 @@ __global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : 3) void k_kv_attend(Att
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Work w = work_of<kAttRows>(a, blockIdx.x);
+  clear_rows<D>(a);
   if (w.s < 0) return;
   const int h = w.h;
   const int T = 1 << a.c.page_shift;

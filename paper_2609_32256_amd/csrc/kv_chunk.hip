@@ -22,6 +22,7 @@ __global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : D == 64 ? 3 : 2) void k
   const int lane = threadIdx.x & 63, c = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Work w = work_of<kRows>(a, blockIdx.x);
+  clear_rows<D>(a);
   if (w.s < 0) return;
   const int T = 1 << a.c.page_shift;
   const int64_t head_bytes = KvLayout<D>::head_bytes(T);

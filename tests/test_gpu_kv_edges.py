@@ -1,5 +1,5 @@
 """The 4-bit key/value cache on the GPU at the edges of its contract: evictions that
-follow each other, and weights added to large ones.  Against the binary64 oracle; tolerances as in test_gpu_kv_attend.
+follow each other, weights added to large ones, rows of no sequence.  Against the binary64 oracle; tolerances as in test_gpu_kv_attend.
 """
 import numpy as np
 import pytest
@@ -67,3 +67,32 @@ def test_small_weights_are_added_to_large_ones_once(lam, n, prior):
     total = before[0, 0].cpu().numpy().astype(np.float64) + want
     got = w[0, 0].cpu().numpy().astype(np.float64)
     assert (np.abs(got - total) <= 2.0 ** -24 * total + tol).all()
+
+
+# ------------------------------------------------------------------ rows and lengths
+@pytest.mark.parametrize("D,G,rows,lens,before,after", [
+    (128, 4, [1, 1, 1], [300, 0, 77], 2, 3),                 # single tokens, whole and in parts
+    (128, 4, [1, 1], [5000, 40], 1, 700),
+    (64, 2, [60, 0, 90], [70, 5, 300], 5, 1),                # chunks
+    (64, 2, [70], [2500], 0, 2),
+    (256, 4, [30, 40], [90, 1500], 3, 0),
+    (64, 1, [1] * 900, [9] * 900, 1, 2),                     # many sequences
+    (64, 3, [0, 0], [40, 50], 4, 1),                         # no row of any sequence
+])
+def test_rows_of_no_sequence_get_nothing(lam, D, G, rows, lens, before, after):
+    """A batch padded to more rows than its sequences have."""
+    c = Case(lam, D, 32, 1, G, "bf16", rows, lens, seed=D + after)
+    n = sum(rows)
+    q = torch.randn((before + n + after, G, D), device="cuda").to(torch.bfloat16)
+    q[before:before + n] = c.q
+    q[:before] = float("nan")
+    starts = _i32([before + int(x) for x in c.starts])
+    out, lse = torch.full_like(q, float("nan")), torch.full(q.shape[:2], float("nan"), device="cuda")
+    w = torch.zeros((len(lens), 1, max(lens)), device="cuda")
+    lam.kv_attend(q, c.pool, c.table, c.lengths, starts=starts, out=out, lse=lse, weights=w)
+    mine = slice(before, before + n)
+    c.check(out[mine], lse=lse[mine], weights=w)
+    for pad in (slice(0, before), slice(before + n, None)):
+        assert not out[pad].any() and torch.isneginf(lse[pad]).all()
+    again = lam.kv_attend(q, c.pool, c.table, c.lengths, starts=starts)
+    assert torch.equal(again, out)
