@@ -74,12 +74,12 @@ struct KvArgs {
     const int64_t r = starts[s];
     return r < 0 ? 0 : (r > rows ? rows : r);
   }
-  // cached tokens of sequence s that the table has columns for
-  __device__ int length(int s) const {
-    const int64_t cap = (int64_t)table_cols << page_shift;
-    const int l = kv_const(lengths)[s];
-    return l < 0 ? 0 : (l > cap ? (int)cap : l);
-  }
+  // Cached tokens of sequence s, whose last are the call's rows: those past the table's
+  // columns count in.  (Room above for the rows past the last of a tile; a sequence
+  // has at most 2^30 tokens with a place, so no causal limit among them is another.)
+  __device__ int tokens(int s) const { return min(max(kv_const(lengths)[s], 0), 0x7fff0000); }
+  // those that the table has columns for
+  __device__ int length(int s) const { return (int)min((int64_t)tokens(s), (int64_t)table_cols << page_shift); }
   // page of column c of sequence s, or -1
   __device__ int64_t page(int s, int c) const {
     const int64_t p = table[s * table_stride + c];

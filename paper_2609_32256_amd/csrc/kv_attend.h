@@ -52,7 +52,7 @@ struct AttendArgs {
   int causal;
   float scale2;           // |scale| * log2(e), above 0
   int flip;               // the scale is negative
-  int64_t cut;            // lengths are cut to it
+  int64_t cut;            // lengths are cut to it: the table's columns and the caller's bound
   int tiles_per_seq;      // where every sequence has the same number of rows
   int join_rows;          // rows a wave joins, 1 or 4
   int kept_waves;         // waves that share a token's kept scores, 1 or 4
@@ -76,7 +76,7 @@ struct Work {
   int64_t first;       // its first row of the call
   int n;               // its rows
   int pairs;           // its pairs, row-major
-  int len, end_full;   // cached tokens, cut and not
+  int len, end_full;   // cached tokens: those with a column of the table, cut to the bound; and all
   int parts, tokens;   // parts of its length, and the tokens of one
   uint32_t base;       // its first workgroup
   int h, r0, part;     // head, first pair of the tile, part
@@ -93,7 +93,7 @@ struct LaneSeq {
     const int q = min(s, a.c.n_seqs - 1);
     first = a.c.start(q);
     n = in ? (int)max((int64_t)0, a.c.start(q + 1) - first) : 0;
-    full = a.c.length(q);
+    full = a.c.tokens(q);
     len = (int)min((int64_t)full, a.cut);
     tiles = tiles_of(n * a.group, R);
   }
@@ -194,7 +194,7 @@ __device__ __forceinline__ Work tile_work(const AttendArgs& a, uint32_t id) {
     w.r0 = (int)(t % per) * R;
     w.first = (int64_t)w.s * a.c.per_seq;
     next = w.first + a.c.per_seq;
-    w.end_full = a.c.length(w.s);
+    w.end_full = a.c.tokens(w.s);
   } else {
     // Sequence s has its tiles from floor(start(s) * group / R) + s on, a bound that
     // leaves room for every partial tile and rises with s: the last s whose bound
@@ -209,7 +209,7 @@ __device__ __forceinline__ Work tile_work(const AttendArgs& a, uint32_t id) {
     for (int b = 0; b < a.c.n_seqs; b += 64) {
       const int s = min(b + lane, a.c.n_seqs - 1);
       const int64_t s0 = a.c.start(s), s1 = a.c.start(s + 1);
-      const int l = a.c.length(s);
+      const int l = a.c.tokens(s);
       const uint32_t at = (uint32_t)(s0 * a.group / R) + (uint32_t)s;
       const unsigned long long in = __ballot(b + lane < a.c.n_seqs && at <= t);
       if (in == 0) break;

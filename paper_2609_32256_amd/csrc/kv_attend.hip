@@ -257,7 +257,7 @@ __device__ __forceinline__ void add_kept(const AttendArgs& a, uint32_t block) {
   const int t = (int)(block % chunks) * tokens + 4 * (share ? lane : (int)threadIdx.x);
   const int h = (int)(block / chunks % (uint32_t)a.c.heads), s = (int)(block / chunks / (uint32_t)a.c.heads);
   const int64_t first = a.c.start(s);
-  const int n = (int)max((int64_t)0, a.c.start(s + 1) - first), full = a.c.length(s);
+  const int n = (int)max((int64_t)0, a.c.start(s + 1) - first), full = a.c.tokens(s);
   const int len = (int)min((int64_t)full, a.cut), pairs = n * a.group;
   if ((int)(block % chunks) * tokens >= len) return;
   // Four rows' scores at a time, the first four on their way before the plan and the
@@ -379,7 +379,7 @@ void k_kv_weights(AttendArgs a) {
   w.first = a.c.start(w.s);
   w.n = (int)max((int64_t)0, a.c.start(w.s + 1) - w.first);
   w.pairs = w.n * a.group;
-  w.end_full = a.c.length(w.s);
+  w.end_full = a.c.tokens(w.s);
   w.len = (int)min((int64_t)w.end_full, a.cut);
   if (t0 >= w.len || w.pairs == 0) return;
   const int T = 1 << a.c.page_shift;

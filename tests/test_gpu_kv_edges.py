@@ -96,3 +96,23 @@ def test_rows_of_no_sequence_get_nothing(lam, D, G, rows, lens, before, after):
         assert not out[pad].any() and torch.isneginf(lse[pad]).all()
     again = lam.kv_attend(q, c.pool, c.table, c.lengths, starts=starts)
     assert torch.equal(again, out)
+
+
+@pytest.mark.parametrize("D,G,rows,lens,cols", [
+    (128, 4, [3, 3], [100, 50], 2),                          # single tokens
+    (128, 2, [8, 4], [5000, 300], 90),                       # in parts
+    (64, 2, [70, 40], [100, 70], 2),                         # chunks
+    (64, 1, [400, 80], [3500, 900], 80),
+    (256, 4, [30, 40], [90, 150], 2),
+])
+def test_a_causal_limit_goes_by_the_length_not_the_table(lam, D, G, rows, lens, cols):
+    """Tokens past the table's columns are as if masked; the rows are still the length's last."""
+    c = Case(lam, D, 32, 2, G, "bf16", rows, lens, seed=D + cols)
+    c.table = c.table[:, :cols].contiguous()
+    there = [(np.arange(n) < 32 * cols)[None] for n in lens]
+    assert not all(m.all() for m in there)
+    lse = torch.empty(c.q.shape[:2], device="cuda")
+    w = torch.zeros((2, 2, max(lens)), device="cuda")
+    c.check(c.call(lse=lse, weights=w), mask=there, lse=lse, weights=w)
+    c.check(c.call(max_length=max(lens)), mask=there)
+    assert not w[..., 32 * cols:].any()
