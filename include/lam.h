@@ -485,7 +485,9 @@ lam_status lam_kv_read(lam_ctx* ctx, const lam_kv_view* view, void* k_dev, void*
  * weights (float32, or NULL): the sum of p over the call's rows of s and the
  * query heads of h is added to element (s, h, t); tokens past its columns are
  * left out.  max_length: an upper bound of lengths that the launch is sized by
- * (longer sequences are cut to it); <= 0 for the table's.  Context scratch: where
+ * (longer sequences are cut to it); <= 0 for the table's.  EINVAL, with nothing written,
+ * where a launch would have 2^24 workgroups or more: with weights one for each head, sequence
+ * and 64 or 128 tokens of the bound, else one for each 16 query rows and heads.  Context scratch: where
  * lengths are split, partial results of at most 45 MB; with weights 4 bytes for each
  * query row and head, and for up to 64 rows times heads of a group per sequence 4
  * bytes for each of them and each token of the bound, at most 1 GiB.  It is kept for later

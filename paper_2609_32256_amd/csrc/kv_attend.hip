@@ -548,7 +548,6 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
     a.split_to = split_to;
     blocks = split_to + units;   // see plan(): at most split_to - units / 2 (or split_to / 2) full parts, and one more a tile
   }
-  LAM_CHECK(blocks < (1LL << 31), LAM_EINVAL, "too many rows for one launch");
   a.blocks = blocks;
 
   // Weights: from scores that the attention keeps (8 bytes a row and token, written
@@ -558,7 +557,22 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
   const int64_t pairs = v.rows * q_heads;
   const int64_t parts = a.split_to ? blocks * rows : 0;
   a.kept_cols = (a.cut + kKeptTokens - 1) / kKeptTokens * kKeptTokens;
-  const bool keep = weights.p_dev && !chunk && pairs * a.kept_cols * 4 <= kKeptBytes;
+  const bool keep = weights.p_dev && !chunk && pairs <= kKeptBytes / 4 / std::max<int64_t>(a.kept_cols, 1);
+  // every launch's size, before the first is queued: a call that is refused has written nothing
+  a.join_rows = units * rows <= kJoinFew ? 1 : kJoinRows;
+  const int64_t join_blocks = a.split_to ? units * (rows / (kAttWaves * a.join_rows)) : 0;
+  int64_t kept_blocks = keep ? a.kept_cols / kKeptTokens * v.kv_heads * v.n_seqs : 0;
+  // (4 sequences of 4,000 tokens, 64 pairs: 51 us with one wave a token, 46 with four;
+  // 4 of 8,192 and 4 pairs: 21 and 22)
+  a.kept_waves = kept_blocks < 1024 && v.rows * a.group > kAttRows * (int64_t)v.n_seqs ? 4 : 1;
+  kept_blocks *= a.kept_waves;
+  const int64_t heads = (int64_t)v.kv_heads * v.n_seqs;
+  auto weight_blocks_of = [&](int strips) { return (a.cut + strips * kKvStrip - 1) / (strips * kKvStrip) * heads; };
+  const bool few = v.head_dim == 256 || weight_blocks_of(4) < kWeightBlocks;
+  const int64_t weight_blocks = weights.p_dev && !keep ? weight_blocks_of(few ? 2 : 4) : 0;   // (a cut of 0: none)
+  LAM_CHECK(std::max({blocks, join_blocks + kept_blocks, weight_blocks}) <= most_blocks(kAttThreads), LAM_EINVAL,
+            "too many rows, or sequences times the bound of lengths, for one launch (%lld tokens: give max_length)",
+            (long long)a.cut);
   const int64_t floats = (keep ? pairs * a.kept_cols : 0) + parts * (v.head_dim + 2) + (weights.p_dev ? pairs : 0);
   void* scratch = nullptr;
   if (floats > 0) LAM_TRY(kv_scratch(ctx, (size_t)floats * 4, &scratch));
@@ -586,15 +600,7 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
 #undef LAM_GO
     LAM_HIP(hipGetLastError());
   }
-  a.join_rows = units * rows <= kJoinFew ? 1 : kJoinRows;
-  const int64_t join_blocks = a.split_to ? units * (rows / (kAttWaves * a.join_rows)) : 0;
-  int64_t kept_blocks = keep ? a.kept_cols / kKeptTokens * v.kv_heads * v.n_seqs : 0;
-  // (4 sequences of 4,000 tokens, 64 pairs: 51 us with one wave a token, 46 with four;
-  // 4 of 8,192 and 4 pairs: 21 and 22)
-  a.kept_waves = kept_blocks < 1024 && v.rows * a.group > kAttRows * (int64_t)v.n_seqs ? 4 : 1;
-  kept_blocks *= a.kept_waves;
   if (join_blocks + kept_blocks > 0) {
-    LAM_CHECK(join_blocks + kept_blocks < (1LL << 31), LAM_EINVAL, "too many rows for one launch");
     LAM_TRY(prof_launch_events(ctx, "kv_finish", &e0, &e1));
     const dim3 grid((unsigned)(join_blocks + kept_blocks));
     const uint32_t jb = (uint32_t)join_blocks;
@@ -610,13 +616,9 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
 #undef LAM_GO
     LAM_HIP(hipGetLastError());
   }
-  if (weights.p_dev && !keep && a.cut > 0) {
-    const int64_t heads = (int64_t)v.kv_heads * v.n_seqs;
-    auto blocks_of = [&](int strips) { return (a.cut + strips * kKvStrip - 1) / (strips * kKvStrip) * heads; };
-    LAM_CHECK(blocks_of(2) < (1LL << 31), LAM_EINVAL, "too many sequences for one launch");
+  if (weight_blocks > 0) {
     LAM_TRY(prof_launch_events(ctx, "kv_weights", &e0, &e1));
-    const bool few = v.head_dim == 256 || blocks_of(4) < kWeightBlocks;
-    const dim3 grid((unsigned)blocks_of(few ? 2 : 4));
+    const dim3 grid((unsigned)weight_blocks);
 #define LAM_GO(D, BF)                                                                                       \
   do {                                                                                                      \
     if (few) launch(k_kv_weights<D, BF, 2>, grid, kAttThreads, ctx->stream, e0, e1, a);                     \

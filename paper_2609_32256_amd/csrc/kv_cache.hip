@@ -807,9 +807,10 @@ lam_status quad_grid(const lam_kv_view& v, int* quads, unsigned* grid) {
     *quads = (int)(n / 4 + (n % 4 > 1 ? 2 : 1));   // n rows from any slot on touch no more
     units = *quads * (int64_t)v.n_seqs;
   }
-  const int64_t per = kKvThreads / (v.head_dim / 8), items = units * v.kv_heads;
-  LAM_CHECK(items < (1LL << 31), LAM_EINVAL, "too many rows for one launch");
-  *grid = (unsigned)((items + per - 1) / per);
+  const int64_t per = kKvThreads / (v.head_dim / 8), items = units * v.kv_heads, blocks = (items + per - 1) / per;
+  LAM_CHECK(items < (1LL << 31) && blocks <= most_blocks(kKvThreads), LAM_EINVAL,
+            "too many rows or sequences for one launch");
+  *grid = (unsigned)blocks;
   return LAM_OK;
 }
 
@@ -866,6 +867,9 @@ lam_status launch_kv_evict(lam_ctx* ctx, const lam_kv_view& v, const lam_kv_slot
   e.lengths_out = lengths_out;
   const bool apart = lengths_out + v.n_seqs <= v.lengths_dev || v.lengths_dev + v.n_seqs <= lengths_out;
   if (e.moves <= kOwnMoves && e.bound <= 64 * kSelThreads && apart) e.head_dim = v.head_dim;
+  const int per = kKvThreads / (v.head_dim / 8) * 4;   // slots a workgroup of the move
+  const int64_t move_blocks = ((int64_t)std::min(budget, std::max(e.bound, 1)) + per - 1) / per;
+  LAM_CHECK(move_blocks <= most_blocks(kKvThreads), LAM_EINVAL, "too many slots for one launch");
   hipEvent_t e0, e1;
   LAM_TRY(prof_launch_events(ctx, "kv_select", &e0, &e1));
 #define LAM_GO(KPT) launch(k_kv_select<KPT>, dim3((unsigned)pairs), kSelThreads, ctx->stream, e0, e1, a, e)
@@ -883,8 +887,7 @@ lam_status launch_kv_evict(lam_ctx* ctx, const lam_kv_view& v, const lam_kv_slot
   LAM_HIP(hipGetLastError());
   if (e.head_dim) return LAM_OK;
   LAM_TRY(prof_launch_events(ctx, "kv_move", &e0, &e1));
-  const int per = kKvThreads / (v.head_dim / 8) * 4;   // slots a workgroup
-  const dim3 grid((unsigned)((std::min(budget, std::max(e.bound, 1)) + per - 1) / per), (unsigned)pairs);
+  const dim3 grid((unsigned)move_blocks, (unsigned)pairs);
 #define LAM_GO(D) launch(k_kv_move<D>, grid, kKvThreads, ctx->stream, e0, e1, a, e)
   if (v.head_dim == 64) LAM_GO(64); else if (v.head_dim == 128) LAM_GO(128); else LAM_GO(256);
 #undef LAM_GO

@@ -183,6 +183,10 @@ lam_status prof_end(lam_ctx* ctx, size_t slot);
 // events for hipExtLaunchKernel (null unless this kernel is profiled)
 lam_status prof_launch_events(lam_ctx* ctx, const char* name, hipEvent_t* start, hipEvent_t* stop);
 
+// Most workgroups of `threads` that one dimension of a launch takes: the runtime refuses
+// 2^32 work-items.
+constexpr int64_t most_blocks(int threads) { return ((1LL << 32) - 1) / threads; }
+
 // A launch, timed by itself (e0, e1 of prof_launch_events) where it is profiled.
 // The plain launch costs the host about a microsecond less than the timed one.
 template <class... P, class... A>

@@ -116,3 +116,38 @@ def test_a_causal_limit_goes_by_the_length_not_the_table(lam, D, G, rows, lens, 
     c.check(c.call(lse=lse, weights=w), mask=there, lse=lse, weights=w)
     c.check(c.call(max_length=max(lens)), mask=there)
     assert not w[..., 32 * cols:].any()
+
+
+# ------------------------------------------------------------------ refusals
+def test_launches_too_large_are_refused_before_anything_is_written(lam):
+    """1,024 sequences of 8 heads of 256 channels with a table of 131,072 tokens and no bound of
+    lengths: 2^24 workgroups of the weights' second pass, one too many."""
+    B, H, D, T = 1024, 8, 256, 1024
+    pool = lam.kv_pages(1, H, D, T)
+    k, v = (torch.randn((1, H, D), device="cuda").half() for _ in range(2))
+    lam.kv_append(k, v, pool, _i32([[0]]), _i32([1]))
+    table = torch.zeros((B, 128), dtype=torch.int32, device="cuda")
+    lengths = torch.ones(B, dtype=torch.int32, device="cuda")
+    q = torch.randn((B, H, D), device="cuda").half()
+    out, w = torch.full_like(q, 7.0), torch.full((B, H, 1), 3.0, device="cuda")
+    lse = torch.full((B, H), 5.0, device="cuda")
+    with pytest.raises(lam.LamError) as e:
+        lam.kv_attend(q, pool, table, lengths, weights=w, out=out, lse=lse)
+    assert e.value.name == "LAM_EINVAL" and "max_length" in str(e.value)
+    assert (out == 7).all() and (w == 3).all() and (lse == 5).all()
+    # one sequence less, or the bound given, and it runs: each token is all that its row sees
+    lam.kv_attend(q[1:], pool, table[1:], lengths[1:], weights=w[1:], out=out[1:])
+    lam.kv_attend(q, pool, table, lengths, weights=w, out=out, lse=lse, max_length=1)
+    a, b = lam.kv_read(pool, _i32([[0]]), _i32([1]), 1, D, dtype=torch.float16)
+    assert torch.equal(out, b.expand_as(out))
+    assert torch.allclose(w[1:], torch.full_like(w[1:], 5.0)) and torch.allclose(w[0], torch.full_like(w[0], 4.0))
+    # one row in a batch of 2^20 sequences of 512 heads
+    n = 1 << 20
+    empty, lengths = torch.empty((n, 0), dtype=torch.int32, device="cuda"), torch.zeros(n, dtype=torch.int32, device="cuda")
+    starts = torch.zeros(n + 1, dtype=torch.int32, device="cuda")
+    none, k = lam.kv_pages(0, 512, D, 32), torch.zeros((1, 512, D), dtype=torch.float16, device="cuda")
+    for call in (lambda: lam.kv_append(k, k, none, empty, lengths, starts=starts),
+                 lambda: lam.kv_read(none, empty, lengths, 1, D, starts=starts)):
+        with pytest.raises(lam.LamError) as e:
+            call()
+        assert e.value.name == "LAM_EINVAL"
