@@ -67,8 +67,18 @@ lam_kv_slots or_none(const lam_kv_slots* s) { return s ? *s : lam_kv_slots{nullp
 // slots that a call writes: one of its own for each sequence and head
 lam_status check_own(const lam_kv_slots& s, const lam_kv_view* v, const char* name) {
   if (s.p_dev == nullptr) return LAM_OK;
-  LAM_CHECK(s.head_stride >= s.cols || v->kv_heads == 1, LAM_EINVAL, "%s: heads overlap", name);
-  LAM_CHECK(s.seq_stride >= s.cols || v->n_seqs <= 1, LAM_EINVAL, "%s: sequences overlap", name);
+  const int64_t n = v->n_seqs, heads = v->kv_heads, cols = s.cols, seq = s.seq_stride, head = s.head_stride;
+  LAM_CHECK(head >= cols || heads == 1, LAM_EINVAL, "%s: heads overlap", name);
+  LAM_CHECK(seq >= cols || n <= 1, LAM_EINVAL, "%s: sequences overlap", name);
+  if (n <= 1 || heads == 1 || cols == 0) return LAM_OK;
+  // heads within a sequence, as they lie mostly; else a head's slots are compared with those of
+  // the sequences that begin next to them
+  if (seq / heads >= head) return LAM_OK;
+  for (int64_t h = 1; h < heads; ++h) {
+    const int64_t at = h * head, q = at / seq;
+    LAM_CHECK(!(q < n && at - q * seq < cols) && !(q + 1 < n && (q + 1) * seq - at < cols), LAM_EINVAL,
+              "%s: heads of one sequence overlap those of another", name);
+  }
   return LAM_OK;
 }
 

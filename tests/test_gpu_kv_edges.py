@@ -151,3 +151,33 @@ def test_launches_too_large_are_refused_before_anything_is_written(lam):
         with pytest.raises(lam.LamError) as e:
             call()
         assert e.value.name == "LAM_EINVAL"
+
+
+def test_slots_that_overlap_are_refused(lam):
+    """Two slots of one element would be written by two workgroups; any layout without is taken."""
+    B, Hk, L = 3, 2, 40
+    c = Case(lam, 64, 32, Hk, 2, "f16", [1] * B, [40, 25, 33], seed=1)
+    k = torch.zeros((B, Hk, 64), dtype=torch.float16, device="cuda")
+
+    def strided(seq, head, dtype=torch.float32):
+        flat = torch.zeros(1 + (B - 1) * seq + (Hk - 1) * head + L, dtype=dtype, device="cuda")
+        return flat[1:].as_strided((B, Hk, L), (seq, head, 1))
+
+    pool = c.pool.clone()
+    for seq, head in ((40, 40), (40, 60), (60, 90), (40, 80), (41, 82), (79, 40), (100, 139), (80, 199)):
+        for call in (lambda: lam.kv_append(k, k, c.pool, c.table, c.lengths, weights=strided(seq, head)),
+                     lambda: lam.kv_append(k, k, c.pool, c.table, c.lengths, first=c.lengths,
+                                           positions=strided(seq, head, torch.int32)),
+                     lambda: c.call(weights=strided(seq, head)),
+                     lambda: lam.kv_evict(c.pool, c.table, c.lengths, torch.zeros((B, Hk, L), device="cuda"), 20, 64,
+                                          out=(strided(seq, head), None, c.lengths))):
+            with pytest.raises(lam.LamError) as e:
+                call()
+            assert e.value.name == "LAM_EINVAL"
+    assert torch.equal(pool, c.pool) and c.lengths.tolist() == c.lens
+    want = torch.zeros((B, Hk, L), device="cuda")
+    c.call(weights=want)
+    for seq, head in ((80, 40), (40, 120), (83, 41), (100, 50), (50, 200), (40, 1000), (100, 140), (80, 200)):
+        w = strided(seq, head)
+        c.call(weights=w)
+        assert torch.equal(w, want)
