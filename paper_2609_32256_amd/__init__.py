@@ -398,6 +398,13 @@ def _kv_view(dev, pages, table, lengths, starts, rows, head_dim, dtype):
     return v, n, heads, (table, lengths, starts)
 
 
+def _kv_graphless(t, name):
+    """Refuses a tensor whose gradient the call would drop: the cache's operators have none."""
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name} requires a gradient, which the 4-bit cache's operators do not have: "
+                         "call them under torch.no_grad() or with a detached tensor")
+
+
 def _kv_elsewhere(ctx):
     """Whether a context's stream is not the current one: copies and outputs of its
     calls are then made on its own."""
@@ -411,6 +418,8 @@ def _kv_rows(t, heads, name, dev):
     _kv_tensor(t, t.dtype, 3, name, dev)
     if heads is not None and t.shape[1] != heads:
         raise ValueError(f"{name} must have {heads} heads")
+    if t.requires_grad:
+        _kv_graphless(t, name)
     row, head, step = t.stride()
     return t if step == 1 and row > 0 and head > 0 else t.contiguous()
 
@@ -425,6 +434,8 @@ def _kv_slots(t, dtype, n, heads, name, dev, shared=False, copy=False):
     seqs, own, cols = t.shape
     if seqs != n or not (own == heads or (shared and own == 1)):
         raise ValueError(f"{name} must be (sequences, heads, slots)")
+    if t.requires_grad:
+        _kv_graphless(t, name)
     if cols > 1 and t.stride(2) != 1:
         if not copy:
             raise ValueError(f"the slots of {name} must be contiguous")
@@ -501,7 +512,8 @@ def kv_attend(q: torch.Tensor, pages: torch.Tensor, table: torch.Tensor, lengths
     tokens out; weights (float32: sequences, kv_heads, slots) is added to what
     each token received; lse (float32: rows, q_heads) receives the scores' log
     sums.  Rows that see no token, those of no sequence among them, get 0 (lse -inf).
-    max_length, where the caller knows a bound of lengths, sizes the launch."""
+    max_length, where the caller knows a bound of lengths, sizes the launch.  There is
+    no gradient: tensors that require one are refused outside torch.no_grad()."""
     if ctx is None:
         ctx = default_context()
     elif _kv_elsewhere(ctx):
@@ -521,10 +533,12 @@ def kv_attend(q: torch.Tensor, pages: torch.Tensor, table: torch.Tensor, lengths
         _kv_tensor(out, q.dtype, 3, "out", dev)
         if out.shape != q.shape or not out.is_contiguous():
             raise ValueError("out must be contiguous and of q's shape")
+        _kv_graphless(out, "out")
     if lse is not None:
         _kv_tensor(lse, torch.float32, 2, "lse", dev)
         if lse.shape != q.shape[:2] or not lse.is_contiguous():
             raise ValueError("lse must be contiguous and (rows, q_heads)")
+        _kv_graphless(lse, "lse")
     _check(_lib.lam_kv_attend(ctx.handle, view, q.data_ptr(), q.stride(0), q.stride(1), q_heads,
                               head_dim ** -0.5 if scale is None else float(scale), 1 if causal else 0,
                               0 if max_length is None else max(1, int(max_length)), m, w, out.data_ptr(),

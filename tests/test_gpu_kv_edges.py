@@ -181,3 +181,29 @@ def test_slots_that_overlap_are_refused(lam):
         w = strided(seq, head)
         c.call(weights=w)
         assert torch.equal(w, want)
+
+
+def test_gradients_are_not_dropped_unseen(lam):
+    """The operators have no gradient: tensors that require one are refused, but under no_grad."""
+    c = Case(lam, 64, 32, 1, 2, "f16", [1], [40], seed=2)
+    k, w = torch.zeros((1, 1, 64), dtype=torch.float16, device="cuda"), torch.zeros((1, 1, 40), device="cuda")
+    out, lse = torch.zeros_like(c.q), torch.zeros((1, 2), device="cuda")
+    want = c.call()
+
+    def grad(t):
+        return t.clone().requires_grad_()
+
+    pool = c.pool.clone()
+    for call in (lambda: lam.kv_attend(grad(c.q), c.pool, c.table, c.lengths),
+                 lambda: lam.kv_attend(grad(c.q) * 2, c.pool, c.table, c.lengths),
+                 lambda: c.call(weights=grad(w)), lambda: c.call(out=grad(out)), lambda: c.call(lse=grad(lse)),
+                 lambda: lam.kv_append(grad(k), k, c.pool, c.table, c.lengths),
+                 lambda: lam.kv_append(k, grad(k), c.pool, c.table, c.lengths),
+                 lambda: lam.kv_evict(c.pool, c.table, c.lengths, grad(w), 20, 64)):
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+    assert torch.equal(pool, c.pool)
+    with torch.no_grad():
+        assert torch.equal(lam.kv_attend(grad(c.q), c.pool, c.table, c.lengths), want)
+    with torch.inference_mode():
+        assert torch.equal(lam.kv_attend(c.q, c.pool, c.table, c.lengths), want)
