@@ -40,7 +40,7 @@ class BoundedContext:
         self.weights = torch.zeros((n_seqs, kv_heads, slots), device=device)
         self.positions = torch.full((n_seqs, kv_heads, slots), -1, dtype=torch.int32, device=device)
         self.lengths = torch.zeros(n_seqs, dtype=torch.int32, device=device)   # cached tokens
-        self.lengths_next = torch.zeros_like(self.lengths)   # their own memory: a step's eviction is then one launch
+        self.lengths_next = torch.zeros_like(self.lengths)   # their own memory, see step()
         self.seen = torch.zeros(n_seqs, dtype=torch.int32, device=device)      # tokens so far: the next position
         self.status = torch.zeros(3, dtype=torch.int32, device=device)
 
@@ -55,8 +55,11 @@ class BoundedContext:
                       first=self.seen, status=self.status)
         self.seen += n
         out = lam.kv_attend(q, self.pages, self.table, self.lengths, weights=self.weights)
-        lam.kv_evict(self.pages, self.table, self.lengths, self.weights, self.budget, self.head_dim,
-                     recent=self.recent, sinks=self.sinks, positions=self.positions,
+        # No sequence has more than budget + n tokens here.  With columns for those alone, and new
+        # lengths in memory of their own, the eviction after a few tokens is one launch.
+        slots = self.budget + n
+        lam.kv_evict(self.pages, self.table, self.lengths, self.weights[..., :slots], self.budget, self.head_dim,
+                     recent=self.recent, sinks=self.sinks, positions=self.positions[..., :slots],
                      out=(self.weights, self.positions, self.lengths_next))
         self.lengths, self.lengths_next = self.lengths_next, self.lengths
         return out

@@ -114,3 +114,29 @@ def test_bad_steps_are_refused_or_reported(example):
     ctx.step(q, k, q)
     with pytest.raises(ValueError):
         ctx.check()
+
+
+def test_a_step_of_few_tokens_evicts_in_one_launch(example, lam):
+    """Whatever chunk the context has room for: the tokens given up are moved by the launch that
+    selects them."""
+    n_seqs, budget, chunk = 2, 128, 512
+    ctx = example.BoundedContext(n_seqs, 1, 64, budget, chunk, recent=8, sinks=2)
+    q, k, v = example.stream(n_seqs, 300, 1, 2, 64, seed=5)
+
+    def step(at, n):
+        return ctx.step(*(x[at:at + n].transpose(0, 1).flatten(0, 1) for x in (q, k, v)))
+
+    step(0, 250)
+    lib = lam.default_context()
+    lib.profile(True)
+    lib.profile_reset()
+    step(250, 1)
+    step(251, 40)
+    lib.synchronize()
+    selects, moves = lib.profile_read("kv_select")[1], lib.profile_read("kv_move")[1]
+    lib.profile(False)
+    assert (selects, moves) == (2, 0)
+    assert ctx.lengths.tolist() == [budget] * n_seqs
+    newest = set(range(291 - 8, 291))
+    for s in range(n_seqs):
+        assert newest <= set(ctx.positions[s, 0, :budget].tolist())
