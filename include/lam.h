@@ -480,7 +480,9 @@ lam_status lam_kv_read(lam_ctx* ctx, const lam_kv_view* view, void* k_dev, void*
  * gets 0 (lse -inf).  Scores, maxima and sums are float32; p enters the product
  * with the values as float16 relative to the row's maximum so far.  A query with
  * NaN or Inf spoils its own row only, and the weights of the tokens that it sees.  q [rows][q_heads][head_dim] of
- * view->dtype, out likewise and contiguous; lse_dev (float32[rows][q_heads], or
+ * view->dtype, out likewise and contiguous (apart from q, or q itself where that is contiguous;
+ * EINVAL where weights need a second pass over the queries: for more than 64 rows times heads
+ * of a group per sequence, or kept scores over the 1 GiB below); lse_dev (float32[rows][q_heads], or
  * NULL): log sum_t exp(scale * q . k_hat_t).
  * weights (float32, or NULL): the sum of p over the call's rows of s and the
  * query heads of h is added to element (s, h, t); tokens past its columns are

@@ -512,7 +512,8 @@ def kv_attend(q: torch.Tensor, pages: torch.Tensor, table: torch.Tensor, lengths
     tokens out; weights (float32: sequences, kv_heads, slots) is added to what
     each token received; lse (float32: rows, q_heads) receives the scores' log
     sums.  Rows that see no token, those of no sequence among them, get 0 (lse -inf).
-    max_length, where the caller knows a bound of lengths, sizes the launch.  There is
+    max_length, where the caller knows a bound of lengths, sizes the launch.  out may be q
+    itself, if contiguous (but for chunks with weights, which read q twice).  There is
     no gradient: tensors that require one are refused outside torch.no_grad()."""
     if ctx is None:
         ctx = default_context()

@@ -166,6 +166,13 @@ lam_status lam_kv_attend(lam_ctx* ctx, const lam_kv_view* view, const void* q_de
   LAM_CHECK(aligned(q_dev, 2) && aligned(out_dev, 16) && aligned(lse_dev, 4), LAM_EINVAL,
             "q must be 2-byte, out 16-byte and lse 4-byte aligned");
   LAM_CHECK(q_row_stride >= 0 && q_head_stride >= 0, LAM_EINVAL, "strides must be >= 0");
+  // a workgroup reads its queries before it writes their results, in the same places where out is q
+  const int64_t row = (int64_t)q_heads * view->head_dim;
+  const uintptr_t q0 = reinterpret_cast<uintptr_t>(q_dev), o0 = reinterpret_cast<uintptr_t>(out_dev);
+  const uintptr_t q1 = q0 + 2 * ((view->rows - 1) * q_row_stride + (q_heads - 1) * q_head_stride + view->head_dim);
+  const bool apart = q1 <= o0 || o0 + 2 * view->rows * row <= q0;
+  const bool same = q0 == o0 && (q_row_stride == row || view->rows == 1) && (q_head_stride == view->head_dim || q_heads == 1);
+  LAM_CHECK(apart || same, LAM_EINVAL, "out overlaps q (it may be q itself, where that is contiguous)");
   DeviceGuard g(ctx->device);
   return launch_kv_attend(ctx, *view, q_dev, q_row_stride, q_head_stride, q_heads, (float)scale, causal != 0,
                           max_length, m, w, out_dev, lse_dev);

@@ -558,7 +558,7 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
   const int64_t parts = a.split_to ? blocks * rows : 0;
   a.kept_cols = (a.cut + kKeptTokens - 1) / kKeptTokens * kKeptTokens;
   const bool keep = weights.p_dev && !chunk && pairs <= kKeptBytes / 4 / std::max<int64_t>(a.kept_cols, 1);
-  // every launch's size, before the first is queued: a call that is refused has written nothing
+  // every refusal, before the first launch is queued: a call that is refused has written nothing
   a.join_rows = units * rows <= kJoinFew ? 1 : kJoinRows;
   const int64_t join_blocks = a.split_to ? units * (rows / (kAttWaves * a.join_rows)) : 0;
   int64_t kept_blocks = keep ? a.kept_cols / kKeptTokens * v.kv_heads * v.n_seqs : 0;
@@ -573,6 +573,7 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
   LAM_CHECK(std::max({blocks, join_blocks + kept_blocks, weight_blocks}) <= most_blocks(kAttThreads), LAM_EINVAL,
             "too many rows, or sequences times the bound of lengths, for one launch (%lld tokens: give max_length)",
             (long long)a.cut);
+  LAM_CHECK(weight_blocks == 0 || q != out, LAM_EINVAL, "out is q, which the weights take a second pass over");
   const int64_t floats = (keep ? pairs * a.kept_cols : 0) + parts * (v.head_dim + 2) + (weights.p_dev ? pairs : 0);
   void* scratch = nullptr;
   if (floats > 0) LAM_TRY(kv_scratch(ctx, (size_t)floats * 4, &scratch));

@@ -207,3 +207,31 @@ def test_gradients_are_not_dropped_unseen(lam):
         assert torch.equal(lam.kv_attend(grad(c.q), c.pool, c.table, c.lengths), want)
     with torch.inference_mode():
         assert torch.equal(lam.kv_attend(c.q, c.pool, c.table, c.lengths), want)
+
+
+@pytest.mark.parametrize("n", [1, 90])
+def test_results_in_place_of_the_queries(lam, n):
+    """out may be q, but where a second pass takes the weights from the queries."""
+    for lens in ([200], [3000]):
+        c = Case(lam, 64, 32, 2, 4, "bf16", [n], lens, seed=n)
+        w = torch.zeros((1, 2, lens[0]), device="cuda")
+        want, q = c.call(weights=w), c.q.clone()
+        again = torch.zeros_like(w)
+        if n > 1:
+            with pytest.raises(lam.LamError) as e:
+                c.call(out=c.q, weights=again)
+            assert e.value.name == "LAM_EINVAL" and torch.equal(c.q, q) and not again.any()
+        else:
+            assert torch.equal(c.call(out=c.q, weights=again), want) and torch.equal(again, w)
+            c.q.copy_(q)
+        assert torch.equal(c.call(out=c.q), want) and torch.equal(c.q, want)
+        flat = torch.zeros((n + 1) * 512, dtype=torch.bfloat16, device="cuda")
+        for at in (8, 256, 504):                             # parts of one buffer
+            a, b = flat[at:at + n * 512].view(n, 8, 64), flat[:n * 512].view(n, 8, 64)
+            for x, y in ((a, b), (b, a)):
+                with pytest.raises(lam.LamError):
+                    lam.kv_attend(x, c.pool, c.table, c.lengths, out=y)
+        assert not flat.any()
+        both = torch.cat([q, q])                             # next to each other
+        lam.kv_attend(both[:n], c.pool, c.table, c.lengths, out=both[n:], weights=torch.zeros_like(w))
+        assert torch.equal(both[n:], want) and torch.equal(both[:n], q)
