@@ -344,10 +344,18 @@ _KV_HEADS = (64, 128, 256)
 _KV_PAGES = (32, 64, 128, 256, 512, 1024)
 
 
+def _kv_int(x, name):
+    """A Python integer that is a C int32 (ctypes would take its low 32 bits)."""
+    x = int(x)
+    if not -(1 << 31) <= x < 1 << 31:
+        raise ValueError(f"{name} must be a 32-bit integer, got {x}")
+    return x
+
+
 def kv_pages(n_pages: int, kv_heads: int, head_dim: int, page_size: int = 64, device=None) -> torch.Tensor:
     """An empty pool of cache pages: uint8 (n_pages, kv_heads, bytes of a head's
     page).  head_dim 64, 128 or 256; page_size a power of two, 32 to 1024."""
-    size = _lib.lam_kv_page_bytes(int(head_dim), int(page_size))
+    size = _lib.lam_kv_page_bytes(_kv_int(head_dim, "head_dim"), _kv_int(page_size, "page_size"))
     if size < 0:
         raise ValueError("head_dim must be 64, 128 or 256 and page_size a power of two from 32 to 1024")
     return torch.zeros((int(n_pages), int(kv_heads), size), dtype=torch.uint8, device=device or "cuda")
@@ -568,17 +576,18 @@ def kv_evict(pages: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, sc
     p, hold_p = _kv_slots(positions, torch.int32, n, heads, "positions", dev, copy=True)
     if s is None:
         raise TypeError("scores must be a CUDA (HIP) tensor")
-    kept = lengths.new_empty((n, heads, int(budget)))
+    budget, recent, sinks = _kv_int(budget, "budget"), _kv_int(recent, "recent"), _kv_int(sinks, "sinks")
+    kept = lengths.new_empty((n, heads, max(budget, 0)))
     if out is None:
         out = (torch.empty_like(kept, dtype=torch.float32), torch.empty_like(kept), torch.empty_like(hold[1]))
-        so, po = (_KV_SLOTS.pack(t.data_ptr(), heads * int(budget), int(budget), int(budget)) for t in out[:2])
+        so, po = (_KV_SLOTS.pack(t.data_ptr(), heads * budget, budget, budget) for t in out[:2])
     else:
         so, _ = _kv_slots(out[0], torch.float32, n, heads, "out scores", dev)
         po, _ = _kv_slots(out[1], torch.int32, n, heads, "out positions", dev)
         _kv_tensor(out[2], torch.int32, 1, "out lengths", dev)
         if out[2].numel() != n or not out[2].is_contiguous():
             raise ValueError("out lengths must be contiguous, an entry for each sequence")
-    _check(_lib.lam_kv_evict(ctx.handle, view, s, p, int(budget), int(recent), int(sinks), kept.data_ptr(), so, po,
+    _check(_lib.lam_kv_evict(ctx.handle, view, s, p, budget, recent, sinks, kept.data_ptr(), so, po,
                              out[2].data_ptr()))
     return kept, out[0], out[1], out[2]
 

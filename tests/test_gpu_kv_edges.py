@@ -235,3 +235,20 @@ def test_results_in_place_of_the_queries(lam, n):
         both = torch.cat([q, q])                             # next to each other
         lam.kv_attend(both[:n], c.pool, c.table, c.lengths, out=both[n:], weights=torch.zeros_like(w))
         assert torch.equal(both[n:], want) and torch.equal(both[:n], q)
+
+
+def test_numbers_beyond_32_bits_are_refused(lam):
+    """Not taken for their low 32 bits."""
+    pool, table, lengths = lam.kv_pages(2, 1, 64, 32), _i32([[0, 1]]), _i32([40])
+    w = torch.zeros((1, 1, 40), device="cuda")
+    for bad in (dict(recent=(1 << 32) + 3), dict(sinks=1 << 32), dict(recent=-(1 << 32)), dict(recent=1 << 31)):
+        with pytest.raises(ValueError):
+            lam.kv_evict(pool, table, lengths, w, 20, 64, **bad)
+    with pytest.raises(ValueError):
+        lam.kv_evict(pool, table, lengths, w, (1 << 32) + 20, 64)
+    with pytest.raises(lam.LamError):
+        lam.kv_evict(pool, table, lengths, w, -5, 64)
+    for bad in (dict(head_dim=(1 << 32) + 64), dict(head_dim=64, page_size=(1 << 32) + 32)):
+        with pytest.raises(ValueError):
+            lam.kv_pages(1, 1, **bad)
+    assert lengths.tolist() == [40]
