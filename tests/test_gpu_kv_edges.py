@@ -252,3 +252,43 @@ def test_numbers_beyond_32_bits_are_refused(lam):
         with pytest.raises(ValueError):
             lam.kv_pages(1, 1, **bad)
     assert lengths.tolist() == [40]
+
+
+# ------------------------------------------------------------------ paths with no other test
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_read_gives_zeros_for_rows_of_no_sequence(lam, D):
+    k, v = (torch.randn((5, 2, D), device="cuda").half() for _ in range(2))
+    pool, table, lens = lam.kv_pages(2, 2, D, 32), _i32([[0], [1]]), _i32([3, 4])
+    lam.kv_append(k, v, pool, table, lens, starts=_i32([0, 3, 5]))
+    for fill in range(2):                                    # memory that another call has just filled
+        full = lam.kv_read(pool, table, lens, 9, D, dtype=torch.float16, starts=_i32([2, 5, 7]))
+        for x, y in zip(full, (k, v)):
+            assert np.array_equal(_np(x[2:7]), kv.rounded(_np(y)))
+            assert not x[:2].any() and not x[7:].any()
+            x.fill_(float("nan"))
+        del full, x
+    a, b = lam.kv_read(pool, table, lens, 700, D, dtype=torch.float16, starts=_i32([700, 700, 700]))
+    assert not a.any() and not b.any()
+
+
+@pytest.mark.parametrize("n", [1, 90])                       # scores kept, a second pass
+@pytest.mark.parametrize("length", [700, 3000])              # whole, in parts
+def test_weights_and_log_sums_of_any_scale(lam, n, length):
+    for spread, scale in ((30.0, None), (1e-3, None), (1.0, 3.0), (1.0, -0.5), (20.0, -0.1), (1.0, 0.0)):
+        c = Case(lam, 128, 64, 1, 4, "bf16", [n], [length], seed=int(spread), spread=spread)
+        lse = torch.empty(c.q.shape[:2], device="cuda")
+        w = torch.zeros((1, 1, length), device="cuda")
+        c.check(c.call(scale=scale, lse=lse, weights=w), scale=scale, lse=lse, weights=w)
+
+
+@pytest.mark.parametrize("G,n", [(4, 1), (16, 4), (4, 40)])  # a wave a token, four, a second pass
+@pytest.mark.parametrize("cols", [0, 1, 33, 130, 255, 1030])
+def test_weights_of_fewer_columns_than_tokens(lam, G, n, cols):
+    lens, Hk = [1200, 90], 2
+    c = Case(lam, 64, 32, Hk, G, "f16", [n] * 2, lens, seed=n)
+    full = torch.zeros((2, Hk, 1200), device="cuda")
+    c.check(c.call(weights=full), weights=full)
+    wide = torch.full((2, Hk, 1200), 9.0, device="cuda")
+    wide[..., :cols] = 0
+    c.call(weights=wide[..., :cols])
+    assert torch.equal(wide[..., :cols], full[..., :cols]) and (wide[..., cols:] == 9).all()
