@@ -493,8 +493,9 @@ lam_status lam_kv_read(lam_ctx* ctx, const lam_kv_view* view, void* k_dev, void*
  * lengths are split, partial results of at most 45 MB; with weights 4 bytes for each
  * query row and head, and for up to 64 rows times heads of a group per sequence 4
  * bytes for each of them and each token of the bound, at most 1 GiB.  It is kept for later
- * calls, grows to twice its size at least, and is freed with the context, also what a larger one
- * replaced: a graph that recorded the call stays valid while the context lives (its replays
+ * calls and grows to twice its size at least, so it may be up to twice what the largest call
+ * needs; what it replaced, together no more than it, stays too, and all is freed with the
+ * context: a graph that recorded the call stays valid while the context lives (its replays
  * and the context's other calls must not overlap, since they share it).  A call that would
  * grow it cannot be recorded; the same call made once before has grown it.  Asynchronous. */
 lam_status lam_kv_attend(lam_ctx* ctx, const lam_kv_view* view, const void* q_dev, int64_t q_row_stride,
@@ -514,8 +515,13 @@ lam_status lam_kv_attend(lam_ctx* ctx, const lam_kv_view* view, const void* q_de
  * length), scores_out and positions_out (at least budget columns, which may be
  * scores and positions themselves; 0 and -1 past the length; positions_out may
  * be NULL), lengths_out_dev (int32 [n_seqs]: min(length, budget); may be the
- * view's).  Lengths are cut to the columns of scores and positions.  view->rows,
- * starts and dtype are not used.  Sequences must not share pages.  Asynchronous. */
+ * view's).  Lengths are cut to the columns of scores and positions; a call whose columns
+ * are few more than budget (64) and whose lengths_out is not the view's takes one launch, others
+ * two.  n_seqs * kv_heads < 65536 (EINVAL).  view->rows, starts and dtype are not used.
+ * Sequences must not share pages.  Context scratch: 8 bytes for each sequence, head and slot
+ * that can move (the lesser of budget and of the bound of lengths less budget), where that bound
+ * (of the table and the columns) is over 65,536 slots, else none; the same memory as
+ * lam_kv_attend's, with its rules for graphs.  Asynchronous. */
 lam_status lam_kv_evict(lam_ctx* ctx, const lam_kv_view* view, const lam_kv_slots* scores,
                         const lam_kv_slots* positions, int32_t budget, int32_t recent, int32_t sinks,
                         int32_t* kept_dev, const lam_kv_slots* scores_out, const lam_kv_slots* positions_out,

@@ -347,7 +347,8 @@ __global__ __launch_bounds__(kAttThreads) void k_kv_finish(AttendArgs a, uint32_
 // whose keys each wave converts once; its waves share the call's rows, 16 at a time, the
 // next 16 on their way; p = 2^(s - lse).  The waves' sums are added in their order, so the
 // result does not depend on timing.  Bound by issue: an exponential, two additions or
-// multiplications a score beside the products, and the queries from the L2 for every
+// multiplications a score beside the products (64 channels: vector instructions active in 62 % of
+// a SIMD's cycles, the matrix unit busy in 20), and the queries from the L2 for every
 // workgroup.  2,048 rows of 32 heads over 16,384 tokens, 8 key/value heads of 128 channels:
 // 267 us (64 tokens a workgroup 490, and 32 with all rows to each wave more).
 template <int D>

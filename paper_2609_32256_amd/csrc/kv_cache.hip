@@ -381,9 +381,11 @@ __device__ __forceinline__ void move_token(const KvArgs& a, int bh, int D, int f
 }
 
 // Most moves of a head that its selection makes itself, which saves the launch that
-// would: 24 sequences of 4,097 tokens and 8 heads of 128 channels cut to 4,096 take 18 us
-// for 26, of 4,160 tokens 22 for 30.  (Not where the new lengths replace those that the
-// other heads' selections still read.)
+// would.  Heads of 128 channels cut to 4,096 tokens, in a recorded graph with a copy of the lengths:
+// 24 sequences of 8 heads with 1 move a head 13 us for 19, with 64 18 for 24, with 128
+// 24 for 27, with 256 36 for 32; 96 sequences with 64 38 for 61, with 512 143 for 115;
+// one sequence with 16 13 for 14, with 64 18 for 15.  (Not where the new lengths replace those
+// that the other heads' selections still read.)
 constexpr int kOwnMoves = 64;
 
 // The largest of the threads' values (one barrier; tops: of the workgroup's own).
@@ -623,8 +625,9 @@ __global__ __launch_bounds__(kSelThreads) void k_kv_select(KvArgs a, EvictArgs e
 }
 
 // The same for longer caches, whose keys are made from memory each time: the
-// budget-th largest key digit by digit (four histograms of 256 counts), then one pass over the
-// slots in order, and lists in memory.
+// newest position, the budget-th largest key digit by digit (four histograms of 256 counts),
+// then one pass over the slots in order, and lists in memory.  Bound by the round trips of one
+// workgroup a head: 4 heads of 131,072 slots cut to 60,000 take 438 us (3 for the bytes).
 __global__ __launch_bounds__(kSelThreads) void k_kv_select_long(KvArgs a, EvictArgs e) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const EvictHead d(a, e, blockIdx.x);
