@@ -345,7 +345,7 @@ _KV_PAGES = (32, 64, 128, 256, 512, 1024)
 
 
 def _kv_int(x, name):
-    """A Python integer that is a C int32 (ctypes would take its low 32 bits)."""
+    """A Python integer as a C int32, of which ctypes would take the low 32 bits."""
     x = int(x)
     if not -(1 << 31) <= x < 1 << 31:
         raise ValueError(f"{name} must be a 32-bit integer, got {x}")
@@ -576,7 +576,9 @@ def kv_evict(pages: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, sc
     p, hold_p = _kv_slots(positions, torch.int32, n, heads, "positions", dev, copy=True)
     if s is None:
         raise TypeError("scores must be a CUDA (HIP) tensor")
-    budget, recent, sinks = _kv_int(budget, "budget"), _kv_int(recent, "recent"), _kv_int(sinks, "sinks")
+    budget, recent, sinks = int(budget), int(recent), int(sinks)
+    if max(budget, recent, sinks) >= 1 << 31 or min(budget, recent, sinks) < -(1 << 31):
+        raise ValueError(f"budget, recent and sinks must be 32-bit integers, got {budget}, {recent}, {sinks}")
     kept = lengths.new_empty((n, heads, max(budget, 0)))
     if out is None:
         out = (torch.empty_like(kept, dtype=torch.float32), torch.empty_like(kept), torch.empty_like(hold[1]))

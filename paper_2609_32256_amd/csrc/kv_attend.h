@@ -234,8 +234,8 @@ __device__ __forceinline__ Work work_of(const AttendArgs& a, uint32_t id) {
   return a.split_to ? plan<R, PlanOf::kWorkgroup>(a, id) : tile_work<R>(a, id);
 }
 
-// Rows of no sequence see no token: 0, and a log sum of -inf.  (Read after the workgroup's
-// work is known, which has brought starts into the caches.)
+// Rows of no sequence see no token: 0, and a log sum of -inf.  (A workgroup's last work:
+// as its first it cost 0.2 us of 26 and registers.)
 template <int D>
 __device__ __forceinline__ void clear_rows(const AttendArgs& a) {
   if (!a.c.starts) return;

@@ -94,8 +94,10 @@ __global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : 3) void k_kv_attend(Att
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Work w = work_of<kAttRows>(a, blockIdx.x);
-  clear_rows<D>(a);
-  if (w.s < 0) return;
+  if (w.s < 0) {
+    clear_rows<D>(a);
+    return;
+  }
   const int h = w.h;
   const int T = 1 << a.c.page_shift;
   const int64_t head_bytes = KvLayout<D>::head_bytes(T);
@@ -159,6 +161,7 @@ __global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : 3) void k_kv_attend(Att
   kv_f4(&o)[kRun] = r.o;
   __shared__ JoinSpace<D> js;
   join_waves<D, BF16>(a, w, w.r0, (int64_t)blockIdx.x * kAttRows, r.row, r.o, js);
+  clear_rows<D>(a);
 }
 
 // Maxima and sums of N rows over their parts, by a wave: lane i reads part i's (a lane

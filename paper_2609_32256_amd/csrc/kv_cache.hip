@@ -449,14 +449,15 @@ __global__ __launch_bounds__(kSelThreads) void k_kv_select(KvArgs a, EvictArgs e
   constexpr int kBatch = KPT < 16 ? KPT : KPT > 32 ? 8 : 16;   // (16 of 64 spill)
   int newest = len - 1;
   if (d.ps) {   // (read twice, the second time from the caches: held in registers, they spill)
+    constexpr int kTops = KPT < 16 ? KPT : 16;
     int top = (int)0x80000000u;
 #pragma unroll 1
-    for (int t0 = tid; t0 < len; t0 += kBatch * kSelThreads) {
-      int p[kBatch];
+    for (int t0 = tid; t0 < len; t0 += kTops * kSelThreads) {
+      int p[kTops];
 #pragma unroll
-      for (int j = 0; j < kBatch; ++j) p[j] = d.ps[(uint32_t)min(t0 + j * kSelThreads, len - 1)];
+      for (int j = 0; j < kTops; ++j) p[j] = d.ps[(uint32_t)min(t0 + j * kSelThreads, len - 1)];
 #pragma unroll
-      for (int j = 0; j < kBatch; ++j) top = max(top, p[j]);
+      for (int j = 0; j < kTops; ++j) top = max(top, p[j]);
     }
     newest = largest(top, sums[0]);
   }

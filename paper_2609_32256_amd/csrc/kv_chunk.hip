@@ -24,8 +24,10 @@ __global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : D == 64 ? 3 : 2) void k
   const int lane = threadIdx.x & 63, c = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Work w = work_of<kRows>(a, blockIdx.x);
-  clear_rows<D>(a);
-  if (w.s < 0) return;
+  if (w.s < 0) {
+    clear_rows<D>(a);
+    return;
+  }
   const int T = 1 << a.c.page_shift;
   const int64_t head_bytes = KvLayout<D>::head_bytes(T);
 
@@ -148,6 +150,7 @@ __global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : D == 64 ? 3 : 2) void k
     if (t > 0) __syncthreads();   // (all 256 threads get here for every tile)
     join_waves<D, BF16>(a, w, w.r0 + 16 * t, (int64_t)blockIdx.x * kRows + 16 * t, row[t], o[t], js);
   }
+  clear_rows<D>(a);
 }
 
 }  // namespace
