@@ -1,5 +1,7 @@
 """The 4-bit key/value cache on the GPU at the edges of its contract: evictions that
-follow each other, weights added to large ones, rows of no sequence.  Against the binary64 oracle; tolerances as in test_gpu_kv_attend.
+follow each other, weights added to large ones, rows of no sequence, lengths beyond
+the table, and what is refused.  Against the binary64 oracle; tolerances as in
+test_gpu_kv_attend where none are given.
 """
 import numpy as np
 import pytest
@@ -292,3 +294,33 @@ def test_weights_of_fewer_columns_than_tokens(lam, G, n, cols):
     wide[..., :cols] = 0
     c.call(weights=wide[..., :cols])
     assert torch.equal(wide[..., :cols], full[..., :cols]) and (wide[..., cols:] == 9).all()
+
+
+@pytest.mark.parametrize("n", [2, 70])
+@pytest.mark.parametrize("cap", [128, 2560])
+def test_lengths_that_cannot_be(lam, n, cap):
+    """A negative length is 0; the rows of one near 2^31 see every token that the table has."""
+    c = Case(lam, 64, 32, 2, 2, "f16", [n] * 3, [cap, cap, cap], seed=n)
+    c.lengths = _i32([-3, (1 << 31) - 1, -(1 << 31)])
+    lse, w = torch.empty(c.q.shape[:2], device="cuda"), torch.zeros((3, 2, cap), device="cuda")
+    out = c.call(lse=lse, weights=w)
+    for s in (0, 2):
+        rows = slice(s * n, s * n + n)
+        assert not out[rows].any() and torch.isneginf(lse[rows]).all() and not w[s].any()
+    want, want_w = torch.empty_like(out), torch.zeros_like(w)
+    c.lengths = _i32([cap, cap, cap])
+    c.call(causal=False, out=want, weights=want_w)
+    assert torch.allclose(out[n:2 * n].float(), want[n:2 * n].float(), rtol=2.0 ** -9, atol=2.0 ** -11)
+    assert torch.allclose(w[1], want_w[1], rtol=2.0 ** -18, atol=0)
+    # nothing of the rows has a place, and nothing is written
+    pool, k = c.pool.clone(), torch.randn((3 * n, 2, 64), device="cuda").half()
+    status = torch.zeros(3, dtype=torch.int32, device="cuda")
+    bad = _i32([-3, (1 << 31) - 1, -(1 << 31)])
+    lam.kv_append(k, k, c.pool, c.table, bad, status=status)
+    assert status.tolist() == [0, 0, 3 * n * 2] and torch.equal(c.pool, pool)
+    assert not lam.kv_read(c.pool, c.table, bad, 3 * n, 64, dtype=torch.float16)[0].any()
+    scores = torch.rand((3, 2, cap), device="cuda")
+    kept, _, _, lo = lam.kv_evict(c.pool, c.table, bad, scores, 100, 64)
+    assert lo.tolist() == [0, 100, 0] and (kept[0] == -1).all() and (kept[2] == -1).all()
+    for h in range(2):
+        assert kept[1, h].tolist() == kv.evict(scores[1, h].tolist(), list(range(cap)), 100, 0, 0)
