@@ -435,8 +435,8 @@ __global__ __launch_bounds__(kSelThreads) void k_kv_select(KvArgs a, EvictArgs e
     return;
   }
   // Rounds of 1,024 slots past the length are skipped, so that a call pays for its length
-  // and not for KPT (4 heads of 43,136 slots cut by half 74 -> 55 us with the moves, one of 14,349
-  // cut to a tenth 26 -> 22).  The counts that are then not written follow all that are used.
+  // and not for KPT (4 heads of 43,136 slots cut by half 74 -> 55 us with the moves, 58 with the
+  // newest position looked for; one of 14,349 cut to a tenth 26 -> 22).  The counts that are then not written follow all that are used.
   const int len = __builtin_amdgcn_readfirstlane(d.len);
   __shared__ int32_t move_to[kOwnMoves], move_from[kOwnMoves];
   if (tid < kOwnMoves) move_to[tid] = -1;
