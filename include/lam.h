@@ -465,6 +465,65 @@ lam_status lam_kv_append(lam_ctx* ctx, const lam_kv_view* view, const void* k_de
                          const lam_kv_slots* weights, const lam_kv_slots* positions, const int32_t* first_dev,
                          uint32_t* status_dev);
 
+/* ---- norms of heads and rotation by position ---- */
+
+/* Frequencies of a rotation, in radians a position: freq[i] = base^(-i / pairs) (host
+ * memory, i < pairs), for contexts beyond the trained one scaled as
+ *   LAM_ROTARY_LINEAR  freq[i] / factor
+ *   LAM_ROTARY_BASE    a base of base * factor^(pairs / (pairs - 1)): the fastest pair keeps its
+ *                      frequency, the slowest has freq / factor
+ *   LAM_ROTARY_PARTS   freq[i] where the pair makes `high` turns or more over `length` positions,
+ *                      freq[i] / factor where it makes `low` or fewer, between them in proportion
+ * and the amplitude that goes with it (or NULL): 0.1 ln(factor) + 1 for PARTS, else 1.  Host only.
+ * EINVAL: base not above 0, factor below 1, low not below high. */
+enum { LAM_ROTARY_PLAIN = 0, LAM_ROTARY_LINEAR = 1, LAM_ROTARY_BASE = 2, LAM_ROTARY_PARTS = 3 };
+lam_status lam_rotary_frequencies(int32_t pairs, double base, int scaling, double factor, double length, double low,
+                                  double high, double* freq, double* amplitude);
+
+/* A rotation: channel pair i (channels i and i + pairs, or 2 i and 2 i + 1) of a row at position p
+ * is turned by a = p freq[i]:  (u, v) -> amplitude (u cos a - v sin a, u sin a + v cos a).
+ * Channels from 2 pairs on stay as they are.  Angles are right to 2^-50 of a turn at every
+ * position, negative ones among them (frequencies of up to 1 radian). */
+enum { LAM_ROTARY_HALF = 0, LAM_ROTARY_INTERLEAVED = 1 };
+typedef struct lam_rotary {
+  const double* freq_dev;        /* [pairs], radians a position */
+  int32_t pairs, layout;
+  double amplitude;
+} lam_rotary;
+
+/* Heads of rows ([rows][heads][head_dim] in 16 bits, strides in elements, channels contiguous) and
+ * where they go.  With gains a head is normed first: x -> gain x / sqrt(sum x^2 / norm_dim + eps),
+ * the sum over all channels; norm_dim (0: head_dim) is fewer where a smaller head is padded with
+ * zeros.  NaN and Inf spoil the pair (with a norm: the head) of their own row. */
+enum { LAM_F32 = 2 };
+typedef struct lam_heads {
+  const void* x_dev;
+  int64_t row_stride, head_stride;
+  void* y_dev;                   /* may be x_dev with x's strides, else apart from it */
+  int64_t y_row_stride, y_head_stride;
+  const void* gain_dev;          /* [head_dim], NULL: no norm */
+  int32_t gain_dtype;            /* LAM_F32 or the rows' type */
+  int32_t heads;
+} lam_heads;
+
+/* Norms and turns rows of queries and, where k is not NULL, of keys, each at its positions_dev
+ * (int32[rows]; may be NULL without pairs).  head_dim: a multiple of 8 up to 256.  Computed in
+ * float32 with angles in binary64, and rounded once.  No result may overlap anything else that the
+ * call reads or writes; rows of one stride that alternate in memory do not.  Asynchronous. */
+lam_status lam_kv_rotate(lam_ctx* ctx, const lam_rotary* rotary, const lam_heads* q, const lam_heads* k, int64_t rows,
+                         int32_t head_dim, int32_t dtype, const int32_t* positions_dev, double eps, int32_t norm_dim);
+
+/* lam_kv_append with the norm and the rotation on the way, in one launch: keys are normed, turned
+ * and then quantized (the code of the exact value, to 2^-50: computed in binary64 and rounded
+ * once), values quantized as they are.  q (NULL, or of any number of heads) is normed and turned at the same
+ * positions; its rows of no sequence become 0.  Row i of sequence s has the position first[s] + i, or,
+ * where first_dev is NULL, its token's slot; positions (optional) get it.  k's y_dev is not
+ * used.  Counts as lam_kv_append's, of the values that are quantized.  Asynchronous. */
+lam_status lam_kv_rotate_append(lam_ctx* ctx, const lam_kv_view* view, const lam_rotary* rotary, const lam_heads* q,
+                                const lam_heads* k, const void* v_dev, int64_t v_row_stride, int64_t v_head_stride,
+                                const lam_kv_slots* weights, const lam_kv_slots* positions, const int32_t* first_dev,
+                                double eps, int32_t norm_dim, uint32_t* status_dev);
+
 /* The values the cache holds for the call's rows, [rows][kv_heads][head_dim] of
  * view->dtype, contiguous (exact in both types).  Tokens without a place read
  * as 0.  Asynchronous. */

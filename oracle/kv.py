@@ -1,8 +1,8 @@
 """Oracle of the 4-bit key/value cache -- test infrastructure only.
 
 Plain binary64 NumPy, sequence by sequence and head by head: the block format
-(code by code, from its definition), the layout of a page, attention over the
-values the cache stands for, and eviction as a sort.
+(code by code, from its definition), the layout of a page, norms and rotations of
+heads, attention over the values the cache stands for, and eviction as a sort.
 """
 from __future__ import annotations
 
@@ -80,7 +80,59 @@ def pack_page(kc, ke, vc, ve):
     return out
 
 
+# ------------------------------------------------------------------ norm and rotation
+PI = Fraction(314159265358979323846264338327950288419716939937510582097494459230781640628621,
+              10 ** 77)
+
+
+def angle(position: int, frequency: float) -> float:
+    """position * frequency modulo a turn, from the exact product."""
+    a = int(position) * Fraction(float(frequency))
+    return float(a - 2 * PI * round(a / (2 * PI)))
+
+
+def frequencies(pairs, base=10000.0, scaling=None, factor=1.0, length=0.0, low=1.0, high=32.0):
+    """Radians a position of each pair, and the amplitude."""
+    if scaling == "base":
+        base = base * factor ** (pairs / (pairs - 1))
+    f = [base ** (-i / pairs) for i in range(pairs)]
+    if scaling == "linear":
+        f = [x / factor for x in f]
+    if scaling == "parts":
+        for i, x in enumerate(f):
+            turns = length * x / (2 * math.pi)
+            f[i] = x if turns >= high else x / factor if turns <= low else \
+                x / factor + (x - x / factor) * (turns - low) / (high - low)
+    return f, 0.1 * math.log(factor) + 1.0 if scaling == "parts" else 1.0
+
+
+def rotate(x, positions, freq, layout="half", amplitude=1.0, gain=None, eps=1e-6, norm_dim=None):
+    """Rows x [n, heads, D] normed and turned: (result, size), size being what the errors of
+    the result scale with: the sum of the sizes of the terms of each element."""
+    y = np.array(x, dtype=np.float64)
+    if gain is not None:
+        mean = (y * y).sum(-1, keepdims=True) / (norm_dim or y.shape[-1])
+        y = y / np.sqrt(mean + eps) * np.asarray(gain, dtype=np.float64)
+    out, size = y.copy(), np.abs(y)
+    n = len(freq)
+    for i, f in enumerate(freq):
+        a, b = (i, i + n) if layout == "half" else (2 * i, 2 * i + 1)
+        t = np.array([angle(p, f) for p in positions])[:, None]
+        u, v = y[..., a], y[..., b]
+        out[..., a] = amplitude * (u * np.cos(t) - v * np.sin(t))
+        out[..., b] = amplitude * (u * np.sin(t) + v * np.cos(t))
+        size[..., a] = size[..., b] = abs(amplitude) * (np.abs(u) + np.abs(v))
+    return out, size
+
+
 # ------------------------------------------------------------------ attention
+def in_window(n, length, window, sinks):
+    """Which tokens [n, length] the last n tokens' rows have in a window that ends with
+    themselves, or among the first."""
+    t, at = np.arange(length)[None, :], (length - n + np.arange(n))[:, None]
+    return (t > at - window) | (t < sinks)
+
+
 def attend(q, k, v, scale, causal=True, mask=None):
     """Rows q [n, D] (one head) over values k, v [len, D]: dict of
     out [n, D], p [n, len], lse [n], and what rounding errors scale with: mean
@@ -92,8 +144,8 @@ def attend(q, k, v, scale, causal=True, mask=None):
     seen = np.ones((n, length), dtype=bool)
     if causal:
         seen &= np.arange(length)[None, :] <= length - n + np.arange(n)[:, None]
-    if mask is not None:
-        seen &= np.asarray(mask, dtype=bool)[None, :]
+    if mask is not None:   # of the tokens, or of each row's
+        seen &= np.asarray(mask, dtype=bool).reshape(-1, length)
     p, lse = np.zeros((n, length)), np.full(n, -math.inf)
     for i in range(n):
         if seen[i].any():

@@ -22,6 +22,9 @@ built (``python paper_2609_32256_amd/build.py``) importing this module fails.
     lam.kv_append(k, v, pages, table, lengths)     # rows quantized into it
     o = lam.kv_attend(q, pages, table, lengths, weights=w)  # attention; what each token received
     lam.kv_evict(pages, table, lengths, w, budget, 128)     # back to the budget
+    f, amplitude = lam.rotary_frequencies(128)     # rotation by position, with a norm of each head where gains are given
+    q, k = lam.kv_rotate(q, f, positions, k=k)
+    q = lam.kv_rotate_append(q, k, v, pages, table, lengths, f, q_norm=gq, k_norm=gk)   # and into the cache
 """
 from __future__ import annotations
 
@@ -91,6 +94,9 @@ class BlockStats(ctypes.Structure):
 # third of the time that filling a ctypes.Structure does, on calls of some microseconds.
 _KV_VIEW = struct.Struct("@PqPqPPqiiiiii")
 _KV_SLOTS = struct.Struct("@Pqqi4x")
+# lam_rotary and lam_heads
+_ROTARY = struct.Struct("@Piid")
+_HEADS = struct.Struct("@PqqPqqPii")
 
 
 class CeilingStats(ctypes.Structure):
@@ -145,6 +151,12 @@ _SIGS = {
     "lam_kv_page_bytes": ([ctypes.c_int32, ctypes.c_int32], _I64),
     "lam_kv_append": ([_P, _P, _P, _I64, _I64, _P, _I64, _I64, _P,
                        _P, _P, _P], ctypes.c_int),
+    "lam_rotary_frequencies": ([ctypes.c_int32, ctypes.c_double, ctypes.c_int, ctypes.c_double, ctypes.c_double,
+                                ctypes.c_double, ctypes.c_double, _P, _P], ctypes.c_int),
+    "lam_kv_rotate": ([_P, _P, _P, _P, _I64, ctypes.c_int32, ctypes.c_int32, _P, ctypes.c_double, ctypes.c_int32],
+                      ctypes.c_int),
+    "lam_kv_rotate_append": ([_P, _P, _P, _P, _P, _P, _I64, _I64, _P, _P, _P, ctypes.c_double, ctypes.c_int32, _P],
+                             ctypes.c_int),
     "lam_kv_read": ([_P, _P, _P, _P], ctypes.c_int),
     "lam_kv_attend": ([_P, _P, _P, _I64, _I64, ctypes.c_int32, ctypes.c_double, ctypes.c_int, _I64,
                        _P, _P, _P, _P], ctypes.c_int),
@@ -452,6 +464,23 @@ def _kv_slots(t, dtype, n, heads, name, dev, shared=False, copy=False):
     return _KV_SLOTS.pack(t.data_ptr(), seq, 0 if own == 1 else head, cols), t
 
 
+def _kv_first(first, n, dev):
+    if first is None:
+        return None
+    _kv_tensor(first, torch.int32, 1, "first", dev)
+    if first.numel() != n:
+        raise ValueError("first must have an entry for each sequence")
+    return first.contiguous()
+
+
+def _kv_status(status, dev):
+    if status is None:
+        return
+    _kv_tensor(status, torch.int32, 1, "status", dev)
+    if not status.is_contiguous() or status.numel() < 3:
+        raise ValueError("status must be a contiguous int32 tensor of at least 3 entries")
+
+
 def kv_append(k: torch.Tensor, v: torch.Tensor, pages: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor,
               starts: torch.Tensor | None = None, weights: torch.Tensor | None = None,
               positions: torch.Tensor | None = None, first: torch.Tensor | None = None,
@@ -477,18 +506,175 @@ def kv_append(k: torch.Tensor, v: torch.Tensor, pages: torch.Tensor, table: torc
         raise ValueError(f"k must have {heads} heads")
     w, _ = _kv_slots(weights, torch.float32, n, heads, "weights", dev)
     p, _ = _kv_slots(positions, torch.int32, n, heads, "positions", dev)
-    if first is not None:
-        _kv_tensor(first, torch.int32, 1, "first", dev)
-        first = first.contiguous()
-        if first.numel() != n:
-            raise ValueError("first must have an entry for each sequence")
-    if status is not None:
-        _kv_tensor(status, torch.int32, 1, "status", dev)
-        if not status.is_contiguous() or status.numel() < 3:
-            raise ValueError("status must be a contiguous int32 tensor of at least 3 entries")
+    first = _kv_first(first, n, dev)
+    _kv_status(status, dev)
     _check(_lib.lam_kv_append(ctx.handle, view, k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0),
                               v.stride(1), w, p, None if first is None else first.data_ptr(),
                               None if status is None else status.data_ptr()))
+
+
+_ROTARY_LAYOUTS = {"half": 0, "interleaved": 1}
+_ROTARY_SCALINGS = {None: 0, "linear": 1, "base": 2, "parts": 3}
+_KV_NO_HEADS = _HEADS.pack(0, 0, 0, 0, 0, 0, 0, 2, 0)
+
+
+def rotary_frequencies(rotary_dim: int, base: float = 10000.0, scaling: str | None = None, factor: float = 1.0,
+                       length: float = 0.0, low: float = 1.0, high: float = 32.0, device=None):
+    """(frequencies, amplitude) of a rotation of the first rotary_dim channels (lam_rotary_frequencies):
+    float64 (rotary_dim / 2,), radians a position, on `device` (the current GPU by default).  scaling,
+    for contexts `factor` times the trained `length`: "linear", "base" or "parts" (pairs of `high` or more
+    turns over `length` as they are, of `low` or fewer slower by factor; the amplitude is then 0.1 ln(factor) + 1)."""
+    pairs, rest = divmod(_kv_int(rotary_dim, "rotary_dim"), 2)
+    if rest or pairs < 0:
+        raise ValueError("rotary_dim must be even and not negative")
+    if scaling not in _ROTARY_SCALINGS:
+        raise ValueError(f"scaling must be one of {list(_ROTARY_SCALINGS)}")
+    out, amplitude = (ctypes.c_double * max(pairs, 1))(), ctypes.c_double()
+    _check(_lib.lam_rotary_frequencies(pairs, float(base), _ROTARY_SCALINGS[scaling], float(factor), float(length),
+                                       float(low), float(high), out, ctypes.addressof(amplitude)))
+    return torch.tensor(out[:pairs], dtype=torch.float64, device=device or "cuda"), amplitude.value
+
+
+def _kv_rotary(frequencies, layout, amplitude, dev):
+    """(lam_rotary, tensor to hold) of a call."""
+    if layout not in _ROTARY_LAYOUTS:
+        raise ValueError(f"layout must be one of {list(_ROTARY_LAYOUTS)}")
+    if frequencies is None:
+        return _ROTARY.pack(0, 0, 0, 1.0), None
+    _kv_tensor(frequencies, torch.float64, 1, "frequencies", dev)
+    _kv_graphless(frequencies, "frequencies")
+    f = frequencies.contiguous()
+    return _ROTARY.pack(f.data_ptr(), f.numel(), _ROTARY_LAYOUTS[layout], float(amplitude)), f
+
+
+def _kv_heads(x, gain, out, name, dev):
+    """(lam_heads, result, tensor to hold) of rows that are normed and turned; out: True for a new
+    result, False for none."""
+    rows, heads, head_dim = x.shape
+    row, head, _ = x.stride()
+    g, g_type = 0, 2
+    if gain is not None:
+        if not isinstance(gain, torch.Tensor) or gain.dtype not in (torch.float32, x.dtype):
+            raise TypeError(f"{name}_norm must be a tensor of float32 or of {name}'s type")
+        _kv_tensor(gain, gain.dtype, 1, name + "_norm", dev)
+        if gain.numel() != head_dim:
+            raise ValueError(f"{name}_norm must have an entry for each of the {head_dim} channels")
+        if gain.requires_grad:
+            _kv_graphless(gain, name + "_norm")
+        gain = gain.contiguous()
+        g = gain.data_ptr()
+        g_type = 2 if gain.dtype is torch.float32 else _KV_DTYPES[gain.dtype]
+    if out is False:
+        return _HEADS.pack(x.data_ptr(), row, head, 0, 0, 0, g, g_type, heads), None, gain
+    if out is True:
+        out = torch.empty((rows, heads, head_dim), dtype=x.dtype, device=x.device)
+    else:
+        _kv_tensor(out, x.dtype, 3, name + "'s out", dev)
+        if out.shape != x.shape or out.stride(2) != 1:
+            raise ValueError(f"{name}'s out must be of {name}'s shape with its channels contiguous")
+        _kv_graphless(out, name + "'s out")
+    y_row, y_head, _ = out.stride()
+    return _HEADS.pack(x.data_ptr(), row, head, out.data_ptr(), y_row, y_head, g, g_type, heads), out, gain
+
+
+def kv_rotate(q: torch.Tensor, frequencies: torch.Tensor | None, positions: torch.Tensor | None = None,
+              k: torch.Tensor | None = None, layout: str = "half", amplitude: float = 1.0,
+              q_norm: torch.Tensor | None = None, k_norm: torch.Tensor | None = None, eps: float = 1e-6,
+              norm_dim: int | None = None, out=None, ctx: Context | None = None):
+    """Norm the heads of rows of queries (rows, heads, head_dim), and of keys, and turn their channel
+    pairs by position times frequency (lam_kv_rotate): layout "half" (channels i and i + pairs) or
+    "interleaved" (2 i and 2 i + 1); frequencies (float64, radians a position) of up to head_dim / 2
+    pairs, None: none is turned.  positions: int32, of each row.  q_norm, k_norm: gains of an RMS norm
+    (float32 or q's type: head_dim), None: no norm; norm_dim: the channels of the mean, head_dim by default.
+    Returns q's result, with k (q's, k's).  out: q's result or (q's, k's) to write to, which may be q
+    and k themselves.  There is no gradient: tensors that require one are refused outside
+    torch.no_grad()."""
+    if ctx is None:
+        ctx = default_context()
+    elif _kv_elsewhere(ctx):
+        with torch.cuda.stream(ctx.stream):
+            return kv_rotate(q, frequencies, positions, k, layout, amplitude, q_norm, k_norm, eps, norm_dim, out, ctx)
+    dev = ctx.device
+    q = _kv_rows(q, None, "q", dev)
+    rows, _, head_dim = q.shape
+    r, hold = _kv_rotary(frequencies, layout, amplitude, dev)
+    if positions is not None:
+        _kv_tensor(positions, torch.int32, 1, "positions", dev)
+        positions = positions.contiguous()
+        if positions.numel() != rows:
+            raise ValueError("positions must have an entry for each row")
+    elif hold is not None and hold.numel() and rows:
+        raise ValueError("a rotation needs positions")
+    if k is None:
+        if isinstance(out, (tuple, list)):
+            out, = out
+    else:
+        k = _kv_rows(k, None, "k", dev)
+        if k.dtype != q.dtype or k.shape[0] != rows or k.shape[2] != head_dim:
+            raise ValueError("k must have q's rows, channels and type")
+        if out is None:
+            out = True, True
+        out, k_out = out
+        kh, k_out, hold_k = _kv_heads(k, k_norm, k_out, "k", dev)
+    qh, out, hold_q = _kv_heads(q, q_norm, True if out is None else out, "q", dev)
+    _check(_lib.lam_kv_rotate(ctx.handle, r, qh, None if k is None else kh, rows, head_dim, _KV_DTYPES[q.dtype],
+                              None if positions is None else positions.data_ptr(), float(eps),
+                              0 if norm_dim is None else _kv_norm_dim(norm_dim)))
+    return out if k is None else (out, k_out)
+
+
+def _kv_norm_dim(n):
+    n = _kv_int(n, "norm_dim")
+    if n < 1:
+        raise ValueError("norm_dim must be at least 1")
+    return n
+
+
+def kv_rotate_append(q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor, pages: torch.Tensor, table: torch.Tensor,
+                     lengths: torch.Tensor, frequencies: torch.Tensor | None, starts: torch.Tensor | None = None,
+                     first: torch.Tensor | None = None, layout: str = "half", amplitude: float = 1.0,
+                     q_norm: torch.Tensor | None = None, k_norm: torch.Tensor | None = None, eps: float = 1e-6,
+                     norm_dim: int | None = None, weights: torch.Tensor | None = None,
+                     positions: torch.Tensor | None = None, status: torch.Tensor | None = None,
+                     out: torch.Tensor | None = None, ctx: Context | None = None):
+    """kv_append with the norm and the rotation of kv_rotate on the way (lam_kv_rotate_append): keys
+    are normed, turned and quantized, values quantized, and q (rows, q_heads, head_dim; or None), normed and
+    turned, is returned (in out, which may be q itself).  Row i of sequence s has the position
+    first[s] + i, without first its token's slot; positions (a value per cached token) get it."""
+    if ctx is None:
+        ctx = default_context()
+    elif _kv_elsewhere(ctx):
+        with torch.cuda.stream(ctx.stream):
+            return kv_rotate_append(q, k, v, pages, table, lengths, frequencies, starts, first, layout, amplitude,
+                                    q_norm, k_norm, eps, norm_dim, weights, positions, status, out, ctx)
+    dev = ctx.device
+    k = _kv_rows(k, None, "k", dev)
+    v = _kv_rows(v, k.shape[1], "v", dev)
+    if v.shape != k.shape or v.dtype != k.dtype:
+        raise ValueError("k and v must have the same shape and dtype")
+    rows, own, head_dim = k.shape
+    view, n, heads, hold = _kv_view(dev, pages, table, lengths, starts, rows, head_dim, k.dtype)
+    if own != heads:
+        raise ValueError(f"k must have {heads} heads")
+    r, hold_f = _kv_rotary(frequencies, layout, amplitude, dev)
+    qh = None
+    if q is not None:
+        q = _kv_rows(q, None, "q", dev)
+        if q.dtype != k.dtype or q.shape[0] != rows or q.shape[2] != head_dim:
+            raise ValueError("q must have k's rows, channels and type")
+        qh, out, hold_q = _kv_heads(q, q_norm, True if out is None else out, "q", dev)
+    elif out is not None:
+        raise ValueError("out without q")
+    kh, _, hold_k = _kv_heads(k, k_norm, False, "k", dev)
+    w, _ = _kv_slots(weights, torch.float32, n, heads, "weights", dev)
+    p, _ = _kv_slots(positions, torch.int32, n, heads, "positions", dev)
+    first = _kv_first(first, n, dev)
+    _kv_status(status, dev)
+    _check(_lib.lam_kv_rotate_append(ctx.handle, view, r, qh, kh, v.data_ptr(), v.stride(0), v.stride(1), w, p,
+                                     None if first is None else first.data_ptr(), float(eps),
+                                     0 if norm_dim is None else _kv_norm_dim(norm_dim),
+                                     None if status is None else status.data_ptr()))
+    return out
 
 
 def kv_read(pages: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, rows: int, head_dim: int,
@@ -769,4 +955,4 @@ class Store:
 
 __all__ = ["LamError", "QParams", "IngestStats", "StoreInfo", "Context", "default_context", "quantize",
            "dequantize", "triad", "Store", "qeps_plan", "removal_ceiling", "CeilingStats", "kv_pages", "kv_append", "kv_read", "kv_attend",
-           "kv_evict", "abi_version", "EXPORTED", "LIB_PATH"]
+           "kv_evict", "rotary_frequencies", "kv_rotate", "kv_rotate_append", "abi_version", "EXPORTED", "LIB_PATH"]

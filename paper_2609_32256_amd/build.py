@@ -23,7 +23,7 @@ INCLUDE = os.path.join(ROOT, "include")
 OUT = os.path.join(HERE, "liblam.so")
 OBJDIR = os.path.join(ROOT, "_build", "lam")
 SOURCES = ["api.cpp", "qeps.hip", "dedup.hip", "score.hip", "exact.cpp", "ceiling.cpp", "blockcodec.hip", "triad.hip",
-           "kv_api.cpp", "kv_cache.hip", "kv_attend.hip", "kv_chunk.hip"]
+           "kv_api.cpp", "kv_cache.hip", "kv_attend.hip", "kv_chunk.hip", "kv_rotate.hip"]
 ARCH = os.environ.get("LAM_OFFLOAD_ARCH", "gfx950")
 
 

@@ -5,6 +5,7 @@
 #include <algorithm>
 #include <cmath>
 
+#include "kv_rotate.h"
 #include "lam_internal.h"
 
 using namespace lam;
@@ -82,6 +83,104 @@ lam_status check_own(const lam_kv_slots& s, const lam_kv_view* v, const char* na
   return LAM_OK;
 }
 
+// heads of rows as a strided array, for the question whether two of them share memory
+struct Strided {
+  const void* p;
+  int64_t row, head, rows, heads, dim;
+  uintptr_t begin() const { return reinterpret_cast<uintptr_t>(p); }
+  int64_t span() const { return (heads - 1) * head + dim; }   // elements of a row, first to last
+  uintptr_t end() const { return begin() + 2 * ((rows - 1) * row + span()); }
+};
+
+bool apart(const Strided& a, const Strided& b) {
+  if (a.end() <= b.begin() || b.end() <= a.begin()) return true;
+  // rows of the same stride, a's and b's in turn (parts of one product's result)
+  if (a.row != b.row || a.span() > a.row || b.span() > b.row) return false;
+  const int64_t step = 2 * a.row;
+  int64_t off = (int64_t)(b.begin() - a.begin()) % step;
+  if (off < 0) off += step;
+  return off >= 2 * a.span() && off + 2 * b.span() <= step;
+}
+
+Strided in_of(const lam_heads& h, int64_t rows, int32_t dim) { return {h.x_dev, h.row_stride, h.head_stride, rows, h.heads, dim}; }
+Strided out_of(const lam_heads& h, int64_t rows, int32_t dim) { return {h.y_dev, h.y_row_stride, h.y_head_stride, rows, h.heads, dim}; }
+
+lam_status check_rotary(const lam_rotary* r, int32_t dim) {
+  LAM_CHECK(r != nullptr, LAM_EINVAL, "rotary is NULL");
+  LAM_CHECK(r->pairs >= 0 && 2 * (int64_t)r->pairs <= dim, LAM_EINVAL, "rotary pairs (%d) must be in [0, head_dim / 2]",
+            r->pairs);
+  LAM_CHECK(r->layout == LAM_ROTARY_HALF || r->layout == LAM_ROTARY_INTERLEAVED, LAM_EINVAL, "unknown rotary layout %d",
+            r->layout);
+  LAM_CHECK(r->pairs == 0 || r->freq_dev != nullptr, LAM_EINVAL, "rotary frequencies are NULL");
+  LAM_CHECK(aligned(r->freq_dev, 8), LAM_EINVAL, "rotary frequencies must be 8-byte aligned");
+  LAM_CHECK(std::isfinite(r->amplitude) && std::isfinite((float)r->amplitude), LAM_EINVAL, "amplitude must be finite");
+  return LAM_OK;
+}
+
+lam_status check_heads(const lam_heads& h, const char* name, int64_t rows, int32_t dim, int32_t dtype, bool out) {
+  LAM_CHECK(h.heads >= 0 && h.heads <= (1 << 20), LAM_EINVAL, "%s: heads must be in [0, 2^20]", name);
+  LAM_CHECK(h.gain_dev == nullptr || h.gain_dtype == LAM_F32 || h.gain_dtype == dtype, LAM_EINVAL,
+            "%s: gains must be LAM_F32 or of the rows' type", name);
+  LAM_CHECK(aligned(h.gain_dev, h.gain_dtype == LAM_F32 ? 4 : 2), LAM_EINVAL, "%s: gains are not aligned", name);
+  if (h.heads == 0 || rows == 0) return LAM_OK;
+  LAM_CHECK(h.x_dev != nullptr, LAM_EINVAL, "%s is NULL", name);
+  LAM_CHECK(aligned(h.x_dev, 2), LAM_EINVAL, "%s must be 2-byte aligned", name);
+  LAM_CHECK(h.row_stride >= 0 && h.head_stride >= 0, LAM_EINVAL, "%s: strides must be >= 0", name);
+  if (!out) return LAM_OK;
+  LAM_CHECK(h.y_dev != nullptr, LAM_EINVAL, "%s: the result is NULL", name);
+  LAM_CHECK(aligned(h.y_dev, 2), LAM_EINVAL, "%s: the result must be 2-byte aligned", name);
+  const int64_t row = h.y_row_stride, head = h.y_head_stride;
+  LAM_CHECK(row >= 0 && head >= 0, LAM_EINVAL, "%s: the result's strides must be >= 0", name);
+  const bool by_row = (head >= dim || h.heads == 1) && (row >= (h.heads - 1) * head + dim || rows == 1);
+  const bool by_head = (row >= dim || rows == 1) && (head >= (rows - 1) * row + dim || h.heads == 1);
+  LAM_CHECK(by_row || by_head, LAM_EINVAL, "%s: rows or heads of the result overlap", name);
+  const bool same = h.x_dev == h.y_dev && (row == h.row_stride || rows == 1) && (head == h.head_stride || h.heads == 1);
+  LAM_CHECK(same || apart(in_of(h, rows, dim), out_of(h, rows, dim)), LAM_EINVAL,
+            "%s: the result overlaps the rows in part (it may be the rows themselves)", name);
+  return LAM_OK;
+}
+
+lam_status check_norm(double eps, int32_t norm_dim, int32_t dim) {
+  LAM_CHECK(std::isfinite(eps) && eps > 0.0, LAM_EINVAL, "eps must be finite and above 0");
+  LAM_CHECK(norm_dim >= 0 && norm_dim <= dim, LAM_EINVAL, "norm_dim must be in [0, head_dim], 0 for head_dim");
+  return LAM_OK;
+}
+
+bool wide(const void* p, int64_t row, int64_t head) { return aligned(p, 16) && row % 8 == 0 && head % 8 == 0; }
+
+RotateHeads heads_of(const lam_heads& h) {
+  RotateHeads r{};
+  r.x = static_cast<const uint16_t*>(h.x_dev);
+  r.x_row = h.row_stride;
+  r.x_head = h.head_stride;
+  r.y = static_cast<uint16_t*>(h.y_dev);
+  r.y_row = h.y_row_stride;
+  r.y_head = h.y_head_stride;
+  r.gain = h.gain_dev;
+  r.gain_f32 = h.gain_dtype == LAM_F32;
+  r.heads = h.heads;
+  r.x_wide = wide(h.x_dev, h.row_stride, h.head_stride);
+  r.y_wide = wide(h.y_dev, h.y_row_stride, h.y_head_stride);
+  return r;
+}
+
+RotateArgs rotate_args(const lam_rotary& r, const lam_heads& q, const lam_heads& k, int64_t rows, int32_t dim,
+                       double eps, int32_t norm_dim) {
+  RotateArgs a{};
+  a.h[0] = heads_of(q);
+  a.h[1] = heads_of(k);
+  a.freq = r.freq_dev;
+  a.pairs = r.pairs;
+  a.interleaved = r.layout == LAM_ROTARY_INTERLEAVED;
+  a.amplitude = (float)r.amplitude;
+  a.amplitude64 = r.amplitude;
+  a.eps = eps;
+  a.inv_dim = 1.0 / (norm_dim ? norm_dim : dim);
+  a.rows = rows;
+  a.dim = dim;
+  return a;
+}
+
 }  // namespace
 
 namespace lam {
@@ -134,6 +233,99 @@ lam_status lam_kv_append(lam_ctx* ctx, const lam_kv_view* view, const void* k_de
   DeviceGuard g(ctx->device);
   return launch_kv_append(ctx, *view, k_dev, k_row_stride, k_head_stride, v_dev, v_row_stride, v_head_stride, w, p,
                           first_dev, status_dev);
+}
+
+lam_status lam_rotary_frequencies(int32_t pairs, double base, int scaling, double factor, double length, double low,
+                                  double high, double* freq, double* amplitude) {
+  LAM_CHECK(pairs >= 0 && pairs <= (1 << 20), LAM_EINVAL, "pairs must be in [0, 2^20]");
+  LAM_CHECK(std::isfinite(base) && base > 0.0, LAM_EINVAL, "base must be finite and above 0");
+  LAM_CHECK(scaling >= LAM_ROTARY_PLAIN && scaling <= LAM_ROTARY_PARTS, LAM_EINVAL, "unknown rotary scaling %d", scaling);
+  LAM_CHECK(freq != nullptr || pairs == 0, LAM_EINVAL, "freq is NULL");
+  if (scaling != LAM_ROTARY_PLAIN)
+    LAM_CHECK(std::isfinite(factor) && factor >= 1.0, LAM_EINVAL, "factor must be finite and at least 1");
+  LAM_CHECK(scaling != LAM_ROTARY_BASE || pairs != 1, LAM_EINVAL, "a base for a longer context needs two pairs");
+  if (scaling == LAM_ROTARY_PARTS)
+    LAM_CHECK(std::isfinite(length) && length > 0.0 && std::isfinite(low) && std::isfinite(high) && low < high, LAM_EINVAL,
+              "length must be above 0 and low below high");
+  const long double two_pi = 6.283185307179586476925286766559L;
+  const long double dim = 2.0L * pairs;
+  long double b = base;
+  if (scaling == LAM_ROTARY_BASE && pairs > 1) b *= powl(factor, dim / (dim - 2.0L));
+  for (int32_t i = 0; i < pairs; ++i) {
+    long double f = powl(b, -2.0L * i / dim);
+    if (scaling == LAM_ROTARY_LINEAR) f /= factor;
+    if (scaling == LAM_ROTARY_PARTS) {
+      const long double turns = length * f / two_pi;
+      const long double keep = std::min(1.0L, std::max(0.0L, (turns - low) / ((long double)high - low)));
+      f = f / factor * (1.0L - keep) + f * keep;
+    }
+    freq[i] = (double)f;
+  }
+  if (amplitude) *amplitude = scaling == LAM_ROTARY_PARTS ? 0.1 * std::log(factor) + 1.0 : 1.0;
+  return LAM_OK;
+}
+
+lam_status lam_kv_rotate(lam_ctx* ctx, const lam_rotary* rotary, const lam_heads* q, const lam_heads* k, int64_t rows,
+                         int32_t head_dim, int32_t dtype, const int32_t* positions_dev, double eps, int32_t norm_dim) {
+  LAM_CHECK(ctx != nullptr, LAM_EINVAL, "ctx is NULL");
+  LAM_CHECK(q != nullptr, LAM_EINVAL, "q is NULL");
+  LAM_CHECK(head_dim >= 8 && head_dim <= 256 && head_dim % 8 == 0, LAM_EINVAL,
+            "head_dim must be a multiple of 8 from 8 to 256 (got %d)", head_dim);
+  LAM_CHECK(dtype == LAM_F16 || dtype == LAM_BF16, LAM_EINVAL, "dtype %d is not LAM_F16 or LAM_BF16", dtype);
+  LAM_CHECK(rows >= 0 && rows < (1LL << 31), LAM_EINVAL, "rows must be in [0, 2^31)");
+  LAM_TRY(check_rotary(rotary, head_dim));
+  LAM_TRY(check_norm(eps, norm_dim, head_dim));
+  const lam_heads none{};
+  const lam_heads& kh = k ? *k : none;
+  LAM_TRY(check_heads(*q, "q", rows, head_dim, dtype, true));
+  LAM_TRY(check_heads(kh, "k", rows, head_dim, dtype, true));
+  if (rows == 0 || (q->heads == 0 && kh.heads == 0)) return LAM_OK;
+  if (q->heads > 0 && kh.heads > 0) {
+    const Strided qx = in_of(*q, rows, head_dim), qy = out_of(*q, rows, head_dim);
+    const Strided kx = in_of(kh, rows, head_dim), ky = out_of(kh, rows, head_dim);
+    LAM_CHECK(apart(qy, kx) && apart(ky, qx) && apart(qy, ky), LAM_EINVAL,
+              "a result overlaps the other's rows or result");
+  }
+  LAM_CHECK(rotary->pairs == 0 || positions_dev != nullptr, LAM_EINVAL, "positions is NULL");
+  LAM_CHECK(aligned(positions_dev, 4), LAM_EINVAL, "positions must be 4-byte aligned");
+  RotateArgs a = rotate_args(*rotary, *q, kh, rows, head_dim, eps, norm_dim);
+  a.positions = positions_dev;
+  DeviceGuard g(ctx->device);
+  return launch_kv_rotate(ctx, a, dtype);
+}
+
+lam_status lam_kv_rotate_append(lam_ctx* ctx, const lam_kv_view* view, const lam_rotary* rotary, const lam_heads* q,
+                                const lam_heads* k, const void* v_dev, int64_t v_row_stride, int64_t v_head_stride,
+                                const lam_kv_slots* weights, const lam_kv_slots* positions, const int32_t* first_dev,
+                                double eps, int32_t norm_dim, uint32_t* status_dev) {
+  LAM_CHECK(ctx != nullptr, LAM_EINVAL, "ctx is NULL");
+  LAM_TRY(check_view(view));
+  LAM_TRY(check_rows(view));
+  LAM_TRY(check_rotary(rotary, view->head_dim));
+  LAM_TRY(check_norm(eps, norm_dim, view->head_dim));
+  LAM_TRY(check_slots(weights, "weights", 4));
+  LAM_TRY(check_slots(positions, "positions", 4));
+  const lam_kv_slots w = or_none(weights), p = or_none(positions);
+  LAM_TRY(check_own(w, view, "weights"));
+  LAM_TRY(check_own(p, view, "positions"));
+  LAM_CHECK(aligned(first_dev, 4) && aligned(status_dev, 4), LAM_EINVAL, "first and status must be 4-byte aligned");
+  LAM_CHECK(k != nullptr && k->heads == view->kv_heads, LAM_EINVAL, "k must have the view's heads");
+  const lam_heads none{};
+  const lam_heads& qh = q ? *q : none;
+  LAM_TRY(check_heads(qh, "q", view->rows, view->head_dim, view->dtype, true));
+  LAM_TRY(check_heads(*k, "k", view->rows, view->head_dim, view->dtype, false));
+  if (view->rows == 0) return LAM_OK;
+  LAM_CHECK(v_dev != nullptr && aligned(v_dev, 2), LAM_EINVAL, "v must be 2-byte aligned and not NULL");
+  LAM_CHECK(v_row_stride >= 0 && v_head_stride >= 0, LAM_EINVAL, "strides must be >= 0");
+  if (qh.heads > 0) {
+    const Strided y = out_of(qh, view->rows, view->head_dim);
+    const Strided v{v_dev, v_row_stride, v_head_stride, view->rows, view->kv_heads, view->head_dim};
+    LAM_CHECK(apart(y, in_of(*k, view->rows, view->head_dim)) && apart(y, v), LAM_EINVAL,
+              "the queries' result overlaps k or v");
+  }
+  DeviceGuard g(ctx->device);
+  return launch_kv_rotate_append(ctx, *view, rotate_args(*rotary, qh, *k, view->rows, view->head_dim, eps, norm_dim), v_dev,
+                                 v_row_stride, v_head_stride, w, p, first_dev, status_dev);
 }
 
 lam_status lam_kv_read(lam_ctx* ctx, const lam_kv_view* view, void* k_dev, void* v_dev) {
