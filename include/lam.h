@@ -561,6 +561,19 @@ lam_status lam_kv_attend(lam_ctx* ctx, const lam_kv_view* view, const void* q_de
                          int64_t q_head_stride, int32_t q_heads, double scale, int causal, int64_t max_length,
                          const lam_kv_slots* mask, const lam_kv_slots* weights, void* out_dev, float* lse_dev);
 
+/* lam_kv_attend with a sliding window: row i of sequence s stands at token p = lengths[s] - n_s + i
+ * and sees, of the tokens that it would see, those of the last `window` up to p (t > p - window)
+ * and the first `sinks` (t < sinks); without a causal limit also those behind p.  By slots: after an
+ * eviction, which moves tokens, a window by position is a mask's work.  window 0: none, as
+ * lam_kv_attend; sinks need one.  What no row of a call sees may hold anything, and pages of such
+ * tokens alone need not be there (their table entries can be -1 or any other).  Lengths are split
+ * and scores kept over what the rows see: context scratch as lam_kv_attend's for the lesser of the
+ * bound of lengths and of window, sinks and rows of a sequence (of the call, with starts) and 64 together. */
+lam_status lam_kv_attend_window(lam_ctx* ctx, const lam_kv_view* view, const void* q_dev, int64_t q_row_stride,
+                                int64_t q_head_stride, int32_t q_heads, double scale, int causal, int64_t max_length,
+                                int64_t window, int64_t sinks, const lam_kv_slots* mask, const lam_kv_slots* weights,
+                                void* out_dev, float* lse_dev);
+
 /* Brings every sequence of more than `budget` tokens back to budget tokens, each
  * head by itself: the tokens that stay are those protected, then those of the
  * largest score, equal ones in the order of their slots.  With position(s, h, t)

@@ -145,7 +145,8 @@ def attend(q, k, v, scale, causal=True, mask=None):
     if causal:
         seen &= np.arange(length)[None, :] <= length - n + np.arange(n)[:, None]
     if mask is not None:   # of the tokens, or of each row's
-        seen &= np.asarray(mask, dtype=bool).reshape(-1, length)
+        m = np.asarray(mask, dtype=bool)
+        seen &= m if m.ndim == 2 else m[None, :]
     p, lse = np.zeros((n, length)), np.full(n, -math.inf)
     for i in range(n):
         if seen[i].any():

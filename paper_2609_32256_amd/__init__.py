@@ -160,6 +160,8 @@ _SIGS = {
     "lam_kv_read": ([_P, _P, _P, _P], ctypes.c_int),
     "lam_kv_attend": ([_P, _P, _P, _I64, _I64, ctypes.c_int32, ctypes.c_double, ctypes.c_int, _I64,
                        _P, _P, _P, _P], ctypes.c_int),
+    "lam_kv_attend_window": ([_P, _P, _P, _I64, _I64, ctypes.c_int32, ctypes.c_double, ctypes.c_int, _I64, _I64, _I64,
+                              _P, _P, _P, _P], ctypes.c_int),
     "lam_kv_evict": ([_P, _P, _P, _P, ctypes.c_int32,
                       ctypes.c_int32, ctypes.c_int32, _P, _P, _P, _P],
                      ctypes.c_int),
@@ -695,25 +697,36 @@ def kv_read(pages: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, row
     return k, v
 
 
+def _kv_count(x, name, least):
+    """A Python integer as a C int64 of at least `least`."""
+    x = int(x)
+    if not least <= x < 1 << 63:
+        raise ValueError(f"{name} must be a 64-bit integer of at least {least}, got {x}")
+    return x
+
+
 def kv_attend(q: torch.Tensor, pages: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor,
               starts: torch.Tensor | None = None, causal: bool = True, scale: float | None = None,
               mask: torch.Tensor | None = None, weights: torch.Tensor | None = None, max_length: int | None = None,
               out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
-              ctx: Context | None = None) -> torch.Tensor:
+              ctx: Context | None = None, window: int | None = None, sinks: int = 0) -> torch.Tensor:
     """Attention of the sequences' last tokens over the cache (lam_kv_attend): q
     and the result (rows, q_heads, head_dim).  scale: 1 / sqrt(head_dim) by
     default.  mask (bool or uint8: sequences, kv_heads or 1, slots) leaves cached
     tokens out; weights (float32: sequences, kv_heads, slots) is added to what
     each token received; lse (float32: rows, q_heads) receives the scores' log
     sums.  Rows that see no token, those of no sequence among them, get 0 (lse -inf).
-    max_length, where the caller knows a bound of lengths, sizes the launch.  out may be q
+    max_length, where the caller knows a bound of lengths, sizes the launch.  With a window a row
+    sees, of those tokens, the last `window` up to its own and the first `sinks` (lam_kv_attend_window);
+    pages that no row sees need not be there.  out may be q
     itself, if contiguous (but for chunks with weights, which read q twice).  There is
     no gradient: tensors that require one are refused outside torch.no_grad()."""
     if ctx is None:
         ctx = default_context()
     elif _kv_elsewhere(ctx):
         with torch.cuda.stream(ctx.stream):
-            return kv_attend(q, pages, table, lengths, starts, causal, scale, mask, weights, max_length, out, lse, ctx)
+            return kv_attend(q, pages, table, lengths, starts, causal, scale, mask, weights, max_length, out, lse, ctx,
+                             window, sinks)
     dev = ctx.device
     q = _kv_rows(q, None, "q", dev)
     rows, q_heads, head_dim = q.shape
@@ -734,10 +747,16 @@ def kv_attend(q: torch.Tensor, pages: torch.Tensor, table: torch.Tensor, lengths
         if lse.shape != q.shape[:2] or not lse.is_contiguous():
             raise ValueError("lse must be contiguous and (rows, q_heads)")
         _kv_graphless(lse, "lse")
-    _check(_lib.lam_kv_attend(ctx.handle, view, q.data_ptr(), q.stride(0), q.stride(1), q_heads,
-                              head_dim ** -0.5 if scale is None else float(scale), 1 if causal else 0,
-                              0 if max_length is None else max(1, int(max_length)), m, w, out.data_ptr(),
-                              None if lse is None else lse.data_ptr()))
+    if window is not None:
+        window, sinks = _kv_count(window, "window", 1), _kv_count(sinks, "sinks", 0)
+    elif sinks:
+        raise ValueError("sinks need a window")
+    else:
+        window = sinks = 0
+    _check(_lib.lam_kv_attend_window(ctx.handle, view, q.data_ptr(), q.stride(0), q.stride(1), q_heads,
+                                     head_dim ** -0.5 if scale is None else float(scale), 1 if causal else 0,
+                                     0 if max_length is None else max(1, int(max_length)), window, sinks, m, w,
+                                     out.data_ptr(), None if lse is None else lse.data_ptr()))
     return out
 
 

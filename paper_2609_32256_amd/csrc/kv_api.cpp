@@ -342,7 +342,17 @@ lam_status lam_kv_read(lam_ctx* ctx, const lam_kv_view* view, void* k_dev, void*
 lam_status lam_kv_attend(lam_ctx* ctx, const lam_kv_view* view, const void* q_dev, int64_t q_row_stride,
                          int64_t q_head_stride, int32_t q_heads, double scale, int causal, int64_t max_length,
                          const lam_kv_slots* mask, const lam_kv_slots* weights, void* out_dev, float* lse_dev) {
+  return lam_kv_attend_window(ctx, view, q_dev, q_row_stride, q_head_stride, q_heads, scale, causal, max_length, 0, 0, mask,
+                              weights, out_dev, lse_dev);
+}
+
+lam_status lam_kv_attend_window(lam_ctx* ctx, const lam_kv_view* view, const void* q_dev, int64_t q_row_stride,
+                                int64_t q_head_stride, int32_t q_heads, double scale, int causal, int64_t max_length,
+                                int64_t window, int64_t sinks, const lam_kv_slots* mask, const lam_kv_slots* weights,
+                                void* out_dev, float* lse_dev) {
   LAM_CHECK(ctx != nullptr, LAM_EINVAL, "ctx is NULL");
+  LAM_CHECK(window >= 0 && sinks >= 0, LAM_EINVAL, "window and sinks must be >= 0");
+  LAM_CHECK(window > 0 || sinks == 0, LAM_EINVAL, "sinks without a window");
   LAM_TRY(check_view(view));
   LAM_TRY(check_rows(view));
   LAM_TRY(check_slots(mask, "mask", 1));
@@ -367,7 +377,7 @@ lam_status lam_kv_attend(lam_ctx* ctx, const lam_kv_view* view, const void* q_de
   LAM_CHECK(apart || same, LAM_EINVAL, "out overlaps q (it may be q itself, where that is contiguous)");
   DeviceGuard g(ctx->device);
   return launch_kv_attend(ctx, *view, q_dev, q_row_stride, q_head_stride, q_heads, (float)scale, causal != 0,
-                          max_length, m, w, out_dev, lse_dev);
+                          max_length, window, sinks, m, w, out_dev, lse_dev);
 }
 
 lam_status lam_kv_evict(lam_ctx* ctx, const lam_kv_view* view, const lam_kv_slots* scores,

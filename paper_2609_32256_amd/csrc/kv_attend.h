@@ -53,6 +53,9 @@ struct AttendArgs {
   float scale2;           // |scale| * log2(e), above 0
   int flip;               // the scale is negative
   int64_t cut;            // lengths are cut to it: the table's columns and the caller's bound
+  int window, sinks;      // a row sees the tokens of its window, which it ends, and the first
+  int reach;              // most tokens that a tile walks, those that no row of it sees left out
+  int64_t seq_reach;      // the same of a sequence's rows together, and at most cut
   int tiles_per_seq;      // where every sequence has the same number of rows
   int join_rows;          // rows a wave joins, 1 or 4
   int kept_waves;         // waves that share a token's kept scores, 1 or 4
@@ -87,14 +90,14 @@ __device__ __forceinline__ int tiles_of(int pairs, int R) { return (pairs + R - 
 // A lane's sequence: its rows, tiles and length.
 struct LaneSeq {
   int64_t first;
-  int n, tiles, full, len;
+  int n, tiles, full, span;   // span: tokens that its tiles walk
   __device__ __forceinline__ LaneSeq(const AttendArgs& a, int s, int R) {
     const bool in = s < a.c.n_seqs;
     const int q = min(s, a.c.n_seqs - 1);
     first = a.c.start(q);
     n = in ? (int)max((int64_t)0, a.c.start(q + 1) - first) : 0;
     full = a.c.tokens(q);
-    len = (int)min((int64_t)full, a.cut);
+    span = (int)min(min((int64_t)full, a.cut), (int64_t)a.reach);
     tiles = tiles_of(n * a.group, R);
   }
 };
@@ -114,7 +117,7 @@ __device__ __forceinline__ Work plan(const AttendArgs& a, uint32_t id) {
   double tokens = 0.0, units = 0.0;
   LaneSeq q(a, lane, R);
   for (int b = 0;;) {
-    tokens += (double)q.tiles * q.len;
+    tokens += (double)q.tiles * q.span;
     units += (double)q.tiles;
     b += 64;
     if (b >= a.c.n_seqs) break;
@@ -131,8 +134,8 @@ __device__ __forceinline__ Work plan(const AttendArgs& a, uint32_t id) {
   uint32_t before = 0, units_before = 0;
   for (int b = 0; b < a.c.n_seqs; b += 64) {
     if (b > 0) q = LaneSeq(a, b + lane, R);
-    const int parts = max(1, (q.len + w.tokens - 1) / w.tokens);
-    const int even = ((q.len + parts - 1) / parts + kStrips - 1) / kStrips * kStrips;   // its parts made equal
+    const int parts = max(1, (q.span + w.tokens - 1) / w.tokens);
+    const int even = ((q.span + parts - 1) / parts + kStrips - 1) / kStrips * kStrips;   // its parts made equal
     const uint32_t my_units = (uint32_t)(q.tiles * a.c.heads), mine = my_units * parts;
     const uint32_t upto = wave_scan_u32(mine) + before;
     unsigned long long hit;
@@ -150,8 +153,8 @@ __device__ __forceinline__ Work plan(const AttendArgs& a, uint32_t id) {
       w.s = b + l;
       w.first = (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)q.first, l);
       w.n = __builtin_amdgcn_readlane(q.n, l);
-      w.len = __builtin_amdgcn_readlane(q.len, l);
       w.end_full = __builtin_amdgcn_readlane(q.full, l);
+      w.len = (int)min((int64_t)w.end_full, a.cut);
       w.parts = __builtin_amdgcn_readlane(parts, l);
       w.tokens = __builtin_amdgcn_readlane(even, l);
       w.base = (uint32_t)__builtin_amdgcn_readlane((int)(upto - mine), l);
@@ -255,6 +258,35 @@ __device__ __forceinline__ void clear_rows(const AttendArgs& a) {
 __device__ __forceinline__ int pair_end(const AttendArgs& a, const Work& w, int r) {
   if (!a.causal) return w.len;
   return max(0, min(w.len, w.end_full - w.n + r / a.group + 1));
+}
+
+// And from where on, but for the first a.sinks.
+__device__ __forceinline__ int pair_begin(const AttendArgs& a, const Work& w, int r) {
+  return (int)max((int64_t)0, (int64_t)w.end_full - w.n + r / a.group + 1 - a.window);
+}
+
+// The strips that rows with a window walk: those with the first tokens and those from the first
+// row's window on, in one sequence of places.  The strips between, which no row sees, are left
+// out: the pages that hold them are not read and need not be there.
+struct Walk {
+  int sinks = 0;   // places of the first tokens, whole strips
+  int gap = 0;     // tokens left out after them
+  __device__ __forceinline__ Walk() {}
+  // begin: of the first row
+  __device__ __forceinline__ Walk(const AttendArgs& a, int len, int begin)
+      : sinks((min(a.sinks, len) + kKvStrip - 1) & ~(kKvStrip - 1)), gap(max(0, (begin & ~(kKvStrip - 1)) - sinks)) {}
+  __device__ __forceinline__ int token(int place) const { return place < sinks ? place : place + gap; }
+  __device__ __forceinline__ int place(int token) const { return token < sinks ? token : token - gap; }
+  // places of the tokens below `end`
+  __device__ __forceinline__ int places(int end) const { return max(min(end, sinks), end - gap); }
+};
+
+// bits 0 to n - 1
+__device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
+
+// Which of a strip's tokens a window from begin on leaves.
+__device__ __forceinline__ uint32_t window_bits(const AttendArgs& a, int t0, int begin) {
+  return ~bits_below(begin - t0) | bits_below(a.sinks - t0);
 }
 
 // B operand of a query row and head: lane (c, g) holds channels g D/4 + 8 j + 0..7
@@ -629,6 +661,7 @@ __device__ __forceinline__ void join_waves(const AttendArgs& a, const Work& w, i
 // Rows of a tile of the kernel for chunks (kv_chunk.hip): 64, or 32 and 48 of 256
 // channels, and its launch.
 constexpr int kChunkRows = 64, kChunkRowsWide = 32, kChunkRowsWider = 48;
-lam_status launch_kv_chunk(lam_ctx* ctx, const lam_kv_view& v, const AttendArgs& a, int rows, int64_t blocks, bool masked);
+lam_status launch_kv_chunk(lam_ctx* ctx, const lam_kv_view& v, const AttendArgs& a, int rows, int64_t blocks, bool masked,
+                           bool windowed);
 
 }  // namespace lam

@@ -43,7 +43,7 @@ __device__ __forceinline__ void keep_nothing(float* scores) {
 }
 
 // The running softmax of 16 query rows over the strips a wave takes.
-template <int D, bool BF16, bool MASK>
+template <int D, bool BF16, bool WINDOW>
 struct Running {
   static constexpr int kRun = D / 16;
   kv_f4 o[kRun];
@@ -54,9 +54,9 @@ struct Running {
     for (int j = 0; j < kRun; ++j) o[j] = kv_f4{0, 0, 0, 0};
   }
 
-  // One strip at t0; whole: every query sees all of its tokens.  scores: where
-  // the query's scores are kept (null: nowhere), slot by slot.
-  __device__ __forceinline__ void add(const AttendArgs& a, int len, int t0, bool whole, int end, uint32_t bits,
+  // One strip at t0; whole: every query sees all of its tokens, else those from begin to end.
+  // scores: where the query's scores of the strip are kept (null: nowhere).
+  __device__ __forceinline__ void add(const AttendArgs& a, int len, int t0, bool whole, int begin, int end, uint32_t bits,
                                       float* scores, uint32_t shift, const uint4 q[D / 32], const Codes<D>& k,
                                       Codes<D>& v) {
     kv_f4 x[2];
@@ -69,11 +69,11 @@ struct Running {
       for (int j = 0; j < D / 32; ++j) x[kt] = mfma<BF16>(y[j], q[j], x[kt]);
     }
     less_reference(x, a.scale2, row);
-    if (!whole) hide(x, seen_bits(bits, t0, end));
+    if (!whole) hide(x, seen_bits(WINDOW ? bits & window_bits(a, t0, begin) : bits, t0, end));
     if (scores) {
       const int g = (threadIdx.x & 63) >> 4;
-      *reinterpret_cast<kv_f4*>(scores + t0 + 4 * g) = x[0] + row.m;
-      *reinterpret_cast<kv_f4*>(scores + t0 + 4 * g + 16) = x[1] + row.m;
+      *reinterpret_cast<kv_f4*>(scores + 4 * g) = x[0] + row.m;
+      *reinterpret_cast<kv_f4*>(scores + 4 * g + 16) = x[1] + row.m;
     }
     const float top = top_of(x);
     if (__any(row.rises(top))) {
@@ -88,7 +88,7 @@ struct Running {
   }
 };
 
-template <int D, bool BF16, bool MASK>
+template <int D, bool BF16, bool MASK, bool WINDOW>
 __global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : 3) void k_kv_attend(AttendArgs a) {
   constexpr int kRun = D / 16;
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
@@ -103,9 +103,19 @@ __global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : 3) void k_kv_attend(Att
   const int64_t head_bytes = KvLayout<D>::head_bytes(T);
 
   const int end = pair_end(a, w, min(w.r0 + c, w.pairs - 1));
-  const int end_first = pair_end(a, w, w.r0), end_last = pair_end(a, w, min(w.r0 + kAttRows, w.pairs) - 1);
+  const int last = min(w.r0 + kAttRows, w.pairs) - 1, end_first = pair_end(a, w, w.r0);
+  int begin = 0, begin_first = 0, begin_last = 0;
+  Walk walk, kept_walk;   // of the tile; of the sequence, by which scores are kept
+  if constexpr (WINDOW) {
+    begin = pair_begin(a, w, min(w.r0 + c, w.pairs - 1));
+    begin_first = pair_begin(a, w, w.r0);
+    begin_last = pair_begin(a, w, last);
+    walk = Walk(a, w.len, begin_first);
+    kept_walk = Walk(a, w.len, pair_begin(a, w, 0));
+  }
+  // places from `from` to `to`, which are tokens where there is no window
   const int64_t part_at = (int64_t)w.part * w.tokens;
-  const int from = (int)min(part_at, (int64_t)w.len), to = (int)min(part_at + w.tokens, (int64_t)end_last);
+  const int from = (int)min(part_at, (int64_t)w.len), to = (int)min(part_at + w.tokens, (int64_t)walk.places(pair_end(a, w, last)));
   const int whole_to = end_first - kKvStrip;   // strips up to here are seen whole
 
   // Strips at t0, t0 + 128, ...: kAhead strips' codes are on their way while one
@@ -121,9 +131,10 @@ __global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : 3) void k_kv_attend(Att
   // that is on its way.
   const kv_const_i32 entries = kv_const(a.c.table + (int64_t)w.s * a.c.table_stride);
   const int last_col = max(a.c.table_cols - 1, 0);
-  auto entry = [&](int t) { return entries[min(t >> a.c.page_shift, last_col)]; };
-  auto load = [&](int b, int32_t page, int t) {
-    ok[b] = t < to && page >= 0 && page < a.c.n_pages;
+  auto entry = [&](int place) { return entries[min(walk.token(place) >> a.c.page_shift, last_col)]; };
+  auto load = [&](int b, int32_t page, int place) {
+    const int t = walk.token(place);
+    ok[b] = place < to && page >= 0 && page < a.c.n_pages;
     const StripRsrc rs = strip_rsrc<D>(a.c.head_page(ok[b] ? page : 0, h, head_bytes), T, t & (T - 1), ok[b]);
     load_keys<D>(rs, at, k[b]);
     load_vals<D>(rs, at, v[b]);
@@ -143,7 +154,7 @@ __global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : 3) void k_kv_attend(Att
     const int r = w.r0 + c;
     scores = a.kept + ((w.first + r / a.group) * a.q_heads + h * a.group + r % a.group) * a.kept_cols;
   }
-  Running<D, BF16, MASK> r;
+  Running<D, BF16, WINDOW> r;
   while (t0 < to) {
 #pragma unroll
     for (int i = 0; i < kBufs; ++i) {
@@ -151,10 +162,17 @@ __global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : 3) void k_kv_attend(Att
       const int32_t page = next;
       next = entry(t0 + (kAhead + 1) * kStep);
       load((i + kAhead) % kBufs, page, t0 + kAhead * kStep);
-      const uint32_t bits = mask_bits<MASK>(mb[i]);
+      const int t = walk.token(t0);
+      uint32_t bits = mask_bits<MASK>(mb[i]);
+      bool whole = t <= whole_to;
+      if constexpr (WINDOW) {
+        bits &= window_bits(a, t, begin_first);   // (what no row sees may hold anything)
+        whole = whole && (t >= begin_last || t + kKvStrip <= a.sinks);
+      }
+      float* const kept = scores ? scores + kept_walk.place(t) : nullptr;
       if (ok[i] && bits != 0)
-        r.add(a, w.len, t0, t0 <= whole_to && bits == kAllTokens, end, bits, scores, at.shift, q, k[i], v[i]);
-      else if (scores) keep_nothing(scores + t0);
+        r.add(a, w.len, t, whole && bits == kAllTokens, begin, end, bits, kept, at.shift, q, k[i], v[i]);
+      else if (scores) keep_nothing(kept);
       t0 += kStep;
     }
   }
@@ -257,24 +275,28 @@ __device__ __forceinline__ void add_kept(const AttendArgs& a, uint32_t block) {
   const int tokens = kKeptTokens / a.kept_waves, wave = (int)threadIdx.x >> 6, lane = (int)threadIdx.x & 63;
   const uint32_t chunks = (uint32_t)(a.kept_cols / tokens);
   const bool share = a.kept_waves > 1;
-  const int t = (int)(block % chunks) * tokens + 4 * (share ? lane : (int)threadIdx.x);
+  const int place = (int)(block % chunks) * tokens + 4 * (share ? lane : (int)threadIdx.x);
   const int h = (int)(block / chunks % (uint32_t)a.c.heads), s = (int)(block / chunks / (uint32_t)a.c.heads);
   const int64_t first = a.c.start(s);
   const int n = (int)max((int64_t)0, a.c.start(s + 1) - first), full = a.c.tokens(s);
   const int len = (int)min((int64_t)full, a.cut), pairs = n * a.group;
-  if ((int)(block % chunks) * tokens >= len) return;
+  const int64_t begin0 = (int64_t)full - n + 1 - a.window;   // of the first row's window
+  const Walk walk(a, len, (int)max((int64_t)0, begin0));
+  if ((int)(block % chunks) * tokens >= walk.places(len)) return;
+  const int t = walk.token(place);
   // Four rows' scores at a time, the first four on their way before the plan and the
   // sums are known.
   kv_f4 x[4];
   auto load = [&](int r) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      // whole strips up to the row's last token were kept, others not
+      // whole strips of the row's first and last tokens, and between, were kept, others not
       const int i = (r + j) / a.group, last = a.causal ? min(len, full - n + i + 1) : len;
+      const bool seen = t < last && (t + 4 > begin0 + i || t < a.sinks);
       const int64_t at = (first + i) * a.q_heads + h * a.group + (r + j) % a.group;
       const float no = -__builtin_inff();
-      x[j] = r + j < pairs && t < last ? *reinterpret_cast<const kv_f4*>(a.kept + at * a.kept_cols + t)
-                                       : kv_f4{no, no, no, no};
+      x[j] = r + j < pairs && seen ? *reinterpret_cast<const kv_f4*>(a.kept + at * a.kept_cols + place)
+                                   : kv_f4{no, no, no, no};
     }
   };
   const int r_first = share ? 4 * wave : 0, r_step = share ? kAttRows : 4;
@@ -361,13 +383,13 @@ constexpr int weight_strips() { return D == 256 ? 2 : 4; }
 // (with 8 heads of 128, 512 workgroups, 75 for 45).
 constexpr int64_t kWeightBlocks = 512;
 
-template <int D, bool BF16, int kStrips>
+template <int D, bool BF16, int kStrips, bool WINDOW>
 __global__ __launch_bounds__(kAttThreads, D == 256 ? 2 : D == 64 && kStrips == 2 ? 4 : D == 64 || kStrips == 2 ? 3 : 2)
 void k_kv_weights(AttendArgs a) {
   constexpr int kSteps = D / 32, kTokens = kStrips * kKvStrip;
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t chunks = (uint32_t)((a.cut + kTokens - 1) / kTokens);
+  const uint32_t chunks = (uint32_t)((a.seq_reach + kTokens - 1) / kTokens);
   // Workgroups of a head read the same queries.  They are dealt out in turn to eight XCDs:
   // where each can have as many heads of every sequence, all of a head go to one and find
   // them in its L2 (2,048 rows of 32 heads over 16,384 tokens and 8 heads: of 64 channels 212
@@ -375,7 +397,7 @@ void k_kv_weights(AttendArgs a) {
   // lengths 106 for 147, so not there).
   const bool by_xcd = a.c.heads % 8 == 0;
   const uint32_t turn = blockIdx.x / 8;
-  const int t0 = (int)((by_xcd ? turn : blockIdx.x) % chunks) * kTokens;
+  const int place0 = (int)((by_xcd ? turn : blockIdx.x) % chunks) * kTokens;
   const uint32_t id = by_xcd ? turn / chunks * 8 + blockIdx.x % 8 : blockIdx.x / chunks;
   const int h = (int)(id % (uint32_t)a.c.heads);
   Work w;
@@ -385,7 +407,13 @@ void k_kv_weights(AttendArgs a) {
   w.pairs = w.n * a.group;
   w.end_full = a.c.tokens(w.s);
   w.len = (int)min((int64_t)w.end_full, a.cut);
-  if (t0 >= w.len || w.pairs == 0) return;
+  // with a causal limit the first row that sees token t is row t - hidden
+  const int hidden = w.end_full - w.n;
+  Walk walk;
+  if constexpr (WINDOW) walk = Walk(a, w.len, pair_begin(a, w, 0));
+  if (place0 >= walk.places(w.len) || w.pairs == 0) return;
+  auto strip = [&](int n) { return walk.token(place0 + n * kKvStrip); };   // its first token
+  const int t0 = strip(0), t1 = strip(kStrips - 1) + kKvStrip;
   const int T = 1 << a.c.page_shift;
   const LaneAt<D> at(T);
   uint4 y[2 * kStrips][kSteps];
@@ -393,7 +421,7 @@ void k_kv_weights(AttendArgs a) {
   bool ok[kStrips];   // the strip's page is there
 #pragma unroll
   for (int n = 0; n < kStrips; ++n) {
-    const int t = t0 + n * kKvStrip;
+    const int t = strip(n);
     const int64_t page = t < w.len ? a.c.page(w.s, t >> a.c.page_shift) : -1;
     ok[n] = page >= 0;
     Codes<D> k;
@@ -410,9 +438,11 @@ void k_kv_weights(AttendArgs a) {
   if (any == 0) return;   // no token gets anything
   float sum[kStrips][8] = {};
 
-  // with a causal limit the first row that sees token t0 is row t0 - (end_full - n)
-  const int hidden = w.end_full - w.n;
   const int first = a.causal ? (int)min(max((int64_t)0, (int64_t)t0 - hidden) * a.group, (int64_t)w.pairs) / 16 * 16 : 0;
+  // past the last row whose window reaches back to t1 - 1, where no row sees them all along
+  int64_t r_end = w.pairs;
+  if constexpr (WINDOW)
+    if (t0 >= a.sinks) r_end = min(r_end, max((int64_t)0, (int64_t)t1 - 1 + a.window - hidden) * a.group);
   int r0 = first + 16 * wave;
   // The lane's pair of the next tile: row i of the sequence, head j of the group, and
   // where its query and its log sum lie; the last pair's stand in past the end.
@@ -446,7 +476,8 @@ void k_kv_weights(AttendArgs a) {
     lp += turn ? l_turn : 0;
   };
   auto add = [&](int b, int r) {
-    const bool whole = all == kAllTokens && t0 + kTokens <= (a.causal ? min(w.len, hidden + r / a.group + 1) : w.len);
+    bool whole = all == kAllTokens && t1 <= (a.causal ? min(w.len, hidden + r / a.group + 1) : w.len);
+    if constexpr (WINDOW) whole = whole && t0 >= pair_begin(a, w, min(r + 15, w.pairs - 1));
     const bool out = r + c >= w.pairs || e[b] == -__builtin_inff();
     const float less = out ? __builtin_inff() : e[b];   // no row, or one that sees no token: 2^(-inf) each
 #pragma unroll
@@ -462,17 +493,19 @@ void k_kv_weights(AttendArgs a) {
       for (int v = 0; v < 8; ++v) x[v >> 2][v & 3] = __builtin_fmaf(x[v >> 2][v & 3], a.scale2, -less);
       if (!whole) {
         const int end = a.causal ? min(w.len, hidden + row[b] + 1) : w.len;
-        hide(x, seen_bits(bits[n], t0 + n * kKvStrip, end));
+        uint32_t in = bits[n];
+        if constexpr (WINDOW) in &= window_bits(a, strip(n), pair_begin(a, w, row[b] * a.group));
+        hide(x, seen_bits(in, strip(n), end));
       }
 #pragma unroll
       for (int v = 0; v < 8; ++v) sum[n][v] += __builtin_amdgcn_exp2f(x[v >> 2][v & 3]);
     }
   };
   load(0, r0);
-  while (r0 < w.pairs) {
+  while (r0 < r_end) {
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      if (r0 >= w.pairs) break;
+      if (r0 >= r_end) break;
       load(1 - b, r0 + kStep);
       add(b, r0);
       r0 += kStep;
@@ -488,7 +521,7 @@ void k_kv_weights(AttendArgs a) {
       if (c == 0) total[wave][n * kKvStrip + 16 * (v >> 2) + 4 * g + (v & 3)] = ok[n] ? sum[n][v] : 0.0f;
     }
   __syncthreads();
-  const int t = t0 + (int)threadIdx.x;
+  const int t = walk.token(place0 + (int)threadIdx.x);
   if ((int)threadIdx.x < kTokens && t < w.len && t < a.weights.cols) {
     float all = 0.0f;
 #pragma unroll
@@ -500,8 +533,8 @@ void k_kv_weights(AttendArgs a) {
 }  // namespace
 
 lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, int64_t q_row, int64_t q_head,
-                            int32_t q_heads, float scale, bool causal, int64_t max_length, const lam_kv_slots& mask,
-                            const lam_kv_slots& weights, void* out, float* lse) {
+                            int32_t q_heads, float scale, bool causal, int64_t max_length, int64_t window,
+                            int64_t sinks, const lam_kv_slots& mask, const lam_kv_slots& weights, void* out, float* lse) {
   AttendArgs a{};
   a.c = KvArgs::of(v);
   if (v.table_cols == 0) a.c.table = v.lengths_dev, a.c.table_stride = 0;   // never used, but read ahead of the length
@@ -518,6 +551,10 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
   a.cut = (int64_t)v.table_cols * v.page_size;
   if (max_length > 0) a.cut = std::min(a.cut, max_length);
   if (v.n_pages == 0) a.cut = 0;
+  const bool windowed = window > 0;
+  constexpr int64_t kMost = 0x7fffffff;
+  a.window = (int)(windowed ? std::min(window, kMost) : kMost);
+  a.sinks = (int)std::min(sinks, (int64_t)1 << 30);
 
   a.mask = mask;
   a.weights = weights;
@@ -546,9 +583,19 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
   // than one (1.06 to 1.31 times: 10 to 19 % less, 36 sequences of 30,000 tokens 598 us to
   // 487; 1.4 times: 2 % more; of 128 channels 1.04 times: 3 % less to 14 % more).
   const int64_t units = units_of(rows);
+  // Rows with a window walk their sinks' strips and the tokens from the first one's window to the
+  // last one's end: what lengths are split by and scores are kept by.
+  a.reach = (int)kMost;
+  a.seq_reach = a.cut;
+  if (windowed) {
+    const int64_t most = v.starts_dev ? v.rows : a.c.per_seq;   // rows of a sequence
+    const int64_t span = (a.sinks + kKvStrip - 1) / kKvStrip * kKvStrip + (int64_t)a.window + kKvStrip;
+    a.reach = (int)std::min(kMost, span + (causal ? (rows - 1) / a.group + 1 : most));
+    a.seq_reach = std::min(a.cut, span + most);
+  }
   const int split_to = v.head_dim == 256 && units >= fill && 8 * units < 11 * fill ? 2 * fill : fill;
   int64_t blocks = units;
-  if (units < split_to && a.cut > (chunk ? kWholeChunk : kWholeDecode)) {
+  if (units < split_to && std::min(a.cut, (int64_t)a.reach) > (chunk ? kWholeChunk : kWholeDecode)) {
     a.split_to = split_to;
     blocks = split_to + units;   // see plan(): at most split_to - units / 2 (or split_to / 2) full parts, and one more a tile
   }
@@ -560,7 +607,7 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
   // a head, 60 and 161 for 16.)
   const int64_t pairs = v.rows * q_heads;
   const int64_t parts = a.split_to ? blocks * rows : 0;
-  a.kept_cols = (a.cut + kKeptTokens - 1) / kKeptTokens * kKeptTokens;
+  a.kept_cols = (a.seq_reach + kKeptTokens - 1) / kKeptTokens * kKeptTokens;
   const bool keep = weights.p_dev && !chunk && pairs <= kKeptBytes / 4 / std::max<int64_t>(a.kept_cols, 1);
   // every refusal, before the first launch is queued: a call that is refused has written nothing
   a.join_rows = units * rows <= kJoinFew ? 1 : kJoinRows;
@@ -571,7 +618,7 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
   a.kept_waves = kept_blocks < 1024 && v.rows * a.group > kAttRows * (int64_t)v.n_seqs ? 4 : 1;
   kept_blocks *= a.kept_waves;
   const int64_t heads = (int64_t)v.kv_heads * v.n_seqs;
-  auto weight_blocks_of = [&](int strips) { return (a.cut + strips * kKvStrip - 1) / (strips * kKvStrip) * heads; };
+  auto weight_blocks_of = [&](int strips) { return (a.seq_reach + strips * kKvStrip - 1) / (strips * kKvStrip) * heads; };
   const bool few = v.head_dim == 256 || weight_blocks_of(4) < kWeightBlocks;
   const int64_t weight_blocks = weights.p_dev && !keep ? weight_blocks_of(few ? 2 : 4) : 0;   // (a cut of 0: none)
   LAM_CHECK(std::max({blocks, join_blocks + kept_blocks, weight_blocks}) <= most_blocks(kAttThreads), LAM_EINVAL,
@@ -593,16 +640,19 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
 
   hipEvent_t e0, e1;
   if (chunk) {
-    LAM_TRY(launch_kv_chunk(ctx, v, a, rows, blocks, mask.p_dev != nullptr));
+    LAM_TRY(launch_kv_chunk(ctx, v, a, rows, blocks, mask.p_dev != nullptr, windowed));
   } else {
     LAM_TRY(prof_launch_events(ctx, "kv_attend", &e0, &e1));
-#define LAM_GO(D, BF)                                                                                          \
-  do {                                                                                                         \
-    if (mask.p_dev) launch(k_kv_attend<D, BF, true>, dim3((unsigned)blocks), kAttThreads, ctx->stream, e0, e1, a); \
-    else launch(k_kv_attend<D, BF, false>, dim3((unsigned)blocks), kAttThreads, ctx->stream, e0, e1, a);       \
+    const dim3 grid((unsigned)blocks);
+#define LAM_VIEW(D, BF, M, W) launch(k_kv_attend<D, BF, M, W>, grid, kAttThreads, ctx->stream, e0, e1, a)
+#define LAM_GO(D, BF)                                                                              \
+  do {                                                                                             \
+    if (windowed) { if (mask.p_dev) LAM_VIEW(D, BF, true, true); else LAM_VIEW(D, BF, false, true); } \
+    else { if (mask.p_dev) LAM_VIEW(D, BF, true, false); else LAM_VIEW(D, BF, false, false); }     \
   } while (0)
     LAM_KV_DISPATCH(v, LAM_GO);
 #undef LAM_GO
+#undef LAM_VIEW
     LAM_HIP(hipGetLastError());
   }
   if (join_blocks + kept_blocks > 0) {
@@ -624,13 +674,19 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
   if (weight_blocks > 0) {
     LAM_TRY(prof_launch_events(ctx, "kv_weights", &e0, &e1));
     const dim3 grid((unsigned)weight_blocks);
-#define LAM_GO(D, BF)                                                                                       \
-  do {                                                                                                      \
-    if (few) launch(k_kv_weights<D, BF, 2>, grid, kAttThreads, ctx->stream, e0, e1, a);                     \
-    else launch(k_kv_weights<D, BF, weight_strips<D>()>, grid, kAttThreads, ctx->stream, e0, e1, a);        \
+#define LAM_STRIPS(D, BF, N)                                                                             \
+  do {                                                                                                 \
+    if (windowed) launch(k_kv_weights<D, BF, N, true>, grid, kAttThreads, ctx->stream, e0, e1, a);     \
+    else launch(k_kv_weights<D, BF, N, false>, grid, kAttThreads, ctx->stream, e0, e1, a);             \
+  } while (0)
+#define LAM_GO(D, BF)                              \
+  do {                                             \
+    if (few) LAM_STRIPS(D, BF, 2);                 \
+    else LAM_STRIPS(D, BF, weight_strips<D>());    \
   } while (0)
     LAM_KV_DISPATCH(v, LAM_GO);
 #undef LAM_GO
+#undef LAM_STRIPS
     LAM_HIP(hipGetLastError());
   }
   return LAM_OK;

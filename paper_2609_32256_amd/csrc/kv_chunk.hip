@@ -18,7 +18,7 @@
 namespace lam {
 namespace {
 
-template <int D, bool BF16, bool MASK, int kRows>
+template <int D, bool BF16, bool MASK, bool WINDOW, int kRows>
 __global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : D == 64 ? 3 : 2) void k_kv_chunk(AttendArgs a) {
   constexpr int kRun = D / 16, kTiles = kRows / 16, kSteps = D / 32;
   const int lane = threadIdx.x & 63, c = lane & 15;
@@ -42,9 +42,17 @@ __global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : D == 64 ? 3 : 2) void k
 
   __syncthreads();
 
-  const int end_first = pair_end(a, w, w.r0), end_last = pair_end(a, w, min(w.r0 + kRows, w.pairs) - 1);
+  const int last = min(w.r0 + kRows, w.pairs) - 1, end_first = pair_end(a, w, w.r0);
+  int begin_first = 0, begin_last = 0;
+  Walk walk;
+  if constexpr (WINDOW) {
+    begin_first = pair_begin(a, w, w.r0);
+    begin_last = pair_begin(a, w, last);
+    walk = Walk(a, w.len, begin_first);
+  }
+  // places from `from` to `to`, which are tokens where there is no window
   const int64_t part_at = (int64_t)w.part * w.tokens;
-  const int from = (int)min(part_at, (int64_t)w.len), to = (int)min(part_at + w.tokens, (int64_t)end_last);
+  const int from = (int)min(part_at, (int64_t)w.len), to = (int)min(part_at + w.tokens, (int64_t)walk.places(pair_end(a, w, last)));
   const int whole_to = end_first - kKvStrip;
 
   kv_f4 o[kTiles][kRun];
@@ -62,7 +70,7 @@ __global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : D == 64 ? 3 : 2) void k
   const __amdgpu_buffer_rsrc_t mrs = mask_rsrc(a, w.s, w.h);
   const kv_const_i32 entries = kv_const(a.c.table + (int64_t)w.s * a.c.table_stride);
   const int last_col = max(a.c.table_cols - 1, 0);
-  auto entry = [&](int t) { return entries[min(t >> a.c.page_shift, last_col)]; };
+  auto entry = [&](int place) { return entries[min(walk.token(place) >> a.c.page_shift, last_col)]; };
   const uint32_t n_pages = (uint32_t)a.c.n_pages;
   // the page of the strip to load next
   uint8_t* head;
@@ -72,27 +80,34 @@ __global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : D == 64 ? 3 : 2) void k
     head = a.c.head_page(ok_page ? page : 0, w.h, head_bytes);
   };
   constexpr int kStep = kKvStrip * kAttWaves;
-  int t0 = from + wave * kKvStrip;
-  int32_t next = entry(t0 + kStep);
-  turn(entry(t0));
-  bool ok = t0 < to && ok_page;
+  int place = from + wave * kKvStrip;
+  int32_t next = entry(place + kStep);
+  turn(entry(place));
+  bool ok = place < to && ok_page;
   {
+    const int t0 = walk.token(place);
     const StripRsrc rs = strip_rsrc<D>(head, T, t0 & (T - 1), ok);
     load_keys<D>(rs, at, k);
     load_vals<D>(rs, at, v);
     if constexpr (MASK) mb = load_mask(mrs, t0);
   }
-  for (; t0 < to; t0 += kStep) {
+  for (; place < to; place += kStep) {
+    const int t0 = walk.token(place);
     uint4 y[2][kSteps];
     key_operand<D, BF16>(k, at.shift, 0, y[0]);
     key_operand<D, BF16>(k, at.shift, 1, y[1]);
-    const int t1 = t0 + kStep;
+    const int t1 = walk.token(place + kStep);
     turn(next);
-    next = entry(t1 + kStep);
-    const bool ok_next = t1 < to && ok_page;
+    next = entry(place + 2 * kStep);
+    const bool ok_next = place + kStep < to && ok_page;
     const StripRsrc rs = strip_rsrc<D>(head, T, t1 & (T - 1), ok_next);
     load_keys<D>(rs, at, k);
-    const uint32_t bits = mask_bits<MASK>(mb);
+    uint32_t bits = mask_bits<MASK>(mb);
+    bool whole = t0 <= whole_to;
+    if constexpr (WINDOW) {
+      bits &= window_bits(a, t0, begin_first);   // (what no row sees may hold anything)
+      whole = whole && (t0 >= begin_last || t0 + kKvStrip <= a.sinks);
+    }
     if (ok && bits != 0) {
       // scores of 32 tokens for every tile of queries, less the row's reference
       kv_f4 x[kTiles][2];
@@ -114,10 +129,14 @@ __global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : D == 64 ? 3 : 2) void k
       value_scales<D>(v, t0, w.len, bits, s);
 #pragma unroll
       for (int t = 0; t < kTiles; ++t) less_reference(x[t], a.scale2, row[t]);
-      if (t0 > whole_to || bits != kAllTokens) {
+      if (!whole || bits != kAllTokens) {
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t)
-          hide(x[t], seen_bits(bits, t0, pair_end(a, w, min(w.r0 + 16 * t + c, w.pairs - 1))));
+        for (int t = 0; t < kTiles; ++t) {
+          const int r = min(w.r0 + 16 * t + c, w.pairs - 1);
+          uint32_t in = bits;
+          if constexpr (WINDOW) in &= window_bits(a, t0, pair_begin(a, w, r));
+          hide(x[t], seen_bits(in, t0, pair_end(a, w, r)));
+        }
       }
       bool up = false;
       float top[kTiles];
@@ -156,14 +175,15 @@ __global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : D == 64 ? 3 : 2) void k
 }  // namespace
 
 lam_status launch_kv_chunk(lam_ctx* ctx, const lam_kv_view& v, const AttendArgs& a, int rows, int64_t blocks,
-                           bool masked) {
+                           bool masked, bool windowed) {
   hipEvent_t e0, e1;
   LAM_TRY(prof_launch_events(ctx, "kv_chunk", &e0, &e1));
   const dim3 grid((unsigned)blocks);
-#define LAM_ROWS(D, BF, R)                                                                        \
-  do {                                                                                            \
-    if (masked) launch(k_kv_chunk<D, BF, true, R>, grid, kAttThreads, ctx->stream, e0, e1, a);    \
-    else launch(k_kv_chunk<D, BF, false, R>, grid, kAttThreads, ctx->stream, e0, e1, a);          \
+#define LAM_VIEW(D, BF, M, W, R) launch(k_kv_chunk<D, BF, M, W, R>, grid, kAttThreads, ctx->stream, e0, e1, a)
+#define LAM_ROWS(D, BF, R)                                                                                 \
+  do {                                                                                                     \
+    if (windowed) { if (masked) LAM_VIEW(D, BF, true, true, R); else LAM_VIEW(D, BF, false, true, R); }    \
+    else { if (masked) LAM_VIEW(D, BF, true, false, R); else LAM_VIEW(D, BF, false, false, R); }           \
   } while (0)
 #define LAM_GO(D, BF)                                                                             \
   do {                                                                                            \
@@ -174,6 +194,7 @@ lam_status launch_kv_chunk(lam_ctx* ctx, const lam_kv_view& v, const AttendArgs&
   LAM_KV_DISPATCH(v, LAM_GO);
 #undef LAM_GO
 #undef LAM_ROWS
+#undef LAM_VIEW
   LAM_HIP(hipGetLastError());
   return LAM_OK;
 }

@@ -255,8 +255,8 @@ lam_status launch_kv_append(lam_ctx* ctx, const lam_kv_view& v, const void* k, i
                             const lam_kv_slots& positions, const int32_t* first, uint32_t* status);
 lam_status launch_kv_read(lam_ctx* ctx, const lam_kv_view& v, void* k, void* val);
 lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, int64_t q_row, int64_t q_head,
-                            int32_t q_heads, float scale, bool causal, int64_t max_length, const lam_kv_slots& mask,
-                            const lam_kv_slots& weights, void* out, float* lse);
+                            int32_t q_heads, float scale, bool causal, int64_t max_length, int64_t window,
+                            int64_t sinks, const lam_kv_slots& mask, const lam_kv_slots& weights, void* out, float* lse);
 lam_status launch_kv_evict(lam_ctx* ctx, const lam_kv_view& v, const lam_kv_slots& scores,
                            const lam_kv_slots& positions, int32_t budget, int32_t recent, int32_t sinks,
                            int32_t* kept, const lam_kv_slots& scores_out, const lam_kv_slots& positions_out,
