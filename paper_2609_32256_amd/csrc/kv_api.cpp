@@ -161,6 +161,7 @@ RotateHeads heads_of(const lam_heads& h) {
   r.heads = h.heads;
   r.x_wide = wide(h.x_dev, h.row_stride, h.head_stride);
   r.y_wide = wide(h.y_dev, h.y_row_stride, h.y_head_stride);
+  r.gain_wide = aligned(h.gain_dev, 16);
   return r;
 }
 

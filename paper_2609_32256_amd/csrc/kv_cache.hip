@@ -42,7 +42,10 @@ __global__ __launch_bounds__(kKvThreads) void k_kv_append(KvArgs a, int quads, R
       kw[i] = quantize8(x[i], &kb[i], &bad, &over);
       vw[i] = quantize8(y[i], &vb[i], &bad, &over);
     }
-    put_quad<D>(q, T, sub, kw, kb, vw, vb);
+    put_values<D>(q, T, sub, vw, vb);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if ((q.rows >> i) & 1u) put_key<D>(q.base, T, (int)(q.slot & (T - 1)) + i, sub, kw[i], kb[i]);
     put_slots(a, q, h, sub, weights, positions, first);
   }
   if (status) count_quad(a, q, sub, bad, over, status);

@@ -15,7 +15,7 @@ struct RotateHeads {   // heads of rows: strides in elements
   const void* gain;    // of each channel, null: no norm
   int gain_f32;        // float32, else of the rows' type
   int heads;
-  int x_wide, y_wide;  // every eight channels are a 16-byte access
+  int x_wide, y_wide, gain_wide;   // every eight channels are a 16-byte access (gains in float32: two)
 };
 
 struct RotateArgs {

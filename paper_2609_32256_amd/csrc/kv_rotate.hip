@@ -93,10 +93,41 @@ struct Lane {
   }
 };
 
-__device__ __forceinline__ float gain_at(const RotateHeads& h, int c, bool bf16) {
+template <bool BF16>
+__device__ __forceinline__ float gain_at(const RotateHeads& h, int c) {
   if (h.gain_f32) return static_cast<const float*>(h.gain)[c];
   const uint16_t g = static_cast<const uint16_t*>(h.gain)[c];
-  return bf16 ? __uint_as_float((uint32_t)g << 16) : (float)__builtin_bit_cast(_Float16, g);
+  return BF16 ? __uint_as_float((uint32_t)g << 16) : (float)__builtin_bit_cast(_Float16, g);
+}
+
+// Gains of eight channels from c on.
+template <bool BF16>
+__device__ __forceinline__ void gains8(const RotateHeads& h, int c, float g[8]) {
+  if (h.gain_wide && h.gain_f32) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const kv_f4 w = reinterpret_cast<const kv_f4*>(static_cast<const float*>(h.gain) + c)[j];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) g[4 * j + i] = w[i];
+    }
+  } else if (h.gain_wide) {
+    unpack8<BF16>(*reinterpret_cast<const kv_u4*>(static_cast<const uint16_t*>(h.gain) + c), g);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) g[e] = gain_at<BF16>(h, c + e);
+  }
+}
+
+// Of a lane's channels and of their pairs' others.
+template <int MODE, bool BF16>
+__device__ __forceinline__ void gains(const RotateHeads& h, const Lane<MODE>& at, float g[8], float go[8]) {
+  gains8<BF16>(h, at.c0, g);
+  if constexpr (MODE == kHalves) {
+    gains8<BF16>(h, at.other(0), go);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) go[e] = MODE == kInterleaved ? g[e ^ 1] : gain_at<BF16>(h, at.other(e));
+  }
 }
 
 // The raw other channels of a lane's eight, given its own.
@@ -139,78 +170,115 @@ __device__ __forceinline__ void store_raw8(void* p, int64_t at, bool wide, kv_u4
   for (int j = 0; j < 4; ++j) h[2 * j] = (uint16_t)w[j], h[2 * j + 1] = (uint16_t)(w[j] >> 16);
 }
 
-// ------------------------------------------------------------------ rows on their own
-// A wave takes a row, or a part of its heads where rows are few, 64/L heads at a time: the sines and
-// cosines are made once for all of them and lie in registers, multiplied by the gains.
+// 1 / sqrt(sum of squares / norm_dim + eps) of a head's eight channels a lane, in float32 where the
+// sum is well inside its range, else in binary64.
+template <int L>
+__device__ __forceinline__ float norm_of(const RotateArgs& a, const float u[8]) {
+  float s = 0.0f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) s = fmaf(u[e], u[e], s);
+  s = group_sum_f32<L>(s);
+  if (__any(!(s >= 1e-24f && s <= 1e37f))) {
+    double d = 0.0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) d = fma((double)u[e], (double)u[e], d);
+    return (float)__builtin_amdgcn_rsq(fma(group_sum_f64<L>(d), a.inv_dim, a.eps));
+  }
+  return __builtin_amdgcn_rsqf(fmaf(s, (float)a.inv_dim, (float)a.eps));
+}
+
+// ------------------------------------------------------------------ rows in 16 bits
+constexpr int kMostPairs = 128;
+
+// Sines and cosines of a wave's row.
+struct __align__(16) RowAngles {
+  float c[kMostPairs], s[kMostPairs];
+};
+
+// A wave norms and turns a row, or where rows are few a part of its heads, 64/L heads at a time.
+// What a lane needs of the sines and cosines for all heads lies in its registers, multiplied by
+// the gains.  kinds: of the queries alone, or of the keys as well.
 template <int L, bool BF16, int MODE>
-__global__ __launch_bounds__(kKvThreads) void k_kv_rotate(RotateArgs a) {
+__device__ __forceinline__ void rotate_row(const RotateArgs& a, int kinds, int64_t row, int part, const RowAngles& angles) {
   constexpr int kAtOnce = 64 / L;
-  const uint32_t wave = blockIdx.x * (kKvThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t row = wave / (uint32_t)a.parts;
-  const int part = (int)(wave % (uint32_t)a.parts);
-  if (row >= a.rows) return;
-  const int sub = threadIdx.x % L, slot = (threadIdx.x & 63) / L;
+  const int lane = threadIdx.x & 63, sub = lane % L, slot = lane / L;
   const Lane<MODE> at{8 * sub, a.pairs};
   const bool live = at.c0 < a.dim;
   float cs[8], sn[8];
-  const int32_t pos = a.pairs ? a.positions[row] : 0;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    if (MODE == kInterleaved && (e & 1)) {
-      cs[e] = cs[e - 1], sn[e] = -sn[e - 1];
-      continue;
-    }
-    cs[e] = 1.0f, sn[e] = 0.0f;
-    if (live && at.turned(e)) {
-      sin_cos(pos, a.freq[at.pair(e)], &cs[e], &sn[e]);
-      cs[e] *= a.amplitude, sn[e] *= a.amplitude;
-      if (at.minus(e)) sn[e] = -sn[e];
-    }
+    const bool turned = live && at.turned(e);
+    const int i = turned ? at.pair(e) : 0;
+    cs[e] = turned ? angles.c[i] : 1.0f;
+    sn[e] = turned ? (at.minus(e) ? -angles.s[i] : angles.s[i]) : 0.0f;
   }
-  int round0 = 0;
+  int before = 0;   // rounds of the kind before
 #pragma unroll 1
-  for (int kind = 0; kind < 2; ++kind) {
+  for (int kind = 0; kind < kinds; ++kind) {
     const RotateHeads& h = a.h[kind];
     const int rounds = (h.heads + kAtOnce - 1) / kAtOnce;
+    int i = (part - before % a.parts + a.parts) % a.parts;
+    before += rounds;
+    if (i >= rounds) continue;
+    auto head_of = [&](int i) { return i * kAtOnce + slot; };
+    auto row_of = [&](int i) { return h.x + row * h.x_row + (int64_t)min(head_of(i), h.heads - 1) * h.x_head; };
+    auto load = [&](int i) {
+      kv_u4 w{};
+      if (live) w = load_raw8(row_of(i), at.c0, h.x_wide);
+      return w;
+    };
+    kv_u4 next = load(i);
     float ga[8], gb[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      ga[e] = cs[e], gb[e] = sn[e];
-      if (h.gain && live) {
-        ga[e] *= gain_at(h, at.c0 + e, BF16);
-        gb[e] *= gain_at(h, at.other(e), BF16);
-      }
+    for (int e = 0; e < 8; ++e) ga[e] = cs[e], gb[e] = sn[e];
+    if (h.gain && live) {
+      float g[8], go[8];
+      gains<MODE, BF16>(h, at, g, go);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) ga[e] *= g[e], gb[e] *= go[e];
     }
-    for (int i = (part - round0 % a.parts + a.parts) % a.parts; i < rounds; i += a.parts) {
-      const int head = i * kAtOnce + slot;
-      const bool there = live && head < h.heads;
-      kv_u4 own{}, other{};
-      const uint16_t* x = h.x + row * h.x_row + (int64_t)(head < h.heads ? head : 0) * h.x_head;
-      if (there) own = load_raw8(x, at.c0, h.x_wide);
-      if constexpr (MODE == kHalvesAnywhere) {
-        if (there) other = others<MODE, L>(at, own, x);
-      } else {
-        other = others<MODE, L>(at, own, x);
-      }
+    for (; i < rounds; i += a.parts) {
+      const kv_u4 own = next;
+      kv_u4 other{};
+      if (MODE != kHalvesAnywhere || live) other = others<MODE, L>(at, own, row_of(i));
+      if (i + a.parts < rounds) next = load(i + a.parts);
       float u[8], v[8], y[8];
       unpack8<BF16>(own, u);
       unpack8<BF16>(other, v);
-      float r = 1.0f;
-      if (h.gain) {
-        double ss = 0.0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) ss = fma((double)u[e], (double)u[e], ss);
-        r = (float)__builtin_amdgcn_rsq(fma(group_sum_f64<L>(ss), a.inv_dim, a.eps));
-      }
+      const float r = h.gain ? norm_of<L>(a, u) : 1.0f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float straight = u[e] * ga[e];
         y[e] = (at.turned(e) ? fmaf(v[e], gb[e], straight) : straight) * r;
       }
-      if (there) store_raw8(h.y, row * h.y_row + (int64_t)head * h.y_head + at.c0, h.y_wide, pack8<BF16>(y));
+      if (live && head_of(i) < h.heads)
+        store_raw8(h.y, row * h.y_row + (int64_t)head_of(i) * h.y_head + at.c0, h.y_wide, pack8<BF16>(y));
     }
-    round0 += rounds;
   }
+}
+
+// A wave's LDS accesses are in order: what its lanes have written is there for the others.
+__device__ __forceinline__ void wave_lds_written() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// Bound by memory.
+template <int L, bool BF16, int MODE>
+__global__ __launch_bounds__(kKvThreads) void k_kv_rotate(RotateArgs a) {
+  __shared__ RowAngles angles[kKvThreads / 64];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t id = blockIdx.x * (kKvThreads / 64) + wave;
+  const int64_t row = id / (uint32_t)a.parts;
+  if (row >= a.rows) return;
+  for (int i = threadIdx.x & 63; i < a.pairs; i += 64) {   // a lane makes a pair's sine and cosine
+    float c, s;
+    sin_cos(a.positions[row], a.freq[i], &c, &s);
+    angles[wave].c[i] = c * a.amplitude;
+    angles[wave].s[i] = s * a.amplitude;
+  }
+  wave_lds_written();
+  rotate_row<L, BF16, MODE>(a, 2, row, (int)(id % (uint32_t)a.parts), angles[wave]);
 }
 
 // ------------------------------------------------------------------ rows into the cache
@@ -224,6 +292,21 @@ __device__ __forceinline__ float to_odd(double x) {
   return __uint_as_float(b);
 }
 
+// Eight values so.  Codes and scales change at numbers of two fraction bits: where no value is next
+// to one, the nearest float32 does as well.
+__device__ __forceinline__ void to_odd8(const double y[8], float x[8]) {
+  uint32_t least = 0xffffffffu;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    x[e] = (float)y[e];
+    least = min(least, __float_as_uint(x[e]) << 11);
+  }
+  if (__any(least == 0)) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = to_odd(y[e]);
+  }
+}
+
 // 1 / sqrt(a) to about 2^-52, for a > 0.
 __device__ __forceinline__ double inverse_root(double a) {
   double y = __builtin_amdgcn_rsq(a);
@@ -232,148 +315,182 @@ __device__ __forceinline__ double inverse_root(double a) {
   return y;
 }
 
-// Sines and cosines of a quad's rows, with the amplitude in them.
-template <int D>
-struct __align__(16) Angles {
-  double c[4][D / 2], s[4][D / 2];
-  float cf[4][D / 2], sf[4][D / 2];
+struct AppendArgs {
+  KvArgs c;
+  int quads;              // of a sequence, where all have as many rows
+  uint32_t v_blocks;      // workgroups of values, those of rows after them
+  RotateArgs r;
+  RowArgs v;
+  lam_kv_slots weights, positions;
+  const int32_t* first;
+  uint32_t* status;
 };
 
-// A workgroup takes a quad of slots and 256 / (D/8) heads: the keys and values of a head, or the
-// queries of one, by D/8 lanes.  The angles of its rows are made by all threads, for all heads, and
-// lie in LDS.  Keys are normed and turned in binary64, which vector units of this chip run at
-// float32's rate, so that no code is decided by a rounding on the way.
-template <int D, bool BF16, int MODE>
-__global__ __launch_bounds__(kKvThreads) void k_kv_rotate_append(KvArgs a, int quads, uint32_t groups, RotateArgs r,
-                                                                 RowArgs vals, lam_kv_slots weights,
-                                                                 lam_kv_slots positions, const int32_t* first,
-                                                                 uint32_t* status) {
-  constexpr int kLanes = D / 8, kItems = kKvThreads / kLanes;
-  __shared__ Angles<D> angles;
-  const uint32_t unit = blockIdx.x / groups;
-  const int item = (int)(blockIdx.x % groups) * kItems + (int)threadIdx.x / kLanes, sub = threadIdx.x % kLanes;
-  const int h = min(item, a.heads - 1);
-  Quad q = quad_at<D>(a, quads, unit, h);
-  const uint32_t rows = __builtin_amdgcn_readfirstlane(q.rows);
+// Values as lam_kv_append has them, by quads of slots, D/8 lanes a quad and head.
+template <int D, bool BF16>
+__device__ __forceinline__ void append_values(const AppendArgs& g) {
+  constexpr int kLanes = D / 8;
+  const KvArgs& a = g.c;
+  const uint32_t item = blockIdx.x * (kKvThreads / kLanes) + threadIdx.x / kLanes;
+  const int sub = threadIdx.x % kLanes;
+  const int h = (int)(item % (uint32_t)a.heads);
+  const Quad q = quad_at<D>(a, g.quads, item / (uint32_t)a.heads, h);
   bool bad = false, over = false;
-  if (rows) {
-    for (int i = threadIdx.x; i < 4 * r.pairs; i += kKvThreads) {
-      const int row = i / r.pairs, pair = i % r.pairs;
-      if (!((rows >> row) & 1u)) continue;
-      double c, s;
-      sin_cos(quad_pos(q, row, first), r.freq[pair], &c, &s);
-      angles.c[row][pair] = c *= r.amplitude64;
-      angles.s[row][pair] = s *= r.amplitude64;
-      angles.cf[row][pair] = (float)c;
-      angles.sf[row][pair] = (float)s;
+  if (q.base) {
+    kv_u4 raw[4];
+    uint32_t w[4], b[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      // a slot that is not the call's repeats one that is
+      const int64_t row = q.row + ((q.rows >> i) & 1u ? i : __builtin_ctz(q.rows));
+      raw[i] = load_raw8(g.v.p, row * g.v.row + h * g.v.head + 8 * sub, g.v.wide);
     }
-    __syncthreads();
-    const Lane<MODE> at{8 * sub, r.pairs};
-    if (item < a.heads) {
-      const RotateHeads& kh = r.h[1];
-      kv_u4 own[4], val[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        // a slot that is not the call's repeats one that is
-        const int64_t row = q.row + ((rows >> i) & 1u ? i : __builtin_ctz(rows));
-        own[i] = load_raw8(kh.x, row * kh.x_row + (int64_t)h * kh.x_head + at.c0, kh.x_wide);
-        val[i] = load_raw8(vals.p, row * vals.row + (int64_t)h * vals.head + at.c0, vals.wide);
-      }
-      float g[8], go[8];
+    for (int i = 0; i < 4; ++i) {
+      float x[8];
+      unpack8<BF16>(raw[i], x);
+      w[i] = quantize8(x, &b[i], &bad, &over);
+    }
+    put_values<D>(q, 1 << a.page_shift, sub, w, b);
+    put_slots(a, q, h, sub, g.weights, g.positions, g.first);
+  }
+  if (g.status) count_quad(a, q, sub, bad, over, g.status);
+}
+
+// What a row's keys are turned by: of every channel the factors of the channel itself and of its
+// pair's other one, gains and amplitude in them.
+template <int D>
+struct __align__(16) Factors {
+  double own[D], other[D];
+};
+
+// Where a row's token lies.
+struct Token {
+  int32_t pos;     // its position
+  int t;           // its place in the page
+  uint8_t* page;   // null: no place
+};
+
+// The keys of a row, by a wave (or a part of them, from round i on), 64 / (D/8) heads at a time, in
+// binary64, which vector units of this chip run at float32's rate, so that no code is decided by a
+// rounding on the way.
+template <int D, bool BF16, int MODE>
+__device__ __forceinline__ void append_keys(const AppendArgs& g, int64_t row, int i, const Token& token,
+                                            const Factors<D>& f) {
+  constexpr int kLanes = D / 8, kAtOnce = 64 / kLanes;
+  const KvArgs& a = g.c;
+  const RotateArgs& r = g.r;
+  const RotateHeads& kh = r.h[1];
+  const int lane = threadIdx.x & 63, sub = lane % kLanes, slot = lane / kLanes, T = 1 << a.page_shift;
+  const Lane<MODE> at{8 * sub, r.pairs};
+  bool bad = false, over = false;
+  auto row_of = [&](int i) { return kh.x + row * kh.x_row + (int64_t)min(i * kAtOnce + slot, a.heads - 1) * kh.x_head; };
+  kv_u4 next = load_raw8(row_of(i), at.c0, kh.x_wide);
+  for (; i * kAtOnce < a.heads; i += r.parts) {
+    const kv_u4 own = next, other = others<MODE, kLanes>(at, own, row_of(i));
+    next = load_raw8(row_of(i + r.parts), at.c0, kh.x_wide);
+    float u[8], v[8], x[8];
+    unpack8<BF16>(own, u);
+    unpack8<BF16>(other, v);
+    double y[8], n = 1.0;
+    if (kh.gain) {
+      double ss = 0.0;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        g[e] = kh.gain ? gain_at(kh, at.c0 + e, BF16) : 1.0f;
-        go[e] = kh.gain ? gain_at(kh, at.other(e), BF16) : 1.0f;
-      }
-      uint32_t kw[4] = {}, vw[4] = {}, kb[4] = {}, vb[4] = {};
+      for (int e = 0; e < 8; ++e) ss = fma((double)u[e], (double)u[e], ss);
+      n = inverse_root(fma(group_sum_f64<kLanes>(ss), r.inv_dim, r.eps));
+    }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (!((rows >> i) & 1u)) continue;
-        const int64_t row = q.row + i;
-        float u[8], v[8], x[8];
-        const kv_u4 other = others<MODE, kLanes>(at, own[i], kh.x + row * kh.x_row + (int64_t)h * kh.x_head);
-        unpack8<BF16>(own[i], u);
-        unpack8<BF16>(other, v);
-        double n = 1.0;
-        if (kh.gain) {
-          double ss = 0.0;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) ss = fma((double)u[e], (double)u[e], ss);
-          n = inverse_root(fma(group_sum_f64<kLanes>(ss), r.inv_dim, r.eps));
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          double y = (double)u[e] * (double)g[e];
-          if (at.turned(e)) {
-            const double s = angles.s[i][at.pair(e)];
-            y = fma((double)v[e] * (double)go[e], at.minus(e) ? -s : s, y * angles.c[i][at.pair(e)]);
-          }
-          x[e] = to_odd(y * n);
-        }
-        kw[i] = quantize8(x, &kb[i], &bad, &over);
-        unpack8<BF16>(val[i], x);
-        vw[i] = quantize8(x, &vb[i], &bad, &over);
-      }
-      if (q.base) {
-        put_quad<D>(q, 1 << a.page_shift, sub, kw, kb, vw, vb);
-        put_slots(a, q, h, sub, weights, positions, first);
-      } else {
-        bad = over = false;   // (not stored, so counted as that alone)
-      }
-    } else if (item < a.heads + r.h[0].heads) {
-      const RotateHeads& qh = r.h[0];
-      const int64_t head = item - a.heads;
-      kv_u4 own[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int64_t row = q.row + ((rows >> i) & 1u ? i : __builtin_ctz(rows));
-        own[i] = load_raw8(qh.x, row * qh.x_row + head * qh.x_head + at.c0, qh.x_wide);
-      }
-      float g[8], go[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        g[e] = qh.gain ? gain_at(qh, at.c0 + e, BF16) : 1.0f;
-        go[e] = qh.gain ? gain_at(qh, at.other(e), BF16) : 1.0f;
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (!((rows >> i) & 1u)) continue;
-        const int64_t row = q.row + i;
-        float u[8], v[8], y[8];
-        const kv_u4 other = others<MODE, kLanes>(at, own[i], qh.x + row * qh.x_row + head * qh.x_head);
-        unpack8<BF16>(own[i], u);
-        unpack8<BF16>(other, v);
-        float n = 1.0f;
-        if (qh.gain) {
-          double ss = 0.0;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) ss = fma((double)u[e], (double)u[e], ss);
-          n = (float)__builtin_amdgcn_rsq(fma(group_sum_f64<kLanes>(ss), r.inv_dim, r.eps));
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          float t = u[e] * g[e];
-          if (at.turned(e)) {
-            const float s = angles.sf[i][at.pair(e)];
-            t = fmaf(v[e] * go[e], at.minus(e) ? -s : s, t * angles.cf[i][at.pair(e)]);
-          }
-          y[e] = t * n;
-        }
-        store_raw8(qh.y, row * qh.y_row + head * qh.y_head + at.c0, qh.y_wide, pack8<BF16>(y));
-      }
+    for (int e = 0; e < 8; ++e) y[e] = fma((double)v[e], f.other[at.c0 + e], (double)u[e] * f.own[at.c0 + e]) * n;
+    to_odd8(y, x);
+    const int h = i * kAtOnce + slot;
+    if (h < a.heads) {
+      uint32_t b;
+      const uint32_t w = quantize8(x, &b, &bad, &over);
+      uint8_t* const base = token.page + (int64_t)h * KvLayout<D>::head_bytes(T);
+      put_key<D>(base, T, token.t, sub, w, b);
     }
   }
-  if (item >= a.heads) q.rows = 0;   // (counts are of keys and values)
-  if (status) count_quad(a, q, sub, bad, over, status);
-  if (a.starts && r.h[0].heads) {   // queries of no sequence
-    const RotateHeads& qh = r.h[0];
-    const int64_t before = a.start(0), after = a.start(a.n_seqs);
-    for (int64_t i = blockIdx.x; i < before + a.rows - after; i += gridDim.x) {
-      const int64_t row = i < before ? i : after + i - before;
-      for (int head = threadIdx.x / kLanes; head < qh.heads; head += kItems)
-        store_raw8(qh.y, row * qh.y_row + (int64_t)head * qh.y_head + 8 * sub, qh.y_wide, kv_u4{0, 0, 0, 0});
+  if (g.status) {
+    count_in(g.status, 0, bad);
+    count_in(g.status, 1, over);
+  }
+}
+
+// A row's token, by all lanes of a wave; false: of no sequence.
+template <int D>
+__device__ __forceinline__ bool row_token(const KvArgs& a, int64_t row, const int32_t* first, Token* token) {
+  int s;
+  if (!a.starts) {
+    s = (int)((uint32_t)row / (uint32_t)a.per_seq);
+  } else {
+    s = -1;
+    for (int b = 0; b < a.n_seqs; b += 64) {
+      const int mine = b + (int)(threadIdx.x & 63);
+      const unsigned long long in = __ballot(mine < a.n_seqs && a.start(min(mine, a.n_seqs)) <= row);
+      if (in == 0) break;
+      s = b + (int)__popcll(in) - 1;
+      if (~in) break;
+    }
+    if (s < 0 || row >= a.start(s + 1)) return false;
+  }
+  const int64_t begin = a.start(s), at = a.lengths[s] - a.start(s + 1) + row;   // its slot
+  token->pos = (int32_t)(first ? first[s] + (row - begin) : at);
+  token->t = (int)(at & ((1 << a.page_shift) - 1));
+  token->page = nullptr;
+  if (at >= 0 && (at >> a.page_shift) < a.table_cols) {
+    const int64_t page = a.page(s, (int)(at >> a.page_shift));
+    if (page >= 0) token->page = a.head_page(page, 0, KvLayout<D>::head_bytes(1 << a.page_shift));
+  }
+  return true;
+}
+
+// Workgroups of values, then waves of a row's queries and keys each (or parts of them).
+template <int D, bool BF16, int MODE>
+__global__ __launch_bounds__(kKvThreads) void k_kv_rotate_append(AppendArgs g) {
+  constexpr int kLanes = D / 8, kAtOnce = 64 / kLanes, kWaves = kKvThreads / 64;
+  __shared__ RowAngles row_angles[kWaves];
+  __shared__ Factors<D> key_factors[kWaves];
+  if (blockIdx.x < g.v_blocks) {
+    append_values<D, BF16>(g);
+    return;
+  }
+  const RotateArgs& r = g.r;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const uint32_t id = (blockIdx.x - g.v_blocks) * kWaves + wave;
+  const int64_t row = id / (uint32_t)r.parts;
+  const int part = (int)(id % (uint32_t)r.parts);
+  if (row >= g.c.rows) return;
+  const RotateHeads &q = r.h[0], &k = r.h[1];
+  Token token;
+  if (!row_token<D>(g.c, row, g.first, &token)) {   // queries of no sequence
+    for (int head = part * kAtOnce + lane / kLanes; head < q.heads; head += r.parts * kAtOnce)
+      store_raw8(q.y, row * q.y_row + (int64_t)head * q.y_head + 8 * (lane % kLanes), q.y_wide, kv_u4{0, 0, 0, 0});
+    return;
+  }
+  const int q_rounds = (q.heads + kAtOnce - 1) / kAtOnce;
+  const int k_first = (part - q_rounds % r.parts + r.parts) % r.parts;   // the wave's first round of keys
+  const bool keys = token.page && k_first * kAtOnce < g.c.heads;
+  RowAngles& angles = row_angles[wave];
+  Factors<D>& f = key_factors[wave];
+  for (int i = lane; i < D / 2; i += 64) {
+    double c = 1.0, s = 0.0;
+    int u = 2 * i, v = u + 1;
+    if (i < r.pairs) {
+      sin_cos(token.pos, r.freq[i], &c, &s);
+      c *= r.amplitude64, s *= r.amplitude64;
+      if (MODE != kInterleaved) u = i, v = i + r.pairs;
+      angles.c[i] = (float)c;
+      angles.s[i] = (float)s;
+    }
+    if (keys) {
+      const double gu = k.gain ? (double)gain_at<BF16>(k, u) : 1.0, gv = k.gain ? (double)gain_at<BF16>(k, v) : 1.0;
+      f.own[u] = c * gu, f.other[u] = -s * gv;
+      f.own[v] = c * gv, f.other[v] = s * gu;
     }
   }
+  wave_lds_written();
+  if (keys) append_keys<D, BF16, MODE>(g, row, k_first, token, f);
+  rotate_row<kLanes, BF16, MODE>(r, 1, row, part, angles);
 }
 
 // Waves that a call of few rows is shared out to.
@@ -381,12 +498,19 @@ constexpr int64_t kRotateWaves = 4096;
 
 }  // namespace
 
+// waves of a call's rows, and those that share one
+static int64_t row_waves(int64_t rows, int heads, int other_heads, int lanes, int* parts) {
+  const int at_once = 64 / lanes;
+  const int rounds = (heads + at_once - 1) / at_once + (other_heads + at_once - 1) / at_once;
+  *parts = (int)std::max<int64_t>(1, std::min<int64_t>(rounds, kRotateWaves / rows));
+  return heads + other_heads > 0 ? rows * *parts : 0;
+}
+
 lam_status launch_kv_rotate(lam_ctx* ctx, RotateArgs a, int dtype) {
-  const int lanes = a.dim <= 64 ? 8 : a.dim <= 128 ? 16 : 32, at_once = 64 / lanes;
-  const int rounds = (a.h[0].heads + at_once - 1) / at_once + (a.h[1].heads + at_once - 1) / at_once;
-  a.parts = (int)std::min<int64_t>(rounds, std::max<int64_t>(1, kRotateWaves / a.rows));
-  const int64_t blocks = (a.rows * a.parts + kKvThreads / 64 - 1) / (kKvThreads / 64);
-  LAM_CHECK(a.rows * a.parts < (1LL << 31) && blocks <= most_blocks(kKvThreads), LAM_EINVAL, "too many rows for one launch");
+  const int lanes = a.dim <= 64 ? 8 : a.dim <= 128 ? 16 : 32;
+  const int64_t waves = row_waves(a.rows, a.h[0].heads, a.h[1].heads, lanes, &a.parts);
+  const int64_t blocks = (waves + kKvThreads / 64 - 1) / (kKvThreads / 64);
+  LAM_CHECK(waves < (1LL << 31) && blocks <= most_blocks(kKvThreads), LAM_EINVAL, "too many rows for one launch");
   hipEvent_t e0, e1;
   LAM_TRY(prof_launch_events(ctx, "kv_rotate", &e0, &e1));
   const dim3 grid((unsigned)blocks);
@@ -408,19 +532,26 @@ lam_status launch_kv_rotate(lam_ctx* ctx, RotateArgs a, int dtype) {
 lam_status launch_kv_rotate_append(lam_ctx* ctx, const lam_kv_view& v, const RotateArgs& r, const void* val,
                                    int64_t v_row, int64_t v_head, const lam_kv_slots& weights,
                                    const lam_kv_slots& positions, const int32_t* first, uint32_t* status) {
-  int quads;
-  const int64_t units = quad_units(v, &quads);
-  const int64_t per = kKvThreads / (v.head_dim / 8), groups = (v.kv_heads + r.h[0].heads + per - 1) / per;
-  LAM_CHECK(units < (1LL << 31) && units * groups <= most_blocks(kKvThreads), LAM_EINVAL,
+  AppendArgs g{};
+  const int lanes = v.head_dim / 8;
+  const int64_t values = quad_units(v, &g.quads) * v.kv_heads, per = kKvThreads / lanes;
+  const int64_t v_blocks = (values + per - 1) / per;
+  g.r = r;
+  const int64_t waves = row_waves(v.rows, r.h[0].heads, r.h[1].heads, lanes, &g.r.parts);
+  const int64_t blocks = v_blocks + (waves + kKvThreads / 64 - 1) / (kKvThreads / 64);
+  LAM_CHECK(values < (1LL << 31) && waves < (1LL << 31) && blocks <= most_blocks(kKvThreads), LAM_EINVAL,
             "too many rows or sequences for one launch");
-  const KvArgs a = KvArgs::of(v);
-  const RowArgs va{val, v_row, v_head, wide_rows(val, v_row, v_head)};
+  g.c = KvArgs::of(v);
+  g.v_blocks = (uint32_t)v_blocks;
+  g.v = RowArgs{val, v_row, v_head, wide_rows(val, v_row, v_head)};
+  g.weights = weights;
+  g.positions = positions;
+  g.first = first;
+  g.status = status;
   hipEvent_t e0, e1;
   LAM_TRY(prof_launch_events(ctx, "kv_rotate_append", &e0, &e1));
-  const dim3 grid((unsigned)(units * groups));
-#define LAM_MODE(D, BF, M)                                                                                        \
-  launch(k_kv_rotate_append<D, BF, M>, grid, kKvThreads, ctx->stream, e0, e1, a, quads, (uint32_t)groups, r, va, weights, \
-         positions, first, status)
+  const dim3 grid((unsigned)blocks);
+#define LAM_MODE(D, BF, M) launch(k_kv_rotate_append<D, BF, M>, grid, kKvThreads, ctx->stream, e0, e1, g)
 #define LAM_GO(D, BF)                                          \
   do {                                                         \
     if (r.interleaved) LAM_MODE(D, BF, kInterleaved);          \

@@ -78,17 +78,23 @@ __device__ __forceinline__ void load8(const void* p, int64_t at, bool wide, floa
 // m 2^x, m in [1, 2), gives e = x - 2 for m <= 1.5 and x - 1 above; the
 // conversion instruction divides by 2^e and rounds to nearest, ties to even.
 __device__ __forceinline__ uint32_t quantize8(float x[8], uint32_t* byte, bool* bad, bool* over) {
-  float a = 0.0f;
+  // sizes in the order of their bits, what is not finite above all
+  constexpr uint32_t kInf = 0x7f800000u, kLargest = 0x47400000u;   // 49152
+  auto size = [&](int j) { return __float_as_uint(x[j]) & 0x7fffffffu; };
+  uint32_t b = 0;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const bool ok = fabsf(x[j]) < __builtin_inff();
-    *bad |= !ok;
-    x[j] = ok ? x[j] : 0.0f;
-    a = fmaxf(a, fabsf(x[j]));
+  for (int j = 0; j < 8; ++j) b = max(b, size(j));
+  if (__any(b >= kInf)) {
+    *bad |= b >= kInf;
+    b = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      x[j] = size(j) < kInf ? x[j] : 0.0f;
+      b = max(b, size(j));
+    }
   }
-  a = quad_max_f32(a);
-  *over |= a > 49152.0f;
-  const uint32_t b = __float_as_uint(a);
+  b = quad_max_u32(b);
+  *over |= b > kLargest;
   int e = (int)(b >> 23) - 129 + ((b & 0x7fffffu) > 0x400000u ? 1 : 0);
   e = min(max(e, kKvExpLo), kKvExpHi);
   *byte = (uint32_t)(e + 127);
@@ -185,10 +191,9 @@ __device__ __forceinline__ Quad quad_at(const KvArgs& a, int quads, uint32_t uni
   return q;
 }
 
-// Stores a quad's codes and scale bytes of eight channels, of the slots that are the call's.
+// Stores a quad's value codes and scale bytes of eight channels, of the slots that are the call's.
 template <int D>
-__device__ __forceinline__ void put_quad(const Quad& q, int T, int sub, const uint32_t kw[4], const uint32_t kb[4],
-                                         const uint32_t vw[4], const uint32_t vb[4]) {
+__device__ __forceinline__ void put_values(const Quad& q, int T, int sub, const uint32_t vw[4], const uint32_t vb[4]) {
   using L = KvLayout<D>;
   const int t = (int)(q.slot & (T - 1));
   uint32_t* vs = reinterpret_cast<uint32_t*>(q.base + L::v_scales(T, t, sub >> 2));
@@ -212,12 +217,14 @@ __device__ __forceinline__ void put_quad(const Quad& q, int T, int sub, const ui
         if ((sub & 3) == 0) reinterpret_cast<uint8_t*>(vs)[i] = (uint8_t)vb[i];
       }
   }
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if ((q.rows >> i) & 1u) {
-      *reinterpret_cast<uint32_t*>(q.base + L::k_codes(t + i) + 4 * sub) = kw[i];
-      if ((sub & 3) == 0) q.base[L::k_scales(T, t + i) + (sub >> 2)] = (uint8_t)kb[i];
-    }
+}
+
+// And the key codes and scale byte of place t of a head's page.
+template <int D>
+__device__ __forceinline__ void put_key(uint8_t* base, int T, int t, int sub, uint32_t w, uint32_t b) {
+  using L = KvLayout<D>;
+  *reinterpret_cast<uint32_t*>(base + L::k_codes(t) + 4 * sub) = w;
+  if ((sub & 3) == 0) base[L::k_scales(T, t) + (sub >> 2)] = (uint8_t)b;
 }
 
 // Position of the quad's i-th slot: what its sequence begins with and the row, or the slot.

@@ -75,14 +75,19 @@ __device__ __forceinline__ float quad_max_f32(float v) {
   return fmaxf(v, __int_as_float(LAM_DPP_MOVE(__float_as_int(v), __float_as_int(v), 0x4e, 0xf)));
 }
 
+__device__ __forceinline__ uint32_t quad_max_u32(uint32_t v) {
+  v = max(v, (uint32_t)LAM_DPP_MOVE(v, v, 0xb1, 0xf));
+  return max(v, (uint32_t)LAM_DPP_MOVE(v, v, 0x4e, 0xf));
+}
+
 // Sums over groups of L consecutive lanes (8, 16 or 32), in all of them, by the same moves:
 // the order is the same in every lane, so all get the same bits.
 template <int L>
 __device__ __forceinline__ float group_sum_f32(float v) {
-  v += __int_as_float(LAM_DPP_MOVE(0, __float_as_int(v), 0xb1, 0xf));
-  v += __int_as_float(LAM_DPP_MOVE(0, __float_as_int(v), 0x4e, 0xf));
-  v += __int_as_float(LAM_DPP_MOVE(0, __float_as_int(v), 0x141, 0xf));
-  if constexpr (L >= 16) v += __int_as_float(LAM_DPP_MOVE(0, __float_as_int(v), 0x140, 0xf));
+  v += __int_as_float(LAM_DPP_MOVE(__float_as_int(v), __float_as_int(v), 0xb1, 0xf));
+  v += __int_as_float(LAM_DPP_MOVE(__float_as_int(v), __float_as_int(v), 0x4e, 0xf));
+  v += __int_as_float(LAM_DPP_MOVE(__float_as_int(v), __float_as_int(v), 0x141, 0xf));
+  if constexpr (L >= 16) v += __int_as_float(LAM_DPP_MOVE(__float_as_int(v), __float_as_int(v), 0x140, 0xf));
   if constexpr (L >= 32) v += __shfl_xor(v, 16);
   return v;
 }
@@ -92,8 +97,8 @@ __device__ __forceinline__ double group_sum_f64(double v) {
 #define LAM_STEP(ctrl)                                                                                \
   {                                                                                                   \
     const unsigned long long b = (unsigned long long)__double_as_longlong(v);                         \
-    const uint32_t lo = (uint32_t)LAM_DPP_MOVE(0, (uint32_t)b, ctrl, 0xf);                             \
-    const uint32_t hi = (uint32_t)LAM_DPP_MOVE(0, (uint32_t)(b >> 32), ctrl, 0xf);                     \
+    const uint32_t lo = (uint32_t)LAM_DPP_MOVE((uint32_t)b, (uint32_t)b, ctrl, 0xf);                   \
+    const uint32_t hi = (uint32_t)LAM_DPP_MOVE((uint32_t)(b >> 32), (uint32_t)(b >> 32), ctrl, 0xf);   \
     v += __longlong_as_double((long long)(((unsigned long long)hi << 32) | lo));                      \
   }
   LAM_STEP(0xb1)
