@@ -517,7 +517,7 @@ def kv_append(k: torch.Tensor, v: torch.Tensor, pages: torch.Tensor, table: torc
 
 _ROTARY_LAYOUTS = {"half": 0, "interleaved": 1}
 _ROTARY_SCALINGS = {None: 0, "linear": 1, "base": 2, "parts": 3}
-_KV_NO_HEADS = _HEADS.pack(0, 0, 0, 0, 0, 0, 0, 2, 0)
+_CONTIGUOUS = torch.contiguous_format
 
 
 def rotary_frequencies(rotary_dim: int, base: float = 10000.0, scaling: str | None = None, factor: float = 1.0,
@@ -544,7 +544,8 @@ def _kv_rotary(frequencies, layout, amplitude, dev):
     if frequencies is None:
         return _ROTARY.pack(0, 0, 0, 1.0), None
     _kv_tensor(frequencies, torch.float64, 1, "frequencies", dev)
-    _kv_graphless(frequencies, "frequencies")
+    if frequencies.requires_grad:
+        _kv_graphless(frequencies, "frequencies")
     f = frequencies.contiguous()
     return _ROTARY.pack(f.data_ptr(), f.numel(), _ROTARY_LAYOUTS[layout], float(amplitude)), f
 
@@ -554,28 +555,32 @@ def _kv_heads(x, gain, out, name, dev):
     result, False for none."""
     rows, heads, head_dim = x.shape
     row, head, _ = x.stride()
+    dtype = x.dtype
     g, g_type = 0, 2
     if gain is not None:
-        if not isinstance(gain, torch.Tensor) or gain.dtype not in (torch.float32, x.dtype):
+        own = gain.dtype if isinstance(gain, torch.Tensor) else None
+        if own is dtype:
+            g_type = _KV_DTYPES[own]
+        elif own is not torch.float32:
             raise TypeError(f"{name}_norm must be a tensor of float32 or of {name}'s type")
-        _kv_tensor(gain, gain.dtype, 1, name + "_norm", dev)
-        if gain.numel() != head_dim:
+        if gain.get_device() != dev or gain.dim() != 1 or gain.numel() != head_dim:
+            _kv_tensor(gain, own, 1, name + "_norm", dev)
             raise ValueError(f"{name}_norm must have an entry for each of the {head_dim} channels")
         if gain.requires_grad:
             _kv_graphless(gain, name + "_norm")
         gain = gain.contiguous()
         g = gain.data_ptr()
-        g_type = 2 if gain.dtype is torch.float32 else _KV_DTYPES[gain.dtype]
+    if out is True:
+        out = torch.empty_like(x, memory_format=_CONTIGUOUS)
+        return _HEADS.pack(x.data_ptr(), row, head, out.data_ptr(), heads * head_dim, head_dim, g, g_type, heads), out, gain
     if out is False:
         return _HEADS.pack(x.data_ptr(), row, head, 0, 0, 0, g, g_type, heads), None, gain
-    if out is True:
-        out = torch.empty((rows, heads, head_dim), dtype=x.dtype, device=x.device)
-    else:
-        _kv_tensor(out, x.dtype, 3, name + "'s out", dev)
-        if out.shape != x.shape or out.stride(2) != 1:
-            raise ValueError(f"{name}'s out must be of {name}'s shape with its channels contiguous")
+    _kv_tensor(out, dtype, 3, name + "'s out", dev)
+    y_row, y_head, step = out.stride()
+    if out.shape != x.shape or step != 1:
+        raise ValueError(f"{name}'s out must be of {name}'s shape with its channels contiguous")
+    if out.requires_grad:
         _kv_graphless(out, name + "'s out")
-    y_row, y_head, _ = out.stride()
     return _HEADS.pack(x.data_ptr(), row, head, out.data_ptr(), y_row, y_head, g, g_type, heads), out, gain
 
 
