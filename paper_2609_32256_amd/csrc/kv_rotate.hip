@@ -493,22 +493,25 @@ __global__ __launch_bounds__(kKvThreads) void k_kv_rotate_append(AppendArgs g) {
   rotate_row<kLanes, BF16, MODE>(r, 1, row, part, angles);
 }
 
-// Waves that a call of few rows is shared out to.
+// Waves that a call of few rows is shared out to, at least for rows on their own, at most on the way
+// into the cache, where every part makes the keys' factors again.  Rows of 40 heads of 128 channels: 300
+// in 10 parts 4.5 us, 1,000 in 4 or 5 7.7 us (1: 10, 8: 9.9), 2,500 in 2 13.8 us (1: 16.5), 4,000 in 2 18.9
+// (1: 19.7); into the cache 2,000 in 2 14.1 us (1: 16.0, 3: 17.8), 3,000 in 1 19.4 (2: 21.9).
 constexpr int64_t kRotateWaves = 4096;
 
 }  // namespace
 
-// waves of a call's rows, and those that share one
-static int64_t row_waves(int64_t rows, int heads, int other_heads, int lanes, int* parts) {
+// waves of a call's rows; parts: those that share one, `waves` / rows or one for each round of heads
+static int64_t row_waves(int64_t waves, int64_t rows, int heads, int other_heads, int lanes, int* parts) {
   const int at_once = 64 / lanes;
   const int rounds = (heads + at_once - 1) / at_once + (other_heads + at_once - 1) / at_once;
-  *parts = (int)std::max<int64_t>(1, std::min<int64_t>(rounds, kRotateWaves / rows));
+  *parts = (int)std::max<int64_t>(1, std::min<int64_t>(rounds, waves / rows));
   return heads + other_heads > 0 ? rows * *parts : 0;
 }
 
 lam_status launch_kv_rotate(lam_ctx* ctx, RotateArgs a, int dtype) {
   const int lanes = a.dim <= 64 ? 8 : a.dim <= 128 ? 16 : 32;
-  const int64_t waves = row_waves(a.rows, a.h[0].heads, a.h[1].heads, lanes, &a.parts);
+  const int64_t waves = row_waves(kRotateWaves + a.rows - 1, a.rows, a.h[0].heads, a.h[1].heads, lanes, &a.parts);
   const int64_t blocks = (waves + kKvThreads / 64 - 1) / (kKvThreads / 64);
   LAM_CHECK(waves < (1LL << 31) && blocks <= most_blocks(kKvThreads), LAM_EINVAL, "too many rows for one launch");
   hipEvent_t e0, e1;
@@ -537,7 +540,7 @@ lam_status launch_kv_rotate_append(lam_ctx* ctx, const lam_kv_view& v, const Rot
   const int64_t values = quad_units(v, &g.quads) * v.kv_heads, per = kKvThreads / lanes;
   const int64_t v_blocks = (values + per - 1) / per;
   g.r = r;
-  const int64_t waves = row_waves(v.rows, r.h[0].heads, r.h[1].heads, lanes, &g.r.parts);
+  const int64_t waves = row_waves(kRotateWaves, v.rows, r.h[0].heads, r.h[1].heads, lanes, &g.r.parts);
   const int64_t blocks = v_blocks + (waves + kKvThreads / 64 - 1) / (kKvThreads / 64);
   LAM_CHECK(values < (1LL << 31) && waves < (1LL << 31) && blocks <= most_blocks(kKvThreads), LAM_EINVAL,
             "too many rows or sequences for one launch");
