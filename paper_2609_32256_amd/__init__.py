@@ -435,6 +435,10 @@ def _kv_elsewhere(ctx):
 
 def _kv_rows(t, heads, name, dev):
     """(rows, heads, head_dim) in float16 or bfloat16, channels contiguous."""
+    if isinstance(t, torch.Tensor) and t.get_device() == dev and t.dtype in _KV_DTYPES and not t.requires_grad \
+            and t.dim() == 3 and (heads is None or t.shape[1] == heads):
+        row, head, step = t.stride()
+        return t if step == 1 and row > 0 and head > 0 else t.contiguous()
     if not isinstance(t, torch.Tensor) or t.dtype not in _KV_DTYPES:
         raise TypeError(f"{name} must be a float16 or bfloat16 tensor")
     _kv_tensor(t, t.dtype, 3, name, dev)

@@ -383,8 +383,24 @@ constexpr int weight_strips() { return D == 256 ? 2 : 4; }
 // (with 8 heads of 128, 512 workgroups, 75 for 45).
 constexpr int64_t kWeightBlocks = 512;
 
-template <int D, bool BF16, int kStrips, bool WINDOW>
-__global__ __launch_bounds__(kAttThreads, D == 256 ? 2 : D == 64 && kStrips == 2 ? 4 : D == 64 || kStrips == 2 ? 3 : 2)
+// Of rows with a window only some tokens get weights, and each from some of the rows: workgroups
+// that have work are few and wait for the longest loop over rows, so where they are (busy: of 64
+// tokens each), they take fewer tokens and share the rows by eight waves.  Heads of 64 channels, us
+// with the attention, tokens/32 x waves: busy 54 1x8 23 (2x4 34, 2x8 29), 283 1x8 65 (2x8 75, 2x4 96),
+// 320 2x8 59 (1x8 63), 1,032 2x8 348 (2x4 398, 4x8 377), 1,728 2x4 64 (2x8 71, 4x4 66), 3,032 4x4 341 (2x4 396);
+// of 128: 54 1x8 32 (2x8 34, 2x4 38), 283 2x8 97 (1x8 102, 4x8 132), 484 4x8 88 (2x8 91), 1,032 4x8 493 (2x8
+// 583, 4x4 601), 1,728 4x4 94 (4x8 113); of 256 two strips and four waves as without a window (2x8 the same).
+struct WeightTile {
+  int strips, waves;
+};
+WeightTile windowed_tile(int head_dim, int64_t busy) {
+  if (head_dim == 256) return {2, kAttWaves};
+  if (head_dim == 64) return busy <= 300 ? WeightTile{1, 8} : busy < 1100 ? WeightTile{2, 8} : WeightTile{busy < 2500 ? 2 : 4, kAttWaves};
+  return busy <= 128 ? WeightTile{1, 8} : busy <= 400 ? WeightTile{2, 8} : WeightTile{4, busy < 1100 ? 8 : kAttWaves};
+}
+
+template <int D, bool BF16, int kStrips, bool WINDOW, int WAVES = kAttWaves>
+__global__ __launch_bounds__(64 * WAVES, kStrips == 1 ? 4 : D == 256 ? 2 : D == 64 && kStrips == 2 ? 4 : WAVES == 8 ? 2 : D == 64 || kStrips == 2 ? 3 : 2)
 void k_kv_weights(AttendArgs a) {
   constexpr int kSteps = D / 32, kTokens = kStrips * kKvStrip;
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
@@ -412,6 +428,7 @@ void k_kv_weights(AttendArgs a) {
   Walk walk;
   if constexpr (WINDOW) walk = Walk(a, w.len, pair_begin(a, w, 0));
   if (place0 >= walk.places(w.len) || w.pairs == 0) return;
+  auto begin_of = [&](int i) { return (int)max((int64_t)0, (int64_t)hidden + i + 1 - a.window); };
   auto strip = [&](int n) { return walk.token(place0 + n * kKvStrip); };   // its first token
   const int t0 = strip(0), t1 = strip(kStrips - 1) + kKvStrip;
   const int T = 1 << a.c.page_shift;
@@ -446,7 +463,7 @@ void k_kv_weights(AttendArgs a) {
   int r0 = first + 16 * wave;
   // The lane's pair of the next tile: row i of the sequence, head j of the group, and
   // where its query and its log sum lie; the last pair's stand in past the end.
-  constexpr int kStep = 16 * kAttWaves;
+  constexpr int kStep = 16 * WAVES;
   int i = (r0 + c) / a.group, j = (r0 + c) % a.group;
   const int di = kStep / a.group, dj = kStep % a.group;
   const int64_t q_step = di * a.q_row + dj * a.q_head, q_turn = a.q_row - a.group * a.q_head;
@@ -476,8 +493,15 @@ void k_kv_weights(AttendArgs a) {
     lp += turn ? l_turn : 0;
   };
   auto add = [&](int b, int r) {
-    bool whole = all == kAllTokens && t1 <= (a.causal ? min(w.len, hidden + r / a.group + 1) : w.len);
-    if constexpr (WINDOW) whole = whole && t0 >= pair_begin(a, w, min(r + 15, w.pairs - 1));
+    bool whole = all == kAllTokens;
+    int begin = 0;
+    if constexpr (WINDOW) {   // lanes 0 and 15 have the first row and the last
+      begin = begin_of(row[b]);
+      const int r_first = __builtin_amdgcn_readlane(row[b], 0);
+      whole = whole && t1 <= (a.causal ? min(w.len, hidden + r_first + 1) : w.len) && t0 >= __builtin_amdgcn_readlane(begin, 15);
+    } else {
+      whole = whole && t1 <= (a.causal ? min(w.len, hidden + r / a.group + 1) : w.len);
+    }
     const bool out = r + c >= w.pairs || e[b] == -__builtin_inff();
     const float less = out ? __builtin_inff() : e[b];   // no row, or one that sees no token: 2^(-inf) each
 #pragma unroll
@@ -494,7 +518,7 @@ void k_kv_weights(AttendArgs a) {
       if (!whole) {
         const int end = a.causal ? min(w.len, hidden + row[b] + 1) : w.len;
         uint32_t in = bits[n];
-        if constexpr (WINDOW) in &= window_bits(a, strip(n), pair_begin(a, w, row[b] * a.group));
+        if constexpr (WINDOW) in &= window_bits(a, strip(n), begin);
         hide(x, seen_bits(in, strip(n), end));
       }
 #pragma unroll
@@ -511,7 +535,7 @@ void k_kv_weights(AttendArgs a) {
       r0 += kStep;
     }
   }
-  __shared__ float total[kAttWaves][kTokens];
+  __shared__ float total[WAVES][kTokens];
 #pragma unroll
   for (int n = 0; n < kStrips; ++n)
 #pragma unroll
@@ -525,7 +549,7 @@ void k_kv_weights(AttendArgs a) {
   if ((int)threadIdx.x < kTokens && t < w.len && t < a.weights.cols) {
     float all = 0.0f;
 #pragma unroll
-    for (int n = 0; n < kAttWaves; ++n) all += total[n][threadIdx.x];
+    for (int n = 0; n < WAVES; ++n) all += total[n][threadIdx.x];
     static_cast<float*>(a.weights.p_dev)[w.s * a.weights.seq_stride + h * a.weights.head_stride + t] += all;
   }
 }
@@ -587,9 +611,10 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
   // last one's end: what lengths are split by and scores are kept by.
   a.reach = (int)kMost;
   a.seq_reach = a.cut;
+  int64_t span = 0;   // but for the rows
   if (windowed) {
     const int64_t most = v.starts_dev ? v.rows : a.c.per_seq;   // rows of a sequence
-    const int64_t span = (a.sinks + kKvStrip - 1) / kKvStrip * kKvStrip + (int64_t)a.window + kKvStrip;
+    span = (a.sinks + kKvStrip - 1) / kKvStrip * kKvStrip + (int64_t)a.window + kKvStrip;
     a.reach = (int)std::min(kMost, span + (causal ? (rows - 1) / a.group + 1 : most));
     a.seq_reach = std::min(a.cut, span + most);
   }
@@ -619,8 +644,9 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
   kept_blocks *= a.kept_waves;
   const int64_t heads = (int64_t)v.kv_heads * v.n_seqs;
   auto weight_blocks_of = [&](int strips) { return (a.seq_reach + strips * kKvStrip - 1) / (strips * kKvStrip) * heads; };
-  const bool few = v.head_dim == 256 || weight_blocks_of(4) < kWeightBlocks;
-  const int64_t weight_blocks = weights.p_dev && !keep ? weight_blocks_of(few ? 2 : 4) : 0;   // (a cut of 0: none)
+  WeightTile tile{v.head_dim == 256 || weight_blocks_of(4) < kWeightBlocks ? 2 : 4, kAttWaves};
+  if (windowed) tile = windowed_tile(v.head_dim, (std::min(a.cut, span + v.rows / v.n_seqs) + 63) / 64 * heads);
+  const int64_t weight_blocks = weights.p_dev && !keep ? weight_blocks_of(tile.strips) : 0;   // (a cut of 0: none)
   LAM_CHECK(std::max({blocks, join_blocks + kept_blocks, weight_blocks}) <= most_blocks(kAttThreads), LAM_EINVAL,
             "too many rows, or sequences times the bound of lengths, for one launch (%lld tokens: give max_length)",
             (long long)a.cut);
@@ -674,19 +700,26 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
   if (weight_blocks > 0) {
     LAM_TRY(prof_launch_events(ctx, "kv_weights", &e0, &e1));
     const dim3 grid((unsigned)weight_blocks);
-#define LAM_STRIPS(D, BF, N)                                                                             \
-  do {                                                                                                 \
-    if (windowed) launch(k_kv_weights<D, BF, N, true>, grid, kAttThreads, ctx->stream, e0, e1, a);     \
-    else launch(k_kv_weights<D, BF, N, false>, grid, kAttThreads, ctx->stream, e0, e1, a);             \
-  } while (0)
-#define LAM_GO(D, BF)                              \
-  do {                                             \
-    if (few) LAM_STRIPS(D, BF, 2);                 \
-    else LAM_STRIPS(D, BF, weight_strips<D>());    \
+#define LAM_TILE(D, BF, N, W, V) launch(k_kv_weights<D, BF, N, W, V>, grid, 64 * V, ctx->stream, e0, e1, a)
+#define LAM_GO(D, BF)                                                                    \
+  do {                                                                                   \
+    if (!windowed) {                                                                     \
+      if (tile.strips == 2) LAM_TILE(D, BF, 2, false, kAttWaves);                        \
+      else LAM_TILE(D, BF, weight_strips<D>(), false, kAttWaves);                        \
+    } else if constexpr (D == 256) {                                                     \
+      LAM_TILE(D, BF, 2, true, kAttWaves);                                               \
+    } else if (tile.waves == 8) {                                                        \
+      if (tile.strips == 1) LAM_TILE(D, BF, 1, true, 8);                                 \
+      else if (tile.strips == 2) LAM_TILE(D, BF, 2, true, 8);                            \
+      else if constexpr (D == 128) LAM_TILE(D, BF, 4, true, 8);                          \
+    } else {                                                                             \
+      if (tile.strips == 4) LAM_TILE(D, BF, 4, true, kAttWaves);                         \
+      else if constexpr (D == 64) LAM_TILE(D, BF, 2, true, kAttWaves);                   \
+    }                                                                                    \
   } while (0)
     LAM_KV_DISPATCH(v, LAM_GO);
 #undef LAM_GO
-#undef LAM_STRIPS
+#undef LAM_TILE
     LAM_HIP(hipGetLastError());
   }
   return LAM_OK;

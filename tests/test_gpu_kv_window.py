@@ -196,7 +196,8 @@ def test_a_window_of_everything_is_none(lam):
             assert torch.equal(c.call(window=window, sinks=1 << 40), want)
         w, w2 = (torch.zeros((len(lens), 2, max(lens)), device="cuda") for _ in range(2))
         c.call(weights=w), c.call(weights=w2, window=max(lens))
-        assert torch.equal(w, w2)
+        # sums of a token's p over the rows and heads of a group, in another order
+        assert ((w - w2).abs() <= max(rows) * c.G * 2.0 ** -24 * w).all()
 
 
 def test_weights_outside_the_window_stay(lam):
