@@ -130,21 +130,39 @@ __device__ __forceinline__ void gains(const RotateHeads& h, const Lane<MODE>& at
   }
 }
 
-// The raw other channels of a lane's eight, given its own.
+// A wave's LDS accesses are in order: what its lanes have written is there for the others.
+__device__ __forceinline__ void wave_lds_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// The raw other channels of a lane's eight, given its own.  pass: 16 bytes of LDS for each lane, for
+// pairs whose channels are no whole number of lanes apart (read from memory once more, 41,569 rows of
+// 108 heads of 64 channels and 20 pairs took 384 us, so 273).
 template <int MODE, int L>
-__device__ __forceinline__ kv_u4 others(const Lane<MODE>& at, kv_u4 own, const uint16_t* head) {
+__device__ __forceinline__ kv_u4 others(const Lane<MODE>& at, kv_u4 own, kv_u4* pass) {
   kv_u4 w = own;
+  const int lane = (int)threadIdx.x & 63, group = lane & ~(L - 1);
   if constexpr (MODE == kHalves) {
-    const int from = ((int)threadIdx.x & 63 & ~(L - 1)) + at.other(0) / 8;
+    const int from = group + at.other(0) / 8;
 #pragma unroll
     for (int j = 0; j < 4; ++j) w[j] = (uint32_t)__shfl((int)own[j], from);
   } else if constexpr (MODE == kInterleaved) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) w[j] = __builtin_amdgcn_alignbit(own[j], own[j], 16);
   } else {
+    wave_lds_order();
+    pass[lane] = own;
+    wave_lds_order();
+    if (at.pairs & 1) {
+      const uint16_t* const c = reinterpret_cast<const uint16_t*>(pass + group);
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      w[j] = (uint32_t)head[at.other(2 * j)] | ((uint32_t)head[at.other(2 * j + 1)] << 16);
+      for (int j = 0; j < 4; ++j) w[j] = (uint32_t)c[at.other(2 * j)] | ((uint32_t)c[at.other(2 * j + 1)] << 16);
+    } else {
+      const uint32_t* const c = reinterpret_cast<const uint32_t*>(pass + group);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[j] = c[at.other(2 * j) / 2];
+    }
   }
   return w;
 }
@@ -195,11 +213,18 @@ struct __align__(16) RowAngles {
   float c[kMostPairs], s[kMostPairs];
 };
 
+// 16 bytes a lane, where others() needs them.
+template <int MODE>
+struct Pass {
+  kv_u4 w[MODE == kHalvesAnywhere ? 64 : 1];
+};
+
 // A wave norms and turns a row, or where rows are few a part of its heads, 64/L heads at a time.
 // What a lane needs of the sines and cosines for all heads lies in its registers, multiplied by
 // the gains.  kinds: of the queries alone, or of the keys as well.
 template <int L, bool BF16, int MODE>
-__device__ __forceinline__ void rotate_row(const RotateArgs& a, int kinds, int64_t row, int part, const RowAngles& angles) {
+__device__ __forceinline__ void rotate_row(const RotateArgs& a, int kinds, int64_t row, int part, const RowAngles& angles,
+                                           kv_u4* pass) {
   constexpr int kAtOnce = 64 / L;
   const int lane = threadIdx.x & 63, sub = lane % L, slot = lane / L;
   const Lane<MODE> at{8 * sub, a.pairs};
@@ -239,8 +264,7 @@ __device__ __forceinline__ void rotate_row(const RotateArgs& a, int kinds, int64
     }
     for (; i < rounds; i += a.parts) {
       const kv_u4 own = next;
-      kv_u4 other{};
-      if (MODE != kHalvesAnywhere || live) other = others<MODE, L>(at, own, row_of(i));
+      const kv_u4 other = others<MODE, L>(at, own, pass);
       if (i + a.parts < rounds) next = load(i + a.parts);
       float u[8], v[8], y[8];
       unpack8<BF16>(own, u);
@@ -257,16 +281,11 @@ __device__ __forceinline__ void rotate_row(const RotateArgs& a, int kinds, int64
   }
 }
 
-// A wave's LDS accesses are in order: what its lanes have written is there for the others.
-__device__ __forceinline__ void wave_lds_written() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-}
-
 // Bound by memory.
 template <int L, bool BF16, int MODE>
 __global__ __launch_bounds__(kKvThreads) void k_kv_rotate(RotateArgs a) {
   __shared__ RowAngles angles[kKvThreads / 64];
+  __shared__ Pass<MODE> pass[kKvThreads / 64];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t id = blockIdx.x * (kKvThreads / 64) + wave;
   const int64_t row = id / (uint32_t)a.parts;
@@ -277,8 +296,8 @@ __global__ __launch_bounds__(kKvThreads) void k_kv_rotate(RotateArgs a) {
     angles[wave].c[i] = c * a.amplitude;
     angles[wave].s[i] = s * a.amplitude;
   }
-  wave_lds_written();
-  rotate_row<L, BF16, MODE>(a, 2, row, (int)(id % (uint32_t)a.parts), angles[wave]);
+  wave_lds_order();
+  rotate_row<L, BF16, MODE>(a, 2, row, (int)(id % (uint32_t)a.parts), angles[wave], pass[wave].w);
 }
 
 // ------------------------------------------------------------------ rows into the cache
@@ -376,7 +395,7 @@ struct Token {
 // rounding on the way.
 template <int D, bool BF16, int MODE>
 __device__ __forceinline__ void append_keys(const AppendArgs& g, int64_t row, int i, const Token& token,
-                                            const Factors<D>& f) {
+                                            const Factors<D>& f, kv_u4* pass) {
   constexpr int kLanes = D / 8, kAtOnce = 64 / kLanes;
   const KvArgs& a = g.c;
   const RotateArgs& r = g.r;
@@ -387,7 +406,7 @@ __device__ __forceinline__ void append_keys(const AppendArgs& g, int64_t row, in
   auto row_of = [&](int i) { return kh.x + row * kh.x_row + (int64_t)min(i * kAtOnce + slot, a.heads - 1) * kh.x_head; };
   kv_u4 next = load_raw8(row_of(i), at.c0, kh.x_wide);
   for (; i * kAtOnce < a.heads; i += r.parts) {
-    const kv_u4 own = next, other = others<MODE, kLanes>(at, own, row_of(i));
+    const kv_u4 own = next, other = others<MODE, kLanes>(at, own, pass);
     next = load_raw8(row_of(i + r.parts), at.c0, kh.x_wide);
     float u[8], v[8], x[8];
     unpack8<BF16>(own, u);
@@ -450,6 +469,7 @@ __global__ __launch_bounds__(kKvThreads) void k_kv_rotate_append(AppendArgs g) {
   constexpr int kLanes = D / 8, kAtOnce = 64 / kLanes, kWaves = kKvThreads / 64;
   __shared__ RowAngles row_angles[kWaves];
   __shared__ Factors<D> key_factors[kWaves];
+  __shared__ Pass<MODE> pass[kWaves];
   if (blockIdx.x < g.v_blocks) {
     append_values<D, BF16>(g);
     return;
@@ -488,9 +508,9 @@ __global__ __launch_bounds__(kKvThreads) void k_kv_rotate_append(AppendArgs g) {
       f.own[v] = c * gv, f.other[v] = s * gu;
     }
   }
-  wave_lds_written();
-  if (keys) append_keys<D, BF16, MODE>(g, row, k_first, token, f);
-  rotate_row<kLanes, BF16, MODE>(r, 1, row, part, angles);
+  wave_lds_order();
+  if (keys) append_keys<D, BF16, MODE>(g, row, k_first, token, f, pass[wave].w);
+  rotate_row<kLanes, BF16, MODE>(r, 1, row, part, angles, pass[wave].w);
 }
 
 // Waves that a call of few rows is shared out to, at least for rows on their own, at most on the way
