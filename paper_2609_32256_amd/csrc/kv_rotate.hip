@@ -206,11 +206,10 @@ __device__ __forceinline__ float norm_of(const RotateArgs& a, const float u[8]) 
 }
 
 // ------------------------------------------------------------------ rows in 16 bits
-constexpr int kMostPairs = 128;
-
-// Sines and cosines of a wave's row.
+// Sines and cosines of a row of at most 8 L channels.
+template <int L>
 struct __align__(16) RowAngles {
-  float c[kMostPairs], s[kMostPairs];
+  float c[4 * L], s[4 * L];
 };
 
 // 16 bytes a lane, where others() needs them.
@@ -223,7 +222,7 @@ struct Pass {
 // What a lane needs of the sines and cosines for all heads lies in its registers, multiplied by
 // the gains.  kinds: of the queries alone, or of the keys as well.
 template <int L, bool BF16, int MODE>
-__device__ __forceinline__ void rotate_row(const RotateArgs& a, int kinds, int64_t row, int part, const RowAngles& angles,
+__device__ __forceinline__ void rotate_row(const RotateArgs& a, int kinds, int64_t row, int part, const RowAngles<L>& angles,
                                            kv_u4* pass) {
   constexpr int kAtOnce = 64 / L;
   const int lane = threadIdx.x & 63, sub = lane % L, slot = lane / L;
@@ -281,10 +280,86 @@ __device__ __forceinline__ void rotate_row(const RotateArgs& a, int kinds, int64
   }
 }
 
+// Few heads leave most of a wave idle while it makes a row's angles and its last heads: there it
+// takes four rows, and the heads of all of them in turn.
+constexpr int kFewRows = 4;
+
+// i / by for i < 512, by <= 128, inverse = 65536 / by + 1
+__device__ __forceinline__ int small_div(int i, uint32_t inverse) { return (int)((uint32_t)i * inverse >> 16); }
+
+// The heads of n rows from row0 on.  none: bit i: row i is of no sequence and gets 0.
+template <int L, bool BF16, int MODE>
+__device__ __forceinline__ void rotate_few(const RotateArgs& a, int kinds, int64_t row0, int n, uint32_t none,
+                                           const RowAngles<L>* angles, kv_u4* pass) {
+  constexpr int kAtOnce = 64 / L;
+  const int lane = threadIdx.x & 63, sub = lane % L, slot = lane / L;
+  const Lane<MODE> at{8 * sub, a.pairs};
+  const bool live = at.c0 < a.dim;
+#pragma unroll 1
+  for (int kind = 0; kind < kinds; ++kind) {
+    const RotateHeads& h = a.h[kind];
+    if (h.heads == 0) continue;
+    const uint32_t inverse = 65536u / (uint32_t)h.heads + 1u;
+    const int items = n * h.heads;
+    float g[8], go[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) g[e] = go[e] = 1.0f;
+    if (h.gain && live) gains<MODE, BF16>(h, at, g, go);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) go[e] = at.minus(e) ? -go[e] : go[e];
+    auto load = [&](int i) {
+      const int item = min(i + slot, items - 1), r = small_div(item, inverse);
+      kv_u4 w{};
+      if (live) w = load_raw8(h.x + (row0 + r) * h.x_row + (int64_t)(item - r * h.heads) * h.x_head, at.c0, h.x_wide);
+      return w;
+    };
+    kv_u4 next = load(0);
+    for (int i = 0; i < items; i += kAtOnce) {
+      const kv_u4 own = next, other = others<MODE, L>(at, own, pass);
+      if (i + kAtOnce < items) next = load(i + kAtOnce);
+      const int item = min(i + slot, items - 1), r = small_div(item, inverse);
+      float u[8], v[8], y[8];
+      unpack8<BF16>(own, u);
+      unpack8<BF16>(other, v);
+      const float norm = h.gain ? norm_of<L>(a, u) : 1.0f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        y[e] = u[e] * g[e];
+        if (live && at.turned(e)) y[e] = fmaf(v[e] * go[e], angles[r].s[at.pair(e)], y[e] * angles[r].c[at.pair(e)]);
+        y[e] *= norm;
+      }
+      kv_u4 w = pack8<BF16>(y);
+      if ((none >> r) & 1u) w = kv_u4{0, 0, 0, 0};
+      if (live && i + slot < items)
+        store_raw8(h.y, (row0 + r) * h.y_row + (int64_t)(item - r * h.heads) * h.y_head + at.c0, h.y_wide, w);
+    }
+  }
+}
+
+template <int L, bool BF16, int MODE>
+__global__ __launch_bounds__(kKvThreads) void k_kv_rotate_few(RotateArgs a) {
+  __shared__ RowAngles<L> angles[kKvThreads / 64][kFewRows];
+  __shared__ Pass<MODE> pass[kKvThreads / 64];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t row0 = ((int64_t)blockIdx.x * (kKvThreads / 64) + wave) * kFewRows;
+  if (row0 >= a.rows) return;
+  const int n = (int)min((int64_t)kFewRows, a.rows - row0);
+  const uint32_t inverse = a.pairs ? 65536u / (uint32_t)a.pairs + 1u : 0u;
+  for (int i = threadIdx.x & 63; i < n * a.pairs; i += 64) {
+    const int r = small_div(i, inverse), pair = i - r * a.pairs;
+    float c, s;
+    sin_cos(a.positions[row0 + r], a.freq[pair], &c, &s);
+    angles[wave][r].c[pair] = c * a.amplitude;
+    angles[wave][r].s[pair] = s * a.amplitude;
+  }
+  wave_lds_order();
+  rotate_few<L, BF16, MODE>(a, 2, row0, n, 0, angles[wave], pass[wave].w);
+}
+
 // Bound by memory.
 template <int L, bool BF16, int MODE>
 __global__ __launch_bounds__(kKvThreads) void k_kv_rotate(RotateArgs a) {
-  __shared__ RowAngles angles[kKvThreads / 64];
+  __shared__ RowAngles<L> angles[kKvThreads / 64];
   __shared__ Pass<MODE> pass[kKvThreads / 64];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t id = blockIdx.x * (kKvThreads / 64) + wave;
@@ -463,11 +538,115 @@ __device__ __forceinline__ bool row_token(const KvArgs& a, int64_t row, const in
   return true;
 }
 
+// What four rows' keys are turned by, the amplitude in it.
+template <int D>
+struct __align__(16) RowTurns {
+  double c[D / 2], s[D / 2];
+};
+
+// append_keys for the keys of n rows from row0 on, the heads of all of them in turn.
+template <int D, bool BF16, int MODE>
+__device__ __forceinline__ void append_few(const AppendArgs& g, int64_t row0, int n, const Token* tokens,
+                                           const RowTurns<D>* turns, kv_u4* pass) {
+  constexpr int kLanes = D / 8, kAtOnce = 64 / kLanes;
+  const RotateArgs& a = g.r;
+  const RotateHeads& h = a.h[1];
+  const int lane = threadIdx.x & 63, sub = lane % kLanes, slot = lane / kLanes, T = 1 << g.c.page_shift;
+  const Lane<MODE> at{8 * sub, a.pairs};
+  const uint32_t inverse = 65536u / (uint32_t)h.heads + 1u;
+  const int items = n * h.heads;
+  bool bad = false, over = false;
+  float gn[8], go[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) gn[e] = go[e] = 1.0f;
+  if (h.gain) gains<MODE, BF16>(h, at, gn, go);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) go[e] = at.minus(e) ? -go[e] : go[e];
+  auto load = [&](int i) {
+    const int item = min(i + slot, items - 1), r = small_div(item, inverse);
+    return load_raw8(h.x + (row0 + r) * h.x_row + (int64_t)(item - r * h.heads) * h.x_head, at.c0, h.x_wide);
+  };
+  kv_u4 next = load(0);
+  for (int i = 0; i < items; i += kAtOnce) {
+    const kv_u4 own = next, other = others<MODE, kLanes>(at, own, pass);
+    next = load(i + kAtOnce);
+    const int item = min(i + slot, items - 1), r = small_div(item, inverse), head = item - r * h.heads;
+    float u[8], v[8], x[8];
+    unpack8<BF16>(own, u);
+    unpack8<BF16>(other, v);
+    double y[8], norm = 1.0;
+    if (h.gain) {
+      double ss = 0.0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) ss = fma((double)u[e], (double)u[e], ss);
+      norm = inverse_root(fma(group_sum_f64<kLanes>(ss), a.inv_dim, a.eps));
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {   // (a product of a gain and 16 bits is exact)
+      y[e] = (double)u[e] * (double)gn[e];
+      if (at.turned(e)) y[e] = fma((double)v[e] * (double)go[e], turns[r].s[at.pair(e)], y[e] * turns[r].c[at.pair(e)]);
+      y[e] *= norm;
+    }
+    to_odd8(y, x);
+    const Token token = tokens[r];
+    if (i + slot < items && token.page) {
+      uint32_t b;
+      const uint32_t w = quantize8(x, &b, &bad, &over);
+      put_key<D>(token.page + (int64_t)head * KvLayout<D>::head_bytes(T), T, token.t, sub, w, b);
+    }
+  }
+  if (g.status) {
+    count_in(g.status, 0, bad);
+    count_in(g.status, 1, over);
+  }
+}
+
+// k_kv_rotate_append for few heads.
+template <int D, bool BF16, int MODE>
+__global__ __launch_bounds__(kKvThreads) void k_kv_rotate_append_few(AppendArgs g) {
+  constexpr int kLanes = D / 8, kWaves = kKvThreads / 64;
+  __shared__ RowAngles<kLanes> row_angles[kWaves][kFewRows];
+  __shared__ RowTurns<D> key_turns[kWaves][kFewRows];
+  __shared__ Token row_tokens[kWaves][kFewRows];
+  __shared__ Pass<MODE> pass[kWaves];
+  if (blockIdx.x < g.v_blocks) {
+    append_values<D, BF16>(g);
+    return;
+  }
+  const RotateArgs& r = g.r;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int64_t row0 = ((int64_t)(blockIdx.x - g.v_blocks) * kWaves + wave) * kFewRows;
+  if (row0 >= g.c.rows) return;
+  const int n = (int)min((int64_t)kFewRows, g.c.rows - row0);
+  uint32_t none = 0, stored = 0;
+#pragma unroll 1
+  for (int i = 0; i < n; ++i) {
+    Token token{0, 0, nullptr};
+    none |= row_token<D>(g.c, row0 + i, g.first, &token) ? 0u : 1u << i;
+    stored |= token.page ? 1u << i : 0u;
+    if (lane == 0) row_tokens[wave][i] = token;
+  }
+  wave_lds_order();
+  const uint32_t inverse = r.pairs ? 65536u / (uint32_t)r.pairs + 1u : 0u;
+  for (int i = lane; i < n * r.pairs; i += 64) {
+    const int row = small_div(i, inverse), pair = i - row * r.pairs;
+    double c, s;
+    sin_cos(row_tokens[wave][row].pos, r.freq[pair], &c, &s);
+    key_turns[wave][row].c[pair] = c *= r.amplitude64;
+    key_turns[wave][row].s[pair] = s *= r.amplitude64;
+    row_angles[wave][row].c[pair] = (float)c;
+    row_angles[wave][row].s[pair] = (float)s;
+  }
+  wave_lds_order();
+  if (stored) append_few<D, BF16, MODE>(g, row0, n, row_tokens[wave], key_turns[wave], pass[wave].w);
+  rotate_few<kLanes, BF16, MODE>(r, 1, row0, n, none, row_angles[wave], pass[wave].w);
+}
+
 // Workgroups of values, then waves of a row's queries and keys each (or parts of them).
 template <int D, bool BF16, int MODE>
 __global__ __launch_bounds__(kKvThreads) void k_kv_rotate_append(AppendArgs g) {
   constexpr int kLanes = D / 8, kAtOnce = 64 / kLanes, kWaves = kKvThreads / 64;
-  __shared__ RowAngles row_angles[kWaves];
+  __shared__ RowAngles<kLanes> row_angles[kWaves];
   __shared__ Factors<D> key_factors[kWaves];
   __shared__ Pass<MODE> pass[kWaves];
   if (blockIdx.x < g.v_blocks) {
@@ -490,7 +669,7 @@ __global__ __launch_bounds__(kKvThreads) void k_kv_rotate_append(AppendArgs g) {
   const int q_rounds = (q.heads + kAtOnce - 1) / kAtOnce;
   const int k_first = (part - q_rounds % r.parts + r.parts) % r.parts;   // the wave's first round of keys
   const bool keys = token.page && k_first * kAtOnce < g.c.heads;
-  RowAngles& angles = row_angles[wave];
+  RowAngles<kLanes>& angles = row_angles[wave];
   Factors<D>& f = key_factors[wave];
   for (int i = lane; i < D / 2; i += 64) {
     double c = 1.0, s = 0.0;
@@ -519,6 +698,16 @@ __global__ __launch_bounds__(kKvThreads) void k_kv_rotate_append(AppendArgs g) {
 // (1: 19.7); into the cache 2,000 in 2 14.1 us (1: 16.0, 3: 17.8), 3,000 in 1 19.4 (2: 21.9).
 constexpr int64_t kRotateWaves = 4096;
 
+// Whether a wave takes four rows: for heads so few that the rounds of one leave lanes idle, and so
+// many rows that a quarter of the waves fills the chip.  65,536 rows, one and four rows a wave, us:
+// 64 channels, 4 + 1 heads 52 and 25 (into the cache 85 and 42), 32 + 4 heads 109 and 108 (144 and
+// 127); 128 channels, 4 + 1 heads 55 and 36 (93 and 60), 16 + 2 111 and 109 (145 and 133), 16 + 4 123
+// and 134 (156 and 164).  16,384 rows: 64 channels, 16 + 4 heads 22 and 21 (33 and 30), 32 + 8 32 and 36
+// (44 and 48); 8,192: 4 + 1 heads 9 and 7 (13 and 10), 16 + 4 13 and 17.  Heads of 256 channels fill a wave by two.
+bool few_heads(int64_t rows, int heads, int lanes) {
+  return heads <= (lanes == 8 ? 40 : lanes == 16 ? 18 : 0) && rows >= std::max(8192, 128 * lanes * heads);
+}
+
 }  // namespace
 
 // waves of a call's rows; parts: those that share one, `waves` / rows or one for each round of heads
@@ -532,22 +721,29 @@ static int64_t row_waves(int64_t waves, int64_t rows, int heads, int other_heads
 lam_status launch_kv_rotate(lam_ctx* ctx, RotateArgs a, int dtype) {
   const int lanes = a.dim <= 64 ? 8 : a.dim <= 128 ? 16 : 32;
   const int64_t waves = row_waves(kRotateWaves + a.rows - 1, a.rows, a.h[0].heads, a.h[1].heads, lanes, &a.parts);
-  const int64_t blocks = (waves + kKvThreads / 64 - 1) / (kKvThreads / 64);
+  const bool few = few_heads(a.rows, a.h[0].heads + a.h[1].heads, lanes);
+  const int64_t blocks = ((few ? (a.rows + kFewRows - 1) / kFewRows : waves) + kKvThreads / 64 - 1) / (kKvThreads / 64);
   LAM_CHECK(waves < (1LL << 31) && blocks <= most_blocks(kKvThreads), LAM_EINVAL, "too many rows for one launch");
   hipEvent_t e0, e1;
   LAM_TRY(prof_launch_events(ctx, "kv_rotate", &e0, &e1));
   const dim3 grid((unsigned)blocks);
-#define LAM_GO(L, BF)                                                                                                  \
-  do {                                                                                                                 \
-    if (a.interleaved) launch(k_kv_rotate<L, BF, kInterleaved>, grid, kKvThreads, ctx->stream, e0, e1, a);             \
-    else if (a.pairs % 8 == 0) launch(k_kv_rotate<L, BF, kHalves>, grid, kKvThreads, ctx->stream, e0, e1, a);          \
-    else launch(k_kv_rotate<L, BF, kHalvesAnywhere>, grid, kKvThreads, ctx->stream, e0, e1, a);                        \
+#define LAM_MODE(L, BF, M)                                                                                  \
+  do {                                                                                                      \
+    if (L < 32 && few) launch(k_kv_rotate_few<L < 32 ? L : 16, BF, M>, grid, kKvThreads, ctx->stream, e0, e1, a); \
+    else launch(k_kv_rotate<L, BF, M>, grid, kKvThreads, ctx->stream, e0, e1, a);                           \
+  } while (0)
+#define LAM_GO(L, BF)                                          \
+  do {                                                         \
+    if (a.interleaved) LAM_MODE(L, BF, kInterleaved);          \
+    else if (a.pairs % 8 == 0) LAM_MODE(L, BF, kHalves);       \
+    else LAM_MODE(L, BF, kHalvesAnywhere);                     \
   } while (0)
   const bool bf = dtype == LAM_BF16;
   if (lanes == 8) { if (bf) LAM_GO(8, true); else LAM_GO(8, false); }
   else if (lanes == 16) { if (bf) LAM_GO(16, true); else LAM_GO(16, false); }
   else { if (bf) LAM_GO(32, true); else LAM_GO(32, false); }
 #undef LAM_GO
+#undef LAM_MODE
   LAM_HIP(hipGetLastError());
   return LAM_OK;
 }
@@ -561,7 +757,8 @@ lam_status launch_kv_rotate_append(lam_ctx* ctx, const lam_kv_view& v, const Rot
   const int64_t v_blocks = (values + per - 1) / per;
   g.r = r;
   const int64_t waves = row_waves(kRotateWaves, v.rows, r.h[0].heads, r.h[1].heads, lanes, &g.r.parts);
-  const int64_t blocks = v_blocks + (waves + kKvThreads / 64 - 1) / (kKvThreads / 64);
+  const bool few = few_heads(v.rows, r.h[0].heads + r.h[1].heads, lanes);
+  const int64_t blocks = v_blocks + ((few ? (v.rows + kFewRows - 1) / kFewRows : waves) + kKvThreads / 64 - 1) / (kKvThreads / 64);
   LAM_CHECK(values < (1LL << 31) && waves < (1LL << 31) && blocks <= most_blocks(kKvThreads), LAM_EINVAL,
             "too many rows or sequences for one launch");
   g.c = KvArgs::of(v);
@@ -574,7 +771,11 @@ lam_status launch_kv_rotate_append(lam_ctx* ctx, const lam_kv_view& v, const Rot
   hipEvent_t e0, e1;
   LAM_TRY(prof_launch_events(ctx, "kv_rotate_append", &e0, &e1));
   const dim3 grid((unsigned)blocks);
-#define LAM_MODE(D, BF, M) launch(k_kv_rotate_append<D, BF, M>, grid, kKvThreads, ctx->stream, e0, e1, g)
+#define LAM_MODE(D, BF, M)                                                                                          \
+  do {                                                                                                              \
+    if (D < 256 && few) launch(k_kv_rotate_append_few<D < 256 ? D : 128, BF, M>, grid, kKvThreads, ctx->stream, e0, e1, g); \
+    else launch(k_kv_rotate_append<D, BF, M>, grid, kKvThreads, ctx->stream, e0, e1, g);                            \
+  } while (0)
 #define LAM_GO(D, BF)                                          \
   do {                                                         \
     if (r.interleaved) LAM_MODE(D, BF, kInterleaved);          \

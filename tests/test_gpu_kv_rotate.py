@@ -93,6 +93,32 @@ def test_rotate_sizes(lam, rows, Hq, Hk, D):
         assert ((y.double() - want).abs() <= 2.0 ** -8 * want.abs() + 1e-4).all()
 
 
+@pytest.mark.parametrize("D,Hq,Hk,layout,pairs", [
+    (64, 4, 1, "half", 32), (64, 3, 2, "half", 21), (40, 5, 0, "interleaved", 20), (64, 24, 16, "interleaved", 8),
+    (128, 4, 1, "half", 64), (128, 7, 2, "half", 33), (96, 1, 1, "interleaved", 16), (128, 16, 2, "half", 0),
+])
+def test_few_heads_of_many_rows(lam, D, Hq, Hk, layout, pairs):
+    """Waves of four rows each: against waves of one (calls of fewer rows), whose results are the same but
+    for the order of a product's factors, and against the oracle at both ends."""
+    n = 40961
+    f = _freq(kv.frequencies(pairs)[0] if pairs else [])
+    q, k = _rows(D, n, Hq, D, "bf16"), _rows(D + 1, n, Hk, D, "bf16") if Hk else None
+    pos = (torch.arange(n, dtype=torch.int32, device="cuda") * 7919) % 100003 - 50
+    g = _gain(D, D)
+    call = dict(layout=layout, amplitude=1.125, q_norm=g, k_norm=g)
+    whole = lam.kv_rotate(q, f, pos, k=k, **call)
+    whole = whole if Hk else (whole,)
+    for x, y in zip((q, k), whole):
+        for a in range(0, n, 4099):
+            part = lam.kv_rotate(x[a:a + 4099], f, pos[a:a + 4099], layout=layout, amplitude=1.125, q_norm=g)
+            got = y[a:a + 4099]
+            assert ((got.float() - part.float()).abs() <= 2.0 ** -7 * part.abs().float() + 2.0 ** -19 * x[a:a + 4099].abs().amax()).all()
+        ends = [0, 1, 2, 3, 4, n - 2, n - 1]
+        _check(y[ends], x[ends], pos[ends].tolist(), f.tolist(), layout, 1.125, g, 1e-6, None, "bf16")
+    lam.kv_rotate(q, f, pos, k=k, out=(q, k) if Hk else q, **call)
+    assert torch.equal(q, whole[0]) and (not Hk or torch.equal(k, whole[1]))
+
+
 @pytest.mark.parametrize("pos", [(1 << 31) - 1, -(1 << 31), (1 << 30) + 12345, 999999937])
 @pytest.mark.parametrize("layout", ["half", "interleaved"])
 def test_far_positions(lam, pos, layout):
@@ -256,6 +282,47 @@ def test_rotate_append(lam, D, T, Hq, Hk, dt, rows, lens, layout, norm):
 def test_rotate_append_parts(lam, D, layout, pairs):
     _append_case(lam, D, 32, 6, 3, "bf16", [9, 2], [40, 2], layout, pairs=pairs, seed=pairs)
     _append_case(lam, D, 32, 6, 3, "f16", [9, 2], [40, 2], layout, pairs=pairs, seed=pairs, packed=True, norm=False, first=[-7, 0])
+
+
+@pytest.mark.parametrize("D,Hq,Hk,layout,pairs,norm", [
+    (64, 4, 1, "half", 32, True), (64, 2, 3, "half", 21, False), (64, 0, 2, "interleaved", 20, True),
+    (128, 4, 1, "half", 64, True), (128, 3, 2, "half", 33, True), (128, 1, 1, "interleaved", 16, False),
+])
+def test_few_heads_of_many_rows_into_the_cache(lam, D, Hq, Hk, layout, pairs, norm):
+    """Waves of four rows each, ragged, with rows of no sequence and tokens without a place: the codes
+    and the queries of calls of fewer rows."""
+    rows, T = [9001, 0, 3, 12345, 1], 64
+    lens = [9001, 7, 100, 12600, 1]
+    before, after = 2, 6
+    n = sum(rows) + before + after
+    f = _freq(kv.frequencies(pairs)[0])
+    q = _rows(D, n, Hq, D, "f16") if Hq else None
+    k, v = _rows(D + 1, n, Hk, D, "f16"), _rows(D + 2, n, Hk, D, "f16")
+    g = _gain(D, D) if norm else None
+    cols = -(-max(lens) // T)
+    table = torch.arange(5 * cols, dtype=torch.int32, device="cuda").view(5, cols).flip(1).contiguous()
+    table[3, 190] = -1
+    first = _i32([0, 5, 100000, -40, 9])
+    starts = np.cumsum([before] + rows)
+    call = dict(layout=layout, amplitude=1.125, q_norm=g if Hq else None, k_norm=g)
+    pool, status = lam.kv_pages(5 * cols, Hk, D, T), _i32([0, 0, 0])
+    got = lam.kv_rotate_append(q, k, v, pool, table, _i32(lens), f, starts=_i32(starts.tolist()), first=first, status=status, **call)
+    lost = min(max(0, 191 * T - (12600 - 12345)), 12345) - max(0, 190 * T - (12600 - 12345))
+    assert status.tolist() == [0, 0, (before + after + lost) * Hk]
+    want_pool = lam.kv_pages(5 * cols, Hk, D, T)
+    for b in range(5):
+        for a in range(0, rows[b], 1000):                         # the same tokens, a thousand at a time
+            m = min(1000, rows[b] - a)
+            at = slice(starts[b] + a, starts[b] + a + m)
+            length = _i32([lens[b] - rows[b] + a + m])
+            part = lam.kv_rotate_append(None if q is None else q[at], k[at], v[at], want_pool, table[b:b + 1], length, f,
+                                        first=first[b:b + 1] + a, **call)
+            if Hq:
+                tol = 2.0 ** -10 * part.float().abs() + 2.0 ** -19 * q[at].float().abs().amax() + 2.0 ** -24
+                assert ((got[at].float() - part.float()).abs() <= tol).all()
+    assert torch.equal(pool, want_pool)
+    if Hq:
+        assert not got[:before].any() and not got[-after:].any()
 
 
 def test_rotate_append_of_padded_heads_and_rows(lam):
