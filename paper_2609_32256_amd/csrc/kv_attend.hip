@@ -390,11 +390,14 @@ constexpr int64_t kWeightBlocks = 512;
 // 320 2x8 59 (1x8 63), 1,032 2x8 348 (2x4 398, 4x8 377), 1,728 2x4 64 (2x8 71, 4x4 66), 3,032 4x4 341 (2x4 396);
 // of 128: 54 1x8 32 (2x8 34, 2x4 38), 283 2x8 97 (1x8 102, 4x8 132), 484 4x8 88 (2x8 91), 1,032 4x8 493 (2x8
 // 583, 4x4 601), 1,728 4x4 94 (4x8 113); of 256 two strips and four waves as without a window (2x8 the same).
+// Up to 400 pairs of a row and head of the group have no work for eight waves, each of which converts the
+// keys: of 64 channels 104 pairs, 813 busy 2x4 23 (2x8 28), 200, 1,082 2x4 40 (2x8 44); 100, 293 1x4 22 (2x4 24).
 struct WeightTile {
   int strips, waves;
 };
-WeightTile windowed_tile(int head_dim, int64_t busy) {
+WeightTile windowed_tile(int head_dim, int64_t busy, int64_t pairs) {
   if (head_dim == 256) return {2, kAttWaves};
+  if (pairs <= 400) return {busy <= 300 ? 1 : 2, kAttWaves};
   if (head_dim == 64) return busy <= 300 ? WeightTile{1, 8} : busy < 1100 ? WeightTile{2, 8} : WeightTile{busy < 2500 ? 2 : 4, kAttWaves};
   return busy <= 128 ? WeightTile{1, 8} : busy <= 400 ? WeightTile{2, 8} : WeightTile{4, busy < 1100 ? 8 : kAttWaves};
 }
@@ -645,7 +648,8 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
   const int64_t heads = (int64_t)v.kv_heads * v.n_seqs;
   auto weight_blocks_of = [&](int strips) { return (a.seq_reach + strips * kKvStrip - 1) / (strips * kKvStrip) * heads; };
   WeightTile tile{v.head_dim == 256 || weight_blocks_of(4) < kWeightBlocks ? 2 : 4, kAttWaves};
-  if (windowed) tile = windowed_tile(v.head_dim, (std::min(a.cut, span + v.rows / v.n_seqs) + 63) / 64 * heads);
+  if (windowed)
+    tile = windowed_tile(v.head_dim, (std::min(a.cut, span + v.rows / v.n_seqs) + 63) / 64 * heads, v.rows / v.n_seqs * a.group);
   const int64_t weight_blocks = weights.p_dev && !keep ? weight_blocks_of(tile.strips) : 0;   // (a cut of 0: none)
   LAM_CHECK(std::max({blocks, join_blocks + kept_blocks, weight_blocks}) <= most_blocks(kAttThreads), LAM_EINVAL,
             "too many rows, or sequences times the bound of lengths, for one launch (%lld tokens: give max_length)",
@@ -713,8 +717,9 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
       else if (tile.strips == 2) LAM_TILE(D, BF, 2, true, 8);                            \
       else if constexpr (D == 128) LAM_TILE(D, BF, 4, true, 8);                          \
     } else {                                                                             \
-      if (tile.strips == 4) LAM_TILE(D, BF, 4, true, kAttWaves);                         \
-      else if constexpr (D == 64) LAM_TILE(D, BF, 2, true, kAttWaves);                   \
+      if (tile.strips == 1) LAM_TILE(D, BF, 1, true, kAttWaves);                         \
+      else if (tile.strips == 2) LAM_TILE(D, BF, 2, true, kAttWaves);                    \
+      else LAM_TILE(D, BF, 4, true, kAttWaves);                                          \
     }                                                                                    \
   } while (0)
     LAM_KV_DISPATCH(v, LAM_GO);

@@ -119,6 +119,18 @@ def test_long_lengths(lam, D, T, Hk, G, dt, rows, lens, window, sinks, masked):
     _run(c, window, sinks, mask=mask, weights=False)
 
 
+@pytest.mark.parametrize("D,B,Hk,n,window", [
+    (64, 1, 8, 410, 100), (64, 8, 8, 410, 100), (64, 25, 8, 410, 100), (64, 50, 8, 410, 100),   # by 1 and 8, 2 and 8, 2 and 4, 4 and 4
+    (128, 1, 8, 410, 100), (128, 6, 8, 410, 100), (128, 8, 8, 410, 100), (128, 25, 8, 410, 100),  # 1 and 8, 2 and 8, 4 and 8, 4 and 4
+    (64, 8, 8, 70, 200), (128, 8, 8, 70, 200), (256, 2, 2, 410, 100),                           # 2 and 4
+])
+def test_weights_by_every_tile(lam, D, B, Hk, n, window):
+    """Strips and waves of the weights' second pass, which go by how many workgroups have work."""
+    c = Case(lam, D, 64, Hk, 1, "bf16", [n] * B, [420 - b % 5 for b in range(B)], seed=B)
+    _poison(c, window, 5, True)
+    _run(c, window, 5)
+
+
 def test_many_sequences(lam):
     rng = np.random.default_rng(3)
     lens = [int(x) for x in rng.integers(0, 400, 130)]
