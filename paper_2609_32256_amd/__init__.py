@@ -624,9 +624,11 @@ def kv_rotate(q: torch.Tensor, frequencies: torch.Tensor | None, positions: torc
         if k.dtype != q.dtype or k.shape[0] != rows or k.shape[2] != head_dim:
             raise ValueError("k must have q's rows, channels and type")
         if out is None:
-            out = True, True
+            out = None, None
+        elif not isinstance(out, (tuple, list)):
+            raise TypeError("out must be (q's result, k's result)")
         out, k_out = out
-        kh, k_out, hold_k = _kv_heads(k, k_norm, k_out, "k", dev)
+        kh, k_out, hold_k = _kv_heads(k, k_norm, True if k_out is None else k_out, "k", dev)
     qh, out, hold_q = _kv_heads(q, q_norm, True if out is None else out, "q", dev)
     _check(_lib.lam_kv_rotate(ctx.handle, r, qh, None if k is None else kh, rows, head_dim, _KV_DTYPES[q.dtype],
                               None if positions is None else positions.data_ptr(), float(eps),

@@ -272,9 +272,11 @@ struct Walk {
   int sinks = 0;   // places of the first tokens, whole strips
   int gap = 0;     // tokens left out after them
   __device__ __forceinline__ Walk() {}
-  // begin: of the first row
+  // begin: of the first row (it goes by the whole length, so it may lie past len, and past what the
+  // table has columns for: no token of a place is then further than len's)
   __device__ __forceinline__ Walk(const AttendArgs& a, int len, int begin)
-      : sinks((min(a.sinks, len) + kKvStrip - 1) & ~(kKvStrip - 1)), gap(max(0, (begin & ~(kKvStrip - 1)) - sinks)) {}
+      : sinks((min(a.sinks, len) + kKvStrip - 1) & ~(kKvStrip - 1)),
+        gap(max(0, (min(begin, len) & ~(kKvStrip - 1)) - sinks)) {}
   __device__ __forceinline__ int token(int place) const { return place < sinks ? place : place + gap; }
   __device__ __forceinline__ int place(int token) const { return token < sinks ? token : token - gap; }
   // places of the tokens below `end`

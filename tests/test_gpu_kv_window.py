@@ -199,6 +199,27 @@ def test_a_window_goes_by_the_length_not_the_table(lam, D, G, rows, lens, cols):
         c.check(out, mask=_seen(c, window, sinks, cut), lse=lse, weights=w)
 
 
+@pytest.mark.parametrize("n,G", [(1, 4), (3, 2), (90, 2)])    # single tokens; scores kept; chunks
+@pytest.mark.parametrize("length", [(1 << 31) - 1, (1 << 31) - 4097, 1 << 30, 5000])
+def test_windows_far_past_the_table(lam, n, G, length):
+    """Lengths that count tokens without a place, to the largest an int32 holds: of 200 tokens with one,
+    rows at the length's end see the first alone, or nothing."""
+    c = Case(lam, 64, 32, 2, G, "bf16", [n] * 2, [200, 200], seed=n)
+    c.lengths = _i32([length, 200])
+    for window, sinks in ((64, 3), (100, 0), (3000, 40)):
+        seen = [[kv.in_window(n, 200, 1 << 40, 0) & (np.arange(200) < sinks)[None]], [kv.in_window(n, 200, window, sinks)]]
+        for causal in (True, False):
+            lse = torch.full(c.q.shape[:2], float("nan"), device="cuda")
+            w = torch.zeros((2, 2, 200), device="cuda")
+            out = c.call(causal=causal, lse=lse, weights=w, window=window, sinks=sinks)
+            for b in range(2):
+                one = Case.__new__(Case)
+                one.D, one.Hk, one.G, one.dt, one.rows, one.lens = c.D, c.Hk, c.G, c.dt, [n], [200]
+                at = slice(b * n, b * n + n)
+                one.q, one.starts, one.k, one.v = c.q[at], [0, n], c.k[b:b + 1], c.v[b:b + 1]
+                one.check(out[at], causal=causal and b == 1, mask=[seen[b]], lse=lse[at], weights=w[b:b + 1])
+
+
 def test_a_window_of_everything_is_none(lam):
     for rows, lens in (([1, 1], [4000, 77]), ([200, 3], [1500, 90]), ([4, 4], [300, 300])):
         c = Case(lam, 128, 64, 2, 4, "bf16", rows, lens, seed=5)
