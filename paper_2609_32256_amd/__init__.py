@@ -391,15 +391,19 @@ def _kv_tensor(t, dtype, dims, name, dev):
 def _kv_view(dev, pages, table, lengths, starts, rows, head_dim, dtype):
     """(lam_kv_view, sequences, kv_heads, tensors to hold until the launch is queued)
     of a call.  Index tensors whose last axis is not contiguous are copied."""
-    _kv_tensor(pages, torch.uint8, 3, "pages", dev)
+    if not (isinstance(pages, torch.Tensor) and isinstance(table, torch.Tensor) and isinstance(lengths, torch.Tensor)
+            and pages.get_device() == dev and table.get_device() == dev and lengths.get_device() == dev
+            and pages.dtype is torch.uint8 and table.dtype is torch.int32 and lengths.dtype is torch.int32
+            and pages.dim() == 3 and table.dim() == 2 and lengths.dim() == 1):
+        _kv_tensor(pages, torch.uint8, 3, "pages", dev)
+        _kv_tensor(table, torch.int32, 2, "table", dev)
+        _kv_tensor(lengths, torch.int32, 1, "lengths", dev)
     if not pages.is_contiguous():
         raise ValueError("pages must be contiguous")
     n_pages, heads, size = pages.shape
     page_size, rest = divmod(size, head_dim + head_dim // 16) if head_dim > 0 else (0, 1)
     if rest or head_dim not in _KV_HEADS or page_size not in _KV_PAGES:
         raise ValueError(f"pages of {size} bytes a head do not hold heads of {head_dim} channels")
-    _kv_tensor(table, torch.int32, 2, "table", dev)
-    _kv_tensor(lengths, torch.int32, 1, "lengths", dev)
     (n, cols), (stride, step) = table.shape, table.stride()
     if step != 1 and cols > 1 or stride < cols:
         table = table.contiguous()
