@@ -498,14 +498,17 @@ void k_kv_weights(AttendArgs a) {
     lp += turn ? l_turn : 0;
   };
   auto add = [&](int b, int r) {
-    bool whole = all == kAllTokens;
+    // with a window, but for what the mask takes out, of all rows alike (not where it spills)
+    constexpr bool kAlike = WINDOW && D * kStrips != 256;
+    bool whole;
     int begin = 0;
     if constexpr (WINDOW) {   // lanes 0 and 15 have the first row and the last
       begin = begin_of(row[b]);
       const int r_first = __builtin_amdgcn_readlane(row[b], 0);
-      whole = whole && t1 <= (a.causal ? min(w.len, hidden + r_first + 1) : w.len) && t0 >= __builtin_amdgcn_readlane(begin, 15);
+      whole = (kAlike || all == kAllTokens) && t1 <= (a.causal ? min(w.len, hidden + r_first + 1) : w.len) &&
+              t0 >= __builtin_amdgcn_readlane(begin, 15);
     } else {
-      whole = whole && t1 <= (a.causal ? min(w.len, hidden + r / a.group + 1) : w.len);
+      whole = all == kAllTokens && t1 <= (a.causal ? min(w.len, hidden + r / a.group + 1) : w.len);
     }
     const bool out = r + c >= w.pairs || e[b] == -__builtin_inff();
     const float less = out ? __builtin_inff() : e[b];   // no row, or one that sees no token: 2^(-inf) each
@@ -525,6 +528,8 @@ void k_kv_weights(AttendArgs a) {
         uint32_t in = bits[n];
         if constexpr (WINDOW) in &= window_bits(a, strip(n), begin);
         hide(x, seen_bits(in, strip(n), end));
+      } else if (kAlike && all != kAllTokens) {
+        hide(x, seen_bits(bits[n], 0, kKvStrip));
       }
 #pragma unroll
       for (int v = 0; v < 8; ++v) sum[n][v] += __builtin_amdgcn_exp2f(x[v >> 2][v & 3]);

@@ -129,7 +129,10 @@ __global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : D == 64 ? 3 : 2) void k
       value_scales<D>(v, t0, w.len, bits, s);
 #pragma unroll
       for (int t = 0; t < kTiles; ++t) less_reference(x[t], a.scale2, row[t]);
-      if (!whole || bits != kAllTokens) {
+      // with a window what the mask takes out of whole strips is taken out of all rows alike (not at 64
+      // channels, where it spills)
+      constexpr bool kAlike = MASK && WINDOW && D != 64;
+      if (!whole || (!kAlike && bits != kAllTokens)) {
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) {
           const int r = min(w.r0 + 16 * t + c, w.pairs - 1);
@@ -137,6 +140,10 @@ __global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : D == 64 ? 3 : 2) void k
           if constexpr (WINDOW) in &= window_bits(a, t0, pair_begin(a, w, r));
           hide(x[t], seen_bits(in, t0, pair_end(a, w, r)));
         }
+      } else if (kAlike && bits != kAllTokens) {
+        const uint32_t in = seen_bits(bits, t0, t0 + kKvStrip);
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) hide(x[t], in);
       }
       bool up = false;
       float top[kTiles];
