@@ -21,8 +21,9 @@
  * rank-invariance certificate (lam_score_topk_certified) and a per-block
  * fixed-length codec of the store's codes (lam_store_block_*,
  * lam_score_topk_blocks).  Beside them stands the memory of the model that
- * reads the retrieved records: a paged key/value cache held in 4 bits, attention
- * over it, and eviction by accumulated attention weight (lam_kv_*).
+ * reads the retrieved records: a paged key/value cache held in 4 bits, norms of
+ * heads and rotation by position on the way into it, attention over it, whole or in
+ * a sliding window, and eviction by accumulated attention weight (lam_kv_*).
  *
  * Conventions for every call:
  *   - Pointers named *_dev are device pointers on the context's device; the

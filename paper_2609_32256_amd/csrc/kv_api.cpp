@@ -1,5 +1,5 @@
 // C entry points of the 4-bit key/value cache (include/lam.h): argument checks.
-// The kernels are in kv_cache.hip and kv_attend.hip.
+// The kernels are in kv_cache.hip, kv_rotate.hip, kv_attend.hip and kv_chunk.hip.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

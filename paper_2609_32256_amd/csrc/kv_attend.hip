@@ -26,6 +26,12 @@
 // units have the time.  Lengths are split where the tiles are fewer than the workgroups
 // that run at once, and joined by a second launch (5 us; a join by the last workgroup of each
 // unit took 2 to 30 us more, since its parts have to leave the caches of the XCDs).
+//
+// Rows with a window walk the strips of the first tokens and those from the tile's first window on, and
+// nothing else is read (Walk): 8 sequences of 131,072 tokens with a window of 8,192 22 us, 72 MB, 37 of
+// 3,000 to 6,000 with one of 1,024 11; latency, since a wave has five to ten strips of 0.7 us.  (Eight
+// waves a workgroup: one sequence and a window of 1,900 12.2 us, with four 14.8; 37 and 1,024 17, with four
+// 14.6.  Split from 600 tokens on: one and 1,800 11 us, whole 14; 37 and 1,000 18.9, whole 14.3.)
 #include <algorithm>
 #include <cmath>
 
@@ -89,7 +95,7 @@ struct Running {
 };
 
 // (With a window heads of 256 channels are held to two workgroups a compute unit, without spills: 64
-// sequences, 8 heads and a window of 500 22 us for 17, 37 of 1,000 30 for 27, one of 1,000 13.9 for 12.6.)
+// sequences, 8 heads and a window of 500 17 us, with one 22; 37 and 1,000 27, with one 30.)
 template <int D, bool BF16, bool MASK, bool WINDOW>
 __global__ __launch_bounds__(kAttThreads, D == 256 ? WINDOW ? 2 : 1 : 3) void k_kv_attend(AttendArgs a) {
   constexpr int kRun = D / 16;

@@ -12,7 +12,8 @@
 // conversion.  2,048 rows of 32 heads over 32,768 tokens (8 key/value heads of 128 channels,
 // bfloat16): 1,045 us, 1,020 TFLOP/s; a library product of 8,192^3 reaches 1,200.  By the
 // counters vector instructions are active in 62 % of a SIMD's cycles there and the matrix unit
-// is busy in 42; with heads of 64 channels in 67 and 26.
+// is busy in 42; with heads of 64 channels in 67 and 26.  4,096 rows over 32,768 tokens with a window of
+// 4,096: 298 us, 923 TFLOP/s, in four rounds of tiles that each begin and end with a wait.
 #include "kv_attend.h"
 
 namespace lam {

@@ -245,7 +245,7 @@ lam_status block_encode(lam_ctx* ctx, lam_store* st, lam_block_stats* out);
 // decode the blocks to float32 (xhat) or back to the b-bit code stream (codes_out)
 lam_status block_decode(lam_ctx* ctx, const lam_store* st, float* xhat, uint32_t* codes_out);
 
-// ------------------------------------------------------------------ 4-bit cache (kv_cache.hip, kv_attend.hip)
+// ------------------------------------------------------------------ 4-bit cache (kv_cache.hip, kv_rotate.hip, kv_attend.hip)
 // The 4-bit cache's scratch, of at least `need` bytes.  Its calls are recorded into graphs,
 // which hold the address: what a larger need replaces is freed with the context only.  It
 // grows to twice its size at least, so all that was replaced is no more than what is used.
