@@ -559,10 +559,16 @@ def _kv_rotary(frequencies, layout, amplitude, dev):
 
 
 def _kv_heads(x, gain, out, name, dev):
-    """(lam_heads, result, tensor to hold) of rows that are normed and turned; out: True for a new
-    result, False for none."""
+    """(lam_heads, the rows as they are taken, result, tensor to hold) of rows that are normed and
+    turned; out: True for a new result, False for none."""
+    if not (isinstance(x, torch.Tensor) and x.get_device() == dev and x.dtype in _KV_DTYPES and x.dim() == 3
+            and not x.requires_grad):
+        x = _kv_rows(x, None, name, dev)
+    row, head, step = x.stride()
+    if step != 1 or row <= 0 or head <= 0:
+        x = x.contiguous()
+        row, head, _ = x.stride()
     rows, heads, head_dim = x.shape
-    row, head, _ = x.stride()
     dtype = x.dtype
     g, g_type = 0, 2
     if gain is not None:
@@ -580,16 +586,16 @@ def _kv_heads(x, gain, out, name, dev):
         g = gain.data_ptr()
     if out is True:
         out = torch.empty_like(x, memory_format=_CONTIGUOUS)
-        return _HEADS.pack(x.data_ptr(), row, head, out.data_ptr(), heads * head_dim, head_dim, g, g_type, heads), out, gain
+        return _HEADS.pack(x.data_ptr(), row, head, out.data_ptr(), heads * head_dim, head_dim, g, g_type, heads), x, out, gain
     if out is False:
-        return _HEADS.pack(x.data_ptr(), row, head, 0, 0, 0, g, g_type, heads), None, gain
+        return _HEADS.pack(x.data_ptr(), row, head, 0, 0, 0, g, g_type, heads), x, None, gain
     _kv_tensor(out, dtype, 3, name + "'s out", dev)
     y_row, y_head, step = out.stride()
     if out.shape != x.shape or step != 1:
         raise ValueError(f"{name}'s out must be of {name}'s shape with its channels contiguous")
     if out.requires_grad:
         _kv_graphless(out, name + "'s out")
-    return _HEADS.pack(x.data_ptr(), row, head, out.data_ptr(), y_row, y_head, g, g_type, heads), out, gain
+    return _HEADS.pack(x.data_ptr(), row, head, out.data_ptr(), y_row, y_head, g, g_type, heads), x, out, gain
 
 
 def kv_rotate(q: torch.Tensor, frequencies: torch.Tensor | None, positions: torch.Tensor | None = None,
@@ -610,7 +616,17 @@ def kv_rotate(q: torch.Tensor, frequencies: torch.Tensor | None, positions: torc
         with torch.cuda.stream(ctx.stream):
             return kv_rotate(q, frequencies, positions, k, layout, amplitude, q_norm, k_norm, eps, norm_dim, out, ctx)
     dev = ctx.device
-    q = _kv_rows(q, None, "q", dev)
+    if k is None:
+        if isinstance(out, (tuple, list)):
+            out, = out
+        k_out = None
+    elif out is None:
+        k_out = None
+    elif not isinstance(out, (tuple, list)):
+        raise TypeError("out must be (q's result, k's result)")
+    else:
+        out, k_out = out
+    qh, q, out, hold_q = _kv_heads(q, q_norm, True if out is None else out, "q", dev)
     rows, _, head_dim = q.shape
     r, hold = _kv_rotary(frequencies, layout, amplitude, dev)
     if positions is not None:
@@ -620,21 +636,12 @@ def kv_rotate(q: torch.Tensor, frequencies: torch.Tensor | None, positions: torc
             raise ValueError("positions must have an entry for each row")
     elif hold is not None and hold.numel() and rows:
         raise ValueError("a rotation needs positions")
-    if k is None:
-        if isinstance(out, (tuple, list)):
-            out, = out
-    else:
-        k = _kv_rows(k, None, "k", dev)
+    kh = None
+    if k is not None:
+        kh, k, k_out, hold_k = _kv_heads(k, k_norm, True if k_out is None else k_out, "k", dev)
         if k.dtype != q.dtype or k.shape[0] != rows or k.shape[2] != head_dim:
             raise ValueError("k must have q's rows, channels and type")
-        if out is None:
-            out = None, None
-        elif not isinstance(out, (tuple, list)):
-            raise TypeError("out must be (q's result, k's result)")
-        out, k_out = out
-        kh, k_out, hold_k = _kv_heads(k, k_norm, True if k_out is None else k_out, "k", dev)
-    qh, out, hold_q = _kv_heads(q, q_norm, True if out is None else out, "q", dev)
-    _check(_lib.lam_kv_rotate(ctx.handle, r, qh, None if k is None else kh, rows, head_dim, _KV_DTYPES[q.dtype],
+    _check(_lib.lam_kv_rotate(ctx.handle, r, qh, kh, rows, head_dim, _KV_DTYPES[q.dtype],
                               None if positions is None else positions.data_ptr(), float(eps),
                               0 if norm_dim is None else _kv_norm_dim(norm_dim)))
     return out if k is None else (out, k_out)
@@ -665,24 +672,22 @@ def kv_rotate_append(q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor, p
             return kv_rotate_append(q, k, v, pages, table, lengths, frequencies, starts, first, layout, amplitude,
                                     q_norm, k_norm, eps, norm_dim, weights, positions, status, out, ctx)
     dev = ctx.device
-    k = _kv_rows(k, None, "k", dev)
-    v = _kv_rows(v, k.shape[1], "v", dev)
+    kh, k, _, hold_k = _kv_heads(k, k_norm, False, "k", dev)
+    rows, own, head_dim = k.shape
+    v = _kv_rows(v, own, "v", dev)
     if v.shape != k.shape or v.dtype != k.dtype:
         raise ValueError("k and v must have the same shape and dtype")
-    rows, own, head_dim = k.shape
     view, n, heads, hold = _kv_view(dev, pages, table, lengths, starts, rows, head_dim, k.dtype)
     if own != heads:
         raise ValueError(f"k must have {heads} heads")
     r, hold_f = _kv_rotary(frequencies, layout, amplitude, dev)
     qh = None
     if q is not None:
-        q = _kv_rows(q, None, "q", dev)
+        qh, q, out, hold_q = _kv_heads(q, q_norm, True if out is None else out, "q", dev)
         if q.dtype != k.dtype or q.shape[0] != rows or q.shape[2] != head_dim:
             raise ValueError("q must have k's rows, channels and type")
-        qh, out, hold_q = _kv_heads(q, q_norm, True if out is None else out, "q", dev)
     elif out is not None:
         raise ValueError("out without q")
-    kh, _, hold_k = _kv_heads(k, k_norm, False, "k", dev)
     w, _ = _kv_slots(weights, torch.float32, n, heads, "weights", dev)
     p, _ = _kv_slots(positions, torch.int32, n, heads, "positions", dev)
     first = _kv_first(first, n, dev)

@@ -157,6 +157,8 @@ def test_strides_and_in_place(lam):
         assert torch.equal(out[..., :D], want[0]) and not out[..., D].any()
         cols = q.transpose(1, 2).contiguous().transpose(1, 2)      # channels apart: copied
         assert torch.equal(lam.kv_rotate(cols, f, pos, layout=layout, q_norm=g), want[0])
+        odd = torch.zeros(D + 1, device="cuda")[1:].copy_(g)       # gains that begin anywhere
+        assert torch.equal(lam.kv_rotate(q, f, pos, layout=layout, q_norm=odd), want[0])
         one = q[:1].expand(n, Hq, D)                               # one row for all positions
         assert torch.equal(lam.kv_rotate(one, f, pos, layout=layout, q_norm=g),
                            lam.kv_rotate(one.contiguous(), f, pos, layout=layout, q_norm=g))
@@ -329,6 +331,21 @@ def test_rotate_append_of_padded_heads_and_rows(lam):
     _append_case(lam, 128, 64, 8, 4, "bf16", [3, 40], [9, 64], real=80, pairs=40, before=2, after=5, seed=4)
     _append_case(lam, 64, 64, 8, 4, "f16", [1, 1, 1], [9, 64, 1], real=40, pairs=20, layout="interleaved", after=300, seed=5)
     _append_case(lam, 64, 64, 2, 1, "f16", [0, 0], [9, 64], before=1, after=2, seed=6)
+
+
+@pytest.mark.parametrize("n", [40, 9000])                         # a wave a part of a row; four rows
+def test_rotate_append_in_place(lam, n):
+    """Queries turned in place beside their keys and values, as one product leaves all three."""
+    D, Hq, Hk, T = 64, 3, 1, 64
+    whole = _rows(n, n, Hq + 2 * Hk, D, "bf16")
+    q, k, v = whole.split((Hq, Hk, Hk), dim=1)
+    table = torch.arange(-(-n // T), dtype=torch.int32, device="cuda").view(1, -1)
+    f, g = _freq(kv.frequencies(32)[0]), _gain(1, D)
+    a, b = (lam.kv_pages(table.numel(), Hk, D, T) for _ in range(2))
+    want = lam.kv_rotate_append(q, k, v, a, table, _i32([n]), f, q_norm=g, k_norm=g)
+    rest = whole[:, Hq:].clone()
+    got = lam.kv_rotate_append(q, k, v, b, table, _i32([n]), f, q_norm=g, k_norm=g, out=q)
+    assert got is q and torch.equal(q, want) and torch.equal(a, b) and torch.equal(whole[:, Hq:], rest)
 
 
 def test_without_norm_and_rotation_it_is_an_append(lam):

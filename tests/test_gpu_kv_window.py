@@ -243,6 +243,20 @@ def test_weights_outside_the_window_stay(lam):
         assert (w[..., :4] > before[..., :4]).all() and (w[..., -99:] != before[..., -99:]).any()
 
 
+@pytest.mark.parametrize("n", [2, 90])                             # scores kept, and a second pass
+def test_weights_and_masks_of_fewer_columns_than_tokens(lam, n):
+    c = Case(lam, 64, 32, 2, 2, "f16", [n], [700], seed=n)
+    whole = torch.zeros((1, 2, 700), device="cuda")
+    c.call(weights=whole, window=300, sinks=40)
+    for cols in (0, 20, 500, 650):
+        w = torch.full((1, 2, cols + 3), 7.0, device="cuda")
+        c.call(weights=w[..., :cols], window=300, sinks=40)
+        assert torch.equal(w[..., :cols] - 7 + 7, whole[..., :cols] + 7) and (w[..., cols:] == 7).all()
+    mask = torch.ones((1, 1, 650), dtype=torch.bool, device="cuda")
+    seen = [m & (np.arange(700) < 650)[None] for m in _seen(c, 300, 40)[0]]
+    c.check(c.call(mask=mask, window=300, sinks=40), mask=[seen])
+
+
 def test_a_graph_whose_lengths_grow(lam):
     c = Case(lam, 128, 64, 2, 4, "bf16", [1, 1], [5000, 300], seed=2)
     full = c.lengths.clone()
