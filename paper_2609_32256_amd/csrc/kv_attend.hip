@@ -123,7 +123,8 @@ __global__ __launch_bounds__(kAttThreads, D == 256 ? WINDOW ? 2 : 1 : 3) void k_
   }
   // places from `from` to `to`, which are tokens where there is no window
   const int64_t part_at = (int64_t)w.part * w.tokens;
-  const int from = (int)min(part_at, (int64_t)walk.places(w.len)), to = (int)min(part_at + w.tokens, (int64_t)walk.places(pair_end(a, w, last)));
+  const int from = (int)min(part_at, (int64_t)walk.places(w.len));
+  const int to = (int)min(part_at + w.tokens, (int64_t)walk.places(pair_end(a, w, last)));
   const int whole_to = end_first - kKvStrip;   // strips up to here are seen whole
 
   // Strips at t0, t0 + 128, ...: kAhead strips' codes are on their way while one
@@ -406,13 +407,19 @@ struct WeightTile {
 WeightTile windowed_tile(int head_dim, int64_t busy, int64_t pairs) {
   if (head_dim == 256) return {2, kAttWaves};
   if (pairs <= 400) return {busy <= 300 ? 1 : 2, kAttWaves};
-  if (head_dim == 64) return busy <= 300 ? WeightTile{1, 8} : busy < 1100 ? WeightTile{2, 8} : WeightTile{busy < 2500 ? 2 : 4, kAttWaves};
-  return busy <= 128 ? WeightTile{1, 8} : busy <= 400 ? WeightTile{2, 8} : WeightTile{4, busy < 1100 ? 8 : kAttWaves};
+  const bool few = busy < 1100;
+  if (head_dim == 64) return few ? WeightTile{busy <= 300 ? 1 : 2, 8} : WeightTile{busy < 2500 ? 2 : 4, kAttWaves};
+  return few ? WeightTile{busy <= 128 ? 1 : busy <= 400 ? 2 : 4, 8} : WeightTile{4, kAttWaves};
+}
+
+// Waves a SIMD that its registers are held to.
+constexpr int weight_fill(int D, int strips, int waves) {
+  if (strips == 1 || (D == 64 && strips == 2)) return 4;
+  return D < 256 && waves == kAttWaves && (D == 64 || strips == 2) ? 3 : 2;
 }
 
 template <int D, bool BF16, int kStrips, bool WINDOW, int WAVES = kAttWaves>
-__global__ __launch_bounds__(64 * WAVES, kStrips == 1 ? 4 : D == 256 ? 2 : D == 64 && kStrips == 2 ? 4 : WAVES == 8 ? 2 : D == 64 || kStrips == 2 ? 3 : 2)
-void k_kv_weights(AttendArgs a) {
+__global__ __launch_bounds__(64 * WAVES, weight_fill(D, kStrips, WAVES)) void k_kv_weights(AttendArgs a) {
   constexpr int kSteps = D / 32, kTokens = kStrips * kKvStrip;
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -664,7 +671,8 @@ lam_status launch_kv_attend(lam_ctx* ctx, const lam_kv_view& v, const void* q, i
   if (windowed)
     tile = windowed_tile(v.head_dim, (std::min(a.cut, span + v.rows / v.n_seqs) + 63) / 64 * heads, v.rows / v.n_seqs * a.group);
   const int64_t weight_blocks = weights.p_dev && !keep ? weight_blocks_of(tile.strips) : 0;   // (a cut of 0: none)
-  LAM_CHECK(std::max({blocks, join_blocks + kept_blocks, weight_blocks}) <= most_blocks(kAttThreads), LAM_EINVAL,
+  LAM_CHECK(std::max(blocks, join_blocks + kept_blocks) <= most_blocks(kAttThreads) &&
+                weight_blocks <= most_blocks(64 * tile.waves), LAM_EINVAL,
             "too many rows, or sequences times the bound of lengths, for one launch (%lld tokens: give max_length)",
             (long long)a.cut);
   LAM_CHECK(weight_blocks == 0 || q != out, LAM_EINVAL, "out is q, which the weights take a second pass over");

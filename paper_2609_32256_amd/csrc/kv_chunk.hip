@@ -53,7 +53,8 @@ __global__ __launch_bounds__(kAttThreads, D == 256 ? 1 : D == 64 ? 3 : 2) void k
   }
   // places from `from` to `to`, which are tokens where there is no window
   const int64_t part_at = (int64_t)w.part * w.tokens;
-  const int from = (int)min(part_at, (int64_t)walk.places(w.len)), to = (int)min(part_at + w.tokens, (int64_t)walk.places(pair_end(a, w, last)));
+  const int from = (int)min(part_at, (int64_t)walk.places(w.len));
+  const int to = (int)min(part_at + w.tokens, (int64_t)walk.places(pair_end(a, w, last)));
   const int whole_to = end_first - kKvStrip;
 
   kv_f4 o[kTiles][kRun];

@@ -70,11 +70,6 @@ __device__ __forceinline__ uint32_t wave_scan_u32(uint32_t v) {
 }
 
 // The largest of each quad's four values, in all four lanes (which must be active together).
-__device__ __forceinline__ float quad_max_f32(float v) {
-  v = fmaxf(v, __int_as_float(LAM_DPP_MOVE(__float_as_int(v), __float_as_int(v), 0xb1, 0xf)));
-  return fmaxf(v, __int_as_float(LAM_DPP_MOVE(__float_as_int(v), __float_as_int(v), 0x4e, 0xf)));
-}
-
 __device__ __forceinline__ uint32_t quad_max_u32(uint32_t v) {
   v = max(v, (uint32_t)LAM_DPP_MOVE(v, v, 0xb1, 0xf));
   return max(v, (uint32_t)LAM_DPP_MOVE(v, v, 0x4e, 0xf));
