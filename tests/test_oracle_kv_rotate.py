@@ -203,3 +203,19 @@ def test_append_refusals():
     mine = _heads(lam, x=A, row=row, y=A, y_row=row)
     assert call(q=mine, k=_heads(lam, x=A + 1024, row=row, y=0), vals=A + 2048, row=row, status=A + 1) == 1
     assert "status" in lam._lib.lam_last_error().decode()
+
+
+@needs_lib
+def test_window_refusals():
+    import paper_2609_32256_amd as lam
+    view = lam._KV_VIEW.pack(A + (1 << 36), 100, A + (1 << 37), 4, A + (1 << 38), 0, 10, 2, 4, 8, 64, 64, 1)
+    empty = lam._KV_VIEW.pack(A + (1 << 36), 100, A + (1 << 37), 4, A + (1 << 38), 0, 0, 2, 4, 8, 64, 64, 1)
+
+    def call(window, sinks, v=view, heads=8, out=A + (1 << 30)):
+        return lam._lib.lam_kv_attend_window(CTX, v, A, 512, 64, heads, 0.125, 1, 0, window, sinks, None, None, out, None)
+
+    for window, sinks in ((-1, 0), (0, 1), (5, -1), (-(1 << 63), 0), (0, 1 << 62)):
+        assert call(window, sinks) == 1
+        assert "window" in lam._lib.lam_last_error().decode()
+    assert call(5, 1, heads=12) == 1 and call(5, 1, out=None) == 1
+    assert call(5, 1, v=empty) == 0 and call((1 << 63) - 1, (1 << 63) - 1, v=empty) == 0
