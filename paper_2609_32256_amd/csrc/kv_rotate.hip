@@ -141,7 +141,8 @@ __device__ __forceinline__ void wave_lds_order() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// The raw other channels of a lane's eight, given its own.  pass: 16 bytes of LDS for each lane, for
+// The raw other channels of a lane's eight, given its own; a channel that is not turned stands in itself, so
+// that a neighbour which is not finite does not get to it by a factor of 0.  pass: 16 bytes of LDS for each lane, for
 // pairs whose channels are no whole number of lanes apart (read from memory once more, 41,569 rows of
 // 108 heads of 64 channels and 20 pairs took 384 us, so 273).
 template <int MODE, int L>
@@ -154,7 +155,7 @@ __device__ __forceinline__ kv_u4 others(const Lane<MODE>& at, kv_u4 own, kv_u4* 
     for (int j = 0; j < 4; ++j) w[j] = (uint32_t)__shfl((int)own[j], from);
   } else if constexpr (MODE == kInterleaved) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) w[j] = __builtin_amdgcn_alignbit(own[j], own[j], 16);
+    for (int j = 0; j < 4; ++j) w[j] = at.turned(2 * j) ? __builtin_amdgcn_alignbit(own[j], own[j], 16) : own[j];
   } else {
     wave_lds_order();
     pass[lane] = own;

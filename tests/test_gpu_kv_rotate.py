@@ -404,6 +404,43 @@ def test_counts_of_what_cannot_be_held(lam):
     assert kk[0, 0, 3] == 0 and kk[0, 0, 35] == 0 and vv[1, 1, 5] == 0 and not kk[4:].any()
 
 
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("D,pairs,Hq,Hk,n", [
+    (64, 0, 0, 2, 5), (64, 3, 2, 3, 40), (128, 16, 4, 2, 5), (128, 33, 0, 5, 12), (256, 20, 1, 2, 9),
+    (64, 8, 1, 2, 8200), (64, 5, 0, 1, 8200), (128, 0, 1, 1, 8200), (128, 24, 0, 2, 8200),     # waves of four rows
+])
+def test_what_is_not_finite_stays_in_its_pair_on_the_way_into_the_cache(lam, D, pairs, Hq, Hk, n, layout):
+    """Channels that are not turned have no other one to spoil, and each is counted by the one thread that holds it."""
+    T = 64
+    q = _rows(1, n, Hq, D, "bf16") if Hq else None
+    k, v = _rows(2, n, Hk, D, "bf16"), _rows(3, n, Hk, D, "bf16")
+    f = kv.frequencies(pairs)[0] if pairs else []
+    exact, _ = kv.rotate(_np(k), range(n), f, layout, 1.0625)
+    # one element a row, so that no thread meets two: channels past the pairs, their neighbours, a turned one
+    spoiled, places = 0, [2 * pairs, 2 * pairs + 1, D - 1, D - 2, 2 * pairs + 6] + ([pairs] if pairs else [])
+    rows = np.linspace(0, n - 1, min(n, 60)).astype(int) // (4 if n > 1000 else 1) * (4 if n > 1000 else 1)
+    for i, r in enumerate(sorted(set(rows.tolist()))):
+        c, h = places[i % len(places)], i % Hk
+        k[r, h, c] = (float("nan"), float("inf"), float("-inf"))[i % 3]
+        other = c
+        if c < 2 * pairs:
+            other = c ^ 1 if layout == "interleaved" else c + pairs if c < pairs else c - pairs
+        exact[r, h, [c, other]] = np.nan
+        spoiled += 1 if c // 8 == other // 8 else 2
+    cols = -(-n // T)
+    pool, status = lam.kv_pages(cols, Hk, D, T), _i32([0, 0, 0])
+    table = torch.arange(cols, dtype=torch.int32, device="cuda").view(1, cols)
+    lam.kv_rotate_append(q, k, v, pool, table, _i32([n]), _freq(f), layout=layout, amplitude=1.0625, status=status)
+    got, _ = lam.kv_read(pool, table, _i32([n]), n, D, dtype=torch.bfloat16)
+    assert np.array_equal(_np(got), kv.rounded(exact))
+    assert status.tolist() == [spoiled, 0, 0]
+    if pairs == 0:                                                # as they are: lam_kv_append's bytes
+        plain = lam.kv_pages(cols, Hk, D, T)
+        lam.kv_rotate_append(None, k, v, pool.zero_(), table, _i32([n]), _freq(f), layout=layout)
+        lam.kv_append(k, v, plain, table, _i32([n]))
+        assert torch.equal(pool, plain)
+
+
 # ------------------------------------------------------------------ streams, graphs, refusals
 def test_another_stream_and_a_graph(lam):
     D, Hq, Hk, B = 128, 8, 2, 3
