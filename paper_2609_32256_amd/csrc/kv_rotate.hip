@@ -141,8 +141,8 @@ __device__ __forceinline__ void wave_lds_order() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// The raw other channels of a lane's eight, given its own; a channel that is not turned stands in itself, so
-// that a neighbour which is not finite does not get to it by a factor of 0.  pass: 16 bytes of LDS for each lane, for
+// The raw other channels of a lane's eight, given its own (interleaved, also of channels that are not
+// turned: their neighbours).  pass: 16 bytes of LDS for each lane, for
 // pairs whose channels are no whole number of lanes apart (read from memory once more, 41,569 rows of
 // 108 heads of 64 channels and 20 pairs took 384 us, so 273).
 template <int MODE, int L>
@@ -155,7 +155,7 @@ __device__ __forceinline__ kv_u4 others(const Lane<MODE>& at, kv_u4 own, kv_u4* 
     for (int j = 0; j < 4; ++j) w[j] = (uint32_t)__shfl((int)own[j], from);
   } else if constexpr (MODE == kInterleaved) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) w[j] = at.turned(2 * j) ? __builtin_amdgcn_alignbit(own[j], own[j], 16) : own[j];
+    for (int j = 0; j < 4; ++j) w[j] = __builtin_amdgcn_alignbit(own[j], own[j], 16);
   } else {
     wave_lds_order();
     pass[lane] = own;
@@ -194,21 +194,41 @@ __device__ __forceinline__ void store_raw8(void* p, int64_t at, bool wide, kv_u4
   for (int j = 0; j < 4; ++j) h[2 * j] = (uint16_t)w[j], h[2 * j + 1] = (uint16_t)(w[j] >> 16);
 }
 
-// 1 / sqrt(sum of squares / norm_dim + eps) of a head's eight channels a lane, in float32 where the
-// sum is well inside its range, else in binary64.
-template <int L>
-__device__ __forceinline__ float norm_of(const RotateArgs& a, const float u[8]) {
+// A pair's two terms, and a value times its gain, can leave float32's range though what comes of them, by
+// the other term or by the norm, is well inside: gains come 2^3 smaller and results are multiplied by it at the end.
+constexpr float kDown = 0x1p-3f, kUp = 0x1p3f;
+
+// 1 / sqrt(sum of squares / norm_dim + eps) of a head's eight channels a lane, in float32 where that is well inside
+// its range, else (for all heads of the wave) in binary64.  Then float32 may hold neither the factor of bfloat16
+// rows nor their product with a gain: true is returned, and its power of two, `by`, is for the channels themselves.
+// (Float16 rows get there by zeros or by eps alone, and what a factor beyond float32 multiplies is 0.)
+template <int L, bool BF16>
+__device__ __forceinline__ bool norm_of(const RotateArgs& a, const float u[8], float* r, int* by) {
   float s = 0.0f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) s = fmaf(u[e], u[e], s);
   s = group_sum_f32<L>(s);
-  if (__any(!(s >= 1e-24f && s <= 1e37f))) {
-    double d = 0.0;
+  const float mean = fmaf(s, (float)a.inv_dim, (float)a.eps);
+  *r = __builtin_amdgcn_rsqf(mean);
+  if (!__any(!(s >= 1e-24f && mean <= 1e37f))) return false;
+  double d = 0.0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) d = fma((double)u[e], (double)u[e], d);
-    return (float)__builtin_amdgcn_rsq(fma(group_sum_f64<L>(d), a.inv_dim, a.eps));
+  for (int e = 0; e < 8; ++e) d = fma((double)u[e], (double)u[e], d);
+  const double n = __builtin_amdgcn_rsq(fma(group_sum_f64<L>(d), a.inv_dim, a.eps));
+  if constexpr (BF16) {
+    *r = (float)__builtin_amdgcn_frexp_mant(n);
+    *by = __builtin_amdgcn_frexp_exp(n);
+    return true;
+  } else {
+    *r = n > 1e38 ? 1e38f : (float)n;
+    return false;
   }
-  return __builtin_amdgcn_rsqf(fmaf(s, (float)a.inv_dim, (float)a.eps));
+}
+
+// Eight channels times 2^by.
+__device__ __forceinline__ void scale8(float x[8], int by) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = ldexpf(x[e], by);
 }
 
 // ------------------------------------------------------------------ rows in 16 bits
@@ -239,8 +259,8 @@ __device__ __forceinline__ void rotate_row(const RotateArgs& a, int kinds, int64
   for (int e = 0; e < 8; ++e) {
     const bool turned = live && at.turned(e);
     const int i = turned ? at.pair(e) : 0;
-    cs[e] = turned ? angles.c[i] : 1.0f;
-    sn[e] = turned ? (at.minus(e) ? -angles.s[i] : angles.s[i]) : 0.0f;
+    cs[e] = turned ? kDown * angles.c[i] : kDown;
+    sn[e] = turned ? kDown * (at.minus(e) ? -angles.s[i] : angles.s[i]) : 0.0f;
   }
   int before = 0;   // rounds of the kind before
 #pragma unroll 1
@@ -271,10 +291,13 @@ __device__ __forceinline__ void rotate_row(const RotateArgs& a, int kinds, int64
       const kv_u4 own = next;
       const kv_u4 other = others<MODE, L>(at, own, pass);
       if (i + a.parts < rounds) next = load(i + a.parts);
-      float u[8], v[8], y[8];
+      float u[8], v[8], y[8], r = 1.0f;
+      int by = 0;
       unpack8<BF16>(own, u);
+      const bool far = h.gain && norm_of<L, BF16>(a, u, &r, &by);
       unpack8<BF16>(other, v);
-      const float r = h.gain ? norm_of<L>(a, u) : 1.0f;
+      if (far) scale8(u, by), scale8(v, by);
+      r *= kUp;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float straight = u[e] * ga[e];
@@ -312,7 +335,7 @@ __device__ __forceinline__ void rotate_few(const RotateArgs& a, int kinds, int64
     for (int e = 0; e < 8; ++e) g[e] = go[e] = 1.0f;
     if (h.gain && live) gains<MODE, BF16>(h, at, g, go);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) go[e] = at.minus(e) ? -go[e] : go[e];
+    for (int e = 0; e < 8; ++e) g[e] *= kDown, go[e] *= at.minus(e) ? -kDown : kDown;
     auto load = [&](int i) {
       const int item = min(i + slot, items - 1), r = small_div(item, inverse);
       kv_u4 w{};
@@ -324,10 +347,13 @@ __device__ __forceinline__ void rotate_few(const RotateArgs& a, int kinds, int64
       const kv_u4 own = next, other = others<MODE, L>(at, own, pass);
       if (i + kAtOnce < items) next = load(i + kAtOnce);
       const int item = min(i + slot, items - 1), r = small_div(item, inverse);
-      float u[8], v[8], y[8];
+      float u[8], v[8], y[8], norm = 1.0f;
+      int by = 0;
       unpack8<BF16>(own, u);
+      const bool far = h.gain && norm_of<L, BF16>(a, u, &norm, &by);
       unpack8<BF16>(other, v);
-      const float norm = h.gain ? norm_of<L>(a, u) : 1.0f;
+      if (far) scale8(u, by), scale8(v, by);
+      norm *= kUp;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         y[e] = u[e] * g[e];
@@ -486,7 +512,12 @@ __device__ __forceinline__ void append_keys(const AppendArgs& g, int64_t row, in
   auto row_of = [&](int i) { return kh.x + row * kh.x_row + (int64_t)min(i * kAtOnce + slot, a.heads - 1) * kh.x_head; };
   kv_u4 next = load_raw8(row_of(i), at.c0, kh.x_wide);
   for (; i * kAtOnce < a.heads; i += r.parts) {
-    const kv_u4 own = next, other = others<MODE, kLanes>(at, own, pass);
+    const kv_u4 own = next;
+    kv_u4 other = others<MODE, kLanes>(at, own, pass);
+    if constexpr (MODE == kInterleaved) {   // what is not turned stands in itself: 0 times a neighbour may be NaN
+#pragma unroll
+      for (int j = 0; j < 4; ++j) other[j] = at.turned(2 * j) ? other[j] : own[j];
+    }
     next = load_raw8(row_of(i + r.parts), at.c0, kh.x_wide);
     float u[8], v[8], x[8];
     unpack8<BF16>(own, u);

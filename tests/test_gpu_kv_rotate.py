@@ -201,6 +201,69 @@ def test_norms_of_extreme_rows(lam):
     assert y[3, 0, 5] == -8 and y[3].abs().sum() == 8
 
 
+@pytest.mark.parametrize("D,Hq,n", [(64, 3, 6), (64, 2, 8200), (128, 1, 8200), (128, 5, 7), (256, 2, 6), (80, 3, 6)])
+@pytest.mark.parametrize("layout,pairs", [("half", None), ("half", 5), ("interleaved", 12), ("half", 0)])
+def test_norms_of_extreme_rows_with_gains_and_rotations(lam, D, Hq, n, layout, pairs):
+    """Rows at both ends of bfloat16's range: what is normed is in the range of its gains, however it is computed
+    (the tolerance counts float32's roundings, not its range, and 2^-134, half of bfloat16's smallest step); on the way
+    into the cache as well."""
+    def check(got, x, pos, gain, eps):
+        want, size = kv.rotate(_np(x), pos, f, layout, 1.25, _np(gain), eps)
+        assert (np.abs(_np(got) - want) <= 2.0 ** -8 * np.abs(want) + 16 * 2.0 ** -24 * size + 2.0 ** -134).all()
+
+    pairs = D // 2 if pairs is None else pairs
+    f = kv.frequencies(pairs)[0] if pairs else []
+    sizes = [3.3e38, 1e38, 1e20, 1.0, 1e-30, 2e-38]
+    x = (_rows(D, n, Hq, D, "f16").float().sign() * torch.tensor([sizes[i % 6] for i in range(n)], device="cuda")[:, None, None])
+    x = (x * (1 - 0.2 * torch.rand(x.shape, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda"))).bfloat16()
+    pos = [7 * i + 1 for i in range(n)]
+    pick = list(range(6)) + [n - 1]
+    for gain, eps in ((4 * _gain(1, D), 1e-6), (_gain(2, D, torch.bfloat16), 1e-80), (1e-3 * _gain(3, D), 1e40)):
+        call = dict(layout=layout, amplitude=1.25, q_norm=gain, eps=eps)
+        got = lam.kv_rotate(x, _freq(f), _i32(pos), **call)
+        assert got.isfinite().all()
+        check(got[pick], x[pick], [pos[i] for i in pick], gain, eps)
+        if D != 80:
+            cols = -(-n // 64)
+            pool, table = lam.kv_pages(cols, 1, D, 64), torch.arange(cols, dtype=torch.int32, device="cuda").view(1, cols)
+            got = lam.kv_rotate_append(x, x[:, :1], x[:, :1], pool, table, _i32([n]), _freq(f), k_norm=gain, **call)
+            check(got[pick], x[pick], pick, gain, eps)
+            k, _ = lam.kv_read(pool, table, _i32([n]), n, D)
+            exact, _ = kv.rotate(_np(x[pick, :1]), pick, f, layout, 1.25, _np(gain), eps)
+            assert np.array_equal(_np(k[pick]), kv.rounded(exact))
+
+
+@pytest.mark.parametrize("n", [5, 8200])
+def test_rotations_of_the_largest_values(lam, n):
+    """Without a norm a result that the type holds is found, also where its two terms are beyond it."""
+    D, layout, f = 64, "half", kv.frequencies(32)[0]
+    x = _rows(4, n, 2, D, "f16").float().sign() * 3.3e38
+    x = (x * torch.rand(x.shape, generator=torch.Generator(device="cuda").manual_seed(2), device="cuda")).bfloat16()
+    got = lam.kv_rotate(x, _freq(f), _i32(list(range(n))), amplitude=1.375)
+    pick = list(range(5)) + [n - 1]
+    want, size = kv.rotate(_np(x[pick]), pick, f, layout, 1.375)
+    y, most = _np(got[pick]), (2 - 2.0 ** -7) * 2.0 ** 127
+    err = 2.0 ** -8 * np.abs(want) + 16 * 2.0 ** -24 * size
+    fits, over = np.abs(want) + err <= most, np.abs(want) > (2 - 2.0 ** -8) * 2.0 ** 127 + 16 * 2.0 ** -24 * size
+    assert fits.sum() > 100 and over.sum() > 10
+    assert (np.abs(y - want)[fits] <= err[fits]).all()
+    assert np.array_equal(y[over], np.sign(want[over]) * np.inf)
+
+
+@pytest.mark.parametrize("eps", [1e-6, 1e-80, 1e-300])
+@pytest.mark.parametrize("n", [3, 8200])
+def test_norms_of_rows_of_zeros(lam, eps, n):
+    D = 128
+    x = torch.zeros((n, 1, D), dtype=torch.bfloat16, device="cuda")
+    g, f = _gain(1, D), _freq(kv.frequencies(64)[0])
+    assert not lam.kv_rotate(x, f, _i32(list(range(n))), q_norm=g, eps=eps).any()
+    cols = -(-n // 64)
+    pool, status = lam.kv_pages(cols, 1, D, 64), _i32([0, 0, 0])
+    table = torch.arange(cols, dtype=torch.int32, device="cuda").view(1, cols)
+    assert not lam.kv_rotate_append(x, x, x, pool, table, _i32([n]), f, q_norm=g, k_norm=g, eps=eps, status=status).any()
+    assert status.tolist() == [0, 0, 0] and not lam.kv_read(pool, table, _i32([n]), n, D)[0].any()
+
+
 def test_rotations_add(lam):
     """A key turned to one position and then by a distance is the key at the other (f16: two roundings)."""
     f, _ = kv.frequencies(64)
