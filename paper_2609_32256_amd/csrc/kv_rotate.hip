@@ -220,7 +220,7 @@ __device__ __forceinline__ bool norm_of(const RotateArgs& a, const float u[8], f
     *by = __builtin_amdgcn_frexp_exp(n);
     return true;
   } else {
-    *r = n > 1e38 ? 1e38f : (float)n;
+    *r = n > 1e37 ? 1e37f : (float)n;   // (times kUp still in range)
     return false;
   }
 }

@@ -250,11 +250,12 @@ def test_rotations_of_the_largest_values(lam, n):
     assert np.array_equal(y[over], np.sign(want[over]) * np.inf)
 
 
-@pytest.mark.parametrize("eps", [1e-6, 1e-80, 1e-300])
+@pytest.mark.parametrize("eps", [1e-6, 1e-80, 1e-300, 5e-324, 1e300])
 @pytest.mark.parametrize("n", [3, 8200])
-def test_norms_of_rows_of_zeros(lam, eps, n):
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+def test_norms_of_rows_of_zeros(lam, eps, n, dt):
     D = 128
-    x = torch.zeros((n, 1, D), dtype=torch.bfloat16, device="cuda")
+    x = torch.zeros((n, 1, D), dtype=DT[dt], device="cuda")
     g, f = _gain(1, D), _freq(kv.frequencies(64)[0])
     assert not lam.kv_rotate(x, f, _i32(list(range(n))), q_norm=g, eps=eps).any()
     cols = -(-n // 64)
