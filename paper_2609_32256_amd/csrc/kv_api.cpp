@@ -309,21 +309,23 @@ lam_status lam_kv_rotate_append(lam_ctx* ctx, const lam_kv_view* view, const lam
   const lam_kv_slots w = or_none(weights), p = or_none(positions);
   LAM_TRY(check_own(w, view, "weights"));
   LAM_TRY(check_own(p, view, "positions"));
-  LAM_CHECK(aligned(first_dev, 4) && aligned(status_dev, 4), LAM_EINVAL, "first and status must be 4-byte aligned");
   LAM_CHECK(k != nullptr && k->heads == view->kv_heads, LAM_EINVAL, "k must have the view's heads");
   const lam_heads none{};
   const lam_heads& qh = q ? *q : none;
   LAM_TRY(check_heads(qh, "q", view->rows, view->head_dim, view->dtype, true));
   LAM_TRY(check_heads(*k, "k", view->rows, view->head_dim, view->dtype, false));
-  if (view->rows == 0) return LAM_OK;
-  LAM_CHECK(v_dev != nullptr && aligned(v_dev, 2), LAM_EINVAL, "v must be 2-byte aligned and not NULL");
-  LAM_CHECK(v_row_stride >= 0 && v_head_stride >= 0, LAM_EINVAL, "strides must be >= 0");
-  if (qh.heads > 0) {
-    const Strided y = out_of(qh, view->rows, view->head_dim);
-    const Strided v{v_dev, v_row_stride, v_head_stride, view->rows, view->kv_heads, view->head_dim};
-    LAM_CHECK(apart(y, in_of(*k, view->rows, view->head_dim)) && apart(y, v), LAM_EINVAL,
-              "the queries' result overlaps k or v");
+  if (view->rows > 0) {
+    LAM_CHECK(v_dev != nullptr && aligned(v_dev, 2), LAM_EINVAL, "v must be 2-byte aligned and not NULL");
+    LAM_CHECK(v_row_stride >= 0 && v_head_stride >= 0, LAM_EINVAL, "strides must be >= 0");
+    if (qh.heads > 0) {
+      const Strided y = out_of(qh, view->rows, view->head_dim);
+      const Strided v{v_dev, v_row_stride, v_head_stride, view->rows, view->kv_heads, view->head_dim};
+      LAM_CHECK(apart(y, in_of(*k, view->rows, view->head_dim)) && apart(y, v), LAM_EINVAL,
+                "the queries' result overlaps k or v");
+    }
   }
+  LAM_CHECK(aligned(first_dev, 4) && aligned(status_dev, 4), LAM_EINVAL, "first and status must be 4-byte aligned");
+  if (view->rows == 0) return LAM_OK;
   DeviceGuard g(ctx->device);
   return launch_kv_rotate_append(ctx, *view, rotate_args(*rotary, qh, *k, view->rows, view->head_dim, eps, norm_dim), v_dev,
                                  v_row_stride, v_head_stride, w, p, first_dev, status_dev);

@@ -206,6 +206,31 @@ def test_append_refusals():
 
 
 @needs_lib
+def test_append_results_beside_keys_and_values():
+    """Queries turned in place beside the keys and values of one product are found to lie apart from them (the
+    call is then refused for its status, so that nothing runs), and moved onto either they are not."""
+    import paper_2609_32256_amd as lam
+    view = lam._KV_VIEW.pack(A + (1 << 36), 100, A + (1 << 37), 4, A + (1 << 38), 0, 10, 2, 4, 8, 64, 64, 1)
+    row = 24 * 64
+
+    def why(at=0, row_q=row, k=A + 1024, v=A + 2048, rows=view):
+        q = _heads(lam, x=A + at, row=row_q, y=A + at, y_row=row_q)
+        assert lam._lib.lam_kv_rotate_append(CTX, rows, _rotary(lam), q, _heads(lam, x=k, row=row, y=0), v, row, 64, None, None,
+                                             None, 1e-6, 0, A + 1) == 1
+        return lam._lib.lam_last_error().decode()
+
+    assert "status" in why()
+    assert "status" in why(k=A + 2048, v=A + 1024)
+    assert "status" in why(at=10 * 2 * row, k=A, v=A + 1024)         # behind the last row
+    for at in (2, 128, 1024, 2048, 3070, 2 * row - 2, 2 * row + 1022):
+        assert "overlaps" in why(at=at), at
+    assert "overlaps" in why(row_q=row + 8) and "overlaps" in why(k=A) and "overlaps" in why(v=A)
+    assert "overlaps" in why(k=A + (1 << 30), v=A + 1022)
+    empty = lam._KV_VIEW.pack(A + (1 << 36), 100, A + (1 << 37), 4, A + (1 << 38), 0, 0, 2, 4, 8, 64, 64, 1)
+    assert "status" in why(rows=empty)
+
+
+@needs_lib
 def test_window_refusals():
     import paper_2609_32256_amd as lam
     view = lam._KV_VIEW.pack(A + (1 << 36), 100, A + (1 << 37), 4, A + (1 << 38), 0, 10, 2, 4, 8, 64, 64, 1)
