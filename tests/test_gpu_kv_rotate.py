@@ -505,6 +505,42 @@ def test_what_is_not_finite_stays_in_its_pair_on_the_way_into_the_cache(lam, D, 
         assert torch.equal(pool, plain)
 
 
+@pytest.mark.parametrize("norm", [False, True])
+@pytest.mark.parametrize("D,Hq,Hk,n,layout", [
+    (64, 3, 1, 48, "half"), (64, 0, 5, 48, "interleaved"), (128, 2, 3, 48, "half"), (128, 8, 6, 5000, "interleaved"), (256, 1, 2, 48, "half"),
+    (64, 4, 1, 8200, "half"), (64, 0, 3, 8200, "interleaved"), (128, 1, 2, 8200, "half"),       # waves of four rows
+])
+def test_counts_are_of_the_threads_that_met_them(lam, D, Hq, Hk, n, layout, norm):
+    """A thread holds eight channels of a token and head, four hold a block: one element that is not finite is met
+    by the one that holds it and by that of its pair's other channel, with a norm by all of its head;
+    a block out of range by its four.  Lanes that repeat a head or a row and waves that share one count nothing twice."""
+    pairs, T, seen = D // 4, 32, [0, 0]
+    q = _rows(1, n, Hq, D, "bf16") if Hq else None
+    k, v = _rows(2, n, Hk, D, "bf16").clamp(-8, 8), _rows(3, n, Hk, D, "bf16").clamp(-8, 8)
+    cols = -(-n // T)
+    last = (cols - 1) * T
+    k[last:], v[last:] = float("nan"), 60000.0                    # without a place: not counted but as such
+    for i, r in enumerate(range(1, last - 6, max(12, n // 50 // 4 * 4))):   # rows apart, so that no thread meets two
+        h, c = (i * 7) % Hk, (i * 13) % D
+        k[r, h, c] = (float("nan"), float("inf"), float("-inf"))[i % 3]
+        other = c if c >= 2 * pairs else c ^ 1 if layout == "interleaved" else (c + pairs) % (2 * pairs)
+        seen[0] += D // 8 if norm else len({c // 8, other // 8})
+        v[r + 4, h, (i * 5) % D] = float("nan")
+        v[r + 4, h, D - 1 - (i * 5) % D] = 60000.0                # another block of the same head
+        seen[0] += 1
+        seen[1] += 4
+        if not norm:
+            k[r + 6, h, 2 * pairs + (i * 3) % (D - 2 * pairs)] = -50000.0
+            seen[1] += 4
+    table = torch.arange(cols, dtype=torch.int32, device="cuda").view(1, cols)
+    table[0, cols - 1] = -1
+    status, pool, f = _i32([0, 0, 0]), lam.kv_pages(cols, Hk, D, T), _freq(kv.frequencies(pairs)[0])
+    for times in (1, 2):                                          # added to
+        lam.kv_rotate_append(q, k, v, pool, table, _i32([n]), f, layout=layout, k_norm=torch.ones(D, device="cuda") if norm else None,
+                             status=status)
+        assert status.tolist() == [times * seen[0], times * seen[1], times * (n - last) * Hk]
+
+
 # ------------------------------------------------------------------ streams, graphs, refusals
 def test_another_stream_and_a_graph(lam):
     D, Hq, Hk, B = 128, 8, 2, 3
