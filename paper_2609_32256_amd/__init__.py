@@ -372,7 +372,7 @@ def kv_pages(n_pages: int, kv_heads: int, head_dim: int, page_size: int = 64, de
     size = _lib.lam_kv_page_bytes(_kv_int(head_dim, "head_dim"), _kv_int(page_size, "page_size"))
     if size < 0:
         raise ValueError("head_dim must be 64, 128 or 256 and page_size a power of two from 32 to 1024")
-    return torch.zeros((int(n_pages), int(kv_heads), size), dtype=torch.uint8, device=device or "cuda")
+    return torch.zeros((int(n_pages), int(kv_heads), size), dtype=torch.uint8, device="cuda" if device is None else device)
 
 
 def _kv_tensor(t, dtype, dims, name, dev):
@@ -542,7 +542,7 @@ def rotary_frequencies(rotary_dim: int, base: float = 10000.0, scaling: str | No
     out, amplitude = (ctypes.c_double * max(pairs, 1))(), ctypes.c_double()
     _check(_lib.lam_rotary_frequencies(pairs, float(base), _ROTARY_SCALINGS[scaling], float(factor), float(length),
                                        float(low), float(high), out, ctypes.addressof(amplitude)))
-    return torch.tensor(out[:pairs], dtype=torch.float64, device=device or "cuda"), amplitude.value
+    return torch.tensor(out[:pairs], dtype=torch.float64, device="cuda" if device is None else device), amplitude.value
 
 
 def _kv_rotary(frequencies, layout, amplitude, dev):

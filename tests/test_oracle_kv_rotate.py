@@ -105,6 +105,25 @@ def test_frequencies_refused():
     assert lam.rotary_frequencies(0, device="cpu")[0].shape == (0,)
 
 
+@needs_lib
+def test_device_0_is_not_the_current_one(monkeypatch):
+    """An index of a device is taken as it is, 0 as well (no device is touched)."""
+    import torch
+
+    import paper_2609_32256_amd as lam
+    asked, make = [], torch.tensor
+    monkeypatch.setattr(torch, "tensor", lambda *a, device, **kw: (asked.append(device), make(*a, **kw))[1])
+    for device in (0, 1, None, "cpu"):
+        lam.rotary_frequencies(8, device=device)
+    assert asked == [0, 1, "cuda", "cpu"]
+    asked.clear()
+    empty = torch.zeros
+    monkeypatch.setattr(torch, "zeros", lambda *a, device, **kw: (asked.append(device), empty(*a, **kw))[1])
+    for device in (0, 1, None, "cpu"):
+        lam.kv_pages(2, 1, 64, device=device)
+    assert asked == [0, 1, "cuda", "cpu"]
+
+
 # ------------------------------------------------------------------ refusals, with addresses that nothing touches
 A = 1 << 40                      # 16-byte aligned addresses, far apart
 CTX = ctypes.c_void_p(A)         # a refused call does not look into its context
