@@ -775,7 +775,7 @@ def kv_attend(q: torch.Tensor, pages: torch.Tensor, table: torch.Tensor, lengths
         window = sinks = 0
     _check(_lib.lam_kv_attend_window(ctx.handle, view, q.data_ptr(), q.stride(0), q.stride(1), q_heads,
                                      head_dim ** -0.5 if scale is None else float(scale), 1 if causal else 0,
-                                     0 if max_length is None else max(1, int(max_length)), window, sinks, m, w,
+                                     0 if max_length is None else max(1, _kv_count(max_length, "max_length", -(1 << 63))), window, sinks, m, w,
                                      out.data_ptr(), None if lse is None else lse.data_ptr()))
     return out
 

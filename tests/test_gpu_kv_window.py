@@ -287,6 +287,19 @@ def test_refusals(lam):
             c.call(**bad)
 
 
+def test_bounds_beyond_64_bits(lam):
+    """A bound of lengths is refused rather than cut to its low bits, which would leave tokens out."""
+    c = Case(lam, 64, 32, 1, 2, "bf16", [1], [50])
+    want = c.call()
+    for bound in ((1 << 63) - 1, 1 << 40, 50):
+        assert torch.equal(c.call(max_length=bound), want)
+        assert torch.equal(c.call(max_length=bound, window=1 << 40), want)
+    for bound in (1 << 63, (1 << 64) + 5, -(1 << 63) - 1):
+        for window in (None, 20):
+            with pytest.raises(ValueError):
+                c.call(max_length=bound, window=window)
+
+
 def test_streaming(lam):
     """Tokens normed, turned and appended, attended to in a window, and the pages behind it
     taken away: the steps of a stream of any length in a fixed number of pages."""
