@@ -355,11 +355,25 @@ __device__ __forceinline__ void rotate_few(const RotateArgs& a, int kinds, int64
       if (far) scale8(u, by), scale8(v, by);
       norm *= kUp;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        y[e] = u[e] * g[e];
-        if (live && at.turned(e)) y[e] = fmaf(v[e] * go[e], angles[r].s[at.pair(e)], y[e] * angles[r].c[at.pair(e)]);
-        y[e] *= norm;
+      for (int e = 0; e < 8; ++e) y[e] = u[e] * g[e];
+      if (MODE != kHalves || at.turned(0)) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          kv_f4 c, t;
+          if constexpr (MODE == kHalves) {   // all eight are turned or none
+            c = *reinterpret_cast<const kv_f4*>(angles[r].c + at.pair(0) + 4 * j);
+            t = *reinterpret_cast<const kv_f4*>(angles[r].s + at.pair(0) + 4 * j);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) c[e] = angles[r].c[at.pair(4 * j + e)], t[e] = angles[r].s[at.pair(4 * j + e)];
+          }
+#pragma unroll
+          for (int e = 4 * j; e < 4 * j + 4; ++e)
+            if (MODE == kHalves || at.turned(e)) y[e] = fmaf(v[e] * go[e], t[e - 4 * j], y[e] * c[e - 4 * j]);
+        }
       }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] *= norm;
       kv_u4 w = pack8<BF16>(y);
       if ((none >> r) & 1u) w = kv_u4{0, 0, 0, 0};
       if (live && i + slot < items)
@@ -368,8 +382,9 @@ __device__ __forceinline__ void rotate_few(const RotateArgs& a, int kinds, int64
   }
 }
 
+// (Waves a SIMD without which the rare far rows cost registers: halves 78, 65,536 rows of 4 + 1 heads of 128 channels 39 us.)
 template <int L, bool BF16, int MODE>
-__global__ __launch_bounds__(kKvThreads) void k_kv_rotate_few(RotateArgs a) {
+__global__ __launch_bounds__(kKvThreads, MODE == kHalvesAnywhere ? 5 : 7) void k_kv_rotate_few(RotateArgs a) {
   __shared__ RowAngles<L> angles[kKvThreads / 64][kFewRows];
   __shared__ Pass<MODE> pass[kKvThreads / 64];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -740,10 +755,11 @@ constexpr int64_t kRotateWaves = 4096;
 
 // Whether a wave takes four rows: for heads so few that the rounds of one leave lanes idle, and so
 // many rows that a quarter of the waves fills the chip.  65,536 rows, one and four rows a wave, us:
-// 64 channels, 4 + 1 heads 52 and 25 (into the cache 85 and 42), 32 + 4 heads 109 and 108 (144 and
-// 127); 128 channels, 4 + 1 heads 55 and 36 (93 and 60), 16 + 2 111 and 109 (145 and 133), 16 + 4 123
-// and 134 (156 and 164).  16,384 rows: 64 channels, 16 + 4 heads 22 and 21 (33 and 30), 32 + 8 32 and 36
-// (44 and 48); 8,192: 4 + 1 heads 9 and 7 (13 and 10), 16 + 4 13 and 17.  Heads of 256 channels fill a wave by two.
+// 64 channels, 4 + 1 heads 53 and 26 (into the cache 86 and 41), 16 + 4 71 and 61 (113 and 81), 32 + 4 113 and 111
+// (146 and 124), 32 + 8 124 and 141 (157 and 152); 128 channels, 4 + 1 heads 56 and 38 (93 and 58), 16 + 2 114 and
+// 115 (148 and 131), 16 + 4 124 and 140 (158 and 160).  16,384 rows: 64 channels, 16 + 4 heads 22 and 21 (34 and
+// 29), 32 + 8 32 and 34 (44 and 46); 8,192: 4 + 1 heads 9 and 6 (13 and 9), 16 + 4 13 and 15.  Between these the borders
+// are not measured.  Heads of 256 channels fill a wave by two.
 bool few_heads(int64_t rows, int heads, int lanes) {
   return heads <= (lanes == 8 ? 40 : lanes == 16 ? 18 : 0) && rows >= std::max(8192, 128 * lanes * heads);
 }
