@@ -483,7 +483,7 @@ lam_status lam_rotary_frequencies(int32_t pairs, double base, int scaling, doubl
 
 /* A rotation: channel pair i (channels i and i + pairs, or 2 i and 2 i + 1) of a row at position p
  * is turned by a = p freq[i]:  (u, v) -> amplitude (u cos a - v sin a, u sin a + v cos a).
- * Channels from 2 pairs on stay as they are.  Angles are right to 2^-50 of a turn at every
+ * Channels from 2 pairs on stay as they are.  Angles are right to 2^-53 of a turn at every
  * position, negative ones among them (frequencies of up to 1 radian). */
 enum { LAM_ROTARY_HALF = 0, LAM_ROTARY_INTERLEAVED = 1 };
 typedef struct lam_rotary {
@@ -510,7 +510,9 @@ typedef struct lam_heads {
 /* Norms and turns rows of queries and, where k is not NULL, of keys, each at its positions_dev
  * (int32[rows]; may be NULL without pairs).  head_dim: a multiple of 8 up to 256.  Computed in
  * float32 with angles in binary64, and rounded once.  No result may overlap anything else that the
- * call reads or writes; rows of one stride that alternate in memory do not.  Asynchronous. */
+ * call reads or writes; rows of one stride that alternate in memory do not.  What float32 holds is
+ * found also where a term or the norm's factor on the way is beyond it (amplitudes up to 4, gains
+ * up to 2^60).  Asynchronous. */
 lam_status lam_kv_rotate(lam_ctx* ctx, const lam_rotary* rotary, const lam_heads* q, const lam_heads* k, int64_t rows,
                          int32_t head_dim, int32_t dtype, const int32_t* positions_dev, double eps, int32_t norm_dim);
 

@@ -28,10 +28,12 @@
 // unit took 2 to 30 us more, since its parts have to leave the caches of the XCDs).
 //
 // Rows with a window walk the strips of the first tokens and those from the tile's first window on, and
-// nothing else is read (Walk): 8 sequences of 131,072 tokens with a window of 8,192 22 us, 72 MB, 37 of
-// 3,000 to 6,000 with one of 1,024 11; latency, since a wave has five to ten strips of 0.7 us.  (Eight
-// waves a workgroup: one sequence and a window of 1,900 12.2 us, with four 14.8; 37 and 1,024 17, with four
-// 14.6.  Split from 600 tokens on: one and 1,800 11 us, whole 14; 37 and 1,000 18.9, whole 14.3.)
+// nothing else is read (Walk).  32 query heads over 8 of 128 channels, 8 sequences of 131,072 tokens: with windows of
+// 8,192, 16,384 and 24,576 this kernel takes 16.6, 28 and 39 us, 6.2 TB/s and 5 us more for the plan, the first loads and
+// the end, the join 5.  28 over 4, 37 sequences of 3,000 to 6,000 and a window of 1,024: 11 us; latency, a wave
+// has nine strips of 0.7 us.  (32 over 8.  Eight waves a workgroup: one sequence and a window of 1,900
+// 12.2 us, with four 14.8; 37 of 28,000 and 1,024 17, with four 14.6.  Split from 600 tokens on: one and 1,800
+// 11 us, whole 14; 37 and 1,000 18.9, whole 14.3.)
 #include <algorithm>
 #include <cmath>
 

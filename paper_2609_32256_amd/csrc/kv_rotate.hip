@@ -71,7 +71,7 @@ __device__ __forceinline__ void sin_cos(int32_t pos, double freq, double* c, dou
 __device__ __forceinline__ void sin_cos(int32_t pos, double freq, float* c, float* s) {
   int quarter;
   const float r = (float)turns_of(pos, freq, &quarter), z = r * r;
-  float a = 42.058693944897655f, b = -26.4262567833744f;   // the next terms: 2e-9, 3e-9
+  float a = 42.058693944897655f, b = -26.4262567833744f;   // the next terms: 2e-9, 1e-10
   a = fmaf(a, z, -76.70585975306139f), b = fmaf(b, z, 60.24464137187666f);
   a = fmaf(a, z, 81.60524927607506f), b = fmaf(b, z, -85.45681720669373f);
   a = fmaf(a, z, -41.34170224039976f), b = fmaf(b, z, 64.9393940226683f);
@@ -144,7 +144,7 @@ __device__ __forceinline__ void wave_lds_order() {
 // The raw other channels of a lane's eight, given its own (interleaved, also of channels that are not
 // turned: their neighbours).  pass: 16 bytes of LDS for each lane, for
 // pairs whose channels are no whole number of lanes apart (read from memory once more, 41,569 rows of
-// 108 heads of 64 channels and 20 pairs took 384 us, so 273).
+// 108 heads of 64 channels and 20 pairs took 384 us, so 233).
 template <int MODE, int L>
 __device__ __forceinline__ kv_u4 others(const Lane<MODE>& at, kv_u4 own, kv_u4* pass) {
   kv_u4 w = own;
@@ -748,7 +748,8 @@ __global__ __launch_bounds__(kKvThreads) void k_kv_rotate_append(AppendArgs g) {
 }
 
 // Waves that a call of few rows is shared out to, at least for rows on their own, at most on the way
-// into the cache, where every part makes the keys' factors again.  Rows of 40 heads of 128 channels: 300
+// into the cache, where every part makes the keys' factors again.  Rows of 40 heads of 128 channels (others are not
+// measured): 300
 // in 10 parts 4.5 us, 1,000 in 4 or 5 7.7 us (1: 10, 8: 9.9), 2,500 in 2 13.8 us (1: 16.5), 4,000 in 2 18.9
 // (1: 19.7); into the cache 2,000 in 2 14.1 us (1: 16.0, 3: 17.8), 3,000 in 1 19.4 (2: 21.9).
 constexpr int64_t kRotateWaves = 4096;
