@@ -382,7 +382,8 @@ __device__ __forceinline__ void rotate_few(const RotateArgs& a, int kinds, int64
   }
 }
 
-// (Waves a SIMD without which the rare far rows cost registers: halves 78, 65,536 rows of 4 + 1 heads of 128 channels 39 us.)
+// (Held to seven waves a SIMD: else halves take 78 registers for the few rows that norm_of finds out of range, and
+// 65,536 rows of 4 + 1 heads of 128 channels 39 us for 38.)
 template <int L, bool BF16, int MODE>
 __global__ __launch_bounds__(kKvThreads, MODE == kHalvesAnywhere ? 5 : 7) void k_kv_rotate_few(RotateArgs a) {
   __shared__ RowAngles<L> angles[kKvThreads / 64][kFewRows];

@@ -250,6 +250,28 @@ def test_rotations_of_the_largest_values(lam, n):
     assert np.array_equal(y[over], np.sign(want[over]) * np.inf)
 
 
+@pytest.mark.parametrize("n", [12, 8200])
+@pytest.mark.parametrize("layout,pairs", [("half", 32), ("interleaved", 20), ("half", 13)])
+def test_amplitudes_and_gains_at_their_limits(lam, n, layout, pairs):
+    """An amplitude of 4 without a norm, and with gains of 2^60 for rows of every size."""
+    D, f = 64, kv.frequencies(pairs)[0]
+    g = torch.Generator(device="cuda").manual_seed(n)
+    x = torch.rand((n, 2, D), generator=g, device="cuda") * 2 - 1
+    pick = list(range(11)) + [n - 1]
+    big = (x * 3.3e38).bfloat16()
+    got = _np(lam.kv_rotate(big, _freq(f), _i32(list(range(n))), layout=layout, amplitude=4.0)[pick])
+    want, size = kv.rotate(_np(big[pick]), pick, f, layout, 4.0)
+    most, err = (2 - 2.0 ** -7) * 2.0 ** 127, 2.0 ** -8 * np.abs(want) + 16 * 2.0 ** -24 * size
+    fits, over = np.abs(want) + err <= most, np.abs(want) > (2 - 2.0 ** -8) * 2.0 ** 127 + 16 * 2.0 ** -24 * size
+    assert fits.sum() > 100 and over.sum() > 100
+    assert (np.abs(got - want)[fits] <= err[fits]).all() and np.array_equal(got[over], np.sign(want[over]) * np.inf)
+    sizes = torch.tensor([10.0 ** (i % 12 * 7 - 37) for i in range(n)], dtype=torch.float64, device="cuda").clamp(max=3.3e38)
+    y = (x.double() * sizes[:, None, None]).bfloat16()            # 1e-37, 1e-30, ... 3e38
+    gain = _gain(1, D) * 2.0 ** 59
+    got = lam.kv_rotate(y, _freq(f), _i32(list(range(n))), layout=layout, amplitude=4.0, q_norm=gain, eps=1e-76)
+    _check(got[pick], y[pick], pick, f, layout, 4.0, gain, 1e-76, None, "bf16")
+
+
 @pytest.mark.parametrize("eps", [1e-6, 1e-80, 1e-300, 5e-324, 1e300])
 @pytest.mark.parametrize("n", [3, 8200])
 @pytest.mark.parametrize("dt", ["bf16", "f16"])
